@@ -393,6 +393,165 @@ int dllm_generate_kv(const dllm_model* model, const dllm_cai_params* params, int
                      int32_t* forwards_host, int32_t* total_forwards, float* conf_trace, int32_t* argmax_trace,
                      void* kv_cache, size_t kv_bytes, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------
+ * Stand-alone operators: the pieces of a step for programs that assemble their
+ * own layers or batches (requests of unlike lengths, other rotary positions,
+ * masks, sampled tokens).  They take no model handle; the conventions above
+ * hold.  The stream's device must be the current one.  Calls may overlap when
+ * they share no output and no workspace; a call captured into a graph uses its
+ * workspace at every replay, so graphs that may run at the same time need one
+ * each.  Sizes, strides and flags are checked on the host; numbers that lie in
+ * device memory (positions, lengths, sampling controls) may take any value: the
+ * text of each operator says what it does with those that make no sense, and
+ * none of them is used as an address unchecked.
+ * ------------------------------------------------------------------------ */
+
+/* Rows of heads: element j of head h of token l of slab b lies at
+ *   data[b * stride_b + l * stride_l + h * stride_h + j]
+ * (strides in elements, >= 0; j contiguous).  A slab is a sequence of a dense
+ * batch, or the whole buffer of packed requests (one slab). */
+typedef struct dllm_view {
+  void* data; /* device */
+  int64_t stride_b, stride_l, stride_h;
+} dllm_view;
+
+/* How the angles of dllm_rotary grow with the position. */
+enum {
+  DLLM_ROPE_PLAIN = 0,  /* f_j                                                     */
+  DLLM_ROPE_LINEAR = 1, /* f_j / factor: positions compressed                      */
+  DLLM_ROPE_PARTS = 2   /* by parts: g f_j + (1 - g) f_j / factor, see below       */
+};
+
+/*
+ * Rotary position embedding of part of each head:
+ *   f_j = base^(-2 j / rot_dim), j < rot_dim / 2; angle of pair j at position p: p f_j
+ *   (a, b) -> gain * (a cos - b sin, b cos + a sin)
+ * where the pair is elements (j, j + rot_dim/2) of the head, or (2j, 2j + 1)
+ * when interleaved; elements rot_dim .. head_dim-1 pass through.
+ * DLLM_ROPE_PARTS: pair j makes r = orig_len f_j / (2 pi) turns over the trained
+ * length; g = clamp((r - low) / (high - low), 0, 1), so fast pairs keep their
+ * rate and slow ones are compressed.  factor, orig_len, low, high are read only
+ * where the scaling names them.  Angles are formed in float64 and reduced there
+ * to within an eighth of a turn, so far positions lose nothing.
+ * Requirements: head_dim in [2, 512], rot_dim even, 2 <= rot_dim <= min(head_dim,
+ * 256), at most 4096 heads each; base, factor, orig_len > 0; high > low; gain finite.
+ */
+typedef struct dllm_rotary_cfg {
+  int32_t head_dim, rot_dim, interleaved, scaling;
+  double base, factor, orig_len, low, high, gain;
+} dllm_rotary_cfg;
+
+/*
+ * Rotate n_q query heads and n_k key heads of B slabs of L tokens in one launch:
+ * q_out = R(q), k_out = R(k).  k and k_out may both be NULL (n_k is then not
+ * read).  dtype: DLLM_F32 or DLLM_BF16, the type of all four; products in
+ * float32, rounded once.  pos: device int32 [B, L], or NULL for pos0 + l; any
+ * value, negative ones turn backwards.  inverse != 0: the transposed map (the
+ * angles negated), which takes gradients back and, at gain 1, undoes a rotation.
+ * An output may be its input (same data and strides); apart from that no output
+ * may overlap anything the call reads or writes.  B, L or head counts of 0: nothing.
+ * Errors: DLLM_EINVAL (null pointer, bad constant), DLLM_ESHAPE (sizes), DLLM_EHIP.
+ */
+int dllm_rotary(const dllm_rotary_cfg* cfg, int32_t dtype, int32_t B, int32_t L, const int32_t* pos, int32_t pos0,
+                const dllm_view* q, const dllm_view* q_out, int32_t n_q, const dllm_view* k, const dllm_view* k_out,
+                int32_t n_k, int32_t inverse, void* stream);
+
+/*
+ * Attention of documents of unlike lengths.  Document d has q_len[d] queries,
+ * tokens q_start[d] .. of its slab of q and out, and kv_len[d] keys and values,
+ * tokens kv_start[d] .. of its slab of k and v; its slab is slab d (packed
+ * documents have stride_b = 0 and differ in their starts).  Query t of a
+ * document stands at position i = q_pos[d] + t, key j at position j:
+ *   s_ij = scale q_i . k_j;  if cap > 0: s_ij = cap tanh(s_ij / cap);
+ *   if slopes: s_ij -= slopes[h] |i - j|
+ *   out_i = sum_j softmax_j(s_ij) v_j  over the visible keys of the document:
+ *   block = 0: all of them; block >= 1: those with
+ *     j < max(prefix[d], (floor(i / block) + 1) block)
+ * (block 1: causal behind a prefix that all queries see; block = a decoder's
+ * block length: everything up to the end of the query's own block).  Query head
+ * h reads key/value head h / (n_heads / n_kv_heads).
+ * A query that sees no key, or none with a score above -inf, gives zeros.  What
+ * lies at invisible keys never reaches a result, NaN and infinities included;
+ * a NaN score makes its query's output NaN, a visible NaN or infinite value the
+ * dimension it stands in.  Rows of out that belong to no document keep their contents.
+ *
+ * Arrays are device int32 [docs]; NULL stands for: starts 0, q_len = q_tokens,
+ * kv_len = kv_tokens, q_pos = kv_len - q_len (queries at the end of the keys),
+ * prefix 0.  Ranges are cut to their slab (start to [0, tokens], then the length
+ * to what is left, negative lengths to 0) and lengths to max_q and max_kv.
+ * Two documents may share keys and values, never queries.
+ * Storage: float32 (products on the float32 matrix cores) or bf16 (products
+ * accumulate in float32, softmax in float32; probabilities enter the second
+ * product as bf16).  Out must not overlap q, k or v.
+ * Requirements: head_dim 64 or 128; n_heads % n_kv_heads == 0; data pointers
+ * 16-byte aligned; strides multiples of 16 bytes, stride_l >= head_dim, and 64
+ * stride_l of k and v below 2^31 bytes; 0 <= max_q <= q_tokens, 0 <= max_kv <=
+ * kv_tokens; docs <= 65535; scale finite, cap >= 0 and finite, block >= 0.
+ * docs or max_q of 0: nothing.
+ */
+typedef struct dllm_attn_args {
+  int32_t dtype, n_heads, n_kv_heads, head_dim;
+  dllm_view q, k, v, out;    /* out is written; n_heads heads in q and out, n_kv_heads in k and v */
+  int32_t docs;
+  int32_t q_tokens, kv_tokens; /* tokens of a slab of q and out, of k and v */
+  int32_t max_q, max_kv;       /* no document has more (longer ones are cut) */
+  const int32_t *q_start, *q_len, *kv_start, *kv_len, *q_pos, *prefix;
+  const float* slopes;         /* device float32 [n_heads], or NULL */
+  float scale, cap;
+  int32_t block;
+} dllm_attn_args;
+
+/* Bytes of workspace dllm_attention needs for these sizes (0 where it splits no
+ * keys; the arrays and tensors are not looked at).  The workspace, 256-byte
+ * aligned, holds nothing between calls.  Errors: as for dllm_attention's sizes. */
+int dllm_attention_workspace_size(const dllm_attn_args* args, size_t* bytes);
+/* Errors: DLLM_EINVAL (null pointer, bad constant), DLLM_ESHAPE (sizes,
+ * strides), DLLM_EUNSUPPORTED (head_dim, alignment), DLLM_ENOMEM (workspace), DLLM_EHIP. */
+int dllm_attention(const dllm_attn_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Sample one token per row of logits [rows, vocab] (row r at logits + r *
+ * row_stride elements) from given random numbers.  Candidates are the tokens v
+ * != mask_id (mask_id outside [0, vocab): all) with a logit above -inf, ranked by
+ * logit, equal ones by index; w_v = exp((logit_v - max) / temperature).
+ *   top_k:  the first top_k candidates stay
+ *   top_p:  of those, a candidate stays while the mass ranked before it is less
+ *           than top_p times their whole mass (the first always stays)
+ *   min_p:  of those, candidates with w_v < min_p go (the first stays)
+ *   token = the lowest index v with sum of w over kept indices <= v  >  u * (sum of w kept)
+ *   conf  = softmax(logits)_token at temperature 1 over v != mask_id (Box 1's
+ *           confidence of the sampled token; what dllm_commit compares)
+ *   prob  = w_token / (sum of w kept)
+ * Controls are device arrays [rows], NULL where unused; per row, temperature <=
+ * 0 or NaN is greedy (the first candidate: dllm_head's argmax and conf; prob 1),
+ * top_k < 1, top_p >= 1 or NaN and min_p <= 0 or NaN are off, a top_p <= 0 keeps
+ * the first, min_p > 1 counts as 1, and u is cut to [0, 1) (NaN: 0).
+ * A row with a NaN or +inf candidate gives the first such index with conf and
+ * prob NaN; a row without candidates gives token -1 with conf and prob 0.
+ * Candidates with w below 2^-64 count as without mass.  Sums are held in 64
+ * bits and do not depend on the order of execution: equal inputs give equal
+ * outputs.
+ */
+typedef struct dllm_sample_args {
+  const void* logits; /* device, dtype */
+  int64_t row_stride; /* >= vocab where rows > 1 */
+  int32_t dtype;      /* DLLM_F32 or DLLM_BF16 */
+  int32_t rows, vocab, mask_id;
+  const float* u;           /* [rows], required */
+  const float* temperature; /* NULL: 1 */
+  const int32_t* top_k;
+  const float* top_p;
+  const float* min_p;
+  int32_t* token; /* [rows], required */
+  float* conf;    /* [rows], may be NULL */
+  float* prob;    /* [rows], may be NULL */
+} dllm_sample_args;
+
+/* rows of 0: nothing.  Errors: DLLM_EINVAL (null pointer, dtype), DLLM_ESHAPE
+ * (sizes: rows >= 0, 1 <= vocab <= 2^22), DLLM_ENOMEM (workspace), DLLM_EHIP. */
+int dllm_sample_workspace_size(int32_t rows, int32_t vocab, size_t* bytes);
+int dllm_sample(const dllm_sample_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing with HIP events recorded on the launch stream around each
  * launch of the selected kernel classes.  kind: 0 = q/k/v GEMM (with RoPE),
  * 1 = attention, 2 = LM head + reduction, 3 = commit, 4 = norms and

@@ -19,11 +19,13 @@ LIB_PATH = os.path.join(_HERE, "libdllm.so")
 
 DLLM_F32, DLLM_BF16 = 0, 1
 F_BLOCK_SCHED, F_POS, F_BUDGET, F_GRIND, F_FIXED = 1, 2, 4, 8, 16
+ROPE_PLAIN, ROPE_LINEAR, ROPE_PARTS = 0, 1, 2
 R_MASKED, R_THRESH, R_BUDGET, R_GRIND, R_FLUSH, R_FIXED = 0, 1, 2, 3, 4, 5
 PROF_QKV, PROF_ATTN, PROF_HEAD, PROF_COMMIT, PROF_NORM, PROF_GATEUP, PROF_OPROJ, PROF_DOWN = range(8)
 
 _c = ctypes
-_i32, _u32, _f32, _f64, _vp, _sz = _c.c_int32, _c.c_uint32, _c.c_float, _c.c_double, _c.c_void_p, _c.c_size_t
+_i32, _i64, _u32 = _c.c_int32, _c.c_int64, _c.c_uint32
+_f32, _f64, _vp, _sz = _c.c_float, _c.c_double, _c.c_void_p, _c.c_size_t
 
 
 class ModelCfg(_c.Structure):
@@ -49,6 +51,28 @@ class State(_c.Structure):
 
 class WsLayout(_c.Structure):
     _fields_ = [(n, _sz) for n in ("total", "h", "a_attn", "q", "k", "vt", "attn", "a_mlp", "u", "hb")]
+
+
+class RotaryCfg(_c.Structure):
+    _fields_ = [("head_dim", _i32), ("rot_dim", _i32), ("interleaved", _i32), ("scaling", _i32), ("base", _f64),
+                ("factor", _f64), ("orig_len", _f64), ("low", _f64), ("high", _f64), ("gain", _f64)]
+
+
+class View(_c.Structure):
+    _fields_ = [("data", _vp), ("stride_b", _i64), ("stride_l", _i64), ("stride_h", _i64)]
+
+
+class AttnArgs(_c.Structure):
+    _fields_ = [("dtype", _i32), ("n_heads", _i32), ("n_kv_heads", _i32), ("head_dim", _i32), ("q", View), ("k", View),
+                ("v", View), ("out", View), ("docs", _i32), ("q_tokens", _i32), ("kv_tokens", _i32), ("max_q", _i32),
+                ("max_kv", _i32), ("q_start", _vp), ("q_len", _vp), ("kv_start", _vp), ("kv_len", _vp), ("q_pos", _vp),
+                ("prefix", _vp), ("slopes", _vp), ("scale", _f32), ("cap", _f32), ("block", _i32)]
+
+
+class SampleArgs(_c.Structure):
+    _fields_ = [("logits", _vp), ("row_stride", _i64), ("dtype", _i32), ("rows", _i32), ("vocab", _i32),
+                ("mask_id", _i32), ("u", _vp), ("temperature", _vp), ("top_k", _vp), ("top_p", _vp), ("min_p", _vp),
+                ("token", _vp), ("conf", _vp), ("prob", _vp)]
 
 
 class DllmError(RuntimeError):
@@ -88,6 +112,12 @@ _SIGS = {
                             _vp, _vp, _vp, _sz, _vp, _sz, _vp]),
     "dllm_generate_kv": (_i32, [_vp, _c.POINTER(CaiParams), _i32, _vp, _i32, _i32, _i32, _c.POINTER(State), _vp,
                                 _vp, _vp, _vp, _vp, _sz, _vp, _sz, _vp]),
+    "dllm_rotary": (_i32, [_c.POINTER(RotaryCfg), _i32, _i32, _i32, _vp, _i32, _c.POINTER(View), _c.POINTER(View), _i32,
+                           _c.POINTER(View), _c.POINTER(View), _i32, _i32, _vp]),
+    "dllm_attention_workspace_size": (_i32, [_c.POINTER(AttnArgs), _c.POINTER(_sz)]),
+    "dllm_attention": (_i32, [_c.POINTER(AttnArgs), _vp, _sz, _vp]),
+    "dllm_sample_workspace_size": (_i32, [_i32, _i32, _c.POINTER(_sz)]),
+    "dllm_sample": (_i32, [_c.POINTER(SampleArgs), _vp, _sz, _vp]),
     "dllm_prof_enable": (_i32, [_vp, _i32]),
     "dllm_prof_read": (_i32, [_vp, _i32, _c.POINTER(_f64), _c.POINTER(_c.c_int64)]),
     "dllm_prof_every": (_i32, [_vp, _i32]),
@@ -476,3 +506,209 @@ def commit(ctl: Controller, st: DecodeState, conf, argmax, block, t, mask_id, al
     c = st.c()
     check(lib().dllm_commit(ctypes.byref(p), ctypes.byref(c), _ptr(conf), _ptr(argmax), st.B, st.P, st.G, block, t,
                             mask_id, _ptr(all_done), _stream(stream)))
+
+
+# ---------------------------------------------------------------- stand-alone operators
+_DTYPES = {torch.float32: DLLM_F32, torch.bfloat16: DLLM_BF16}
+_SCALINGS = {"none": ROPE_PLAIN, "linear": ROPE_LINEAR, "parts": ROPE_PARTS}
+
+
+def _refuse(ok, code, msg):
+    if not ok:
+        raise DllmError(code, msg)
+
+
+def _dtype(t, name):
+    _refuse(t.dtype in _DTYPES, -1, f"{name} must be float32 or bfloat16")
+    return _DTYPES[t.dtype]
+
+
+class _On:
+    """The device and stream of a call: the operands' device is made current, and
+    what the call allocates belongs to the stream that uses it."""
+
+    def __init__(self, device, stream):
+        _refuse(device.type == "cuda", -1, "tensors must be on the GPU")
+        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        _refuse(self.stream.device == device, -1, "the stream is another device's than the tensors")
+        # nothing to change in the common case: this stream and device are current
+        idle = stream is None and torch.cuda.current_device() == device.index
+        self.scope = None if idle else torch.cuda.stream(self.stream)
+
+    def __enter__(self):
+        if self.scope is not None:
+            self.scope.__enter__()
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc):
+        if self.scope is not None:
+            self.scope.__exit__(*exc)
+
+
+def _column(t, n, dtype, device, name):
+    """The address of a device array of n elements (None: 0)."""
+    if t is None:
+        return None
+    _refuse(t.dtype == dtype and t.device == device, -1, f"{name} must be {dtype} on {device}")
+    _refuse(t.numel() == n and t.is_contiguous(), -2, f"{name} must be {n} contiguous elements")
+    return t.data_ptr()
+
+
+def _rows(t, shape, like, name):
+    """The view of a [B, L, H, hd] tensor whose last dimension is contiguous."""
+    _refuse(tuple(t.shape) == tuple(shape), -2, f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+    _refuse(t.dtype == like.dtype and t.device == like.device, -1, f"{name} must be {like.dtype} on {like.device}")
+    st = t.stride()
+    _refuse(st[3] == 1, -2, f"{name}: elements of a head must be contiguous")
+    # a dimension of one element is never stepped over: its stride says nothing
+    return View(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else shape[3],
+                st[2] if shape[2] > 1 else 0)
+
+
+@dataclass(frozen=True)
+class Rotary:
+    """Constants of a rotary embedding (dllm_rotary_cfg); scaling: none, linear or parts."""
+    head_dim: int
+    rot_dim: int = 0            # 0: the whole head
+    interleaved: bool = False
+    base: float = 10000.0
+    scaling: str = "none"
+    factor: float = 1.0
+    orig_len: float = 0.0
+    low: float = 1.0
+    high: float = 32.0
+    gain: float = 1.0
+
+    def to_c(self) -> RotaryCfg:
+        if self.scaling not in _SCALINGS:
+            raise KeyError(f"unknown rotary scaling {self.scaling!r}; known: {sorted(_SCALINGS)}")
+        return RotaryCfg(self.head_dim, self.rot_dim or self.head_dim, int(self.interleaved), _SCALINGS[self.scaling],
+                         self.base, self.factor, self.orig_len, self.low, self.high, self.gain)
+
+
+def rotary(cfg: Rotary, q, k=None, pos=None, pos0=0, q_out=None, k_out=None, inverse=False, stream=None):
+    """dllm_rotary on q [B, L, Hq, hd] and (optionally) k [B, L, Hkv, hd], any strides with contiguous heads.
+    pos: int32 [B, L], or None for pos0 + l.  Outputs are new tensors unless given (q_out=q: in place).
+    Returns (q_out, k_out)."""
+    _refuse(q.dim() == 4 and (k is None or k.dim() == 4), -2, "q and k must be [B, L, heads, head_dim]")
+    dt = _dtype(q, "q")
+    B, L, n_q, hd = q.shape
+    _refuse(hd == cfg.head_dim, -2, f"q has heads of {hd} elements, cfg of {cfg.head_dim}")
+    with _On(q.device, stream) as s:
+        p = _column(pos, B * L, torch.int32, q.device, "pos")
+        q_out = torch.empty((B, L, n_q, hd), dtype=q.dtype, device=q.device) if q_out is None else q_out
+        vq, vqo = _rows(q, (B, L, n_q, hd), q, "q"), _rows(q_out, (B, L, n_q, hd), q, "q_out")
+        vk = vko = None
+        n_k = 0
+        if k is not None:
+            n_k = k.shape[2]
+            k_out = torch.empty((B, L, n_k, hd), dtype=q.dtype, device=q.device) if k_out is None else k_out
+            vk, vko = _rows(k, (B, L, n_k, hd), q, "k"), _rows(k_out, (B, L, n_k, hd), q, "k_out")
+        check(lib().dllm_rotary(cfg.to_c(), dt, B, L, p, pos0, vq, vqo, n_q, vk, vko, n_k, int(bool(inverse)), s))
+    return q_out, (k_out if k is not None else None)
+
+
+@dataclass
+class Docs:
+    """The documents of an attention call: int32 device arrays [docs] (or None: see dllm_attn_args) and the
+    longest lengths among them.  Documents of a dense batch need no arrays but their lengths."""
+    q_start: torch.Tensor | None = None
+    q_len: torch.Tensor | None = None
+    kv_start: torch.Tensor | None = None
+    kv_len: torch.Tensor | None = None
+    max_q: int | None = None       # None: the slab's tokens
+    max_kv: int | None = None
+    q_pos: torch.Tensor | None = None
+    prefix: torch.Tensor | None = None
+    count: int | None = None       # documents; None: the arrays' length, or the slabs
+
+    @classmethod
+    def packed(cls, q_lens, kv_lens=None, q_pos=None, prefix=None, device="cuda"):
+        """Documents that follow each other without gaps, from host lists."""
+        kv_lens = q_lens if kv_lens is None else kv_lens
+        ints = lambda v: None if v is None else torch.tensor(list(v), dtype=torch.int32, device=device)  # noqa: E731
+        starts = lambda v: [sum(v[:i]) for i in range(len(v))]  # noqa: E731
+        return cls(ints(starts(q_lens)), ints(q_lens), ints(starts(kv_lens)), ints(kv_lens), max(q_lens, default=0),
+                   max(kv_lens, default=0), ints(q_pos), ints(prefix))
+
+
+def attention(q, k, v, docs: Docs | None = None, block=0, scale=None, cap=0.0, slopes=None, out=None, ws=None,
+              stream=None):
+    """dllm_attention.  q [T, Hq, hd] with k, v [S, Hkv, hd]: packed documents in one slab; q [B, T, Hq, hd] with k, v
+    [B, S, Hkv, hd]: a slab per document.  scale None: 1 / sqrt(hd).  out: written and returned (new, zeroed, if
+    None); ws: a device_buffer of attention_workspace_size bytes (allocated here if None)."""
+    _refuse(q.dim() in (3, 4) and k.dim() == q.dim() and v.dim() == q.dim(), -2,
+            "q, k and v must be [tokens, heads, head_dim] or [docs, tokens, heads, head_dim]")
+    dt = _dtype(q, "q")
+    dev = q.device
+    with _On(dev, stream) as s:
+        out = torch.zeros(q.shape, dtype=q.dtype, device=dev) if out is None else out
+        a = _attn_args(dt, q, k, v, out, docs or Docs(), block, scale, cap, slopes)
+        n = _sz()
+        check(lib().dllm_attention_workspace_size(a, n))
+        if ws is None and n.value:
+            ws = device_buffer(n.value, dev)
+        check(lib().dllm_attention(a, _ptr(ws), 0 if ws is None else ws.numel(), s))
+    return out
+
+
+def attention_workspace_size(q, k, v, docs: Docs | None = None):
+    """Bytes of workspace that attention() needs for operands and documents of these sizes."""
+    n = _sz()
+    check(lib().dllm_attention_workspace_size(
+        _attn_args(_dtype(q, "q"), q, k, v, q, docs or Docs(), 0, None, 0.0, None), n))
+    return n.value
+
+
+def _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes):
+    dev = q.device
+    one = q.dim() == 3
+    if one:
+        q, k, v, out = q[None], k[None], v[None], out[None]
+    B, T, Hq, hd = q.shape
+    S, Hkv = k.shape[1], k.shape[2]
+    views = [_rows(q, (B, T, Hq, hd), q, "q"), _rows(k, (B, S, Hkv, hd), q, "k"), _rows(v, (B, S, Hkv, hd), q, "v"),
+             _rows(out, (B, T, Hq, hd), q, "out")]
+    arrays = [docs.q_start, docs.q_len, docs.kv_start, docs.kv_len, docs.q_pos, docs.prefix]
+    n = docs.count
+    if n is None:
+        n = next((t.numel() for t in arrays if t is not None), 1) if one else B
+    _refuse(one or n == B, -2, "a dense batch has one document per slab")
+    if one:
+        for w in views:
+            w.stride_b = 0
+    names = ("q_start", "q_len", "kv_start", "kv_len", "q_pos", "prefix")
+    ptrs = [_column(t, n, torch.int32, dev, name) for t, name in zip(arrays, names)]
+    return AttnArgs(dt, Hq, Hkv, hd, *views, n, T, S, T if docs.max_q is None else docs.max_q,
+                    S if docs.max_kv is None else docs.max_kv, *ptrs, _column(slopes, Hq, torch.float32, dev, "slopes"),
+                    1.0 / math.sqrt(hd) if scale is None else scale, cap, block)
+
+
+def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask_id=-1, ws=None, stream=None):
+    """dllm_sample on logits [rows, V] (rows of any stride) with uniform random numbers u [rows].  Controls are device
+    arrays [rows] (top_k int32, the others float32).  Returns (token int32, conf, prob float32), each [rows]."""
+    _refuse(logits.dim() == 2, -2, "logits must be [rows, vocab]")
+    dt = _dtype(logits, "logits")
+    R, V = logits.shape
+    dev = logits.device
+    st = logits.stride()
+    _refuse(st[1] == 1 or V == 1, -2, "logits: a row must be contiguous")
+    with _On(dev, stream) as s:
+        cols = [_column(u, R, torch.float32, dev, "u"), _column(temperature, R, torch.float32, dev, "temperature"),
+                _column(top_k, R, torch.int32, dev, "top_k"), _column(top_p, R, torch.float32, dev, "top_p"),
+                _column(min_p, R, torch.float32, dev, "min_p")]
+        token = torch.empty((R,), dtype=torch.int32, device=dev)
+        conf = torch.empty((2, R), dtype=torch.float32, device=dev)
+        a = SampleArgs(logits.data_ptr(), st[0], dt, R, V, mask_id, *cols, token.data_ptr(), conf.data_ptr(),
+                       conf.data_ptr() + 4 * R)
+        n = sample_workspace_size(R, V)
+        if ws is None and n:
+            ws = device_buffer(n, dev)
+        check(lib().dllm_sample(a, _ptr(ws), 0 if ws is None else ws.numel(), s))
+    return token, conf[0], conf[1]
+
+
+def sample_workspace_size(rows, vocab):
+    n = _sz()
+    check(lib().dllm_sample_workspace_size(rows, vocab, n))
+    return n.value

@@ -19,29 +19,17 @@
 #include <string>
 #include <vector>
 
-#include "../../include/dllm.h"
-
+#include "api.h"
 #include "kernels.h"
 
 using namespace dllm;
 
-namespace {
-
-thread_local std::string g_last_error;
-
-struct ApiError {
-  int code;
-  std::string msg;
-};
-
-[[noreturn]] void fail(int code, const std::string& msg) { throw ApiError{code, msg}; }
-void require(bool ok, int code, const std::string& msg) {
-  if (!ok) fail(code, msg);
+namespace dllm {
+std::string& last_error() {
+  static thread_local std::string msg;
+  return msg;
 }
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-}  // namespace
+}  // namespace dllm
 
 struct ProfEvent {
   int kind;
@@ -757,11 +745,6 @@ void raise_step_errors(int flag) {
     fail(DLLM_EUNSUPPORTED, "a value of v is beyond IEEE half's range (stored as +-65504 for the attention)");
 }
 
-int finish(const ApiError& e) {
-  g_last_error = e.msg;
-  return e.code;
-}
-
 }  // namespace
 
 // ---------------------------------------------------------------- static scratch
@@ -816,27 +799,9 @@ size_t noalloc_head_layout(const dllm_model_cfg& c, int R, char* base, HeadBufs*
 }
 }  // namespace
 
-#define API_BEGIN \
-  g_last_error.clear(); \
-  try {
-#define API_END                                   \
-  }                                               \
-  catch (const ApiError& e) {                     \
-    return finish(e);                             \
-  }                                               \
-  catch (const HipError& e) {                     \
-    g_last_error = e.what();                      \
-    return DLLM_EHIP;                             \
-  }                                               \
-  catch (const std::exception& e) {               \
-    g_last_error = e.what();                      \
-    return DLLM_EINVAL;                           \
-  }                                               \
-  return DLLM_OK;
-
 extern "C" {
 
-const char* dllm_last_error(void) { return g_last_error.c_str(); }
+const char* dllm_last_error(void) { return last_error().c_str(); }
 
 int dllm_model_buffer_size(const dllm_model_cfg* cfg, size_t* bytes) {
   API_BEGIN

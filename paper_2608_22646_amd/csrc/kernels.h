@@ -1,5 +1,6 @@
 // Internal launchers of the dllm HIP kernels (not part of the C ABI).
 #pragma once
+#include "../../include/dllm.h"
 #include "common.h"
 
 namespace dllm {
@@ -198,5 +199,47 @@ struct CommitArgs {
   int seq;
 };
 void launch_commit(const CommitArgs& a, hipStream_t s);
+
+// ---- stand-alone operators ---------------------------------------------------
+// k_rotary.hip: see dllm_rotary; heads n_q of q to q_out and n_k of k to k_out.
+struct RotaryRows {
+  void* data;
+  int64_t stride_b, stride_l, stride_h;
+};
+struct RotaryArgs {
+  int dtype, B, L, n_q, n_k, hd, rot, inter, scaling, inverse, pos0;
+  const int32_t* pos;
+  RotaryRows q, q_out, k, k_out;
+  double log2_base, factor, orig_len, low, high;
+  float gain;
+  int tokens;  // of a workgroup (set by the launcher)
+};
+void launch_rotary(RotaryArgs a, hipStream_t s);
+
+// k_attn_docs.hip: see dllm_attention; ws of attn_docs_bytes(a) bytes.
+struct AttnView {
+  void* data;
+  int64_t stride_b, stride_l, stride_h;
+};
+struct AttnArgs {
+  int dtype, Hq, Hkv, hd, docs, q_tokens, kv_tokens, max_q, max_kv, block;
+  AttnView q, k, v, out;
+  const int32_t *q_start, *q_len, *kv_start, *kv_len, *q_pos, *prefix;
+  const float* slopes;
+  float scale, cap;
+};
+size_t attn_docs_bytes(const AttnArgs& a);
+void launch_attn_docs(const AttnArgs& a, void* ws, hipStream_t s);
+
+// k_sample.hip: see dllm_sample; ws of sample_bytes(rows, vocab) bytes.
+struct SampleArgs {
+  const void* logits;
+  int64_t row_stride;
+  int dtype, rows, vocab, mask_id;
+  const float* u; const float* temperature; const int32_t* top_k; const float* top_p; const float* min_p;
+  int32_t* token; float* conf; float* prob;
+};
+size_t sample_bytes(int rows, int vocab);
+void launch_sample(const SampleArgs& a, void* ws, hipStream_t s);
 
 }  // namespace dllm
