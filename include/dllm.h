@@ -486,7 +486,7 @@ int dllm_rotary(const dllm_rotary_cfg* cfg, int32_t dtype, int32_t B, int32_t L,
  * Requirements: head_dim 64 or 128; n_heads % n_kv_heads == 0; data pointers
  * 16-byte aligned; strides multiples of 16 bytes, stride_l >= head_dim, and 64
  * stride_l of k and v below 2^31 bytes; 0 <= max_q <= q_tokens, 0 <= max_kv <=
- * kv_tokens; docs <= 65535; scale finite, cap >= 0 and finite, block >= 0.
+ * kv_tokens, both at most 2^30; docs <= 65535; scale finite, cap >= 0 and finite, block >= 0.
  * docs or max_q of 0: nothing.
  */
 typedef struct dllm_attn_args {

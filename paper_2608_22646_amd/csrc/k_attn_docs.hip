@@ -1,5 +1,24 @@
 // Attention of documents of unlike lengths (dllm_attention): grouped heads,
 // positional masks, capped scores and distance biases.
+//
+// A row is one query of one head.  The G = n_heads / n_kv_heads query heads of a
+// key/value head are rows of the same tile (row r = query r / G, head r % G), so
+// each key and value is read once for all of them.  A wave owns 32 rows and
+// computes, per tile of KT keys,
+//   S^T (keys x 32 rows) = K . Q^T      (Q held in registers)
+// so that a lane holds scores of a single row, and the running maximum and sum of
+// the softmax cost one exchange with lane ^ 32; then
+//   O^T (hd x 32 rows) += V^T . P^T
+// whose P^T operand is the score registers as they stand: the V^T operand takes
+// its keys in the same order (bf16: LDS reads that transpose 4 x 16 blocks;
+// float32: one key per lane half), so V is staged as it lies in memory.
+//
+// A workgroup has QG x KG waves: wave w takes the 32 rows w % QG of its row tile
+// and the key tiles of group w / QG; the groups' states meet in LDS at the end.
+// Each step brings KG tiles of K and V into an S-stage LDS ring by LDS-DMA.
+// Where rows are few, the keys of a document are also split over workgroups
+// (chunks of whole steps); each leaves its state in the workspace and
+// attn_join_kernel joins them in chunk order.
 #include <algorithm>
 
 #include "kernels.h"
@@ -8,91 +27,597 @@ namespace dllm {
 
 namespace {
 
-__device__ __forceinline__ float to_f(float x) { return x; }
-__device__ __forceinline__ float to_f(bf16_t x) { return bf2f(x); }
-__device__ __forceinline__ void from_f(float& y, float x) { y = x; }
-__device__ __forceinline__ void from_f(bf16_t& y, float x) { y = f2bf(x); }
+typedef __attribute__((address_space(3))) void* lds_ptr_t;
+typedef short v4s_t __attribute__((ext_vector_type(4)));
+typedef unsigned short v2us_t __attribute__((ext_vector_type(2)));
+typedef __attribute__((address_space(3))) v4s_t* lds_v4s_t;
+
+constexpr float LOG2E = 1.4426950408889634f;
 
 // A document's ranges, cut to its slab and to the maxima.
 struct Doc {
   int q0, nq, k0, nk, pos, prefix;
 };
 __device__ __forceinline__ Doc doc_of(const AttnArgs& a, int d) {
-  auto cut = [](const int32_t* start, const int32_t* len, int d, int tokens, int most, int& s, int& n) {
-    s = start ? min(max(start[d], 0), tokens) : 0;
-    n = min(min(max(len ? len[d] : tokens, 0), tokens - s), most);
-  };
   Doc r;
-  cut(a.q_start, a.q_len, d, a.q_tokens, a.max_q, r.q0, r.nq);
-  cut(a.kv_start, a.kv_len, d, a.kv_tokens, a.max_kv, r.k0, r.nk);
+  r.q0 = a.q_start ? min(max(a.q_start[d], 0), a.q_tokens) : 0;
+  r.nq = min(min(max(a.q_len ? a.q_len[d] : a.q_tokens, 0), a.q_tokens - r.q0), a.max_q);
+  r.k0 = a.kv_start ? min(max(a.kv_start[d], 0), a.kv_tokens) : 0;
+  r.nk = min(min(max(a.kv_len ? a.kv_len[d] : a.kv_tokens, 0), a.kv_tokens - r.k0), a.max_kv);
   r.pos = a.q_pos ? a.q_pos[d] : r.nk - r.nq;
   r.prefix = a.prefix ? a.prefix[d] : 0;
   return r;
 }
-// Keys 0 .. n - 1 that a query at position i sees.
-__device__ __forceinline__ int sees(const AttnArgs& a, const Doc& d, long i) {
+// Keys 0 .. n - 1 that query t of the document sees.
+__device__ __forceinline__ int sees(const AttnArgs& a, const Doc& d, int t) {
   if (a.block == 0) return d.nk;
-  const long f = i >= 0 ? i / a.block : -((-i + a.block - 1) / a.block);  // floor
-  return (int)min((long)d.nk, max(max((f + 1) * a.block, (long)d.prefix), 0l));
+  const long i = (long)d.pos + t;
+  if (i < 0) return min(d.nk, max(d.prefix, 0));  // its own block ends at or before position 0
+  return (int)min((long)d.nk, max((i / a.block + 1) * a.block, (long)d.prefix));
 }
 
-// One wave per (query, head): 64 keys at a time, one per lane, then the lanes
-// take two dimensions each.
+template <int N>
+__device__ __forceinline__ void wait_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (15 << 8) | ((N >> 4) << 14));
+}
+__device__ __forceinline__ void barrier_nofence() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+// 2^x by the hardware instruction alone: results below 2^-126 count as zero.
+__device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+// max / sum over lanes l and l ^ 32, which hold the halves of one row's scores
+__device__ __forceinline__ float max_pair32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float sum_pair32(float x) {
+  const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// LDS tiles: rows of HD elements (one key each) in 16-byte chunks, chunk c of
+// row r in slot c ^ swizzle(r), such that the lanes of one pass of a read meet
+// all 64 banks: K is read in 16-byte chunks of 16 consecutive rows; V in four
+// consecutive rows of 32 bf16 (the transposing read), or in 32 floats of rows r
+// and r + 4.
 template <typename T, int HD>
-__global__ void __launch_bounds__(64) attn_plain_kernel(AttnArgs a) {
-  const int lane = threadIdx.x, h = blockIdx.y, dn = blockIdx.z;
+struct Tile {
+  static constexpr int ROW = HD * (int)sizeof(T), CH = ROW / 16;  // bytes and chunks of a row
+  static __device__ __forceinline__ int k_swz(int r) { return (CH >= 16 ? r : r >> 1) & (CH >= 16 ? 15 : 7); }
+  static __device__ __forceinline__ int v_swz(int r) {
+    if (sizeof(T) == 4) return ((r >> 2) & 1) << 3;
+    return CH >= 16 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
+  }
+};
+
+// State of 32 rows: running maximum (log2 units), sum and output.
+template <int HD>
+struct State {
+  f32x16_t o[HD / 32];
+  float m, l;
+};
+
+// One row tile against the keys kb .. ke - 1 of its document.
+template <typename T, int HD, int QG, int KG, int KT, int S>
+__global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, AttnPlan p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  typedef Tile<T, HD> TL;
+  constexpr bool BF = sizeof(T) == 2;
+  constexpr int NW = QG * KG, D = S - 1, ND = HD / 32;
+  constexpr int K_BYTES = KT * TL::ROW, TILE = 2 * K_BYTES, STAGE = KG * TILE;
+  constexpr int TP = TILE / 1024, PER = TP / QG;  // LDS-DMA instructions of 1 KiB: of a tile, of a wave
+  static_assert(TP % (2 * QG) == 0, "the waves of a key group share a tile's loads evenly");
+  constexpr int MERGE = (NW - QG) * (ND * 4 + 1) * 64 * 16;
+  __shared__ __attribute__((aligned(1024))) char lds[S * STAGE > MERGE ? S * STAGE : MERGE];
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qg = wave % QG, kg = wave / QG;
+  const int lq = lane & 31, half = lane >> 5;
+
+  // Workgroup i runs on XCD i % 8.  A unit is (document, chunk, key/value head);
+  // its row tiles, which read the same keys, go to one XCD (to `parts` of them
+  // where units are too few for eight), the tiles with most keys first.
+  const int i8 = (int)blockIdx.x >> 3, x8 = (int)blockIdx.x & 7;
+  const int up = (i8 / p.part_tiles) * 8 + x8;  // unit and part
+  const int unit = up / p.parts, tile = p.tiles - 1 - ((i8 % p.part_tiles) * p.parts + up % p.parts);
+  if (unit >= p.units || tile < 0) return;
+  const int g = unit % a.Hkv, rest = unit / a.Hkv, chunk = rest % p.chunks, dn = rest / p.chunks;
   const Doc d = doc_of(a, dn);
-  const int t = blockIdx.x;
-  if (t >= d.nq) return;
-  const int g = h / (a.Hq / a.Hkv);
-  const T* q = static_cast<const T*>(a.q.data) + dn * a.q.stride_b + (long)(d.q0 + t) * a.q.stride_l + h * a.q.stride_h;
-  const T* kb = static_cast<const T*>(a.k.data) + dn * a.k.stride_b + (long)d.k0 * a.k.stride_l + g * a.k.stride_h;
-  const T* vb = static_cast<const T*>(a.v.data) + dn * a.v.stride_b + (long)d.k0 * a.v.stride_l + g * a.v.stride_h;
-  T* o = static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h;
-  const long pos = (long)d.pos + t;
-  const int n = sees(a, d, pos);
-  const float slope = a.slopes ? a.slopes[h] : 0.f;
-  __shared__ float ps[64];
-  float m = -INFINITY, l = 0.f, acc[HD / 64] = {};
-  for (int k0 = 0; k0 < n; k0 += 64) {
-    const int j = k0 + lane;
-    float s = -INFINITY;
-    if (j < n) {
-      s = 0.f;
-      for (int e = 0; e < HD; ++e) s = fmaf(to_f(q[e]), to_f(kb[(long)j * a.k.stride_l + e]), s);
-      s *= a.scale;
-      if (a.cap > 0) s = a.cap * tanhf(s / a.cap);
-      if (a.slopes) s -= slope * fabsf((float)(pos - j));
+  const int G = a.Hq / a.Hkv, rows = d.nq * G, r0 = tile * 32 * QG;
+  if (r0 >= rows) return;
+  const int t_last = (min(r0 + 32 * QG, rows) - 1) / G;
+  const int kb = chunk * p.chunk_keys, ke = min(sees(a, d, t_last), p.chunks > 1 ? kb + p.chunk_keys : 0x7fffffff);
+  if (chunk > 0 && kb >= ke) return;
+  // this wave's rows and this lane's
+  const int w0 = r0 + 32 * qg, w1 = min(w0 + 32, rows);
+  const int see_first = w0 < rows ? sees(a, d, w0 / G) : 0, see_last = w0 < rows ? sees(a, d, (w1 - 1) / G) : 0;
+  const int row = w0 + lq, t = row / G, h = g * G + row % G;
+  const bool mine = row < rows;
+  const int my_end = mine ? sees(a, d, t) : 0;
+  const float slope = a.slopes && mine ? a.slopes[h] * LOG2E : 0.f;
+  const bool neg = a.scale < 0.f;  // scores are formed with |scale| and, where it is negative, -q
+  const float sc = fabsf(a.scale) * LOG2E;
+  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f;
+  const bool direct = a.cap == 0.f && !a.slopes;
+
+  // K and V of this head, as bytes; a tile's buffer starts at its first key
+  const char* kp = static_cast<const char*>(a.k.data) +
+                   (dn * a.k.stride_b + d.k0 * a.k.stride_l + g * a.k.stride_h) * (long)sizeof(T);
+  const char* vp = static_cast<const char*>(a.v.data) +
+                   (dn * a.v.stride_b + d.k0 * a.v.stride_l + g * a.v.stride_h) * (long)sizeof(T);
+  const uint32_t ksb = (uint32_t)(a.k.stride_l * sizeof(T)), vsb = (uint32_t)(a.v.stride_l * sizeof(T));
+  // The waves of a key group load its tile: wave qg the parts qg, qg + QG, ..,
+  // K's before V's; a part is 1 KiB of whole rows, lane l filling slot l % CH
+  // of row l / CH
+  constexpr int RPP = 1024 / TL::ROW;  // rows of a part
+  uint32_t off[PER];
+#pragma unroll
+  for (int x = 0; x < PER; ++x) {
+    const bool isk = x < PER / 2;
+    const int r = (qg + QG * (x % (PER / 2))) * RPP + lane / TL::CH;
+    const int c = (lane % TL::CH) ^ (isk ? TL::k_swz(r) : TL::v_swz(r));
+    off[x] = r * (isk ? ksb : vsb) + c * 16;
+  }
+  auto issue = [&](int u) {
+    char* base = lds + (u % S) * STAGE + kg * TILE + qg * 1024;
+    const int t0 = kb + (u * KG + kg) * KT;
+    const int left = min(ke - t0, KT);  // reads past the last key give zeros
+    const uint32_t n = left > 0 ? left - 1 : 0, any = left > 0 ? TL::ROW : 0u;
+    const long from = left > 0 ? t0 : 0;
+    const __amdgpu_buffer_rsrc_t rk =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(kp + from * ksb), 0, n * ksb + any, 0x00020000);
+    const __amdgpu_buffer_rsrc_t rv =
+        __builtin_amdgcn_make_buffer_rsrc((void*)(vp + from * vsb), 0, n * vsb + any, 0x00020000);
+#pragma unroll
+    for (int x = 0; x < PER; ++x) {
+      const bool isk = x < PER / 2;
+      char* to = base + (isk ? x * QG * 1024 : K_BYTES + (x - PER / 2) * QG * 1024);
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(isk ? rk : rv, (lds_ptr_t)to, 16, off[x], 0, 0, 0);
     }
-    float top = s;
-    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
-    const float m_new = fmaxf(m, top);
-    const float ref = m_new == -INFINITY ? 0.f : m_new;
-    const float alpha = expf(m - ref), p = j < n ? expf(s - ref) : 0.f;
-    m = m_new;
-    l = l * alpha + warp_sum(p);
-    __syncthreads();
-    ps[lane] = p;
-    __syncthreads();
-    for (int e = 0; e < HD / 64; ++e) {
-      acc[e] *= alpha;
-      for (int x = 0; x < min(64, n - k0); ++x)
-        acc[e] = fmaf(ps[x], to_f(vb[(long)(k0 + x) * a.v.stride_l + e * 64 + lane]), acc[e]);
+  };
+  const int nsteps = ke > kb ? (ke - kb + KG * KT - 1) / (KG * KT) : 0;
+
+  // Q operand: this lane's row, dims 16 ks + 8 half .. (bf16), 8 c + 4 half .. (float32)
+  constexpr int NQ = BF ? HD / 16 : HD / 8;
+  typedef float f32x4v __attribute__((ext_vector_type(4)));
+  bf16x8_t qb[BF ? NQ : 1];
+  f32x4v qf[BF ? 1 : NQ];
+  {
+    const T* qrow = static_cast<const T*>(a.q.data) + dn * a.q.stride_b + (long)(d.q0 + (mine ? t : 0)) * a.q.stride_l +
+                    (mine ? h : 0) * a.q.stride_h;
+#pragma unroll
+    for (int c = 0; c < NQ; ++c) {
+      uint4 w = *reinterpret_cast<const uint4*>(qrow + c * (BF ? 16 : 8) + half * (BF ? 8 : 4));
+      const uint32_t flip = neg ? (BF ? 0x80008000u : 0x80000000u) : 0u;
+      w.x ^= flip;
+      w.y ^= flip;
+      w.z ^= flip;
+      w.w ^= flip;
+      if (!mine) w = make_uint4(0, 0, 0, 0);
+      if constexpr (BF)
+        qb[c] = __builtin_bit_cast(bf16x8_t, w);
+      else
+        qf[c] = __builtin_bit_cast(f32x4v, w);
     }
   }
-  for (int e = 0; e < HD / 64; ++e) from_f(o[e * 64 + lane], l == 0.f ? 0.f : acc[e] / l);
+
+  State<HD> st;
+#pragma unroll
+  for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) st.o[ds][r] = 0.f;
+  st.m = -INFINITY;
+  st.l = 0.f;
+  float m_ref = 0.f;  // the maximum that exponents are taken against: m, or 0 while m is -inf
+
+#pragma unroll
+  for (int s = 0; s < D; ++s)
+    if (s < nsteps) issue(s);
+  constexpr int NS = KT / 32;  // 32-key score blocks of a tile
+  for (int u = 0; u < nsteps; ++u) {
+    // stages in flight behind this one: D - 1, fewer at the end
+    if (u + D <= nsteps)
+      wait_vmcnt<PER*(D - 1)>();
+    else
+      wait_vmcnt<0>();
+    // stage u is there; every wave is done with the one refilled next (with one
+    // row group a wave reads only what it loaded itself)
+    if constexpr (QG > 1)
+      barrier_nofence();
+    else
+      asm volatile("" ::: "memory");
+    if (u + D < nsteps) issue(u + D);
+    const int t0 = kb + (u * KG + kg) * KT;
+    if (t0 >= min(ke, see_last)) continue;  // nothing that this wave's rows see
+    const char* kt = lds + (u % S) * STAGE + kg * TILE;
+    const char* vt = kt + K_BYTES;
+
+    f32x16_t s2[NS];
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) s2[b][r] = 0.f;
+    if constexpr (BF) {
+      bf16x8_t kf[NQ][NS];
+#pragma unroll
+      for (int c = 0; c < NQ; ++c)
+#pragma unroll
+        for (int b = 0; b < NS; ++b) {
+          const int r = b * 32 + lq;
+          kf[c][b] = *reinterpret_cast<const bf16x8_t*>(kt + r * TL::ROW + (((c * 2 + half) ^ TL::k_swz(r)) << 4));
+        }
+#pragma unroll
+      for (int c = 0; c < NQ; ++c)
+#pragma unroll
+        for (int b = 0; b < NS; ++b) s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c][b], qb[c], s2[b], 0, 0, 0);
+    } else {
+#pragma unroll
+      for (int c = 0; c < NQ; ++c)
+#pragma unroll
+        for (int b = 0; b < NS; ++b) {
+          const int r = b * 32 + lq;
+          const f32x4v k4 = *reinterpret_cast<const f32x4v*>(kt + r * TL::ROW + (((c * 2 + half) ^ TL::k_swz(r)) << 4));
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s2[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[c][e], s2[b], 0, 0, 0);
+        }
+    }
+
+    // register r of block b holds key t0 + 32 b + 8 (r / 4) + 4 half + r % 4
+    const bool whole = t0 + KT <= min(ke, see_first);
+    float mt = -INFINITY;
+    float fold = sc;  // factor still to be applied in the exponent
+    if (direct && whole) {
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s2[b][r]);
+      mt *= sc;
+    } else {
+      fold = 1.f;
+      if (a.cap > 0.f) {
+        // cap tanh(x / cap) = cap - 2 cap / (e^(2 x / cap) + 1)
+#pragma unroll
+        for (int b = 0; b < NS; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s2[b][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(exp2_hw(s2[b][r] * cap_in) + 1.f), cap2);
+      } else {
+#pragma unroll
+        for (int b = 0; b < NS; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) s2[b][r] *= sc;
+      }
+      if (a.slopes) {
+        const float at = (float)((long)d.pos + t - t0 - 4 * half);
+#pragma unroll
+        for (int b = 0; b < NS; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r)
+            s2[b][r] = fmaf(-slope, fabsf(at - (float)(32 * b + 8 * (r >> 2) + (r & 3))), s2[b][r]);
+      }
+      const int end = min(my_end, ke) - t0 - 4 * half;
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          if (!whole && 32 * b + 8 * (r >> 2) + (r & 3) >= end) s2[b][r] = -INFINITY;
+          mt = fmaxf(mt, s2[b][r]);
+        }
+    }
+    mt = max_pair32(mt);
+    // the maximum is raised only when it grows by more than 2^8 (probabilities
+    // then stay below 2^8, at the same relative precision)
+    if (__ballot(mt > st.m + 8.f) != 0ull) {
+      const float m_new = fmaxf(st.m, mt);
+      const float alpha = exp2_hw(st.m - (m_new == -INFINITY ? 0.f : m_new));
+      st.m = m_new;
+      m_ref = m_new == -INFINITY ? 0.f : m_new;
+      st.l *= alpha;
+#pragma unroll
+      for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) st.o[ds][r] *= alpha;
+    }
+    float psum = 0.f;
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const float e = exp2_hw(fmaf(s2[b][r], fold, -m_ref));
+        s2[b][r] = e;
+        psum += e;
+      }
+    st.l += psum;
+
+    // values of keys that some row of the tile does not see, where they are no
+    // numbers, must not meet that row's zero probability in a product
+    bool broken = false;
+    if (!whole) {
+      constexpr uint32_t E = BF ? 0x7f807f80u : 0x7f800000u;  // exponents of a word
+      uint32_t top = 0;
+      const uint4* words = reinterpret_cast<const uint4*>(vt);
+#pragma unroll 4
+      for (int i = lane; i < K_BYTES / 16; i += 64) {
+        const uint4 w = words[i];
+        for (const uint32_t x : {w.x & E, w.y & E, w.z & E, w.w & E})
+          if constexpr (BF)
+            top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us_t, top), __builtin_bit_cast(v2us_t, x)));
+          else
+            top = max(top, x);
+      }
+      broken = __ballot((top & 0xffffu) == 0x7f80u || (top >> 16) == 0x7f80u) != 0ull;
+    }
+    if (broken) {
+      for (int key = 0; key < KT; ++key) {
+        const char* vrow = vt + key * TL::ROW;
+        const bool seen = t0 + key < min(my_end, ke);
+#pragma unroll
+        for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const int e = ds * 32 + 8 * (r >> 2) + 4 * half + (r & 3), b = e * (int)sizeof(T);
+            const T w = *reinterpret_cast<const T*>(vrow + ((((b >> 4) ^ TL::v_swz(key)) << 4) | (b & 15)));
+            float f;
+            if constexpr (BF)
+              f = bf2f(w);
+            else
+              f = w;
+            if (seen && !(fabsf(f) < INFINITY)) st.o[ds][r] += f;
+          }
+      }
+    }
+    auto number = [&](uint32_t w) {  // non-numbers as zero
+      if constexpr (BF) {
+        if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+        if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+      } else {
+        if ((w & 0x7f800000u) == 0x7f800000u) w = 0;
+      }
+      return w;
+    };
+    if constexpr (BF) {
+      // slice jk: keys 16 jk + 4 half .. and 16 jk + 8 + 4 half ..; lane n of 16
+      // gives the address of row n / 4, columns 4 (n % 4) .. of its 4 x 16 block
+      // and receives column n
+      const int n = lane & 15, c16 = (lane >> 4) & 1, vr = n >> 2;
+      const char* vb = vt + (4 * half + vr) * TL::ROW;
+#pragma unroll
+      for (int jk = 0; jk < KT / 16; ++jk) {
+        bf16x8_t pf;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t w = pack_bf16x2(s2[jk >> 1][(jk & 1) * 8 + 2 * e], s2[jk >> 1][(jk & 1) * 8 + 2 * e + 1]);
+          pf[2 * e] = (short)(w & 0xffff);
+          pf[2 * e + 1] = (short)(w >> 16);
+        }
+#pragma unroll
+        for (int ds = 0; ds < ND; ++ds) {
+          const int e = ds * 32 + c16 * 16 + 4 * (n & 3);
+          const char* at = vb + jk * 16 * TL::ROW + ((((e >> 3) ^ TL::v_swz(vr)) << 4) | ((e & 7) * 2));
+          const v4s_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)at);
+          const v4s_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(at + 8 * TL::ROW));
+          uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
+          if (broken) {
+            x.x = number(x.x);
+            x.y = number(x.y);
+            y.x = number(y.x);
+            y.y = number(y.y);
+          }
+          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(x.x, x.y, y.x, y.y));
+          st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, st.o[ds], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int b = 0; b < NS; ++b)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int key = 32 * b + 8 * (r >> 2) + (r & 3);
+#pragma unroll
+          for (int ds = 0; ds < ND; ++ds) {
+            const int e = ds * 32 + lq;
+            uint32_t w = *reinterpret_cast<const uint32_t*>(vt + (key + 4 * half) * TL::ROW +
+                                                            ((((e >> 2) ^ (half << 3)) << 4) | ((e & 3) * 4)));
+            if (broken) w = number(w);
+            st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w), s2[b][r], st.o[ds], 0, 0, 0);
+          }
+        }
+    }
+  }
+  st.l = sum_pair32(st.l);
+
+  if constexpr (KG > 1) {
+    // the key groups' states join in group order: group 0's wave takes the others'
+    __syncthreads();
+    float4* sh = reinterpret_cast<float4*>(lds);
+    if (kg > 0) {
+      float4* to = sh + (size_t)(wave - QG) * (ND * 4 + 1) * 64 + lane;
+#pragma unroll
+      for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          to[(ds * 4 + r) * 64] = make_float4(st.o[ds][4 * r], st.o[ds][4 * r + 1], st.o[ds][4 * r + 2], st.o[ds][4 * r + 3]);
+      to[ND * 4 * 64] = make_float4(st.m, st.l, 0.f, 0.f);
+    }
+    __syncthreads();
+    if (kg > 0) return;
+    for (int k2 = 1; k2 < KG; ++k2) {
+      const float4* from = sh + (size_t)(k2 * QG + qg - QG) * (ND * 4 + 1) * 64 + lane;
+      const float4 ml = from[ND * 4 * 64];
+      const float m_new = fmaxf(st.m, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float fa = exp2_hw(st.m - ref), fb = exp2_hw(ml.x - ref);
+      st.m = m_new;
+      st.l = st.l * fa + ml.y * fb;
+#pragma unroll
+      for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+          const float4 w = from[(ds * 4 + r) * 64];
+          st.o[ds][4 * r] = st.o[ds][4 * r] * fa + w.x * fb;
+          st.o[ds][4 * r + 1] = st.o[ds][4 * r + 1] * fa + w.y * fb;
+          st.o[ds][4 * r + 2] = st.o[ds][4 * r + 2] * fa + w.z * fb;
+          st.o[ds][4 * r + 3] = st.o[ds][4 * r + 3] * fa + w.w * fb;
+        }
+    }
+  }
+  if (!mine) return;
+  if (p.chunks > 1) {
+    // state of (document, query, head) for this chunk: hd outputs, then (m, l)
+    const size_t at = (((size_t)dn * a.max_q + t) * a.Hq + h) * p.chunks + chunk;
+    float* to = p.part + at * HD;
+#pragma unroll
+    for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+      for (int r = 0; r < 4; ++r)
+        *reinterpret_cast<float4*>(to + ds * 32 + 8 * r + 4 * half) =
+            make_float4(st.o[ds][4 * r], st.o[ds][4 * r + 1], st.o[ds][4 * r + 2], st.o[ds][4 * r + 3]);
+    if (half == 0) p.part_ml[at] = make_float2(st.m, st.l);
+    return;
+  }
+  const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
+  T* to = static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h;
+#pragma unroll
+  for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int e = ds * 32 + 8 * r + 4 * half;
+      const float4 w = make_float4(st.o[ds][4 * r] * inv, st.o[ds][4 * r + 1] * inv, st.o[ds][4 * r + 2] * inv, st.o[ds][4 * r + 3] * inv);
+      if constexpr (BF)
+        *reinterpret_cast<uint2*>(to + e) = make_uint2(pack_bf16x2(w.x, w.y), pack_bf16x2(w.z, w.w));
+      else
+        *reinterpret_cast<float4*>(to + e) = w;
+    }
+#endif
 }
+
+// Joins a row's chunk states in chunk order: one thread per four dimensions.
+template <typename T, int HD>
+__global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) {
+  constexpr int TPR = HD / 4, RPW = 256 / TPR;  // threads per row, rows per workgroup
+  const long row = (long)blockIdx.x * RPW + threadIdx.x / TPR;
+  const int e = threadIdx.x % TPR * 4;
+  if (row >= (long)a.docs * a.max_q * a.Hq) return;
+  const int h = (int)(row % a.Hq);
+  const long dt = row / a.Hq;
+  const int t = (int)(dt % a.max_q), dn = (int)(dt / a.max_q);
+  const Doc d = doc_of(a, dn);
+  if (t >= d.nq) return;
+  // chunks that the row's tile ran: all that it sees a key of
+  const int n = (sees(a, d, t) + p.chunk_keys - 1) / p.chunk_keys;
+  const float2* ml = p.part_ml + row * p.chunks;
+  const float* part = p.part + row * p.chunks * HD + e;
+  float m = -INFINITY;
+  for (int c = 0; c < n; ++c) m = fmaxf(m, ml[c].x);
+  const float ref = m == -INFINITY ? 0.f : m;
+  float l = 0.f;
+  float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int c = 0; c < n; ++c) {
+    const float2 s = ml[c];
+    const float f = exp2_hw(s.x - ref);
+    const float4 w = *reinterpret_cast<const float4*>(part + (size_t)c * HD);
+    l += s.y * f;
+    o.x += w.x * f;
+    o.y += w.y * f;
+    o.z += w.z * f;
+    o.w += w.w * f;
+  }
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  T* to = static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h + e;
+  if constexpr (sizeof(T) == 2)
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+  else
+    *reinterpret_cast<float4*>(to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+}
+
+// Which kernel a call takes and how its grid is laid out.  Sizes only.
+struct Choice {
+  int qg, kg, kt;
+  AttnPlan plan;
+  long grid;
+};
+Choice choose(const AttnArgs& a) {
+  Choice c{};
+  const bool f32 = a.dtype == DLLM_F32, wide_row = f32 && a.hd == 128;
+  const int rows = a.max_q * (a.Hq / a.Hkv);
+  if (rows <= 32) {
+    c.qg = 1;
+    c.kg = wide_row ? 2 : 4;
+    c.kt = 32;
+  } else if (rows <= 64) {
+    c.qg = 2;
+    c.kg = wide_row ? 2 : 4;
+    c.kt = 32;
+  } else {
+    c.qg = f32 ? 4 : 8;
+    c.kg = 1;
+    c.kt = f32 ? 32 : 64;
+  }
+  AttnPlan& p = c.plan;
+  p.tiles = ceil_div(rows, 32 * c.qg);
+  const long heads = (long)a.docs * a.Hkv, wgs = heads * p.tiles, cus = device_cu_count();
+  const int step = c.kg * c.kt, steps = std::max(1, ceil_div(a.max_kv, step));
+  int chunks = 1;
+  if (wgs < 2 * cus) chunks = (int)std::max(1l, std::min((2 * cus + wgs - 1) / wgs, (long)steps * step / 256));
+  const int per = ceil_div(steps, chunks);
+  p.chunk_keys = per * step;
+  p.chunks = ceil_div(steps, per);
+  const long units = heads * p.chunks;
+  p.units = (int)std::min(units, 0x7fffffffl);
+  p.parts = units % 8 == 0 || units >= 512 ? 1 : units >= 64 ? 2 : 8;
+  while (p.parts < 8 && units * p.parts % 8 && units < 64) p.parts *= 2;
+  p.part_tiles = ceil_div(p.tiles, p.parts);
+  c.grid = (long)ceil_div(units * p.parts, 8) * 8 * p.part_tiles;
+  return c;
+}
+
+template <typename T, int HD, int QG, int KG, int KT, int S>
+void go(const AttnArgs& a, const Choice& c, hipStream_t s) {
+  attn_docs_kernel<T, HD, QG, KG, KT, S><<<(unsigned)c.grid, 64 * QG * KG, 0, s>>>(a, c.plan);
+  DLLM_LAUNCH_CHECK("attn_docs_kernel");
+}
+template <typename T, int HD>
+void launch(const AttnArgs& a, const Choice& c, hipStream_t s) {
+  constexpr bool WIDE = sizeof(T) * HD == 512;  // rows of 512 bytes: half the keys fit
+  if (c.qg == 1)
+    go<T, HD, 1, WIDE ? 2 : 4, 32, 2>(a, c, s);
+  else if (c.qg == 2)
+    go<T, HD, 2, WIDE ? 2 : 4, 32, 2>(a, c, s);
+  else if constexpr (sizeof(T) == 4)
+    go<T, HD, 4, 1, 32, 3>(a, c, s);
+  else
+    go<T, HD, 8, 1, 64, 3>(a, c, s);
+  if (c.plan.chunks > 1) {
+    const long rows = (long)a.docs * a.max_q * a.Hq;
+    attn_join_kernel<T, HD><<<ceil_div(rows, 1024 / HD), 256, 0, s>>>(a, c.plan);
+    DLLM_LAUNCH_CHECK("attn_join_kernel");
+  }
+}
+
+size_t part_values(const AttnArgs& a, const AttnPlan& p) { return (size_t)a.docs * a.max_q * a.Hq * p.chunks; }
 
 }  // namespace
 
-size_t attn_docs_bytes(const AttnArgs&) { return 0; }
+size_t attn_docs_bytes(const AttnArgs& a) {
+  const Choice c = choose(a);
+  return c.plan.chunks > 1 ? part_values(a, c.plan) * (a.hd * 4 + 8) + 256 : 0;
+}
 
-void launch_attn_docs(const AttnArgs& a, void*, hipStream_t s) {
-  const dim3 grid(a.max_q, a.Hq, a.docs);
-  auto* f = a.dtype == DLLM_F32 ? (a.hd == 64 ? attn_plain_kernel<float, 64> : attn_plain_kernel<float, 128>)
-                                : (a.hd == 64 ? attn_plain_kernel<bf16_t, 64> : attn_plain_kernel<bf16_t, 128>);
-  f<<<grid, 64, 0, s>>>(a);
-  DLLM_LAUNCH_CHECK("attn_plain_kernel");
+bool attn_docs_fits(const AttnArgs& a) {
+  return (long)a.docs * a.Hkv * ceil_div((long)a.max_q * (a.Hq / a.Hkv), 32) < (1l << 28);
+}
+
+void launch_attn_docs(const AttnArgs& a, void* ws, hipStream_t s) {
+  Choice c = choose(a);
+  if (c.plan.chunks > 1) {
+    c.plan.part = static_cast<float*>(ws);
+    c.plan.part_ml = reinterpret_cast<float2*>(c.plan.part + part_values(a, c.plan) * a.hd);
+  }
+  if (a.dtype == DLLM_F32)
+    a.hd == 64 ? launch<float, 64>(a, c, s) : launch<float, 128>(a, c, s);
+  else
+    a.hd == 64 ? launch<bf16_t, 64>(a, c, s) : launch<bf16_t, 128>(a, c, s);
 }
 
 }  // namespace dllm

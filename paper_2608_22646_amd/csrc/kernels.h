@@ -228,7 +228,15 @@ struct AttnArgs {
   const float* slopes;
   float scale, cap;
 };
+// Layout of a call's grid: row tiles, units of (document, key chunk, key/value
+// head), and the chunks' states (part: hd floats each; part_ml: maximum and sum).
+struct AttnPlan {
+  int tiles, parts, part_tiles, units, chunks, chunk_keys;
+  float* part;
+  float2* part_ml;
+};
 size_t attn_docs_bytes(const AttnArgs& a);
+bool attn_docs_fits(const AttnArgs& a);  // its grid can be launched
 void launch_attn_docs(const AttnArgs& a, void* ws, hipStream_t s);
 
 // k_sample.hip: see dllm_sample; ws of sample_bytes(rows, vocab) bytes.

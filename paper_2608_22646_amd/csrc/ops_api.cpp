@@ -58,6 +58,7 @@ bool attn_args(const dllm_attn_args* p, AttnArgs* a) {
   require(p->docs >= 0 && p->docs <= 65535, DLLM_ESHAPE, "docs must be in [0, 65535]");
   require(p->max_q >= 0 && p->max_q <= p->q_tokens && p->max_kv >= 0 && p->max_kv <= p->kv_tokens, DLLM_ESHAPE,
           "max_q and max_kv must be in [0, q_tokens] and [0, kv_tokens]");
+  require(p->q_tokens <= (1 << 30) && p->kv_tokens <= (1 << 30), DLLM_ESHAPE, "a slab holds at most 2^30 tokens");
   require((int64_t)p->max_q * (p->n_heads / p->n_kv_heads) <= 0x7fffff00, DLLM_ESHAPE, "too many query rows");
   require(std::isfinite(p->scale), DLLM_EINVAL, "scale must be finite");
   require(std::isfinite(p->cap) && p->cap >= 0, DLLM_EINVAL, "cap must be finite and not negative");
@@ -74,6 +75,7 @@ bool attn_args(const dllm_attn_args* p, AttnArgs* a) {
   a->block = p->block;
   a->scale = p->scale;
   a->cap = p->cap;
+  require(attn_docs_fits(*a), DLLM_ESHAPE, "too many documents, heads and queries for one call");
   return p->docs > 0 && p->max_q > 0;
 }
 
