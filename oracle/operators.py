@@ -84,8 +84,9 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask_id=-1
     order = order[x[order] > -np.inf]
     if not temperature > 0:
         return int(order[0]), float(1.0 / e.sum()), 1.0
-    with np.errstate(over="ignore"):
+    with np.errstate(over="ignore", invalid="ignore"):
         w = np.exp((x - top) / temperature)
+    w[w < 2.0 ** -66] = 0.0
     if top_k >= 1:
         order = order[:top_k]
     if top_p < 1:
@@ -94,7 +95,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask_id=-1
         stay[0] = True
         order = order[stay]
     if min_p > 0:
-        order = order[w[order] >= min(min_p, 1.0)]
+        order = order[(top - x[order]) / temperature <= -math.log(min(min_p, 1.0))]    # w >= min_p
     kept = np.zeros(len(x), dtype=bool)
     kept[order] = True
     c = np.cumsum(np.where(kept, w, 0.0))
