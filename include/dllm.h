@@ -528,7 +528,7 @@ int dllm_attention(const dllm_attn_args* args, void* workspace, size_t workspace
  * the first, min_p > 1 counts as 1, and u is cut to [0, 1) (NaN: 0).
  * A row with a NaN or +inf candidate gives the first such index with conf and
  * prob NaN; a row without candidates gives token -1 with conf and prob 0.
- * Candidates with w below 2^-66 count as without mass.  Sums are held in 64
+ * Candidates with w below 2^-63 count as without mass.  Sums are held in 64
  * bits and do not depend on the order of execution: equal inputs give equal
  * outputs.
  */
@@ -548,7 +548,7 @@ typedef struct dllm_sample_args {
 } dllm_sample_args;
 
 /* rows of 0: nothing.  Errors: DLLM_EINVAL (null pointer, dtype), DLLM_ESHAPE
- * (sizes: rows >= 0, 1 <= vocab <= 2^22), DLLM_ENOMEM (workspace), DLLM_EHIP. */
+ * (sizes: 1 <= vocab <= 2^22, rows >= 0 and below 2^22 / ceil(vocab / 8192)), DLLM_ENOMEM (workspace), DLLM_EHIP. */
 int dllm_sample_workspace_size(int32_t rows, int32_t vocab, size_t* bytes);
 int dllm_sample(const dllm_sample_args* args, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -86,7 +86,7 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask_id=-1
         return int(order[0]), float(1.0 / e.sum()), 1.0
     with np.errstate(over="ignore", invalid="ignore"):
         w = np.exp((x - top) / temperature)
-    w[w < 2.0 ** -66] = 0.0
+    w[w < 2.0 ** -63] = 0.0
     if top_k >= 1:
         order = order[:top_k]
     if top_p < 1:

@@ -2,17 +2,22 @@
 //
 // Temperature, top-k, top-p and min-p each keep a prefix of one ranking (logit
 // descending, index ascending), so the kept set is a boundary in that ranking.
-// Two launches find it with one read of the logits and a part of a second:
+// It is found with one read of all logits and a second read of few:
 //
-//   sample_chunk_kernel  one workgroup per CHUNK logits of a row, held in
-//     registers: their maximum, the sum of the weights exp((x - max) / T), and a
-//     histogram of counts and weights over BINS classes of x / T, BINS_PER_NAT
-//     to a unit.  The classes lie on one grid for all chunks, so no chunk has to
-//     know the row's maximum.
-//   sample_row_kernel    one workgroup per row: joins the histograms, finds the
-//     class in which the boundary falls, orders that class's members alone by
-//     (logit, index), then finds the chunk and the token where the running sum of
-//     kept weights, in index order, passes u times its total.
+//   sample_chunk_kernel    a workgroup per CHUNK logits of a row, held in
+//     registers: their maximum, the sum of their weights exp((x - max) / T), and
+//     counts and weights of BINS classes of x / T, eight to an octave of weight.
+//     The classes lie on one grid for all chunks, so no chunk has to know the
+//     row's maximum.
+//   sample_edge_kernel     a workgroup per row: joins the classes and finds those
+//     in which the boundary may fall.
+//   sample_collect_kernel  a workgroup per chunk that has members of them: lists
+//     their (logit, index).
+//   sample_pick_kernel     a workgroup per row: the boundary among the listed
+//     members, the kept mass of each chunk, and the chunk and then the token where
+//     the running sum of kept weights, in index order, passes u times its total.
+//
+// Calls without top-k, top-p and min-p need the first and the last alone.
 //
 // Which token wins must not depend on rounding or on the order of execution.
 // Weights are float64 throughout; where threads add concurrently they add whole
@@ -26,11 +31,21 @@ namespace dllm {
 
 namespace {
 
-constexpr int CHUNK = 8192, NT1 = 512, E1 = CHUNK / NT1;
-constexpr int BINS = 512;               // the last one takes everything without mass
-constexpr double BINS_PER_NAT = 11.0;   // 510 / 11 = 46.3 > 66 ln 2
-constexpr double LEAST = 0x1p-66;       // weights below count as none
-constexpr int NT2 = 512, LIST = 4096, MAX_CHUNKS = (1 << 22) / CHUNK;
+constexpr int CHUNK = 8192, NT = 512, E = CHUNK / NT, NW = NT / 64;
+constexpr int BINS = 512;               // 64 octaves; the last class takes everything without mass
+constexpr double PER_NAT = 11.541560327111707;  // 8 / ln 2
+constexpr double LEAST = 0x1p-63;       // weights below count as none
+constexpr int LIST = 8192;              // members listed of a row
+constexpr int SLOTS = 4;                // classes listed of a row
+constexpr int MAX_CHUNKS = (1 << 22) / CHUNK;
+static_assert(BINS == NT, "a thread per class");
+
+// Global memory, said outright: pointers out of structures are else read as flat ones.
+#if defined(__HIP_DEVICE_COMPILE__)
+#define GLOBAL __attribute__((address_space(1)))
+#else
+#define GLOBAL
+#endif
 
 __device__ __forceinline__ float to_f(float x) { return x; }
 __device__ __forceinline__ float to_f(bf16_t x) { return bf2f(x); }
@@ -44,26 +59,27 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
-// e^x for x <= 0 to 1e-14 relative: 2^k times the Taylor polynomial of degree 11
-// over half a binade (its remainder is 6e-15); 0 below e^-700.
-__device__ __forceinline__ double exp_neg(double x) {
-  x = fmax(x, -700.0);
-  const double k = rint(x * 1.4426950408889634);
-  double r = fma(k, -0.693147180559945286, x);
-  r = fma(k, -2.319046813846299558e-17, r);
-  double p = 1.0 / 39916800;
-  p = fma(p, r, 1.0 / 3628800);
-  p = fma(p, r, 1.0 / 362880);
-  p = fma(p, r, 1.0 / 40320);
-  p = fma(p, r, 1.0 / 5040);
-  p = fma(p, r, 1.0 / 720);
-  p = fma(p, r, 1.0 / 120);
-  p = fma(p, r, 1.0 / 24);
-  p = fma(p, r, 1.0 / 6);
-  p = fma(p, r, 0.5);
-  p = fma(p, r, 1.0);
-  p = fma(p, r, 1.0);
-  return ldexp(p, (int)k);
+// 2^(j / 8), j < 8, in LDS.
+__device__ __forceinline__ void fill_eighths(double* t) {
+  if (threadIdx.x < 8) t[threadIdx.x] = exp2(threadIdx.x * 0.125);
+}
+// 2^(d / 8) for d <= 0: whole eighths by table and exponent, the rest (at most
+// half of one) by the Taylor polynomial of degree 7, whose remainder is 3e-16.
+// Exactly 1 at 0; 2^-1000 stands for everything below.
+__device__ __forceinline__ double weight_of(double d, const double* eighths) {
+  constexpr double L = 0.08664339756999316;  // ln 2 / 8
+  d = fmax(d, -8000.0);
+  const double n = rint(d), f = (d - n) * L;
+  double p = 1.0 / 5040;
+  p = fma(p, f, 1.0 / 720);
+  p = fma(p, f, 1.0 / 120);
+  p = fma(p, f, 1.0 / 24);
+  p = fma(p, f, 1.0 / 6);
+  p = fma(p, f, 0.5);
+  p = fma(p, f, 1.0);
+  p = fma(p, f, 1.0);
+  const int i = (int)n;
+  return ldexp(p * eighths[i & 7], i >> 3);
 }
 // A weight w in [0, 1] as a whole number of 2^-50: the mantissa of 4 + w.
 __device__ __forceinline__ uint64_t fixed50(double w) {
@@ -76,6 +92,16 @@ __device__ __forceinline__ V wave_all(V x, F f) {
   for (int s = 32; s > 0; s >>= 1) x = f(x, (V)__shfl_xor(x, s, 64));
   return x;
 }
+struct Max {
+  template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a > b ? a : b; }
+};
+struct Min {
+  template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a < b ? a : b; }
+};
+struct Sum {
+  template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
+};
+typedef unsigned long long u64;
 
 // What a chunk leaves: its largest logit, the lowest index of a NaN or +inf (or
 // ~0), the lowest index of the maximum, and its sums at the row's temperature
@@ -83,21 +109,34 @@ __device__ __forceinline__ V wave_all(V x, F f) {
 struct ChunkStat {
   float top;
   uint32_t bad, arg, pad;
-  uint64_t sum;
+  u64 sum;
   double sum1;
+};
+// What sample_edge_kernel leaves: the boundary as far as the classes tell it.
+// Under top-k the classes below `ek` stay, of class ek - 1 the first rk members
+// only where rk > 0; [lo, hi] are the classes in which top-p's boundary can fall;
+// class bm holds min-p's (-1: none).
+struct RowState {
+  int ek, rk, lo, hi, bm;
+  int slot[SLOTS];  // classes listed, -1: none
 };
 
 struct SampleWs {
   ChunkStat* stat;   // [rows, chunks]
-  uint64_t* mass;    // [rows, chunks, BINS] in 2^-50
+  u64* mass;         // [rows, chunks, BINS] in 2^-50
   uint32_t* count;   // [rows, chunks, BINS]
+  double* prefix;    // [rows, BINS]: mass of the classes up to each
+  uint32_t* prefix_n;
+  RowState* state;   // [rows]
+  uint2* list;       // [rows, LIST]: key, index | slot << 24
+  uint32_t* listed;  // [rows]
   int chunks;
 };
 
 // A row's controls.
 struct Controls {
   bool greedy, filter;
-  double inv_t, top_p, min_p;
+  double inv_t, rate, top_p, min_p;  // rate: classes per unit of logit
   int top_k;
 };
 __device__ __forceinline__ Controls controls_of(const SampleArgs& a, int r) {
@@ -105,6 +144,7 @@ __device__ __forceinline__ Controls controls_of(const SampleArgs& a, int r) {
   const float t = a.temperature ? a.temperature[r] : 1.f;
   c.greedy = !(t > 0.f);
   c.inv_t = c.greedy ? 1.0 : 1.0 / (double)t;
+  c.rate = c.inv_t * PER_NAT;
   const int k = a.top_k ? a.top_k[r] : 0;
   c.top_k = k >= 1 && k < a.vocab ? k : 0;
   const float p = a.top_p ? a.top_p[r] : 1.f;
@@ -114,8 +154,16 @@ __device__ __forceinline__ Controls controls_of(const SampleArgs& a, int r) {
   c.filter = !c.greedy && (c.top_k > 0 || c.top_p < 1.0 || c.min_p > 0.0);
   return c;
 }
-// Class of a logit on the grid that all rows of a temperature share.
-__device__ __forceinline__ double class_of(float x, double rate) { return floor((double)x * rate); }
+// A logit in units of classes.  Never fused into a following subtraction: the
+// largest logit then stands at a distance of exactly 0 from itself.
+__device__ __forceinline__ double in_classes(float x, double rate) {
+#pragma clang fp contract(off)
+  return (double)x * rate;
+}
+// Class of a logit in a row whose maximum lies in class `base` of the grid.
+__device__ __forceinline__ int class_of(float x, double rate, double base) {
+  return (int)fmin(base - floor(in_classes(x, rate)), (double)(BINS - 1));
+}
 
 // N consecutive logits from v on (rows may start at any element: the loads are
 // only as aligned as the type); -inf past the row and at the mask token.
@@ -124,13 +172,14 @@ __device__ __forceinline__ void load_logits(const T* x, int v, int V, int mask_i
   struct __attribute__((packed, aligned(sizeof(T)))) Run {
     T e[N];
   };
+  const GLOBAL T* g = (const GLOBAL T*)x + v;
   if (v + N <= V) {
-    const Run r = *reinterpret_cast<const Run*>(x + v);
+    const Run r = *(const GLOBAL Run*)g;
 #pragma unroll
     for (int i = 0; i < N; ++i) f[i] = to_f(r.e[i]);
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i) f[i] = v + i < V ? to_f(x[v + i]) : -INFINITY;
+    for (int i = 0; i < N; ++i) f[i] = v + i < V ? to_f(g[i]) : -INFINITY;
   }
   if ((uint32_t)(mask_id - v) < (uint32_t)N) {
 #pragma unroll
@@ -140,21 +189,23 @@ __device__ __forceinline__ void load_logits(const T* x, int v, int V, int mask_i
 }
 
 template <typename T>
-__global__ void __launch_bounds__(NT1) sample_chunk_kernel(SampleArgs a, SampleWs w) {
-  __shared__ uint64_t mass[BINS];
+__global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs w) {
+  __shared__ u64 mass[BINS];
   __shared__ uint32_t count[BINS];
-  __shared__ float s_top[NT1 / 64];
-  __shared__ uint32_t s_bad[NT1 / 64], s_arg[NT1 / 64];
-  __shared__ uint64_t s_sum[NT1 / 64];
-  __shared__ double s_sum1[NT1 / 64];
+  __shared__ double eighths[8];
+  __shared__ float s_top[NW];
+  __shared__ uint32_t s_bad[NW], s_arg[NW];
+  __shared__ u64 s_sum[NW];
+  __shared__ double s_sum1[NW];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, v0 = chunk * CHUNK;
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
-  const Controls c = controls_of(a, row);
-  constexpr int N = 16 / sizeof(T), RUNS = E1 / N;  // 16-byte runs
+  constexpr int N = 16 / sizeof(T), RUNS = E / N;  // 16-byte runs
   float f[RUNS][N];
 #pragma unroll
-  for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT1 + tid) * N, a.vocab, a.mask_id, f[i]);
+  for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT + tid) * N, a.vocab, a.mask_id, f[i]);
+  const Controls c = controls_of(a, row);
+  fill_eighths(eighths);
   if (c.filter) {
     mass[tid] = 0;
     count[tid] = 0;
@@ -166,20 +217,20 @@ __global__ void __launch_bounds__(NT1) sample_chunk_kernel(SampleArgs a, SampleW
 #pragma unroll
     for (int e = 0; e < N; ++e) {
       if (!(f[i][e] < INFINITY)) {
-        bad = min(bad, (uint32_t)(v0 + (i * NT1 + tid) * N + e));
+        bad = min(bad, (uint32_t)(v0 + (i * NT + tid) * N + e));
         f[i][e] = -INFINITY;
       }
       top = fmaxf(top, f[i][e]);
     }
-  top = wave_all(top, [](float p, float q) { return fmaxf(p, q); });
-  bad = wave_all(bad, [](uint32_t p, uint32_t q) { return min(p, q); });
+  top = wave_all(top, Max{});
+  bad = wave_all(bad, Min{});
   if (lane == 0) {
     s_top[wave] = top;
     s_bad[wave] = bad;
   }
   __syncthreads();
 #pragma unroll
-  for (int i = 0; i < NT1 / 64; ++i) {
+  for (int i = 0; i < NW; ++i) {
     top = fmaxf(top, s_top[i]);
     bad = min(bad, s_bad[i]);
   }
@@ -189,30 +240,38 @@ __global__ void __launch_bounds__(NT1) sample_chunk_kernel(SampleArgs a, SampleW
     return;
   }
   uint32_t arg = ~0u;
-  uint64_t sum = 0;
+  u64 sum = 0;
   float sum1 = 0.f;
-  const double rate = c.inv_t * BINS_PER_NAT, base = class_of(top, rate);
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
-    for (int e = 0; e < N; ++e) {
-      const float y = f[i][e];
-      sum1 += __builtin_amdgcn_exp2f((y - top) * 1.4426950408889634f);
-      if (c.greedy) {
-        if (y == top) arg = min(arg, (uint32_t)(v0 + (i * NT1 + tid) * N + e));
-      } else if (y > -INFINITY) {
-        const uint64_t u = fixed50(exp_neg(((double)y - top) * c.inv_t));
+    for (int e = 0; e < N; ++e) sum1 += __builtin_amdgcn_exp2f((f[i][e] - top) * 1.4426950408889634f);
+  if (c.greedy) {
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e)
+        if (f[i][e] == top) arg = min(arg, (uint32_t)(v0 + (i * NT + tid) * N + e));
+  } else {
+    const double qtop = in_classes(top, c.rate), base = floor(qtop);
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        const float y = f[i][e];
+        const double q = in_classes(y, c.rate);
+        const u64 u = y > -INFINITY ? fixed50(weight_of(q - qtop, eighths)) : 0;
         sum += u;
-        if (c.filter) {
-          const int b = (int)fmin(base - class_of(y, rate), (double)(BINS - 1));
-          atomicAdd(reinterpret_cast<unsigned long long*>(mass + b), (unsigned long long)u);
+        if (c.filter && y > -INFINITY) {
+          const int b = (int)fmin(base - floor(q), (double)(BINS - 1));
+          atomicAdd(mass + b, u);
           atomicAdd(count + b, 1u);
         }
       }
-    }
-  arg = wave_all(arg, [](uint32_t p, uint32_t q) { return min(p, q); });
-  sum = wave_all((unsigned long long)sum, [](unsigned long long p, unsigned long long q) { return p + q; });
-  const double d1 = wave_all((double)sum1, [](double p, double q) { return p + q; });
+  }
+  arg = wave_all(arg, Min{});
+  sum = wave_all(sum, Sum{});
+  const double d1 = wave_all((double)sum1, Sum{});
   if (lane == 0) {
     s_arg[wave] = arg;
     s_sum[wave] = sum;
@@ -221,7 +280,7 @@ __global__ void __launch_bounds__(NT1) sample_chunk_kernel(SampleArgs a, SampleW
   __syncthreads();
   if (tid == 0) {
     ChunkStat s{top, bad, ~0u, 0, 0, 0.0};
-    for (int i = 0; i < NT1 / 64; ++i) {
+    for (int i = 0; i < NW; ++i) {
       s.arg = min(s.arg, s_arg[i]);
       s.sum += s_sum[i];
       s.sum1 += s_sum1[i];
@@ -246,36 +305,397 @@ __device__ __forceinline__ V block_scan(V x, V* buf) {
   if (lane == 63) buf[wave] = x;
   __syncthreads();
   V before = 0;
-  for (int i = 0; i < wave; ++i) before += buf[i];
+#pragma unroll
+  for (int i = 0; i < NW - 1; ++i) before += i < wave ? buf[i] : (V)0;
   __syncthreads();
   return x + before;
 }
 
-// A class's members up to a boundary: those with a key above `cut`, and those
+// The chunks of a row, in LDS: the weight of each one's maximum (0: without
+// mass), and the classes between the row's maximum and its own (BINS: none).
+struct Chunks {
+  double fac[MAX_CHUNKS];
+  int shift[MAX_CHUNKS];
+};
+struct RowTop {
+  float big;
+  uint32_t bad;
+  double qtop, base;
+};
+// Fills `ch` (no barrier after it) and returns the row's maximum, to every thread.
+__device__ __forceinline__ RowTop join_chunks(const ChunkStat* stat, int nch, const Controls& c, const double* eighths,
+                                              Chunks& ch) {
+  RowTop r{-INFINITY, ~0u, 0.0, 0.0};
+  const int lane = threadIdx.x & 63;
+  for (int i = lane; i < nch; i += 64) {  // every wave by itself
+    r.big = fmaxf(r.big, stat[i].top);
+    r.bad = min(r.bad, stat[i].bad);
+  }
+  r.big = wave_all(r.big, Max{});
+  r.bad = wave_all(r.bad, Min{});
+  if (r.big == -INFINITY) return r;
+  r.qtop = in_classes(r.big, c.rate);
+  r.base = floor(r.qtop);
+  for (int i = threadIdx.x; i < nch; i += NT) {
+    const float top = stat[i].top;
+    // a chunk with mass has a token with mass: its maximum
+    const double q = in_classes(top, c.rate), e = top > -INFINITY ? weight_of(q - r.qtop, eighths) : 0.0;
+    ch.fac[i] = e >= LEAST ? e : 0.0;
+    ch.shift[i] = e >= LEAST ? (int)(r.base - floor(q)) : BINS;
+  }
+  return r;
+}
+
+__global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs w) {
+  __shared__ Chunks ch;
+  __shared__ double eighths[8], binw[BINS], bufd[NW];
+  __shared__ uint32_t binc[BINS], bufu[NW];
+  __shared__ int s_k, s_lo, s_hi;
+  const int tid = threadIdx.x, row = blockIdx.x, nch = w.chunks;
+  const Controls c = controls_of(a, row);
+  if (!c.filter) return;
+  fill_eighths(eighths);
+  if (tid == 0) {
+    s_k = s_lo = s_hi = -1;
+    w.listed[row] = 0;
+  }
+  __syncthreads();
+  const RowTop top = join_chunks(w.stat + (size_t)row * nch, nch, c, eighths, ch);
+  if (top.bad != ~0u || top.big == -INFINITY) return;
+  __syncthreads();
+  const GLOBAL u64* hm = (const GLOBAL u64*)w.mass + (size_t)row * nch * BINS;
+  const GLOBAL uint32_t* hc = (const GLOBAL uint32_t*)w.count + (size_t)row * nch * BINS;
+  double m = 0;
+  uint32_t n = 0;
+  constexpr int U = 8;
+  for (int i0 = 0; i0 < nch; i0 += U) {
+    u64 um[U];
+    uint32_t uc[U];
+    bool in[U];
+#pragma unroll
+    for (int j = 0; j < U; ++j) {
+      const int i = min(i0 + j, nch - 1), k = tid - ch.shift[i];
+      // what lies in a chunk's last class has no mass in the row either
+      in[j] = i0 + j < nch && k >= 0 && k < BINS - 1 && tid < BINS - 1;
+      const size_t at = (size_t)i * BINS + (in[j] ? k : 0);
+      um[j] = hm[at];
+      uc[j] = hc[at];
+    }
+#pragma unroll
+    for (int j = 0; j < U; ++j)
+      if (in[j]) {
+        m += (double)um[j] * 0x1p-50 * ch.fac[i0 + j];
+        n += uc[j];
+      }
+  }
+  m = block_scan(m, bufd);
+  n = block_scan(n, bufu);
+  binw[tid] = m;
+  binc[tid] = n;
+  w.prefix[(size_t)row * BINS + tid] = m;
+  w.prefix_n[(size_t)row * BINS + tid] = n;
+  __syncthreads();
+  RowState st{BINS, 0, 0, -1, -1, {-1, -1, -1, -1}};
+  double least = binw[BINS - 2], most = least;  // bounds of the mass that top-p is a share of
+  if (c.top_k) {
+    if (tid < BINS - 1 && n >= (uint32_t)c.top_k && (tid == 0 || binc[tid - 1] < (uint32_t)c.top_k)) s_k = tid;
+    __syncthreads();
+    const int b = s_k;
+    if (b >= 0) {
+      most = least = binw[b];
+      st.ek = b + 1;
+      if ((uint32_t)c.top_k < binc[b]) {
+        st.rk = c.top_k - (int)(b ? binc[b - 1] : 0u);
+        least = b ? binw[b - 1] : 0.0;
+      }
+    }
+  }
+  int edge = st.ek;  // the classes below it may stay
+  if (c.top_p < 1.0) {
+    const double t0 = fmax(c.top_p * least * (1.0 - 1e-9), 0.0), t1 = fmax(c.top_p * most * (1.0 + 1e-9), 0.0);
+    if (tid < BINS - 1) {
+      const double before = tid ? binw[tid - 1] : -1.0;
+      if (m >= t0 && before < t0) s_lo = tid;
+      if (m >= t1 && before < t1) s_hi = tid;
+    }
+    __syncthreads();
+    st.lo = max(s_lo, 0);
+    st.hi = min(s_hi >= 0 ? s_hi : BINS - 2, edge - 1);
+    edge = min(edge, st.hi + 1);
+  }
+  if (c.min_p > 0.0) {
+    // w >= min_p as a distance, which stays exact where every w rounds to 1
+    st.bm = max((int)fmin(top.base - floor(top.qtop + log(c.min_p) * PER_NAT), (double)(BINS - 1)), 0);
+    edge = min(edge, st.bm + 1);
+  }
+  if (tid == 0) {
+    // members are needed of the classes in which the boundary may fall, and of
+    // top-k's where top-p is a share of what it keeps
+    int used = 0;
+    auto want = [&](int b) {
+      for (int i = 0; i < used; ++i)
+        if (st.slot[i] == b) return;
+      if (used < SLOTS) st.slot[used++] = b;
+    };
+    const bool by_p = c.top_p < 1.0 && st.lo < edge;  // top-p may decide
+    if (st.rk > 0 && (by_p || st.ek == edge)) want(st.ek - 1);
+    if (st.bm >= 0 && st.bm < BINS - 1 && st.bm + 1 == edge) want(st.bm);
+    if (by_p)
+      for (int b = st.lo; b <= st.hi && b < edge && used < SLOTS; ++b) want(b);
+    w.state[row] = st;
+  }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, SampleWs w) {
+  __shared__ uint32_t s_n[NW], s_at;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, v0 = chunk * CHUNK;
+  const Controls c = controls_of(a, row);
+  if (!c.filter) return;
+  const ChunkStat* stat = w.stat + (size_t)row * w.chunks;
+  float big = -INFINITY;
+  uint32_t bad = ~0u;
+  for (int i = lane; i < w.chunks; i += 64) {
+    big = fmaxf(big, stat[i].top);
+    bad = min(bad, stat[i].bad);
+  }
+  big = wave_all(big, Max{});
+  bad = wave_all(bad, Min{});
+  if (bad != ~0u || stat[chunk].top == -INFINITY) return;
+  const RowState st = w.state[row];
+  const double base = floor(in_classes(big, c.rate));
+  const double shift = base - floor(in_classes(stat[chunk].top, c.rate));
+  if (shift >= BINS) return;
+  uint32_t have = 0;
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i)
+    if (st.slot[i] >= 0 && st.slot[i] >= (int)shift)
+      have |= w.count[((size_t)row * w.chunks + chunk) * BINS + st.slot[i] - (int)shift];
+  if (have == 0) return;
+  const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
+  constexpr int N = 16 / sizeof(T), RUNS = E / N;
+  float f[RUNS][N];
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT + tid) * N, a.vocab, a.mask_id, f[i]);
+  uint32_t hit = 0, slots = 0;
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (f[i][e] > -INFINITY) {
+        const int b = class_of(f[i][e], c.rate, base);
+#pragma unroll
+        for (int k = 0; k < SLOTS; ++k)
+          if (b == st.slot[k]) {
+            hit |= 1u << (i * N + e);
+            slots |= (uint32_t)k << 2 * (i * N + e);
+          }
+      }
+  // places in the row's list: one reservation per workgroup
+  uint32_t n = __popc(hit), incl = n;
+#pragma unroll
+  for (int s = 1; s < 64; s <<= 1) {
+    const uint32_t y = __shfl_up(incl, s, 64);
+    if (lane >= s) incl += y;
+  }
+  if (lane == 63) s_n[wave] = incl;
+  __syncthreads();
+  if (tid == 0) {
+    uint32_t all = 0;
+    for (int i = 0; i < NW; ++i) {
+      const uint32_t k = s_n[i];
+      s_n[i] = all;
+      all += k;
+    }
+    s_at = all ? atomicAdd(w.listed + row, all) : 0;
+  }
+  __syncthreads();
+  uint32_t at = s_at + s_n[wave] + incl - n;
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (hit >> (i * N + e) & 1) {
+        if (at < LIST)
+          w.list[(size_t)row * LIST + at] =
+              make_uint2(key_of(f[i][e]), (uint32_t)(v0 + (i * NT + tid) * N + e) | (slots >> 2 * (i * N + e) & 3) << 24);
+        ++at;
+      }
+}
+
+// A class's members up to a boundary: those with a key above `key`, and those
 // with it up to index `last`.
 struct Cut {
   uint32_t key, last;
-  double mass;  // of the members kept
+  double mass;  // of the members kept, where a limit was reached
 };
 
 template <typename T>
-__global__ void __launch_bounds__(NT2) sample_row_kernel(SampleArgs a, SampleWs w) {
-  __shared__ double fac[MAX_CHUNKS];    // weight of a chunk's maximum
-  __shared__ int shift[MAX_CHUNKS];     // classes between the row's maximum and the chunk's
-  __shared__ double part[MAX_CHUNKS];   // kept mass of a chunk
-  __shared__ uint64_t extra[MAX_CHUNKS];
-  __shared__ uint2 list[LIST];          // (key, index) of a class's members
-  __shared__ uint64_t sub_mass[NT2];
-  __shared__ uint32_t sub_count[NT2];
-  __shared__ double binw[BINS];         // inclusive prefix sums
-  __shared__ uint32_t binc[BINS];
-  __shared__ double bufd[NT2 / 64];
-  __shared__ uint32_t bufu[NT2 / 64];
-  __shared__ uint32_t s_a, s_b, s_n;
-  __shared__ int s_i;
+struct Picker {
+  // LDS
+  struct Shared {
+    Chunks ch;
+    double part[MAX_CHUNKS];  // kept mass of a chunk
+    u64 extra[MAX_CHUNKS];
+    u64 sub_mass[NT];
+    uint32_t sub_count[NT];
+    double eighths[8], bufd[NW];
+    uint32_t bufu[NW], a, b, n;
+    int i;
+  };
+  Shared& sh;
+  const T* x;
+  const GLOBAL uint2* list;
+  RowTop top;
+  double rate;
+  int V, mask_id;
+  uint32_t listed;
+  RowState st;
+
+  __device__ __forceinline__ double weight(float f) const {
+    const double e = weight_of(in_classes(f, rate) - top.qtop, sh.eighths);
+    return e < LEAST ? 0.0 : e;
+  }
+  // f(key, index) for every member of class b: from the row's list, or where the
+  // list does not hold them all, from the logits.
+  template <typename F>
+  __device__ __forceinline__ void members(int b, F f) const {
+    int slot = -1;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i)
+      if (st.slot[i] == b) slot = i;
+    if (slot >= 0 && listed <= LIST) {
+      for (uint32_t i = threadIdx.x; i < listed; i += NT) {
+        const uint2 m = {list[i].x, list[i].y};
+        if ((int)(m.y >> 24) == slot) f(m.x, m.y & 0xffffffu);
+      }
+      return;
+    }
+    constexpr int N = 16 / sizeof(T), U = 16 / N;
+    for (int v0 = 0; v0 < V; v0 += NT * N * U) {
+      float y[U][N];
+#pragma unroll
+      for (int i = 0; i < U; ++i) load_logits<T, N>(x, v0 + (i * NT + (int)threadIdx.x) * N, V, mask_id, y[i]);
+#pragma unroll 1
+      for (int i = 0; i < U * N; ++i) {
+        float f1 = 0.f;  // y[i / N][i % N], from registers
+#pragma unroll
+        for (int j = 0; j < U * N; ++j) f1 = j == i ? y[j / N][j % N] : f1;
+        if (f1 > -INFINITY && class_of(f1, rate, top.base) == b)
+          f(key_of(f1), (uint32_t)(v0 + (i / N * NT + (int)threadIdx.x) * N + i % N));
+      }
+    }
+  }
+  // Class b's weights are at most 2^top_of(b); its sums are whole numbers of 2^(top_of(b) - 40).
+  static __device__ __forceinline__ int top_of(int b) { return ((1 - b) >> 3) + 1; }
+
+  // The members of class b that stay when at most `limit` of them may, and the mass
+  // of the members before one must be less than `target`: narrows the range of keys,
+  // then of indices among equal keys, NT parts at a time.
+  __device__ __forceinline__ Cut select(int b, uint32_t limit, double target) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const double unit = ldexp(1.0, top_of(b) - 40), units = ldexp(1.0, 40 - top_of(b));
+    target = fmax(target, 1e-300);  // the first of all stays
+    __syncthreads();
+    if (tid == 0) {
+      sh.a = ~0u;
+      sh.b = 0;
+      sh.n = 0;
+    }
+    __syncthreads();
+    uint32_t lo = ~0u, hi = 0, tied = 0;
+    members(b, [&](uint32_t key, uint32_t) {
+      lo = min(lo, key);
+      hi = max(hi, key);
+      ++tied;
+    });
+    lo = wave_all(lo, Min{});
+    hi = wave_all(hi, Max{});
+    tied = wave_all(tied, Sum{});
+    if (lane == 0) {
+      atomicMin(&sh.a, lo);
+      atomicMax(&sh.b, hi);
+      atomicAdd(&sh.n, tied);
+    }
+    __syncthreads();
+    lo = sh.a;
+    hi = sh.b;
+    tied = sh.n;  // members in the range
+    // the range is keys [lo, hi] from above, then indices [lo, hi] from below
+    bool by_key = true;
+    uint32_t n0 = 0;  // members ranked before the range, and their mass
+    double m0 = 0;
+    Cut r{0, ~0u, 0};
+    for (;;) {
+      if (by_key && hi == lo) {
+        const double each = weight(value_of(lo));
+        const uint32_t ties = (uint32_t)fmax(fmin((double)(limit - n0), ceil((target - m0) / each)), 1.0);
+        r.key = lo;
+        r.mass = m0 + (double)ties * each;
+        if (ties >= tied) return r;  // every one of the equal members
+        by_key = false;
+        limit = n0 + ties;
+        target = INFINITY;
+        lo = 0;
+        hi = (uint32_t)V - 1;
+      }
+      if (!by_key && hi == lo) {
+        r.last = lo;
+        return r;
+      }
+      const uint32_t span = hi - lo;
+      const int down = span >= NT ? 32 - __clz(span) - 9 : 0;  // span >> down < NT = 2^9
+      sh.sub_mass[tid] = 0;
+      sh.sub_count[tid] = 0;
+      if (tid == 0) sh.i = -1;
+      __syncthreads();
+      const uint32_t key0 = r.key;
+      members(b, [&](uint32_t key, uint32_t v) {
+        const uint32_t at = by_key ? hi - key : v - lo;
+        if (at <= span && (by_key || key == key0)) {
+          if (by_key) atomicAdd(sh.sub_mass + (at >> down), (u64)(weight(value_of(key)) * units));
+          atomicAdd(sh.sub_count + (at >> down), 1u);
+        }
+      });
+      __syncthreads();
+      const uint32_t mine = sh.sub_count[tid];
+      const double mass = (double)sh.sub_mass[tid] * unit;
+      const uint32_t n1 = block_scan(mine, sh.bufu);
+      const double m1 = block_scan(mass, sh.bufd);
+      const bool reached = n0 + n1 >= limit || m0 + m1 >= target;
+      const bool before = tid > 0 && (n0 + n1 - mine >= limit || m0 + (m1 - mass) >= target);
+      if (reached && !before && mine > 0) {
+        sh.i = tid;
+        sh.a = n1 - mine;
+        sh.b = mine;
+        sh.bufd[0] = m1 - mass;
+      }
+      __syncthreads();
+      const int i = sh.i;
+      if (i < 0) return Cut{0, ~0u, 0};  // no limit is reached: all stay
+      n0 += sh.a;
+      m0 += sh.bufd[0];
+      tied = sh.b;
+      const uint32_t p = (uint32_t)i << down, q = min(span, (((uint32_t)i + 1) << down) - 1);
+      if (by_key) {
+        lo = hi - q;
+        hi = hi - p;
+      } else {
+        hi = lo + q;
+        lo = lo + p;
+      }
+      __syncthreads();
+    }
+  }
+};
+
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs w) {
+  typedef Picker<T> P;
+  __shared__ typename P::Shared sh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int row = blockIdx.x, nch = w.chunks, V = a.vocab;
-  const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
   const ChunkStat* stat = w.stat + (size_t)row * nch;
   const Controls c = controls_of(a, row);
   auto answer = [&](int token, float conf, float prob) {
@@ -283,382 +703,221 @@ __global__ void __launch_bounds__(NT2) sample_row_kernel(SampleArgs a, SampleWs 
     if (a.conf) a.conf[row] = conf;
     if (a.prob) a.prob[row] = prob;
   };
-
-  // ---- the row's maximum, and what ends the search at once
-  float big = -INFINITY;
-  uint32_t bad = ~0u;
-  for (int i = lane; i < nch; i += 64) {  // every wave by itself
-    big = fmaxf(big, stat[i].top);
-    bad = min(bad, stat[i].bad);
-  }
-  big = wave_all(big, [](float p, float q) { return fmaxf(p, q); });
-  bad = wave_all(bad, [](uint32_t p, uint32_t q) { return min(p, q); });
-  if (bad != ~0u || big == -INFINITY) {
+  fill_eighths(sh.eighths);
+  __syncthreads();
+  P p{sh, static_cast<const T*>(a.logits) + (long)row * a.row_stride, (const GLOBAL uint2*)w.list + (size_t)row * LIST,
+      join_chunks(stat, nch, c, sh.eighths, sh.ch), c.rate, V, a.mask_id, 0, RowState{}};
+  const RowTop& top = p.top;
+  if (top.bad != ~0u || top.big == -INFINITY) {
     if (tid == 0) {
-      if (bad != ~0u)
-        answer((int)bad, NAN, NAN);
+      if (top.bad != ~0u)
+        answer((int)top.bad, NAN, NAN);
       else
         answer(-1, 0.f, 0.f);
     }
     return;
   }
-  double all1 = 0;
+  double all1 = 0;  // the row's sum at temperature 1
   uint32_t arg = ~0u;
   for (int i = lane; i < nch; i += 64) {
     const ChunkStat s = stat[i];
-    if (s.top > -INFINITY) all1 += s.sum1 * exp_neg((double)s.top - big);
-    if (s.top == big) arg = min(arg, s.arg);
+    if (s.top > -INFINITY) all1 += s.sum1 * weight_of(((double)s.top - top.big) * PER_NAT, sh.eighths);
+    if (s.top == top.big) arg = min(arg, s.arg);
   }
-  all1 = wave_all(all1, [](double p, double q) { return p + q; });
+  all1 = wave_all(all1, Sum{});
   if (c.greedy) {
-    arg = wave_all(arg, [](uint32_t p, uint32_t q) { return min(p, q); });
+    arg = wave_all(arg, Min{});
     if (tid == 0) answer((int)arg, (float)(1.0 / all1), 1.f);
     return;
   }
-  const double rate = c.inv_t * BINS_PER_NAT, base = class_of(big, rate);
-  for (int i = tid; i < nch; i += NT2) {
-    const ChunkStat s = stat[i];
-    // a chunk with mass has a token with mass: its maximum
-    const double e = s.top > -INFINITY ? exp_neg(((double)s.top - big) * c.inv_t) : 0.0;
-    const bool some = e >= LEAST;
-    fac[i] = some ? e : 0.0;
-    shift[i] = some ? (int)fmin(base - class_of(s.top, rate), (double)BINS) : BINS;
-    part[i] = (double)s.sum * 0x1p-50 * fac[i];  // everything kept
-    extra[i] = 0;
-  }
-  auto weight = [&](float f) {
-    const double e = exp_neg(((double)f - big) * c.inv_t);
-    return e < LEAST ? 0.0 : e;
-  };
-  auto bin_of = [&](float f) { return (int)fmin(base - class_of(f, rate), (double)(BINS - 1)); };
-  __syncthreads();
 
-  // ---- the boundary: classes below `edge` are kept whole, of class `edge` the members up to `cut`
+  // ---- the boundary: classes below `edge` are kept whole, of class `edge` the members that stay
   int edge = BINS;
-  Cut cut{0, ~0u, 0};
-  double scale = 1.0, reach = INFINITY;  // reach: the largest (max - x) / T that min-p keeps in class `edge`
-  auto stays = [&](float f, uint32_t key, uint32_t v) {  // a member of class `edge`
-    return ((double)big - f) * c.inv_t <= reach && (key > cut.key || (key == cut.key && v <= cut.last));
+  Cut cut{~0u, 0, 0};  // of that class: none
+  double reach = INFINITY;  // the largest (max - x) / T that min-p keeps in it
+  auto stays = [&](float f, uint32_t key, uint32_t v) {
+    return ((double)top.big - f) * c.inv_t <= reach && (key > cut.key || (key == cut.key && v <= cut.last));
   };
   if (c.filter) {
-    double m = 0;
-    uint32_t n = 0;
-    if (tid < BINS) {
-      const uint64_t* hm = w.mass + (size_t)row * nch * BINS;
-      const uint32_t* hc = w.count + (size_t)row * nch * BINS;
-      for (int i = 0; i < nch; ++i) {
-        const int k = tid - shift[i];
-        // what a chunk's last class holds has no mass in the row either
-        if (k >= 0 && shift[i] < BINS && tid < BINS - 1 && k < BINS - 1) {
-          m += (double)hm[(size_t)i * BINS + k] * 0x1p-50 * fac[i];
-          n += hc[(size_t)i * BINS + k];
-        }
-      }
-    }
-    const double cm = block_scan(m, bufd);
-    const uint32_t cn = block_scan(n, bufu);
-    if (tid < BINS) {
-      binw[tid] = cm;
-      binc[tid] = cn;
-    }
-    __syncthreads();
-    auto mass_before = [&](int b) { return b > 0 ? binw[b - 1] : 0.0; };
-    auto count_before = [&](int b) { return b > 0 ? binc[b - 1] : 0u; };
-
-    // members of class b: into the list where they fit, else they are found in the row each time
-    int listed = -1;
-    auto scan_row = [&](int b, auto&& f) {
-      // logits that can be in the class, with a margin that covers float32
-      const double hi = (base - b + 1) / rate, lo = (base - b) / rate;
-      const float fhi = rate > 0 ? (float)(hi + fabs(hi) * 1e-6) : INFINITY, flo = rate > 0 ? (float)(lo - fabs(lo) * 1e-6) : -INFINITY;
-      constexpr int N = 16 / sizeof(T), U = 32 / N;
-      for (int v0 = 0; v0 < V; v0 += NT2 * N * U) {
-        float y[U][N];
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int v = v0 + (i * NT2 + tid) * N;
-          load_logits<T, N>(x, v, V, a.mask_id, y[i]);
-        }
-#pragma unroll
-        for (int i = 0; i < U; ++i) {
-          const int v = v0 + (i * NT2 + tid) * N;
-#pragma unroll
-          for (int e = 0; e < N; ++e)
-            if (y[i][e] >= flo && y[i][e] <= fhi && y[i][e] > -INFINITY && bin_of(y[i][e]) == b)
-              f(key_of(y[i][e]), (uint32_t)(v + e));
-        }
-      }
-    };
-    auto members = [&](int b, auto&& f) {
-      const uint32_t n = binc[b] - count_before(b);
-      if (n > LIST) {
-        scan_row(b, f);
-        return;
-      }
-      if (listed != b) {
-        __syncthreads();
-        if (tid == 0) s_n = 0;
-        __syncthreads();
-        scan_row(b, [&](uint32_t key, uint32_t v) {
-          const uint32_t at = atomicAdd(&s_n, 1u);
-          if (at < LIST) list[at] = make_uint2(key, v);
-        });
-        __syncthreads();
-        listed = b;
-      }
-      const int have = min((int)s_n, LIST);
-      for (int i = tid; i < have; i += NT2) f(list[i].x, list[i].y);
-    };
-    // The members of class b that stay when at most `limit` of them may and, with
-    // `mass` of them before it, one must have less than `target`: narrows the
-    // range of keys, then of indices, by NT2 parts at a time.
-    auto select = [&](int b, uint32_t limit, double target) {
-      target = fmax(target, 1e-300);  // the first of all stays
-      // whole numbers in 2^-40 of the class's largest possible weight
-      scale = 0x1p40 / fmin(exp_neg(-(double)(b - 1) / BINS_PER_NAT), 1.0);
-      auto fixed = [&](uint32_t key) { return (unsigned long long)(weight(value_of(key)) * scale); };
-      __syncthreads();
-      if (tid == 0) {
-        s_a = ~0u;
-        s_b = 0;
-      }
-      __syncthreads();
-      uint32_t lo = ~0u, hi = 0;
-      members(b, [&](uint32_t key, uint32_t) {
-        lo = min(lo, key);
-        hi = max(hi, key);
-      });
-      lo = wave_all(lo, [](uint32_t p, uint32_t q) { return min(p, q); });
-      hi = wave_all(hi, [](uint32_t p, uint32_t q) { return max(p, q); });
-      if (lane == 0) {
-        atomicMin(&s_a, lo);
-        atomicMax(&s_b, hi);
-      }
-      __syncthreads();
-      lo = s_a;
-      hi = s_b;
-      uint32_t n0 = 0;   // members and mass ranked before the range
-      double m0 = 0;
-      // part i of the range, highest keys first; returns false if nothing reaches a limit
-      auto narrow = [&](uint32_t span, auto&& each, uint32_t& from, uint32_t& to) {
-        const int sh = span >= NT2 ? 32 - __clz(span) - 9 : 0;  // span >> sh < NT2 = 2^9
-        sub_mass[tid] = 0;
-        sub_count[tid] = 0;
-        if (tid == 0) s_i = -1;
-        __syncthreads();
-        each([&](uint32_t at, uint32_t key) {
-          atomicAdd(reinterpret_cast<unsigned long long*>(sub_mass + (at >> sh)), fixed(key));
-          atomicAdd(sub_count + (at >> sh), 1u);
-        });
-        __syncthreads();
-        const uint32_t n1 = block_scan(sub_count[tid], bufu);
-        const double m1 = block_scan((double)sub_mass[tid] / scale, bufd);
-        const double mb = m1 - (double)sub_mass[tid] / scale;
-        const uint32_t nb = n1 - sub_count[tid];
-        const bool reached = n0 + n1 >= limit || m0 + m1 >= target;
-        const bool before = tid > 0 && (n0 + nb >= limit || m0 + mb >= target);
-        if (reached && !before && sub_count[tid] > 0) s_i = tid;
-        __syncthreads();
-        const int i = s_i;
-        if (i < 0) return false;
-        if (tid == i) {
-          s_a = nb;
-          bufd[0] = mb;
-        }
-        __syncthreads();
-        n0 += s_a;
-        m0 += bufd[0];
-        from = (uint32_t)i << sh;
-        to = min(span, (((uint32_t)i + 1) << sh) - 1);
-        __syncthreads();
-        return true;
-      };
-      Cut r{0, ~0u, 0};
-      while (hi > lo) {
-        uint32_t p = 0, q = 0;
-        const uint32_t top = hi, bottom = lo;
-        if (!narrow(hi - lo, [&](auto&& add) { members(b, [&](uint32_t key, uint32_t) { if (key >= bottom && key <= top) add(top - key, key); }); }, p, q)) {
-          r.mass = binw[b] - mass_before(b);
-          return r;  // all of them
-        }
-        hi = top - p;
-        lo = top - q;
-      }
-      // the members equal to lo: those with the lowest indices
-      const double each = weight(value_of(lo));
-      const uint32_t ties = (uint32_t)fmax(fmin((double)(limit - n0), ceil((target - m0) / each)), 1.0);
-      r.key = lo;
-      r.mass = m0;
-      uint32_t first = 0, last = (uint32_t)V - 1;
-      const uint32_t want = n0 + ties;
-      limit = want;
-      target = INFINITY;
-      bool all = false;
-      while (last > first && !all) {
-        uint32_t p = 0, q = 0;
-        const uint32_t f0 = first, l0 = last;
-        all = !narrow(last - first, [&](auto&& add) { members(b, [&](uint32_t key, uint32_t v) { if (key == lo && v >= f0 && v <= l0) add(v - f0, key); }); }, p, q);
-        if (!all) {
-          first = f0 + p;
-          last = f0 + q;
-        }
-      }
-      r.last = all ? ~0u : last;
-      r.mass += (double)ties * each;
-      return r;
-    };
-    // first class whose inclusive prefix reaches the limit, or -1
-    auto find = [&](auto&& reached) {
-      __syncthreads();
-      if (tid == 0) s_i = -1;
-      __syncthreads();
-      if (tid < BINS - 1 && reached(tid) && (tid == 0 || !reached(tid - 1))) s_i = tid;
-      __syncthreads();
-      return s_i;
-    };
-    int bk = -1, bp = -1;
-    uint32_t rk = 0;
-    double target = INFINITY, whole = binw[BINS - 2];
-    if (c.top_k) {
-      bk = find([&](int b) { return binc[b] >= (uint32_t)c.top_k; });
-      if (bk >= 0) {
-        rk = c.top_k - count_before(bk);
-        whole = binw[bk];
-        if (rk == binc[bk] - count_before(bk)) {
-          edge = bk + 1;  // the class stays whole
-          bk = -1;
-        } else {
-          edge = bk;
-          if (c.top_p < 1.0) {
-            cut = select(bk, rk, INFINITY);
-            whole = mass_before(bk) + cut.mass;
+    p.st = w.state[row];
+    p.listed = w.listed[row];
+    const RowState& st = p.st;
+    const double* prefix = w.prefix + (size_t)row * BINS;
+    auto mass_before = [&](int b) { return b > 0 ? prefix[b - 1] : 0.0; };
+    const int bk = st.rk > 0 ? st.ek - 1 : -1;
+    edge = bk >= 0 ? bk : st.ek;
+    // the boundary by top-k and top-p: class `edge` holds it where limit or target say so
+    uint32_t limit = bk >= 0 ? (uint32_t)st.rk : ~0u;
+    double target = INFINITY;
+    bool ranked = bk >= 0;
+    // first pass: the mass that top-k keeps; second: the boundary itself
+    const bool by_p = c.top_p < 1.0 && (st.bm < 0 || st.lo <= st.bm);
+#pragma unroll 1
+    for (int pass = by_p && bk >= 0 ? 0 : 1; pass < 2; ++pass) {
+      if (pass == 1) {
+        if (by_p) {
+          const double all = c.top_p * (bk >= 0 ? mass_before(bk) + cut.mass : prefix[min(st.ek, BINS - 1) - 1]);
+          int b = st.lo;
+          while (b < st.hi && prefix[b] < all) ++b;
+          if (b < edge) {
+            edge = b;
+            limit = ~0u;
+          }
+          if (b == edge) {
+            ranked = true;
+            target = all - mass_before(b);
           }
         }
+        if (st.bm >= 0 && st.bm <= edge) {
+          if (st.bm < edge) ranked = false;
+          edge = st.bm;
+          reach = -log(c.min_p);
+        }
+        cut = edge < BINS - 1 && reach < INFINITY ? Cut{0, ~0u, 0} : Cut{~0u, 0, 0};
+        if (edge >= BINS - 1 || !ranked) break;
       }
+      cut = p.select(edge, limit, target);
     }
-    if (c.top_p < 1.0) {
-      target = c.top_p * whole;
-      bp = find([&](int b) { return binw[b] >= target; });
-      if (bp >= 0 && (bp < edge || bp == bk)) edge = bp;
-      if (bp > edge) bp = -1;
-    }
-    int bm = -1;
-    if (c.min_p > 0.0) {
-      // w >= min_p as a distance, which stays exact where every w rounds to 1
-      const double d = -log(c.min_p);
-      bm = max((int)fmin(base - floor(((double)big * c.inv_t - d) * BINS_PER_NAT), (double)(BINS - 1)), 0);
-      if (bm <= edge) {
-        edge = bm;
-        reach = d;
-      }
-    }
-    const bool ranked = edge == bk || edge == bp, split = edge < BINS - 1 && (ranked || reach < INFINITY);
-    if (split && ranked)
-      cut = select(edge, edge == bk ? rk : ~0u, edge == bp ? target - mass_before(edge) : INFINITY);
-    else
-      cut = Cut{split ? 0 : ~0u, 0, 0};  // every member that min-p leaves, or none
-
     // ---- kept mass of each chunk: its classes before the edge, then the edge's members
-    scale = 0x1p40 / fmin(exp_neg(-(double)(edge - 1) / BINS_PER_NAT), 1.0);
+    sh.extra[tid] = 0;
     __syncthreads();
-    if (split)
-      members(edge, [&](uint32_t key, uint32_t v) {
-        if (stays(value_of(key), key, v))
-          atomicAdd(reinterpret_cast<unsigned long long*>(extra + v / CHUNK), (unsigned long long)(weight(value_of(key)) * scale));
+    const double unit = ldexp(1.0, P::top_of(edge) - 40), units = ldexp(1.0, 40 - P::top_of(edge));
+    if (edge < BINS - 1 && cut.key != ~0u)
+      p.members(edge, [&](uint32_t key, uint32_t v) {
+        const float f = value_of(key);
+        if (stays(f, key, v)) atomicAdd(sh.extra + v / CHUNK, (u64)(p.weight(f) * units));
       });
-    __syncthreads();
-    for (int i = wave; i < nch; i += NT2 / 64) {
-      const uint64_t* h = w.mass + ((size_t)row * nch + i) * BINS;
-      unsigned long long s = 0;
-      const int end = min(edge, BINS - 1) - shift[i];  // classes of the chunk before the edge
-      for (int k = lane; k < min(end, BINS - 1); k += 64) s += h[k];
-      s = wave_all(s, [](unsigned long long p, unsigned long long q) { return p + q; });
-      if (lane == 0) part[i] = (double)s * 0x1p-50 * fac[i] + (double)extra[i] / scale;
+    for (int i = wave; i < nch; i += NW) {
+      const GLOBAL u64* h = (const GLOBAL u64*)w.mass + ((size_t)row * nch + i) * BINS;
+      const int end = min(edge, BINS - 1) - sh.ch.shift[i];  // classes of the chunk before the edge
+      u64 s = 0;
+#pragma unroll
+      for (int k = 0; k < BINS / 64; ++k) {
+        const int at = k * 64 + lane;
+        if (at < end) s += h[at];
+      }
+      s = wave_all(s, Sum{});
+      if (lane == 0) sh.part[i] = (double)s * 0x1p-50 * sh.ch.fac[i];
     }
     __syncthreads();
+    if (tid < nch) sh.part[tid] += (double)sh.extra[tid] * unit;
+  } else if (tid < nch) {
+    sh.part[tid] = (double)stat[tid].sum * 0x1p-50 * sh.ch.fac[tid];
   }
-  auto kept = [&](float f, uint32_t v) {
-    if (!(f > -INFINITY)) return 0.0;
-    const double e = weight(f);
-    if (!c.filter) return e;
-    const int b = bin_of(f);
-    if (b > edge || b >= BINS - 1) return 0.0;
-    if (b < edge) return e;
-    const uint32_t key = key_of(f);
-    return stays(f, key, v) ? e : 0.0;
-  };
 
   // ---- the chunk, then the token, where the running sum passes u times the whole
-  double total = 0;
-  for (int i = 0; i < nch; ++i) total += part[i];
+  const double part = tid < nch ? sh.part[tid] : 0.0;
+  const double upto = block_scan(part, sh.bufd);
+  __syncthreads();
+  sh.part[tid] = upto;
+  if (tid == 0) {
+    sh.a = ~0u;
+    sh.b = 0;
+  }
+  __syncthreads();
+  const double total = sh.part[nch - 1];
   float u = a.u[row];
   u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
   const double want = (double)u * total;
-  double before = 0;
-  int at = 0;  // the sums run as the total's did, and want is less than that
-  for (; at < nch - 1 && before + part[at] <= want; ++at) before += part[at];
-  constexpr int E = CHUNK / NT2;
+  if (part > 0.0) {
+    if (upto > want) atomicMin(&sh.a, (uint32_t)tid);
+    atomicMax(&sh.b, (uint32_t)tid);  // rounding: the last chunk with mass
+  }
+  __syncthreads();
+  const int at = (int)min(sh.a, sh.b);
+  double run = at > 0 ? sh.part[at - 1] : 0.0;
+  __syncthreads();
+  if (tid == 0) {
+    sh.a = ~0u;
+    sh.b = 0;
+  }
   const int v0 = at * CHUNK + tid * E;
   float y[E];
-  load_logits<T, E>(x, v0, V, a.mask_id, y);
+  load_logits<T, E>(p.x, v0, V, a.mask_id, y);
   double e[E], sum = 0;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
-    e[i] = kept(y[i], v0 + i);
+    const float f = y[i];
+    bool keep = f > -INFINITY;
+    if (c.filter && keep) {
+      const int b = class_of(f, c.rate, top.base);
+      keep = b < edge ? b < BINS - 1 : b == edge && edge < BINS - 1 && stays(f, key_of(f), v0 + i);
+    }
+    e[i] = keep ? p.weight(f) : 0.0;
     sum += e[i];
   }
-  __syncthreads();
-  if (tid == 0) {
-    s_a = ~0u;
-    s_b = 0;
-  }
-  const double incl = block_scan(sum, bufd);  // has barriers
-  double run = before + (incl - sum);
-  uint32_t mine = ~0u, final = 0;
+  const double incl = block_scan(sum, sh.bufd);  // has barriers
+  run += incl - sum;
+  uint32_t mine = ~0u, last = 0;
 #pragma unroll
   for (int i = 0; i < E; ++i) {
     run += e[i];
     if (e[i] > 0.0) {
-      final = v0 + i + 1;
+      last = v0 + i + 1;
       if (run > want && mine == ~0u) mine = v0 + i;
     }
   }
-  if (mine != ~0u) atomicMin(&s_a, mine);
-  if (final) atomicMax(&s_b, final);
+  if (mine != ~0u) atomicMin(&sh.a, mine);
+  if (last) atomicMax(&sh.b, last);
   __syncthreads();
   if (tid == 0) {
     // (rounding inside the chunk: its last kept token)
-    const uint32_t token = min(s_a != ~0u ? s_a : s_b - 1, (uint32_t)V - 1);
-    const float f = to_f(x[token]);
-    answer((int)token, (float)(exp_neg((double)f - big) / all1), (float)(weight(f) / total));
+    const uint32_t token = min(sh.a != ~0u ? sh.a : sh.b - 1, (uint32_t)V - 1);
+    const float f = to_f(p.x[token]);
+    answer((int)token, (float)(weight_of(((double)f - top.big) * PER_NAT, sh.eighths) / all1), (float)(p.weight(f) / total));
   }
 }
 
 int chunks_of(int vocab) { return ceil_div(vocab, CHUNK); }
 
+// Carves the workspace (null: sizes only); returns the bytes.
+size_t carve(void* base, size_t rows, size_t chunks, SampleWs* w) {
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    char* at = static_cast<char*>(base) + off;
+    off += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  w->chunks = (int)chunks;
+  w->stat = reinterpret_cast<ChunkStat*>(take(rows * chunks * sizeof(ChunkStat)));
+  w->mass = reinterpret_cast<u64*>(take(rows * chunks * BINS * sizeof(u64)));
+  w->count = reinterpret_cast<uint32_t*>(take(rows * chunks * BINS * sizeof(uint32_t)));
+  w->prefix = reinterpret_cast<double*>(take(rows * BINS * sizeof(double)));
+  w->prefix_n = reinterpret_cast<uint32_t*>(take(rows * BINS * sizeof(uint32_t)));
+  w->state = reinterpret_cast<RowState*>(take(rows * sizeof(RowState)));
+  w->list = reinterpret_cast<uint2*>(take(rows * LIST * sizeof(uint2)));
+  w->listed = reinterpret_cast<uint32_t*>(take(rows * sizeof(uint32_t)));
+  return off;
+}
+
+template <typename T>
+void launch(const SampleArgs& a, const SampleWs& w, hipStream_t s) {
+  const unsigned n = (unsigned)a.rows * w.chunks;
+  sample_chunk_kernel<T><<<n, NT, 0, s>>>(a, w);
+  DLLM_LAUNCH_CHECK("sample_chunk_kernel");
+  if (a.top_k || a.top_p || a.min_p) {
+    sample_edge_kernel<<<a.rows, NT, 0, s>>>(a, w);
+    DLLM_LAUNCH_CHECK("sample_edge_kernel");
+    sample_collect_kernel<T><<<n, NT, 0, s>>>(a, w);
+    DLLM_LAUNCH_CHECK("sample_collect_kernel");
+  }
+  sample_pick_kernel<T><<<a.rows, NT, 0, s>>>(a, w);
+  DLLM_LAUNCH_CHECK("sample_pick_kernel");
+}
+
 }  // namespace
 
+bool sample_fits(int rows, int vocab) { return (long)rows * chunks_of(vocab) < (1l << 22); }
+
 size_t sample_bytes(int rows, int vocab) {
-  return (size_t)rows * chunks_of(vocab) * (sizeof(ChunkStat) + BINS * 12) + 256;
+  SampleWs w;
+  return carve(nullptr, rows, chunks_of(vocab), &w);
 }
 
 void launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {
-  SampleWs w{};
-  w.chunks = chunks_of(a.vocab);
-  const size_t n = (size_t)a.rows * w.chunks;
-  w.mass = static_cast<uint64_t*>(ws);
-  w.stat = reinterpret_cast<ChunkStat*>(w.mass + n * BINS);
-  w.count = reinterpret_cast<uint32_t*>(w.stat + n);
-  auto go = [&](auto* chunk, auto* row) {
-    chunk<<<(unsigned)n, NT1, 0, s>>>(a, w);
-    DLLM_LAUNCH_CHECK("sample_chunk_kernel");
-    row<<<a.rows, NT2, 0, s>>>(a, w);
-    DLLM_LAUNCH_CHECK("sample_row_kernel");
-  };
-  if (a.dtype == DLLM_F32)
-    go(sample_chunk_kernel<float>, sample_row_kernel<float>);
-  else
-    go(sample_chunk_kernel<bf16_t>, sample_row_kernel<bf16_t>);
+  SampleWs w;
+  carve(ws, a.rows, chunks_of(a.vocab), &w);
+  a.dtype == DLLM_F32 ? launch<float>(a, w, s) : launch<bf16_t>(a, w, s);
 }
 
 }  // namespace dllm

@@ -248,6 +248,7 @@ struct SampleArgs {
   int32_t* token; float* conf; float* prob;
 };
 size_t sample_bytes(int rows, int vocab);
+bool sample_fits(int rows, int vocab);  // its grid can be launched
 void launch_sample(const SampleArgs& a, void* ws, hipStream_t s);
 
 }  // namespace dllm

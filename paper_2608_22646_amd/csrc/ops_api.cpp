@@ -90,6 +90,7 @@ void check_workspace(const void* ws, size_t bytes, size_t need) {
 
 void check_sample_sizes(int rows, int vocab) {
   require(rows >= 0 && vocab >= 1 && vocab <= (1 << 22), DLLM_ESHAPE, "rows must be >= 0 and vocab in [1, 2^22]");
+  require(sample_fits(rows, vocab), DLLM_ESHAPE, "too many rows of this vocabulary for one call");
 }
 
 }  // namespace
