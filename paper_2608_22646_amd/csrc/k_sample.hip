@@ -32,7 +32,7 @@ namespace dllm {
 namespace {
 
 constexpr int CHUNK = 8192, NT = 512, E = CHUNK / NT, NW = NT / 64;
-constexpr int BINS = 512;               // 64 octaves; the last class takes everything without mass
+constexpr int BINS = 512;               // 64 octaves; the last class stands for everything without mass
 constexpr double PER_NAT = 11.541560327111707;  // 8 / ln 2
 constexpr double LEAST = 0x1p-63;       // weights below count as none
 constexpr int LIST = 8192;              // members listed of a row
@@ -59,28 +59,28 @@ __device__ __forceinline__ float value_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
-// 2^(j / 8), j < 8, in LDS.
-__device__ __forceinline__ void fill_eighths(double* t) {
-  if (threadIdx.x < 8) t[threadIdx.x] = exp2(threadIdx.x * 0.125);
+// 2^(j / STEPS), j < STEPS, in LDS.
+constexpr int STEPS = 512;
+__device__ __forceinline__ void fill_powers(double* t) {
+  static_assert(STEPS == NT, "an entry per thread");
+  t[threadIdx.x] = exp2((double)threadIdx.x / STEPS);
 }
-// 2^(d / 8) for d <= 0: whole eighths by table and exponent, the rest (at most
-// half of one) by the Taylor polynomial of degree 7, whose remainder is 3e-16.
-// Exactly 1 at 0; 2^-1000 stands for everything below.
-__device__ __forceinline__ double weight_of(double d, const double* eighths) {
+// 2^(d / 8) for d in [-8000, 0]: whole steps of 1 / 512 octave by
+// table and exponent, the rest (f, at most half a step, or 7e-4 nats) by the Taylor
+// polynomial of degree 3, whose remainder is 1e-14.  Exactly 1 at 0.  Adding 1.5 x
+// 2^46 leaves d in steps (units of 1 / 64) in the low word.
+__device__ __forceinline__ double power_of(double d, const double* powers) {
   constexpr double L = 0.08664339756999316;  // ln 2 / 8
-  d = fmax(d, -8000.0);
-  const double n = rint(d), f = (d - n) * L;
-  double p = 1.0 / 5040;
-  p = fma(p, f, 1.0 / 720);
-  p = fma(p, f, 1.0 / 120);
-  p = fma(p, f, 1.0 / 24);
-  p = fma(p, f, 1.0 / 6);
-  p = fma(p, f, 0.5);
-  p = fma(p, f, 1.0);
-  p = fma(p, f, 1.0);
-  const int i = (int)n;
-  return ldexp(p * eighths[i & 7], i >> 3);
+  const double t = d + 0x1.8p46, f = d - (t - 0x1.8p46);
+  const int n = __double2loint(t);
+  const double p = f * fma(fma(L * L * L / 6, f, L * L / 2), f, L);
+  const double w = powers[n & (STEPS - 1)];
+  const double r = fma(w, p, w);
+  return __hiloint2double(__double2hiint(r) + ((n >> 9) << 20), __double2loint(r));
 }
+// The same for any d <= 0 (2^-1000 for what lies below, and for NaN: -inf at an
+// infinite temperature).
+__device__ __forceinline__ double weight_of(double d, const double* powers) { return power_of(fmax(d, -8000.0), powers); }
 // A weight w in [0, 1] as a whole number of 2^-50: the mantissa of 4 + w.
 __device__ __forceinline__ uint64_t fixed50(double w) {
   return __double_as_longlong(4.0 + w) - 0x4010000000000000ull;
@@ -105,12 +105,11 @@ typedef unsigned long long u64;
 
 // What a chunk leaves: its largest logit, the lowest index of a NaN or +inf (or
 // ~0), the lowest index of the maximum, and its sums at the row's temperature
-// (in 2^-50 of the largest weight) and at temperature 1 (of the largest).
+// (where nothing is filtered) and at temperature 1, relative to the largest weight.
 struct ChunkStat {
   float top;
   uint32_t bad, arg, pad;
-  u64 sum;
-  double sum1;
+  double sum, sum1;
 };
 // What sample_edge_kernel leaves: the boundary as far as the classes tell it.
 // Under top-k the classes below `ek` stay, of class ek - 1 the first rk members
@@ -162,7 +161,7 @@ __device__ __forceinline__ double in_classes(float x, double rate) {
 }
 // Class of a logit in a row whose maximum lies in class `base` of the grid.
 __device__ __forceinline__ int class_of(float x, double rate, double base) {
-  return (int)fmin(base - floor(in_classes(x, rate)), (double)(BINS - 1));
+  return (int)fmin(base - rint(in_classes(x, rate)), (double)(BINS - 1));
 }
 
 // N consecutive logits from v on (rows may start at any element: the loads are
@@ -192,11 +191,10 @@ template <typename T>
 __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs w) {
   __shared__ u64 mass[BINS];
   __shared__ uint32_t count[BINS];
-  __shared__ double eighths[8];
+  __shared__ double powers[STEPS];
   __shared__ float s_top[NW];
   __shared__ uint32_t s_bad[NW], s_arg[NW];
-  __shared__ u64 s_sum[NW];
-  __shared__ double s_sum1[NW];
+  __shared__ double s_sum[NW], s_sum1[NW];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, v0 = chunk * CHUNK;
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
@@ -205,23 +203,27 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
 #pragma unroll
   for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT + tid) * N, a.vocab, a.mask_id, f[i]);
   const Controls c = controls_of(a, row);
-  fill_eighths(eighths);
+  fill_powers(powers);
   if (c.filter) {
     mass[tid] = 0;
     count[tid] = 0;
   }
   float top = -INFINITY;
-  uint32_t bad = ~0u;
+  bool broken = false;  // a NaN or +inf among mine
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-      if (!(f[i][e] < INFINITY)) {
-        bad = min(bad, (uint32_t)(v0 + (i * NT + tid) * N + e));
-        f[i][e] = -INFINITY;
-      }
+      broken |= __builtin_amdgcn_classf(f[i][e], 0x203);
       top = fmaxf(top, f[i][e]);
     }
+  uint32_t bad = ~0u;
+  if (broken)
+#pragma unroll
+    for (int i = RUNS - 1; i >= 0; --i)
+#pragma unroll
+      for (int e = N - 1; e >= 0; --e)
+        if (!(f[i][e] < INFINITY)) bad = v0 + (i * NT + tid) * N + e;
   top = wave_all(top, Max{});
   bad = wave_all(bad, Min{});
   if (lane == 0) {
@@ -235,39 +237,59 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
     bad = min(bad, s_bad[i]);
   }
   ChunkStat* out = w.stat + blockIdx.x;
-  if (top == -INFINITY) {  // no candidate here
-    if (tid == 0) *out = ChunkStat{top, bad, ~0u, 0, 0, 0.0};
+  if (bad != ~0u || top == -INFINITY) {  // the row is decided, or no candidate here
+    if (tid == 0) *out = ChunkStat{top, bad, ~0u, 0, 0.0, 0.0};
     return;
   }
-  uint32_t arg = ~0u;
-  u64 sum = 0;
-  float sum1 = 0.f;
+  float sum1 = 0.f;  // at temperature 1
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
     for (int e = 0; e < N; ++e) sum1 += __builtin_amdgcn_exp2f((f[i][e] - top) * 1.4426950408889634f);
+  uint32_t arg = ~0u;
+  double sum = 0;
+  const double qtop = in_classes(top, c.rate);
   if (c.greedy) {
 #pragma unroll
     for (int i = 0; i < RUNS; ++i)
 #pragma unroll
       for (int e = 0; e < N; ++e)
         if (f[i][e] == top) arg = min(arg, (uint32_t)(v0 + (i * NT + tid) * N + e));
-  } else {
-    const double qtop = in_classes(top, c.rate), base = floor(qtop);
+  } else if (!c.filter) {
 #pragma unroll
     for (int i = 0; i < RUNS; ++i)
 #pragma unroll
-      for (int e = 0; e < N; ++e) {
-        const float y = f[i][e];
-        const double q = in_classes(y, c.rate);
-        const u64 u = y > -INFINITY ? fixed50(weight_of(q - qtop, eighths)) : 0;
-        sum += u;
-        if (c.filter && y > -INFINITY) {
-          const int b = (int)fmin(base - floor(q), (double)(BINS - 1));
-          atomicAdd(mass + b, u);
-          atomicAdd(count + b, 1u);
-        }
+      for (int e = 0; e < N; ++e) sum += weight_of(in_classes(f[i][e], c.rate) - qtop, powers);
+  } else {
+    auto add = [&](int b, double weight) {
+      if (b < BINS - 1) {
+        atomicAdd(mass + b, fixed50(weight));
+        if (c.top_k) atomicAdd(count + b, 1u);
       }
+    };
+    const double base = rint(qtop);
+    if (fabs(qtop) < 0x1p30) {
+      // the class: the nearest whole number to q, in the low word of q + 1.5 x 2^52;
+      // logits far below (and -inf) stand 600 classes below the top
+      const int base_i = (int)base;
+      const double least = qtop - 600.0;
+#pragma unroll
+      for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e) {
+          const double q = fmax(in_classes(f[i][e], c.rate), least);
+          add(base_i - __double2loint(q + 0x1.8p52), power_of(q - qtop, powers));
+        }
+    } else {
+#pragma unroll 1
+      for (int i = 0; i < E; ++i) {
+        float y = 0.f;
+#pragma unroll
+        for (int j = 0; j < E; ++j) y = j == i ? f[j / N][j % N] : y;
+        const double q = in_classes(y, c.rate);
+        add((int)fmin(base - rint(q), (double)BINS), weight_of(q - qtop, powers));
+      }
+    }
   }
   arg = wave_all(arg, Min{});
   sum = wave_all(sum, Sum{});
@@ -279,7 +301,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
   }
   __syncthreads();
   if (tid == 0) {
-    ChunkStat s{top, bad, ~0u, 0, 0, 0.0};
+    ChunkStat s{top, bad, ~0u, 0, 0.0, 0.0};
     for (int i = 0; i < NW; ++i) {
       s.arg = min(s.arg, s_arg[i]);
       s.sum += s_sum[i];
@@ -289,7 +311,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
   }
   if (c.filter) {
     w.mass[(size_t)blockIdx.x * BINS + tid] = mass[tid];
-    w.count[(size_t)blockIdx.x * BINS + tid] = count[tid];
+    if (c.top_k) w.count[(size_t)blockIdx.x * BINS + tid] = count[tid];
   }
 }
 
@@ -323,7 +345,7 @@ struct RowTop {
   double qtop, base;
 };
 // Fills `ch` (no barrier after it) and returns the row's maximum, to every thread.
-__device__ __forceinline__ RowTop join_chunks(const ChunkStat* stat, int nch, const Controls& c, const double* eighths,
+__device__ __forceinline__ RowTop join_chunks(const ChunkStat* stat, int nch, const Controls& c, const double* powers,
                                               Chunks& ch) {
   RowTop r{-INFINITY, ~0u, 0.0, 0.0};
   const int lane = threadIdx.x & 63;
@@ -335,32 +357,32 @@ __device__ __forceinline__ RowTop join_chunks(const ChunkStat* stat, int nch, co
   r.bad = wave_all(r.bad, Min{});
   if (r.big == -INFINITY) return r;
   r.qtop = in_classes(r.big, c.rate);
-  r.base = floor(r.qtop);
+  r.base = rint(r.qtop);
   for (int i = threadIdx.x; i < nch; i += NT) {
     const float top = stat[i].top;
     // a chunk with mass has a token with mass: its maximum
-    const double q = in_classes(top, c.rate), e = top > -INFINITY ? weight_of(q - r.qtop, eighths) : 0.0;
+    const double q = in_classes(top, c.rate), e = top > -INFINITY ? weight_of(q - r.qtop, powers) : 0.0;
     ch.fac[i] = e >= LEAST ? e : 0.0;
-    ch.shift[i] = e >= LEAST ? (int)(r.base - floor(q)) : BINS;
+    ch.shift[i] = e >= LEAST ? (int)(r.base - rint(q)) : BINS;
   }
   return r;
 }
 
 __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs w) {
   __shared__ Chunks ch;
-  __shared__ double eighths[8], binw[BINS], bufd[NW];
+  __shared__ double powers[STEPS], binw[BINS], bufd[NW];
   __shared__ uint32_t binc[BINS], bufu[NW];
   __shared__ int s_k, s_lo, s_hi;
   const int tid = threadIdx.x, row = blockIdx.x, nch = w.chunks;
   const Controls c = controls_of(a, row);
   if (!c.filter) return;
-  fill_eighths(eighths);
+  fill_powers(powers);
   if (tid == 0) {
     s_k = s_lo = s_hi = -1;
     w.listed[row] = 0;
   }
   __syncthreads();
-  const RowTop top = join_chunks(w.stat + (size_t)row * nch, nch, c, eighths, ch);
+  const RowTop top = join_chunks(w.stat + (size_t)row * nch, nch, c, powers, ch);
   if (top.bad != ~0u || top.big == -INFINITY) return;
   __syncthreads();
   const GLOBAL u64* hm = (const GLOBAL u64*)w.mass + (size_t)row * nch * BINS;
@@ -375,11 +397,11 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int i = min(i0 + j, nch - 1), k = tid - ch.shift[i];
-      // what lies in a chunk's last class has no mass in the row either
+      // what lies behind a chunk's classes has no mass in the row either
       in[j] = i0 + j < nch && k >= 0 && k < BINS - 1 && tid < BINS - 1;
       const size_t at = (size_t)i * BINS + (in[j] ? k : 0);
       um[j] = hm[at];
-      uc[j] = hc[at];
+      uc[j] = c.top_k ? hc[at] : 0u;
     }
 #pragma unroll
     for (int j = 0; j < U; ++j)
@@ -425,7 +447,7 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   }
   if (c.min_p > 0.0) {
     // w >= min_p as a distance, which stays exact where every w rounds to 1
-    st.bm = max((int)fmin(top.base - floor(top.qtop + log(c.min_p) * PER_NAT), (double)(BINS - 1)), 0);
+    st.bm = max((int)fmin(top.base - rint(top.qtop + log(c.min_p) * PER_NAT), (double)(BINS - 1)), 0);
     edge = min(edge, st.bm + 1);
   }
   if (tid == 0) {
@@ -464,15 +486,25 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
   bad = wave_all(bad, Min{});
   if (bad != ~0u || stat[chunk].top == -INFINITY) return;
   const RowState st = w.state[row];
-  const double base = floor(in_classes(big, c.rate));
-  const double shift = base - floor(in_classes(stat[chunk].top, c.rate));
+  const double base = rint(in_classes(big, c.rate));
+  const double shift = base - rint(in_classes(stat[chunk].top, c.rate));
   if (shift >= BINS) return;
-  uint32_t have = 0;
+  u64 have = 0;
 #pragma unroll
   for (int i = 0; i < SLOTS; ++i)
     if (st.slot[i] >= 0 && st.slot[i] >= (int)shift)
-      have |= w.count[((size_t)row * w.chunks + chunk) * BINS + st.slot[i] - (int)shift];
+      have |= w.mass[((size_t)row * w.chunks + chunk) * BINS + st.slot[i] - (int)shift];
   if (have == 0) return;
+  // logits outside [least, most] lie in none of the classes (a margin covers float32)
+  int first = BINS, final = 0;
+#pragma unroll
+  for (int i = 0; i < SLOTS; ++i)
+    if (st.slot[i] >= 0) {
+      first = min(first, st.slot[i]);
+      final = max(final, st.slot[i]);
+    }
+  const double hi = (base - first + 1) / c.rate, lo = (base - final - 1) / c.rate;
+  const float most = c.rate > 0 ? (float)(hi + fabs(hi) * 1e-6) : INFINITY, least = c.rate > 0 ? (float)(lo - fabs(lo) * 1e-6) : -INFINITY;
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
   constexpr int N = 16 / sizeof(T), RUNS = E / N;
   float f[RUNS][N];
@@ -483,7 +515,7 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (f[i][e] > -INFINITY) {
+      if (f[i][e] >= least && f[i][e] <= most && f[i][e] > -INFINITY) {
         const int b = class_of(f[i][e], c.rate, base);
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k)
@@ -540,7 +572,7 @@ struct Picker {
     u64 extra[MAX_CHUNKS];
     u64 sub_mass[NT];
     uint32_t sub_count[NT];
-    double eighths[8], bufd[NW];
+    double powers[STEPS], bufd[NW];
     uint32_t bufu[NW], a, b, n;
     int i;
   };
@@ -554,7 +586,7 @@ struct Picker {
   RowState st;
 
   __device__ __forceinline__ double weight(float f) const {
-    const double e = weight_of(in_classes(f, rate) - top.qtop, sh.eighths);
+    const double e = weight_of(in_classes(f, rate) - top.qtop, sh.powers);
     return e < LEAST ? 0.0 : e;
   }
   // f(key, index) for every member of class b: from the row's list, or where the
@@ -703,10 +735,10 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     if (a.conf) a.conf[row] = conf;
     if (a.prob) a.prob[row] = prob;
   };
-  fill_eighths(sh.eighths);
+  fill_powers(sh.powers);
   __syncthreads();
   P p{sh, static_cast<const T*>(a.logits) + (long)row * a.row_stride, (const GLOBAL uint2*)w.list + (size_t)row * LIST,
-      join_chunks(stat, nch, c, sh.eighths, sh.ch), c.rate, V, a.mask_id, 0, RowState{}};
+      join_chunks(stat, nch, c, sh.powers, sh.ch), c.rate, V, a.mask_id, 0, RowState{}};
   const RowTop& top = p.top;
   if (top.bad != ~0u || top.big == -INFINITY) {
     if (tid == 0) {
@@ -721,7 +753,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
   uint32_t arg = ~0u;
   for (int i = lane; i < nch; i += 64) {
     const ChunkStat s = stat[i];
-    if (s.top > -INFINITY) all1 += s.sum1 * weight_of(((double)s.top - top.big) * PER_NAT, sh.eighths);
+    if (s.top > -INFINITY) all1 += s.sum1 * weight_of(((double)s.top - top.big) * PER_NAT, sh.powers);
     if (s.top == top.big) arg = min(arg, s.arg);
   }
   all1 = wave_all(all1, Sum{});
@@ -802,7 +834,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     __syncthreads();
     if (tid < nch) sh.part[tid] += (double)sh.extra[tid] * unit;
   } else if (tid < nch) {
-    sh.part[tid] = (double)stat[tid].sum * 0x1p-50 * sh.ch.fac[tid];
+    sh.part[tid] = stat[tid].sum * sh.ch.fac[tid];
   }
 
   // ---- the chunk, then the token, where the running sum passes u times the whole
@@ -864,7 +896,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     // (rounding inside the chunk: its last kept token)
     const uint32_t token = min(sh.a != ~0u ? sh.a : sh.b - 1, (uint32_t)V - 1);
     const float f = to_f(p.x[token]);
-    answer((int)token, (float)(weight_of(((double)f - top.big) * PER_NAT, sh.eighths) / all1), (float)(p.weight(f) / total));
+    answer((int)token, (float)(weight_of(((double)f - top.big) * PER_NAT, sh.powers) / all1), (float)(p.weight(f) / total));
   }
 }
 
