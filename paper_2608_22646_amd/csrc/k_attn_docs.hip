@@ -20,6 +20,7 @@
 // (chunks of whole steps); each leaves its state in the workspace and
 // attn_join_kernel joins them in chunk order.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -27,10 +28,9 @@ namespace dllm {
 
 namespace {
 
-typedef __attribute__((address_space(3))) void* lds_ptr_t;
 typedef short v4s_t __attribute__((ext_vector_type(4)));
-typedef unsigned short v2us_t __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) v4s_t* lds_v4s_t;
+typedef unsigned short v2us_t __attribute__((ext_vector_type(2)));
 
 constexpr float LOG2E = 1.4426950408889634f;
 
@@ -52,8 +52,12 @@ __device__ __forceinline__ Doc doc_of(const AttnArgs& a, int d) {
 __device__ __forceinline__ int sees(const AttnArgs& a, const Doc& d, int t) {
   if (a.block == 0) return d.nk;
   const long i = (long)d.pos + t;
-  if (i < 0) return min(d.nk, max(d.prefix, 0));  // its own block ends at or before position 0
-  return (int)min((long)d.nk, max((i / a.block + 1) * a.block, (long)d.prefix));
+  int n = 0;  // a position before 0: its own block ends at or before position 0
+  if (i >= d.nk)
+    n = d.nk;
+  else if (i >= 0)
+    n = (int)min((long)d.nk, ((long)((uint32_t)i / (uint32_t)a.block) + 1) * a.block);
+  return max(n, min(d.prefix, d.nk));
 }
 
 template <int N>
@@ -66,6 +70,28 @@ __device__ __forceinline__ void barrier_nofence() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint32_t lo = uniform((int)(uint64_t)p), hi = uniform((int)((uint64_t)p >> 32));
+  return (const char*)((uint64_t)hi << 32 | lo);
+}
+// Buffer descriptor of `bytes` bytes from p on (both the same in every lane):
+// reads past its end give zeros.
+typedef uint32_t rsrc_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ rsrc_t rsrc_of(const char* p, uint32_t bytes) {
+  return rsrc_t{(uint32_t)uniform((int)(uint64_t)p), (uint32_t)uniform((int)((uint64_t)p >> 32)) & 0xffffu, (uint32_t)uniform((int)bytes), 0x00020000u};
+}
+__device__ __forceinline__ uint32_t lds_address(const char* p) {
+  return (uint32_t)(uintptr_t)(__attribute__((address_space(3))) const char*)p;
+}
+// 16 bytes per lane from the buffer to LDS at `to` + 16 lane.  Written out, since
+// the compiler lets no transposing LDS read pass while an LDS-DMA load that it
+// knows of is in flight; the waits for these loads are wait_vmcnt's alone.  (m0 is
+// nobody else's here: nothing in this file makes the compiler use it.  The idle
+// cycles are what a descriptor fresh from readfirstlane needs before its use.)
+__device__ __forceinline__ void dma16(rsrc_t rs, uint32_t off, uint32_t to) {
+  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform((int)to)), "v"(off), "s"(rs) : "memory");
+}
 // 2^x by the hardware instruction alone: results below 2^-126 count as zero.
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 // max / sum over lanes l and l ^ 32, which hold the halves of one row's scores
@@ -76,6 +102,18 @@ __device__ __forceinline__ float max_pair32(float x) {
 __device__ __forceinline__ float sum_pair32(float x) {
   const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
   return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+
+// Two bf16, or a float, with NaN and infinities as zero.
+template <typename T>
+__device__ __forceinline__ uint32_t numbers(uint32_t w) {
+  if constexpr (sizeof(T) == 2) {
+    if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
+    if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
+  } else {
+    if ((w & 0x7f800000u) == 0x7f800000u) w = 0;
+  }
+  return w;
 }
 
 // LDS tiles: rows of HD elements (one key each) in 16-byte chunks, chunk c of
@@ -124,15 +162,17 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
   const int unit = up / p.parts, tile = p.tiles - 1 - ((i8 % p.part_tiles) * p.parts + up % p.parts);
   if (unit >= p.units || tile < 0) return;
   const int g = unit % a.Hkv, rest = unit / a.Hkv, chunk = rest % p.chunks, dn = rest / p.chunks;
-  const Doc d = doc_of(a, dn);
+  Doc d = doc_of(a, dn);
+  d = Doc{uniform(d.q0), uniform(d.nq), uniform(d.k0), uniform(d.nk), uniform(d.pos), uniform(d.prefix)};
   const int G = a.Hq / a.Hkv, rows = d.nq * G, r0 = tile * 32 * QG;
   if (r0 >= rows) return;
   const int t_last = (min(r0 + 32 * QG, rows) - 1) / G;
-  const int kb = chunk * p.chunk_keys, ke = min(sees(a, d, t_last), p.chunks > 1 ? kb + p.chunk_keys : 0x7fffffff);
+  const int kb = uniform(chunk * p.chunk_keys), ke = uniform(min(sees(a, d, t_last), p.chunks > 1 ? kb + p.chunk_keys : 0x7fffffff));
   if (chunk > 0 && kb >= ke) return;
+  const int tile_first = uniform(sees(a, d, r0 / G));  // keys that every row of the tile sees
   // this wave's rows and this lane's
   const int w0 = r0 + 32 * qg, w1 = min(w0 + 32, rows);
-  const int see_first = w0 < rows ? sees(a, d, w0 / G) : 0, see_last = w0 < rows ? sees(a, d, (w1 - 1) / G) : 0;
+  const int see_first = uniform(w0 < rows ? sees(a, d, w0 / G) : 0), see_last = uniform(w0 < rows ? sees(a, d, (w1 - 1) / G) : 0);
   const int row = w0 + lq, t = row / G, h = g * G + row % G;
   const bool mine = row < rows;
   const int my_end = mine ? sees(a, d, t) : 0;
@@ -143,10 +183,10 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
   const bool direct = a.cap == 0.f && !a.slopes;
 
   // K and V of this head, as bytes; a tile's buffer starts at its first key
-  const char* kp = static_cast<const char*>(a.k.data) +
-                   (dn * a.k.stride_b + d.k0 * a.k.stride_l + g * a.k.stride_h) * (long)sizeof(T);
-  const char* vp = static_cast<const char*>(a.v.data) +
-                   (dn * a.v.stride_b + d.k0 * a.v.stride_l + g * a.v.stride_h) * (long)sizeof(T);
+  const char* kp = uniform(static_cast<const char*>(a.k.data) +
+                           (dn * a.k.stride_b + d.k0 * a.k.stride_l + g * a.k.stride_h) * (long)sizeof(T));
+  const char* vp = uniform(static_cast<const char*>(a.v.data) +
+                           (dn * a.v.stride_b + d.k0 * a.v.stride_l + g * a.v.stride_h) * (long)sizeof(T));
   const uint32_t ksb = (uint32_t)(a.k.stride_l * sizeof(T)), vsb = (uint32_t)(a.v.stride_l * sizeof(T));
   // The waves of a key group load its tile: wave qg the parts qg, qg + QG, ..,
   // K's before V's; a part is 1 KiB of whole rows, lane l filling slot l % CH
@@ -160,21 +200,18 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
     const int c = (lane % TL::CH) ^ (isk ? TL::k_swz(r) : TL::v_swz(r));
     off[x] = r * (isk ? ksb : vsb) + c * 16;
   }
+  const uint32_t lds0 = lds_address(lds) + kg * TILE + qg * 1024;
   auto issue = [&](int u) {
-    char* base = lds + (u % S) * STAGE + kg * TILE + qg * 1024;
+    const uint32_t to = lds0 + (u % S) * STAGE;
     const int t0 = kb + (u * KG + kg) * KT;
     const int left = min(ke - t0, KT);  // reads past the last key give zeros
     const uint32_t n = left > 0 ? left - 1 : 0, any = left > 0 ? TL::ROW : 0u;
     const long from = left > 0 ? t0 : 0;
-    const __amdgpu_buffer_rsrc_t rk =
-        __builtin_amdgcn_make_buffer_rsrc((void*)(kp + from * ksb), 0, n * ksb + any, 0x00020000);
-    const __amdgpu_buffer_rsrc_t rv =
-        __builtin_amdgcn_make_buffer_rsrc((void*)(vp + from * vsb), 0, n * vsb + any, 0x00020000);
+    const rsrc_t rk = rsrc_of(kp + from * ksb, n * ksb + any), rv = rsrc_of(vp + from * vsb, n * vsb + any);
 #pragma unroll
     for (int x = 0; x < PER; ++x) {
       const bool isk = x < PER / 2;
-      char* to = base + (isk ? x * QG * 1024 : K_BYTES + (x - PER / 2) * QG * 1024);
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(isk ? rk : rv, (lds_ptr_t)to, 16, off[x], 0, 0, 0);
+      dma16(isk ? rk : rv, off[x], to + (isk ? x * QG * 1024 : K_BYTES + (x - PER / 2) * QG * 1024));
     }
   };
   const int nsteps = ke > kb ? (ke - kb + KG * KT - 1) / (KG * KT) : 0;
@@ -230,9 +267,51 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
       asm volatile("" ::: "memory");
     if (u + D < nsteps) issue(u + D);
     const int t0 = kb + (u * KG + kg) * KT;
+    char* kt = lds + (u % S) * STAGE + kg * TILE;
+    char* vt = kt + K_BYTES;
+    if (kb + (u + 1) * KG * KT > tile_first) {
+      // Some row does not see some key of this step.  A zero probability still
+      // makes NaN of a value that is no number: such values are added to the rows
+      // that see them here, and zeroed before the products.
+      constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7f800000u;  // exponents of a word
+      uint32_t top = 0;
+      for (int i = qg * 64 + lane; i < K_BYTES / 16; i += QG * 64) {
+        const uint4 w = reinterpret_cast<const uint4*>(vt)[i];
+        for (const uint32_t x : {w.x & EXP, w.y & EXP, w.z & EXP, w.w & EXP})
+          if constexpr (BF)
+            top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us_t, top), __builtin_bit_cast(v2us_t, x)));
+          else
+            top = max(top, x);
+      }
+      bool broken = __ballot((top & 0xffffu) == 0x7f80u || (top >> 16) == 0x7f80u) != 0ull;
+      if constexpr (QG > 1) broken = __syncthreads_or(broken);
+      if (broken) {
+        for (int key = 0; key < KT; ++key) {
+          const char* vrow = vt + key * TL::ROW;
+          const bool seen = t0 + key < min(my_end, ke);
+#pragma unroll
+          for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const int e = ds * 32 + 8 * (r >> 2) + 4 * half + (r & 3), b = e * (int)sizeof(T);
+              const T w = *reinterpret_cast<const T*>(vrow + ((((b >> 4) ^ TL::v_swz(key)) << 4) | (b & 15)));
+              float f;
+              if constexpr (BF)
+                f = bf2f(w);
+              else
+                f = w;
+              if (seen && !(fabsf(f) < INFINITY)) st.o[ds][r] += f;
+            }
+        }
+        if constexpr (QG > 1) __syncthreads();
+        for (int i = qg * 64 + lane; i < K_BYTES / 4; i += QG * 64) {
+          uint32_t* w = reinterpret_cast<uint32_t*>(vt) + i;
+          *w = numbers<T>(*w);
+        }
+        if constexpr (QG > 1) __syncthreads();
+      }
+    }
     if (t0 >= min(ke, see_last)) continue;  // nothing that this wave's rows see
-    const char* kt = lds + (u % S) * STAGE + kg * TILE;
-    const char* vt = kt + K_BYTES;
 
     f32x16_t s2[NS];
 #pragma unroll
@@ -252,6 +331,15 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
       for (int c = 0; c < NQ; ++c)
 #pragma unroll
         for (int b = 0; b < NS; ++b) s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c][b], qb[c], s2[b], 0, 0, 0);
+      // the K reads run six ahead of their MFMAs
+      constexpr int KR = NQ * NS, AHEAD = 6;
+      __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
+#pragma unroll
+      for (int i = 0; i < KR - AHEAD; ++i) {
+        __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+        __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+      }
+      __builtin_amdgcn_sched_group_barrier(0x008, AHEAD, 0);
     } else {
 #pragma unroll
       for (int c = 0; c < NQ; ++c)
@@ -331,83 +419,36 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
       }
     st.l += psum;
 
-    // values of keys that some row of the tile does not see, where they are no
-    // numbers, must not meet that row's zero probability in a product
-    bool broken = false;
-    if (!whole) {
-      constexpr uint32_t E = BF ? 0x7f807f80u : 0x7f800000u;  // exponents of a word
-      uint32_t top = 0;
-      const uint4* words = reinterpret_cast<const uint4*>(vt);
-#pragma unroll 4
-      for (int i = lane; i < K_BYTES / 16; i += 64) {
-        const uint4 w = words[i];
-        for (const uint32_t x : {w.x & E, w.y & E, w.z & E, w.w & E})
-          if constexpr (BF)
-            top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us_t, top), __builtin_bit_cast(v2us_t, x)));
-          else
-            top = max(top, x);
-      }
-      broken = __ballot((top & 0xffffu) == 0x7f80u || (top >> 16) == 0x7f80u) != 0ull;
-    }
-    if (broken) {
-      for (int key = 0; key < KT; ++key) {
-        const char* vrow = vt + key * TL::ROW;
-        const bool seen = t0 + key < min(my_end, ke);
-#pragma unroll
-        for (int ds = 0; ds < ND; ++ds)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int e = ds * 32 + 8 * (r >> 2) + 4 * half + (r & 3), b = e * (int)sizeof(T);
-            const T w = *reinterpret_cast<const T*>(vrow + ((((b >> 4) ^ TL::v_swz(key)) << 4) | (b & 15)));
-            float f;
-            if constexpr (BF)
-              f = bf2f(w);
-            else
-              f = w;
-            if (seen && !(fabsf(f) < INFINITY)) st.o[ds][r] += f;
-          }
-      }
-    }
-    auto number = [&](uint32_t w) {  // non-numbers as zero
-      if constexpr (BF) {
-        if ((w & 0x7f80u) == 0x7f80u) w &= 0xffff0000u;
-        if ((w & 0x7f800000u) == 0x7f800000u) w &= 0xffffu;
-      } else {
-        if ((w & 0x7f800000u) == 0x7f800000u) w = 0;
-      }
-      return w;
-    };
     if constexpr (BF) {
       // slice jk: keys 16 jk + 4 half .. and 16 jk + 8 + 4 half ..; lane n of 16
       // gives the address of row n / 4, columns 4 (n % 4) .. of its 4 x 16 block
       // and receives column n
       const int n = lane & 15, c16 = (lane >> 4) & 1, vr = n >> 2;
-      const char* vb = vt + (4 * half + vr) * TL::ROW;
+      char* vb = vt + (4 * half + vr) * TL::ROW;
+      char* va[ND];
+#pragma unroll
+      for (int ds = 0; ds < ND; ++ds) {
+        const int e = ds * 32 + c16 * 16 + 4 * (n & 3);
+        va[ds] = vb + ((((e >> 3) ^ TL::v_swz(vr)) << 4) | ((e & 7) * 2));
+      }
 #pragma unroll
       for (int jk = 0; jk < KT / 16; ++jk) {
-        bf16x8_t pf;
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const uint32_t w = pack_bf16x2(s2[jk >> 1][(jk & 1) * 8 + 2 * e], s2[jk >> 1][(jk & 1) * 8 + 2 * e + 1]);
-          pf[2 * e] = (short)(w & 0xffff);
-          pf[2 * e + 1] = (short)(w >> 16);
-        }
+        v4s_t x[ND], y[ND];
 #pragma unroll
         for (int ds = 0; ds < ND; ++ds) {
-          const int e = ds * 32 + c16 * 16 + 4 * (n & 3);
-          const char* at = vb + jk * 16 * TL::ROW + ((((e >> 3) ^ TL::v_swz(vr)) << 4) | ((e & 7) * 2));
-          const v4s_t lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)at);
-          const v4s_t hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(at + 8 * TL::ROW));
-          uint2 x = __builtin_bit_cast(uint2, lo), y = __builtin_bit_cast(uint2, hi);
-          if (broken) {
-            x.x = number(x.x);
-            x.y = number(x.y);
-            y.x = number(y.x);
-            y.y = number(y.y);
-          }
-          const bf16x8_t vf = __builtin_bit_cast(bf16x8_t, make_uint4(x.x, x.y, y.x, y.y));
-          st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf, st.o[ds], 0, 0, 0);
+          x[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + jk * 16 * TL::ROW));
+          y[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + (jk * 16 + 8) * TL::ROW));
         }
+        uint4 pw;
+        const f32x16_t& sp = s2[jk >> 1];
+        pw.x = pack_bf16x2(sp[(jk & 1) * 8 + 0], sp[(jk & 1) * 8 + 1]);
+        pw.y = pack_bf16x2(sp[(jk & 1) * 8 + 2], sp[(jk & 1) * 8 + 3]);
+        pw.z = pack_bf16x2(sp[(jk & 1) * 8 + 4], sp[(jk & 1) * 8 + 5]);
+        pw.w = pack_bf16x2(sp[(jk & 1) * 8 + 6], sp[(jk & 1) * 8 + 7]);
+#pragma unroll
+        for (int ds = 0; ds < ND; ++ds)
+          st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(x[ds], y[ds], 0, 1, 2, 3, 4, 5, 6, 7),
+                                                             __builtin_bit_cast(bf16x8_t, pw), st.o[ds], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -418,10 +459,9 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
 #pragma unroll
           for (int ds = 0; ds < ND; ++ds) {
             const int e = ds * 32 + lq;
-            uint32_t w = *reinterpret_cast<const uint32_t*>(vt + (key + 4 * half) * TL::ROW +
-                                                            ((((e >> 2) ^ (half << 3)) << 4) | ((e & 3) * 4)));
-            if (broken) w = number(w);
-            st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(w), s2[b][r], st.o[ds], 0, 0, 0);
+            const float w =
+                *reinterpret_cast<const float*>(vt + (key + 4 * half) * TL::ROW + ((((e >> 2) ^ (half << 3)) << 4) | ((e & 3) * 4)));
+            st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, s2[b][r], st.o[ds], 0, 0, 0);
           }
         }
     }
