@@ -70,6 +70,15 @@ __device__ __forceinline__ void barrier_nofence() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
+typedef float f2_t __attribute__((ext_vector_type(2)));
+// Two floats to bf16 in one instruction, and acc + the sum of two bf16.
+__device__ __forceinline__ uint32_t pack2(float lo, float hi) {
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(f2_t{lo, hi}, bf2_t));
+}
+__device__ __forceinline__ float add2(float acc, uint32_t w) {
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2_t, w), __builtin_bit_cast(bf2_t, 0x3f803f80u), acc, false);
+}
 __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ const char* uniform(const char* p) {
   const uint32_t lo = uniform((int)(uint64_t)p), hi = uniform((int)((uint64_t)p >> 32));
@@ -179,7 +188,10 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
   const float slope = a.slopes && mine ? a.slopes[h] * LOG2E : 0.f;
   const bool neg = a.scale < 0.f;  // scores are formed with |scale| and, where it is negative, -q
   const float sc = fabsf(a.scale) * LOG2E;
-  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f;
+  // capped scores: cap in log2 units, 2 log2(e) / cap per unit of score, and the
+  // coefficients of tanh for small ones
+  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f, cap_z = a.cap > 0.f ? 1.f / (cap2 * cap2) : 0.f;
+  const float th1 = -0.333313563f * cap_z, th2 = 0.132708743f * cap_z * cap_z, th3 = -0.0475493467f * cap_z * cap_z * cap_z;
   const bool direct = a.cap == 0.f && !a.slopes;
 
   // K and V of this head, as bytes; a tile's buffer starts at its first key
@@ -314,10 +326,7 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
     if (t0 >= min(ke, see_last)) continue;  // nothing that this wave's rows see
 
     f32x16_t s2[NS];
-#pragma unroll
-    for (int b = 0; b < NS; ++b)
-#pragma unroll
-      for (int r = 0; r < 16; ++r) s2[b][r] = 0.f;
+    const f32x16_t zero = {};
     if constexpr (BF) {
       bf16x8_t kf[NQ][NS];
 #pragma unroll
@@ -330,7 +339,7 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
 #pragma unroll
       for (int c = 0; c < NQ; ++c)
 #pragma unroll
-        for (int b = 0; b < NS; ++b) s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c][b], qb[c], s2[b], 0, 0, 0);
+        for (int b = 0; b < NS; ++b) s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c][b], qb[c], c ? s2[b] : zero, 0, 0, 0);
       // the K reads run six ahead of their MFMAs
       constexpr int KR = NQ * NS, AHEAD = 6;
       __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
@@ -348,7 +357,7 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
           const int r = b * 32 + lq;
           const f32x4v k4 = *reinterpret_cast<const f32x4v*>(kt + r * TL::ROW + (((c * 2 + half) ^ TL::k_swz(r)) << 4));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s2[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[c][e], s2[b], 0, 0, 0);
+          for (int e = 0; e < 4; ++e) s2[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[c][e], c + e ? s2[b] : zero, 0, 0, 0);
         }
     }
 
@@ -365,12 +374,29 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
     } else {
       fold = 1.f;
       if (a.cap > 0.f) {
-        // cap tanh(x / cap) = cap - 2 cap / (e^(2 x / cap) + 1)
+        float far = 0.f;
 #pragma unroll
         for (int b = 0; b < NS; ++b)
 #pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s2[b][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(exp2_hw(s2[b][r] * cap_in) + 1.f), cap2);
+          for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(s2[b][r]));
+        if (BF && __ballot(!(far * cap_in <= 0.8f)) == 0ull) {
+          // |x / cap| <= 0.4: tanh(y) = y P(y^2), P of degree 3 to 1e-7 (six
+          // instructions in place of two transcendental ones and three)
+#pragma unroll
+          for (int b = 0; b < NS; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r) {
+              const float x = s2[b][r] * sc, z = x * x;
+              s2[b][r] = x * fmaf(fmaf(fmaf(th3, z, th2), z, th1), z, 0.999999901f);
+            }
+        } else {
+          // cap tanh(x / cap) = cap - 2 cap / (e^(2 x / cap) + 1)
+#pragma unroll
+          for (int b = 0; b < NS; ++b)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              s2[b][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(exp2_hw(s2[b][r] * cap_in) + 1.f), cap2);
+        }
       } else {
 #pragma unroll
         for (int b = 0; b < NS; ++b)
@@ -408,14 +434,22 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
 #pragma unroll
         for (int r = 0; r < 16; ++r) st.o[ds][r] *= alpha;
     }
+    // bf16: the sum is that of the rounded probabilities, which the products see
     float psum = 0.f;
+    uint32_t pw[BF ? NS * 8 : 1];
 #pragma unroll
     for (int b = 0; b < NS; ++b)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        const float e = exp2_hw(fmaf(s2[b][r], fold, -m_ref));
-        s2[b][r] = e;
-        psum += e;
+      for (int r = 0; r < 16; r += 2) {
+        const float e0 = exp2_hw(fmaf(s2[b][r], fold, -m_ref)), e1 = exp2_hw(fmaf(s2[b][r + 1], fold, -m_ref));
+        if constexpr (BF) {
+          pw[b * 8 + r / 2] = pack2(e0, e1);
+          psum = add2(psum, pw[b * 8 + r / 2]);
+        } else {
+          s2[b][r] = e0;
+          s2[b][r + 1] = e1;
+          psum += e0 + e1;
+        }
       }
     st.l += psum;
 
@@ -439,16 +473,11 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
           x[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + jk * 16 * TL::ROW));
           y[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + (jk * 16 + 8) * TL::ROW));
         }
-        uint4 pw;
-        const f32x16_t& sp = s2[jk >> 1];
-        pw.x = pack_bf16x2(sp[(jk & 1) * 8 + 0], sp[(jk & 1) * 8 + 1]);
-        pw.y = pack_bf16x2(sp[(jk & 1) * 8 + 2], sp[(jk & 1) * 8 + 3]);
-        pw.z = pack_bf16x2(sp[(jk & 1) * 8 + 4], sp[(jk & 1) * 8 + 5]);
-        pw.w = pack_bf16x2(sp[(jk & 1) * 8 + 6], sp[(jk & 1) * 8 + 7]);
+        const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, make_uint4(pw[jk * 4], pw[jk * 4 + 1], pw[jk * 4 + 2], pw[jk * 4 + 3]));
 #pragma unroll
         for (int ds = 0; ds < ND; ++ds)
           st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(x[ds], y[ds], 0, 1, 2, 3, 4, 5, 6, 7),
-                                                             __builtin_bit_cast(bf16x8_t, pw), st.o[ds], 0, 0, 0);
+                                                             pf, st.o[ds], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -525,7 +554,7 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
       const int e = ds * 32 + 8 * r + 4 * half;
       const float4 w = make_float4(st.o[ds][4 * r] * inv, st.o[ds][4 * r + 1] * inv, st.o[ds][4 * r + 2] * inv, st.o[ds][4 * r + 3] * inv);
       if constexpr (BF)
-        *reinterpret_cast<uint2*>(to + e) = make_uint2(pack_bf16x2(w.x, w.y), pack_bf16x2(w.z, w.w));
+        *reinterpret_cast<uint2*>(to + e) = make_uint2(pack2(w.x, w.y), pack2(w.z, w.w));
       else
         *reinterpret_cast<float4*>(to + e) = w;
     }
@@ -566,7 +595,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* to = static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h + e;
   if constexpr (sizeof(T) == 2)
-    *reinterpret_cast<uint2*>(to) = make_uint2(pack_bf16x2(o.x * inv, o.y * inv), pack_bf16x2(o.z * inv, o.w * inv));
+    *reinterpret_cast<uint2*>(to) = make_uint2(pack2(o.x * inv, o.y * inv), pack2(o.z * inv, o.w * inv));
   else
     *reinterpret_cast<float4*>(to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
