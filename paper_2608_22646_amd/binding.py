@@ -523,46 +523,51 @@ def _dtype(t, name):
     return _DTYPES[t.dtype]
 
 
-class _On:
-    """The device and stream of a call: the operands' device is made current, and
-    what the call allocates belongs to the stream that uses it."""
+def _raw_stream(index):
+    """The current stream of device `index` as an address, without the cost of a Stream object where torch has a way."""
+    get = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    return get(index) if get else torch.cuda.current_stream(index).cuda_stream
 
-    def __init__(self, device, stream):
-        _refuse(device.type == "cuda", -1, "tensors must be on the GPU")
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
-        _refuse(self.stream.device == device, -1, "the stream is another device's than the tensors")
-        # nothing to change in the common case: this stream and device are current
-        idle = stream is None and torch.cuda.current_device() == device.index
-        self.scope = None if idle else torch.cuda.stream(self.stream)
 
-    def __enter__(self):
-        if self.scope is not None:
-            self.scope.__enter__()
-        return self.stream.cuda_stream
-
-    def __exit__(self, *exc):
-        if self.scope is not None:
-            self.scope.__exit__(*exc)
+def _elsewhere(device, stream):
+    """None where a call can go to the current stream of the current device; else the scope it runs in: the operands'
+    device made current, and what the call allocates owned by the stream that uses it."""
+    _refuse(device.type == "cuda", -1, "tensors must be on the GPU")
+    if stream is None and torch.cuda.current_device() == device.index:
+        return None
+    stream = torch.cuda.current_stream(device) if stream is None else stream
+    _refuse(stream.device == device, -1, "the stream is another device's than the tensors")
+    return torch.cuda.stream(stream)
 
 
 def _column(t, n, dtype, device, name):
     """The address of a device array of n elements (None: 0)."""
     if t is None:
         return None
-    _refuse(t.dtype == dtype and t.device == device, -1, f"{name} must be {dtype} on {device}")
-    _refuse(t.numel() == n and t.is_contiguous(), -2, f"{name} must be {n} contiguous elements")
+    if t.dtype != dtype or t.device != device:
+        _refuse(False, -1, f"{name} must be {dtype} on {device}")
+    if t.numel() != n or not t.is_contiguous():
+        _refuse(False, -2, f"{name} must be {n} contiguous elements")
     return t.data_ptr()
 
 
 def _rows(t, shape, like, name):
     """The view of a [B, L, H, hd] tensor whose last dimension is contiguous."""
-    _refuse(tuple(t.shape) == tuple(shape), -2, f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-    _refuse(t.dtype == like.dtype and t.device == like.device, -1, f"{name} must be {like.dtype} on {like.device}")
-    st = t.stride()
-    _refuse(st[3] == 1, -2, f"{name}: elements of a head must be contiguous")
+    b, l, h, e = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
+    if t.shape != shape or e != 1:
+        _refuse(t.shape == shape, -2, f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+        _refuse(e == 1 or t.numel() == 0, -2, f"{name}: elements of a head must be contiguous")
+    if t.dtype != like.dtype or t.device != like.device:
+        _refuse(False, -1, f"{name} must be {like.dtype} on {like.device}")
     # a dimension of one element is never stepped over: its stride says nothing
-    return View(t.data_ptr(), st[0] if shape[0] > 1 else 0, st[1] if shape[1] > 1 else shape[3],
-                st[2] if shape[2] > 1 else 0)
+    n = t.shape
+    return View(t.data_ptr(), b if n[0] > 1 else 0, l if n[1] > 1 else n[3], h if n[2] > 1 else 0)
+
+
+def _workspace(nbytes, device):
+    """A 256-byte aligned buffer (torch's own allocations are)."""
+    buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
+    return buf if buf.data_ptr() % 256 == 0 else device_buffer(nbytes, device)
 
 
 @dataclass(frozen=True)
@@ -591,20 +596,25 @@ def rotary(cfg: Rotary, q, k=None, pos=None, pos0=0, q_out=None, k_out=None, inv
     pos: int32 [B, L], or None for pos0 + l.  Outputs are new tensors unless given (q_out=q: in place).
     Returns (q_out, k_out)."""
     _refuse(q.dim() == 4 and (k is None or k.dim() == 4), -2, "q and k must be [B, L, heads, head_dim]")
+    scope = _elsewhere(q.device, stream)
+    if scope is not None:
+        with scope:
+            return rotary(cfg, q, k, pos, pos0, q_out, k_out, inverse)
     dt = _dtype(q, "q")
     B, L, n_q, hd = q.shape
     _refuse(hd == cfg.head_dim, -2, f"q has heads of {hd} elements, cfg of {cfg.head_dim}")
-    with _On(q.device, stream) as s:
-        p = _column(pos, B * L, torch.int32, q.device, "pos")
-        q_out = torch.empty((B, L, n_q, hd), dtype=q.dtype, device=q.device) if q_out is None else q_out
-        vq, vqo = _rows(q, (B, L, n_q, hd), q, "q"), _rows(q_out, (B, L, n_q, hd), q, "q_out")
-        vk = vko = None
-        n_k = 0
-        if k is not None:
-            n_k = k.shape[2]
-            k_out = torch.empty((B, L, n_k, hd), dtype=q.dtype, device=q.device) if k_out is None else k_out
-            vk, vko = _rows(k, (B, L, n_k, hd), q, "k"), _rows(k_out, (B, L, n_k, hd), q, "k_out")
-        check(lib().dllm_rotary(cfg.to_c(), dt, B, L, p, pos0, vq, vqo, n_q, vk, vko, n_k, int(bool(inverse)), s))
+    p = _column(pos, B * L, torch.int32, q.device, "pos")
+    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
+    vq, vqo = _rows(q, q.shape, q, "q"), _rows(q_out, q.shape, q, "q_out")
+    vk = vko = None
+    n_k = 0
+    if k is not None:
+        n_k = k.shape[2]
+        k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device) if k_out is None else k_out
+        shape = (B, L, n_k, hd)
+        vk, vko = _rows(k, shape, q, "k"), _rows(k_out, shape, q, "k_out")
+    check(lib().dllm_rotary(cfg.to_c(), dt, B, L, p, pos0, vq, vqo, n_q, vk, vko, n_k, int(bool(inverse)),
+                            _raw_stream(q.device.index)))
     return q_out, (k_out if k is not None else None)
 
 
@@ -632,6 +642,9 @@ class Docs:
                    max(kv_lens, default=0), ints(q_pos), ints(prefix))
 
 
+_DOC_ARRAYS = ("q_start", "q_len", "kv_start", "kv_len", "q_pos", "prefix")
+
+
 def attention(q, k, v, docs: Docs | None = None, block=0, scale=None, cap=0.0, slopes=None, out=None, ws=None,
               stream=None):
     """dllm_attention.  q [T, Hq, hd] with k, v [S, Hkv, hd]: packed documents in one slab; q [B, T, Hq, hd] with k, v
@@ -639,16 +652,19 @@ def attention(q, k, v, docs: Docs | None = None, block=0, scale=None, cap=0.0, s
     None); ws: a device_buffer of attention_workspace_size bytes (allocated here if None)."""
     _refuse(q.dim() in (3, 4) and k.dim() == q.dim() and v.dim() == q.dim(), -2,
             "q, k and v must be [tokens, heads, head_dim] or [docs, tokens, heads, head_dim]")
-    dt = _dtype(q, "q")
     dev = q.device
-    with _On(dev, stream) as s:
-        out = torch.zeros(q.shape, dtype=q.dtype, device=dev) if out is None else out
-        a = _attn_args(dt, q, k, v, out, docs or Docs(), block, scale, cap, slopes)
+    scope = _elsewhere(dev, stream)
+    if scope is not None:
+        with scope:
+            return attention(q, k, v, docs, block, scale, cap, slopes, out, ws)
+    dt = _dtype(q, "q")
+    out = torch.zeros(q.shape, dtype=q.dtype, device=dev) if out is None else out
+    a = _attn_args(dt, q, k, v, out, docs or Docs(), block, scale, cap, slopes)
+    if ws is None:
         n = _sz()
         check(lib().dllm_attention_workspace_size(a, n))
-        if ws is None and n.value:
-            ws = device_buffer(n.value, dev)
-        check(lib().dllm_attention(a, _ptr(ws), 0 if ws is None else ws.numel(), s))
+        ws = _workspace(n.value, dev) if n.value else None
+    check(lib().dllm_attention(a, _ptr(ws), 0 if ws is None else ws.numel(), _raw_stream(dev.index)))
     return out
 
 
@@ -667,9 +683,9 @@ def _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes):
         q, k, v, out = q[None], k[None], v[None], out[None]
     B, T, Hq, hd = q.shape
     S, Hkv = k.shape[1], k.shape[2]
-    views = [_rows(q, (B, T, Hq, hd), q, "q"), _rows(k, (B, S, Hkv, hd), q, "k"), _rows(v, (B, S, Hkv, hd), q, "v"),
-             _rows(out, (B, T, Hq, hd), q, "out")]
-    arrays = [docs.q_start, docs.q_len, docs.kv_start, docs.kv_len, docs.q_pos, docs.prefix]
+    kv = (B, S, Hkv, hd)
+    views = [_rows(q, q.shape, q, "q"), _rows(k, kv, q, "k"), _rows(v, kv, q, "v"), _rows(out, q.shape, q, "out")]
+    arrays = (docs.q_start, docs.q_len, docs.kv_start, docs.kv_len, docs.q_pos, docs.prefix)
     n = docs.count
     if n is None:
         n = next((t.numel() for t in arrays if t is not None), 1) if one else B
@@ -677,8 +693,7 @@ def _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes):
     if one:
         for w in views:
             w.stride_b = 0
-    names = ("q_start", "q_len", "kv_start", "kv_len", "q_pos", "prefix")
-    ptrs = [_column(t, n, torch.int32, dev, name) for t, name in zip(arrays, names)]
+    ptrs = [_column(t, n, torch.int32, dev, name) for t, name in zip(arrays, _DOC_ARRAYS)]
     return AttnArgs(dt, Hq, Hkv, hd, *views, n, T, S, T if docs.max_q is None else docs.max_q,
                     S if docs.max_kv is None else docs.max_kv, *ptrs, _column(slopes, Hq, torch.float32, dev, "slopes"),
                     1.0 / math.sqrt(hd) if scale is None else scale, cap, block)
@@ -688,24 +703,27 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask
     """dllm_sample on logits [rows, V] (rows of any stride) with uniform random numbers u [rows].  Controls are device
     arrays [rows] (top_k int32, the others float32).  Returns (token int32, conf, prob float32), each [rows]."""
     _refuse(logits.dim() == 2, -2, "logits must be [rows, vocab]")
+    dev = logits.device
+    scope = _elsewhere(dev, stream)
+    if scope is not None:
+        with scope:
+            return sample(logits, u, temperature, top_k, top_p, min_p, mask_id, ws)
     dt = _dtype(logits, "logits")
     R, V = logits.shape
-    dev = logits.device
     st = logits.stride()
     _refuse(st[1] == 1 or V == 1, -2, "logits: a row must be contiguous")
-    with _On(dev, stream) as s:
-        cols = [_column(u, R, torch.float32, dev, "u"), _column(temperature, R, torch.float32, dev, "temperature"),
-                _column(top_k, R, torch.int32, dev, "top_k"), _column(top_p, R, torch.float32, dev, "top_p"),
-                _column(min_p, R, torch.float32, dev, "min_p")]
-        token = torch.empty((R,), dtype=torch.int32, device=dev)
-        conf = torch.empty((2, R), dtype=torch.float32, device=dev)
-        a = SampleArgs(logits.data_ptr(), st[0], dt, R, V, mask_id, *cols, token.data_ptr(), conf.data_ptr(),
-                       conf.data_ptr() + 4 * R)
+    cols = [_column(u, R, torch.float32, dev, "u"), _column(temperature, R, torch.float32, dev, "temperature"),
+            _column(top_k, R, torch.int32, dev, "top_k"), _column(top_p, R, torch.float32, dev, "top_p"),
+            _column(min_p, R, torch.float32, dev, "min_p")]
+    token = torch.empty((R,), dtype=torch.int32, device=dev)
+    conf, prob = torch.empty((2, R), dtype=torch.float32, device=dev).unbind(0)
+    a = SampleArgs(logits.data_ptr(), st[0], dt, R, V, mask_id, *cols, token.data_ptr(), conf.data_ptr(),
+                   prob.data_ptr())
+    if ws is None:
         n = sample_workspace_size(R, V)
-        if ws is None and n:
-            ws = device_buffer(n, dev)
-        check(lib().dllm_sample(a, _ptr(ws), 0 if ws is None else ws.numel(), s))
-    return token, conf[0], conf[1]
+        ws = _workspace(n, dev) if n else None
+    check(lib().dllm_sample(a, _ptr(ws), 0 if ws is None else ws.numel(), _raw_stream(dev.index)))
+    return token, conf, prob
 
 
 def sample_workspace_size(rows, vocab):

@@ -561,12 +561,14 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
 #endif
 }
 
-// Joins a row's chunk states in chunk order: one thread per four dimensions.
+// Joins a row's chunk states in chunk order: a wave per row, its lanes first a
+// chunk's (maximum, sum) each, then 16 bytes of output each, in HD / 4 lanes per
+// chunk, 256 / HD chunks side by side.
 template <typename T, int HD>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) {
-  constexpr int TPR = HD / 4, RPW = 256 / TPR;  // threads per row, rows per workgroup
-  const long row = (long)blockIdx.x * RPW + threadIdx.x / TPR;
-  const int e = threadIdx.x % TPR * 4;
+  constexpr int LPC = HD / 4, SIDE = 64 / LPC;  // lanes per chunk, chunks side by side
+  const int lane = threadIdx.x & 63;
+  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
   if (row >= (long)a.docs * a.max_q * a.Hq) return;
   const int h = (int)(row % a.Hq);
   const long dt = row / a.Hq;
@@ -576,22 +578,46 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
   // chunks that the row's tile ran: all that it sees a key of
   const int n = (sees(a, d, t) + p.chunk_keys - 1) / p.chunk_keys;
   const float2* ml = p.part_ml + row * p.chunks;
+  const int e = lane % LPC * 4, side = lane / LPC;
   const float* part = p.part + row * p.chunks * HD + e;
-  float m = -INFINITY;
-  for (int c = 0; c < n; ++c) m = fmaxf(m, ml[c].x);
-  const float ref = m == -INFINITY ? 0.f : m;
-  float l = 0.f;
+  float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-  for (int c = 0; c < n; ++c) {
-    const float2 s = ml[c];
+  for (int c0 = 0; c0 < n; c0 += 64) {  // 64 chunks at a time, on the maximum so far
+    float2 s = make_float2(-INFINITY, 0.f);
+    if (c0 + lane < n) s = ml[c0 + lane];
+    float top = s.x;
+#pragma unroll
+    for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
+    const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.f : m_new, f0 = exp2_hw(m - ref);
+    m = m_new;
     const float f = exp2_hw(s.x - ref);
-    const float4 w = *reinterpret_cast<const float4*>(part + (size_t)c * HD);
-    l += s.y * f;
-    o.x += w.x * f;
-    o.y += w.y * f;
-    o.z += w.z * f;
-    o.w += w.w * f;
+    l = l * f0 + warp_sum(s.y * f);
+    o.x *= f0;
+    o.y *= f0;
+    o.z *= f0;
+    o.w *= f0;
+    const int here = min(64, n - c0);
+#pragma unroll 4
+    for (int i = 0; i < here; i += SIDE) {
+      const int c = min(i + side, here - 1);
+      const float fc = __shfl(f, c, 64);
+      const float4 w = *reinterpret_cast<const float4*>(part + (size_t)(c0 + c) * HD);
+      if (i + side < here) {
+        o.x += w.x * fc;
+        o.y += w.y * fc;
+        o.z += w.z * fc;
+        o.w += w.w * fc;
+      }
+    }
   }
+#pragma unroll
+  for (int x = LPC; x < 64; x <<= 1) {
+    o.x += __shfl_xor(o.x, x, 64);
+    o.y += __shfl_xor(o.y, x, 64);
+    o.z += __shfl_xor(o.z, x, 64);
+    o.w += __shfl_xor(o.w, x, 64);
+  }
+  if (side > 0) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
   T* to = static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h + e;
   if constexpr (sizeof(T) == 2)
@@ -600,6 +626,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
     *reinterpret_cast<float4*>(to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
+constexpr int CHUNK_MIN = 512, CHUNK_LEAST = 256, FEW_KG = 4, FEW_SLOTS = 1;
 // Which kernel a call takes and how its grid is laid out.  Sizes only.
 struct Choice {
   int qg, kg, kt;
@@ -610,25 +637,22 @@ Choice choose(const AttnArgs& a) {
   Choice c{};
   const bool f32 = a.dtype == DLLM_F32, wide_row = f32 && a.hd == 128;
   const int rows = a.max_q * (a.Hq / a.Hkv);
-  if (rows <= 32) {
-    c.qg = 1;
-    c.kg = wide_row ? 2 : 4;
-    c.kt = 32;
-  } else if (rows <= 64) {
-    c.qg = 2;
-    c.kg = wide_row ? 2 : 4;
-    c.kt = 32;
-  } else {
-    c.qg = f32 ? 4 : 8;
-    c.kg = 1;
-    c.kt = f32 ? 32 : 64;
-  }
+  const long heads = (long)a.docs * a.Hkv, cus = device_cu_count();
+  // the widest row tile with which row tiles and chunks of CHUNK_MIN keys can
+  // still give every CU a workgroup, else the narrowest: a wide tile reads keys and
+  // values for more rows, a narrow one leaves more waves to split the keys
+  const long chunks_max = std::max(1, a.max_kv / CHUNK_MIN);
+  c.qg = f32 ? 4 : 8;
+  while (c.qg > 1 && (rows <= 16 * c.qg || heads * ceil_div(rows, 32 * c.qg) * chunks_max < cus)) c.qg /= 2;
+  c.kg = c.qg == 8 ? 1 : c.qg == 4 ? (f32 ? 1 : 2) : wide_row ? 2 : c.qg == 2 ? 4 : FEW_KG;
+  c.kt = c.qg == 8 ? 64 : 32;
   AttnPlan& p = c.plan;
   p.tiles = ceil_div(rows, 32 * c.qg);
-  const long heads = (long)a.docs * a.Hkv, wgs = heads * p.tiles, cus = device_cu_count();
+  const long wgs = heads * p.tiles;
   const int step = c.kg * c.kt, steps = std::max(1, ceil_div(a.max_kv, step));
+  const long slots = c.qg == 1 ? FEW_SLOTS * cus : cus;
   int chunks = 1;
-  if (wgs < 2 * cus) chunks = (int)std::max(1l, std::min((2 * cus + wgs - 1) / wgs, (long)steps * step / 256));
+  if (wgs < slots) chunks = (int)std::max(1l, std::min(ceil_div(slots, wgs) + 0l, (long)a.max_kv / CHUNK_LEAST));
   const int per = ceil_div(steps, chunks);
   p.chunk_keys = per * step;
   p.chunks = ceil_div(steps, per);
@@ -648,18 +672,18 @@ void go(const AttnArgs& a, const Choice& c, hipStream_t s) {
 }
 template <typename T, int HD>
 void launch(const AttnArgs& a, const Choice& c, hipStream_t s) {
-  constexpr bool WIDE = sizeof(T) * HD == 512;  // rows of 512 bytes: half the keys fit
+  constexpr bool F32 = sizeof(T) == 4, WIDE = F32 && HD == 128;  // WIDE: rows of 512 bytes, half the keys fit
   if (c.qg == 1)
-    go<T, HD, 1, WIDE ? 2 : 4, 32, 2>(a, c, s);
+    go<T, HD, 1, WIDE ? 2 : FEW_KG, 32, 2>(a, c, s);
   else if (c.qg == 2)
     go<T, HD, 2, WIDE ? 2 : 4, 32, 2>(a, c, s);
-  else if constexpr (sizeof(T) == 4)
-    go<T, HD, 4, 1, 32, 3>(a, c, s);
-  else
+  else if (c.qg == 4)
+    go<T, HD, 4, F32 ? 1 : 2, 32, 3>(a, c, s);
+  else if constexpr (!F32)
     go<T, HD, 8, 1, 64, 3>(a, c, s);
   if (c.plan.chunks > 1) {
     const long rows = (long)a.docs * a.max_q * a.Hq;
-    attn_join_kernel<T, HD><<<ceil_div(rows, 1024 / HD), 256, 0, s>>>(a, c.plan);
+    attn_join_kernel<T, HD><<<ceil_div(rows, 4), 256, 0, s>>>(a, c.plan);
     DLLM_LAUNCH_CHECK("attn_join_kernel");
   }
 }
