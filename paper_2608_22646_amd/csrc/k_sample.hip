@@ -24,6 +24,7 @@
 // numbers (a weight in units of 2^-50 of its chunk's largest, 2^-40 of its
 // class's), so every sum is the same in any order and good to about 1e-12.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
 
@@ -117,7 +118,9 @@ struct ChunkStat {
 // class bm holds min-p's (-1: none).
 struct RowState {
   int ek, rk, lo, hi, bm;
-  int slot[SLOTS];  // classes listed, -1: none
+  int slot[SLOTS];    // classes listed, -1: none
+  float least, most;  // every listed member lies within
+  double base;        // class of the row's maximum
 };
 
 struct SampleWs {
@@ -129,6 +132,7 @@ struct SampleWs {
   RowState* state;   // [rows]
   uint2* list;       // [rows, LIST]: key, index | slot << 24
   uint32_t* listed;  // [rows]
+  uint8_t* holds;    // [rows, chunks]: 1 where a chunk has members of the listed classes
   int chunks;
 };
 
@@ -187,10 +191,40 @@ __device__ __forceinline__ void load_logits(const T* x, int v, int V, int mask_i
   }
 }
 
+// A thread's logits of a chunk: runs of 16 bytes, NT threads apart.
+template <typename T>
+__device__ __forceinline__ void load_chunk(const T* x, int v0, int V, int mask_id, float (&f)[E / (16 / (int)sizeof(T))][16 / (int)sizeof(T)]) {
+  constexpr int N = 16 / (int)sizeof(T), RUNS = E / N;
+  const int tid = threadIdx.x;
+  if (v0 + CHUNK <= V) {
+    struct __attribute__((packed, aligned(sizeof(T)))) Run {
+      T e[N];
+    };
+    const GLOBAL T* g = (const GLOBAL T*)x + v0;
+    Run r[RUNS];
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) r[i] = *(const GLOBAL Run*)(g + (i * NT + tid) * N);
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+      for (int e = 0; e < N; ++e) f[i][e] = to_f(r[i].e[e]);
+    if ((uint32_t)(mask_id - v0) < (uint32_t)CHUNK) {
+#pragma unroll
+      for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+        for (int e = 0; e < N; ++e)
+          if (v0 + (i * NT + tid) * N + e == mask_id) f[i][e] = -INFINITY;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT + tid) * N, V, mask_id, f[i]);
+  }
+}
+
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs w) {
-  __shared__ u64 mass[BINS];
-  __shared__ uint32_t count[BINS];
+  __shared__ u64 mass[BINS + 64];  // 64 places for what has no class
+  __shared__ uint32_t count[BINS + 64];
   __shared__ double powers[STEPS];
   __shared__ float s_top[NW];
   __shared__ uint32_t s_bad[NW], s_arg[NW];
@@ -200,8 +234,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
   constexpr int N = 16 / sizeof(T), RUNS = E / N;  // 16-byte runs
   float f[RUNS][N];
-#pragma unroll
-  for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT + tid) * N, a.vocab, a.mask_id, f[i]);
+  load_chunk<T>(x, v0, a.vocab, a.mask_id, f);
   const Controls c = controls_of(a, row);
   fill_powers(powers);
   if (c.filter) {
@@ -261,25 +294,39 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
 #pragma unroll
       for (int e = 0; e < N; ++e) sum += weight_of(in_classes(f[i][e], c.rate) - qtop, powers);
   } else {
-    auto add = [&](int b, double weight) {
-      if (b < BINS - 1) {
-        atomicAdd(mass + b, fixed50(weight));
-        if (c.top_k) atomicAdd(count + b, 1u);
-      }
-    };
     const double base = rint(qtop);
     if (fabs(qtop) < 0x1p30) {
       // the class: the nearest whole number to q, in the low word of q + 1.5 x 2^52;
-      // logits far below (and -inf) stand 600 classes below the top
+      // logits far below (and -inf) stand 600 classes below the top.  No branch
+      // per logit: what has no class goes to a place of the lane's own.
       const int base_i = (int)base;
       const double least = qtop - 600.0;
+      auto fill = [&](auto counted) {
 #pragma unroll
-      for (int i = 0; i < RUNS; ++i)
+        for (int i = 0; i < RUNS; ++i) {
+          double q[N];
+          int b[N];
+          u64 u[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) {
-          const double q = fmax(in_classes(f[i][e], c.rate), least);
-          add(base_i - __double2loint(q + 0x1.8p52), power_of(q - qtop, powers));
+          for (int e = 0; e < N; ++e) q[e] = fmax(in_classes(f[i][e], c.rate), least);
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            b[e] = base_i - __double2loint(q[e] + 0x1.8p52);
+            b[e] = b[e] < BINS - 1 ? b[e] : BINS + lane;
+          }
+#pragma unroll
+          for (int e = 0; e < N; ++e) u[e] = fixed50(power_of(q[e] - qtop, powers));
+#pragma unroll
+          for (int e = 0; e < N; ++e) {
+            atomicAdd(mass + b[e], u[e]);
+            if constexpr (decltype(counted)::value) atomicAdd(count + b[e], 1u);
+          }
         }
+      };
+      if (c.top_k)
+        fill(std::true_type{});
+      else
+        fill(std::false_type{});
     } else {
 #pragma unroll 1
       for (int i = 0; i < E; ++i) {
@@ -287,7 +334,11 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
 #pragma unroll
         for (int j = 0; j < E; ++j) y = j == i ? f[j / N][j % N] : y;
         const double q = in_classes(y, c.rate);
-        add((int)fmin(base - rint(q), (double)BINS), weight_of(q - qtop, powers));
+        const int b = (int)fmin(base - rint(q), (double)BINS);
+        if (b < BINS - 1) {
+          atomicAdd(mass + b, fixed50(weight_of(q - qtop, powers)));
+          atomicAdd(count + b, 1u);
+        }
       }
     }
   }
@@ -383,7 +434,10 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   }
   __syncthreads();
   const RowTop top = join_chunks(w.stat + (size_t)row * nch, nch, c, powers, ch);
-  if (top.bad != ~0u || top.big == -INFINITY) return;
+  if (top.bad != ~0u || top.big == -INFINITY) {  // decided without a boundary
+    for (int i = tid; i < nch; i += NT) w.holds[(size_t)row * nch + i] = 0;
+    return;
+  }
   __syncthreads();
   const GLOBAL u64* hm = (const GLOBAL u64*)w.mass + (size_t)row * nch * BINS;
   const GLOBAL uint32_t* hc = (const GLOBAL uint32_t*)w.count + (size_t)row * nch * BINS;
@@ -417,7 +471,7 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   w.prefix[(size_t)row * BINS + tid] = m;
   w.prefix_n[(size_t)row * BINS + tid] = n;
   __syncthreads();
-  RowState st{BINS, 0, 0, -1, -1, {-1, -1, -1, -1}};
+  RowState st{BINS, 0, 0, -1, -1, {-1, -1, -1, -1}, 0.f, 0.f, top.base};
   double least = binw[BINS - 2], most = least;  // bounds of the mass that top-p is a share of
   if (c.top_k) {
     if (tid < BINS - 1 && n >= (uint32_t)c.top_k && (tid == 0 || binc[tid - 1] < (uint32_t)c.top_k)) s_k = tid;
@@ -450,21 +504,39 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
     st.bm = max((int)fmin(top.base - rint(top.qtop + log(c.min_p) * PER_NAT), (double)(BINS - 1)), 0);
     edge = min(edge, st.bm + 1);
   }
-  if (tid == 0) {
-    // members are needed of the classes in which the boundary may fall, and of
-    // top-k's where top-p is a share of what it keeps
-    int used = 0;
-    auto want = [&](int b) {
-      for (int i = 0; i < used; ++i)
-        if (st.slot[i] == b) return;
-      if (used < SLOTS) st.slot[used++] = b;
-    };
-    const bool by_p = c.top_p < 1.0 && st.lo < edge;  // top-p may decide
-    if (st.rk > 0 && (by_p || st.ek == edge)) want(st.ek - 1);
-    if (st.bm >= 0 && st.bm < BINS - 1 && st.bm + 1 == edge) want(st.bm);
-    if (by_p)
-      for (int b = st.lo; b <= st.hi && b < edge && used < SLOTS; ++b) want(b);
-    w.state[row] = st;
+  // members are needed of the classes in which the boundary may fall, and of
+  // top-k's where top-p is a share of what it keeps
+  int used = 0, first = BINS, final = 0;
+  auto list = [&](int b) {
+    bool there = false;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i) there |= st.slot[i] == b;
+    if (there || used >= SLOTS) return;
+#pragma unroll
+    for (int i = 0; i < SLOTS; ++i)
+      if (i == used) st.slot[i] = b;
+    ++used;
+    first = min(first, b);
+    final = max(final, b);
+  };
+  const bool by_p = c.top_p < 1.0 && st.lo < edge;  // top-p may decide
+  if (st.rk > 0 && (by_p || st.ek == edge)) list(st.ek - 1);
+  if (st.bm >= 0 && st.bm < BINS - 1 && st.bm + 1 == edge) list(st.bm);
+  if (by_p)
+    for (int b = st.lo; b <= st.hi && b < edge && used < SLOTS; ++b) list(b);
+  // logits outside [least, most] lie in none of them (a margin covers float32)
+  const double hi = (top.base - first + 1) / c.rate, lo = (top.base - final - 1) / c.rate;
+  st.most = c.rate > 0 ? (float)(hi + fabs(hi) * 1e-6) : INFINITY;
+  st.least = c.rate > 0 ? (float)(lo - fabs(lo) * 1e-6) : -INFINITY;
+  if (tid == 0) w.state[row] = st;
+  for (int i = tid; i < nch; i += NT) {
+    u64 have = 0;
+#pragma unroll
+    for (int j = 0; j < SLOTS; ++j) {
+      const int k = st.slot[j] - ch.shift[i];
+      if (st.slot[j] >= 0 && k >= 0) have |= hm[(size_t)i * BINS + k];
+    }
+    w.holds[(size_t)row * nch + i] = have != 0;
   }
 }
 
@@ -474,49 +546,19 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, v0 = chunk * CHUNK;
   const Controls c = controls_of(a, row);
-  if (!c.filter) return;
-  const ChunkStat* stat = w.stat + (size_t)row * w.chunks;
-  float big = -INFINITY;
-  uint32_t bad = ~0u;
-  for (int i = lane; i < w.chunks; i += 64) {
-    big = fmaxf(big, stat[i].top);
-    bad = min(bad, stat[i].bad);
-  }
-  big = wave_all(big, Max{});
-  bad = wave_all(bad, Min{});
-  if (bad != ~0u || stat[chunk].top == -INFINITY) return;
+  if (!c.filter || !w.holds[blockIdx.x]) return;
   const RowState st = w.state[row];
-  const double base = rint(in_classes(big, c.rate));
-  const double shift = base - rint(in_classes(stat[chunk].top, c.rate));
-  if (shift >= BINS) return;
-  u64 have = 0;
-#pragma unroll
-  for (int i = 0; i < SLOTS; ++i)
-    if (st.slot[i] >= 0 && st.slot[i] >= (int)shift)
-      have |= w.mass[((size_t)row * w.chunks + chunk) * BINS + st.slot[i] - (int)shift];
-  if (have == 0) return;
-  // logits outside [least, most] lie in none of the classes (a margin covers float32)
-  int first = BINS, final = 0;
-#pragma unroll
-  for (int i = 0; i < SLOTS; ++i)
-    if (st.slot[i] >= 0) {
-      first = min(first, st.slot[i]);
-      final = max(final, st.slot[i]);
-    }
-  const double hi = (base - first + 1) / c.rate, lo = (base - final - 1) / c.rate;
-  const float most = c.rate > 0 ? (float)(hi + fabs(hi) * 1e-6) : INFINITY, least = c.rate > 0 ? (float)(lo - fabs(lo) * 1e-6) : -INFINITY;
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
   constexpr int N = 16 / sizeof(T), RUNS = E / N;
   float f[RUNS][N];
-#pragma unroll
-  for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT + tid) * N, a.vocab, a.mask_id, f[i]);
+  load_chunk<T>(x, v0, a.vocab, a.mask_id, f);
   uint32_t hit = 0, slots = 0;
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (f[i][e] >= least && f[i][e] <= most && f[i][e] > -INFINITY) {
-        const int b = class_of(f[i][e], c.rate, base);
+      if (f[i][e] >= st.least && f[i][e] <= st.most && f[i][e] > -INFINITY) {
+        const int b = class_of(f[i][e], c.rate, st.base);
 #pragma unroll
         for (int k = 0; k < SLOTS; ++k)
           if (b == st.slot[k]) {
@@ -565,16 +607,21 @@ struct Cut {
 
 template <typename T>
 struct Picker {
+  static constexpr int KEPT = 4096, FEW = 64;
   // LDS
   struct Shared {
     Chunks ch;
     double part[MAX_CHUNKS];  // kept mass of a chunk
     u64 extra[MAX_CHUNKS];
+    double prefix[BINS];
+    uint2 list[KEPT];  // the row's list, where it fits
     u64 sub_mass[NT];
     uint32_t sub_count[NT];
+    uint2 few[FEW];
     double powers[STEPS], bufd[NW];
     uint32_t bufu[NW], a, b, n;
     int i;
+    double m;
   };
   Shared& sh;
   const T* x;
@@ -599,7 +646,13 @@ struct Picker {
       if (st.slot[i] == b) slot = i;
     if (slot >= 0 && listed <= LIST) {
       for (uint32_t i = threadIdx.x; i < listed; i += NT) {
-        const uint2 m = {list[i].x, list[i].y};
+        uint2 m;
+        if (listed <= KEPT) {
+          m = sh.list[i];
+        } else {
+          m.x = list[i].x;
+          m.y = list[i].y;
+        }
         if ((int)(m.y >> 24) == slot) f(m.x, m.y & 0xffffffu);
       }
       return;
@@ -623,58 +676,65 @@ struct Picker {
   static __device__ __forceinline__ int top_of(int b) { return ((1 - b) >> 3) + 1; }
 
   // The members of class b that stay when at most `limit` of them may, and the mass
-  // of the members before one must be less than `target`: narrows the range of keys,
-  // then of indices among equal keys, NT parts at a time.
+  // of the members before one must be less than `target`: the range of keys, then of
+  // indices among equal keys, is narrowed NT parts at a time until few members are
+  // left in it, which one wave then ranks.
   __device__ __forceinline__ Cut select(int b, uint32_t limit, double target) {
     const int tid = threadIdx.x, lane = tid & 63;
     const double unit = ldexp(1.0, top_of(b) - 40), units = ldexp(1.0, 40 - top_of(b));
     target = fmax(target, 1e-300);  // the first of all stays
-    __syncthreads();
-    if (tid == 0) {
-      sh.a = ~0u;
-      sh.b = 0;
-      sh.n = 0;
-    }
-    __syncthreads();
-    uint32_t lo = ~0u, hi = 0, tied = 0;
-    members(b, [&](uint32_t key, uint32_t) {
-      lo = min(lo, key);
-      hi = max(hi, key);
-      ++tied;
-    });
-    lo = wave_all(lo, Min{});
-    hi = wave_all(hi, Max{});
-    tied = wave_all(tied, Sum{});
-    if (lane == 0) {
-      atomicMin(&sh.a, lo);
-      atomicMax(&sh.b, hi);
-      atomicAdd(&sh.n, tied);
-    }
-    __syncthreads();
-    lo = sh.a;
-    hi = sh.b;
-    tied = sh.n;  // members in the range
-    // the range is keys [lo, hi] from above, then indices [lo, hi] from below
+    // the range: keys [lo, hi] from above, then indices [lo, hi] from below
+    const double edge0 = (top.base - b - 1) / rate, edge1 = (top.base - b + 1) / rate;
+    const float f0 = (float)(edge0 - fabs(edge0) * 1e-6), f1 = (float)(edge1 + fabs(edge1) * 1e-6);
+    uint32_t lo = rate > 0 ? key_of(f0) : key_of(-INFINITY), hi = rate > 0 ? key_of(f1) : key_of(INFINITY);
+    uint32_t inside = listed <= LIST ? listed : ~0u;  // members in the range, at most
     bool by_key = true;
-    uint32_t n0 = 0;  // members ranked before the range, and their mass
+    uint32_t n0 = 0, key0 = 0;  // members ranked before the range, and their mass; its key, once it is one
     double m0 = 0;
-    Cut r{0, ~0u, 0};
+    auto in_range = [&](uint32_t key, uint32_t v) { return by_key ? key >= lo && key <= hi : key == key0 && v >= lo && v <= hi; };
     for (;;) {
+      if (inside <= FEW) {
+        __syncthreads();
+        if (tid == 0) sh.n = 0;
+        __syncthreads();
+        members(b, [&](uint32_t key, uint32_t v) {
+          if (in_range(key, v)) sh.few[min(atomicAdd(&sh.n, 1u), (uint32_t)FEW - 1)] = make_uint2(key, v);
+        });
+        __syncthreads();
+        const int n = (int)sh.n;
+        const uint2 mine = lane < n ? sh.few[lane] : make_uint2(0, ~0u);
+        const u64 fixed = lane < n ? (u64)(weight(value_of(mine.x)) * units) : 0;
+        uint32_t rank = 0;
+        u64 before = 0;
+        for (int j = 0; j < n; ++j) {
+          const uint32_t kj = __shfl(mine.x, j, 64), vj = __shfl(mine.y, j, 64);
+          const u64 wj = __shfl(fixed, j, 64);
+          if (kj > mine.x || (kj == mine.x && vj < mine.y)) {
+            ++rank;
+            before += wj;
+          }
+        }
+        const double mass = m0 + (double)before * unit;
+        const bool stays = lane < n && n0 + rank < limit && mass < target;
+        // the last that stays: the one of the highest rank
+        const uint32_t r = wave_all(stays ? rank + 1 : 0u, Max{});
+        const u64 who = __ballot(stays && rank + 1 == r);
+        if (who == 0) return Cut{by_key && n0 == 0 ? ~0u : key0, 0, m0};  // (none of them)
+        const int l = __ffsll(who) - 1;
+        return Cut{(uint32_t)__shfl(mine.x, l, 64), (uint32_t)__shfl(mine.y, l, 64),
+                   __shfl(mass + (double)fixed * unit, l, 64)};
+      }
       if (by_key && hi == lo) {
+        // many equal members: those with the lowest indices
         const double each = weight(value_of(lo));
         const uint32_t ties = (uint32_t)fmax(fmin((double)(limit - n0), ceil((target - m0) / each)), 1.0);
-        r.key = lo;
-        r.mass = m0 + (double)ties * each;
-        if (ties >= tied) return r;  // every one of the equal members
+        if (ties >= inside) return Cut{lo, ~0u, m0 + (double)inside * each};
         by_key = false;
+        key0 = lo;
         limit = n0 + ties;
         target = INFINITY;
         lo = 0;
         hi = (uint32_t)V - 1;
-      }
-      if (!by_key && hi == lo) {
-        r.last = lo;
-        return r;
       }
       const uint32_t span = hi - lo;
       const int down = span >= NT ? 32 - __clz(span) - 9 : 0;  // span >> down < NT = 2^9
@@ -682,12 +742,11 @@ struct Picker {
       sh.sub_count[tid] = 0;
       if (tid == 0) sh.i = -1;
       __syncthreads();
-      const uint32_t key0 = r.key;
       members(b, [&](uint32_t key, uint32_t v) {
-        const uint32_t at = by_key ? hi - key : v - lo;
-        if (at <= span && (by_key || key == key0)) {
-          if (by_key) atomicAdd(sh.sub_mass + (at >> down), (u64)(weight(value_of(key)) * units));
-          atomicAdd(sh.sub_count + (at >> down), 1u);
+        if (in_range(key, v)) {
+          const uint32_t at = (by_key ? hi - key : v - lo) >> down;
+          atomicAdd(sh.sub_mass + at, (u64)(weight(value_of(key)) * units));
+          atomicAdd(sh.sub_count + at, 1u);
         }
       });
       __syncthreads();
@@ -696,19 +755,19 @@ struct Picker {
       const uint32_t n1 = block_scan(mine, sh.bufu);
       const double m1 = block_scan(mass, sh.bufd);
       const bool reached = n0 + n1 >= limit || m0 + m1 >= target;
-      const bool before = tid > 0 && (n0 + n1 - mine >= limit || m0 + (m1 - mass) >= target);
+      const bool before = n0 + n1 - mine >= limit || m0 + (m1 - mass) >= target;
       if (reached && !before && mine > 0) {
         sh.i = tid;
         sh.a = n1 - mine;
         sh.b = mine;
-        sh.bufd[0] = m1 - mass;
+        sh.m = m1 - mass;
       }
       __syncthreads();
       const int i = sh.i;
       if (i < 0) return Cut{0, ~0u, 0};  // no limit is reached: all stay
       n0 += sh.a;
-      m0 += sh.bufd[0];
-      tied = sh.b;
+      m0 += sh.m;
+      inside = sh.b;
       const uint32_t p = (uint32_t)i << down, q = min(span, (((uint32_t)i + 1) << down) - 1);
       if (by_key) {
         lo = hi - q;
@@ -736,6 +795,8 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     if (a.prob) a.prob[row] = prob;
   };
   fill_powers(sh.powers);
+  if (c.filter) sh.prefix[tid] = w.prefix[(size_t)row * BINS + tid];
+  sh.extra[tid] = 0;
   __syncthreads();
   P p{sh, static_cast<const T*>(a.logits) + (long)row * a.row_stride, (const GLOBAL uint2*)w.list + (size_t)row * LIST,
       join_chunks(stat, nch, c, sh.powers, sh.ch), c.rate, V, a.mask_id, 0, RowState{}};
@@ -774,7 +835,10 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     p.st = w.state[row];
     p.listed = w.listed[row];
     const RowState& st = p.st;
-    const double* prefix = w.prefix + (size_t)row * BINS;
+    const double* prefix = sh.prefix;
+    if (p.listed <= P::KEPT)
+      for (uint32_t i = tid; i < p.listed; i += NT) sh.list[i] = make_uint2(p.list[i].x, p.list[i].y);
+    __syncthreads();
     auto mass_before = [&](int b) { return b > 0 ? prefix[b - 1] : 0.0; };
     const int bk = st.rk > 0 ? st.ek - 1 : -1;
     edge = bk >= 0 ? bk : st.ek;
@@ -811,25 +875,33 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
       cut = p.select(edge, limit, target);
     }
     // ---- kept mass of each chunk: its classes before the edge, then the edge's members
-    sh.extra[tid] = 0;
-    __syncthreads();
     const double unit = ldexp(1.0, P::top_of(edge) - 40), units = ldexp(1.0, 40 - P::top_of(edge));
     if (edge < BINS - 1 && cut.key != ~0u)
       p.members(edge, [&](uint32_t key, uint32_t v) {
         const float f = value_of(key);
         if (stays(f, key, v)) atomicAdd(sh.extra + v / CHUNK, (u64)(p.weight(f) * units));
       });
-    for (int i = wave; i < nch; i += NW) {
-      const GLOBAL u64* h = (const GLOBAL u64*)w.mass + ((size_t)row * nch + i) * BINS;
-      const int end = min(edge, BINS - 1) - sh.ch.shift[i];  // classes of the chunk before the edge
-      u64 s = 0;
+    const GLOBAL u64* h = (const GLOBAL u64*)w.mass + (size_t)row * nch * BINS;
+    constexpr int U = 4;  // chunks of a wave at a time
+    for (int i0 = wave; i0 < nch; i0 += NW * U) {
+      u64 s[U];
 #pragma unroll
-      for (int k = 0; k < BINS / 64; ++k) {
-        const int at = k * 64 + lane;
-        if (at < end) s += h[at];
+      for (int j = 0; j < U; ++j) {
+        const int i = i0 + j * NW;
+        // classes of the chunk before the edge
+        const int end = i < nch ? min(edge, BINS - 1) - sh.ch.shift[min(i, nch - 1)] : 0;
+        s[j] = 0;
+#pragma unroll
+        for (int k = 0; k < BINS / 64; ++k) {
+          const int at = k * 64 + lane;
+          if (at < end) s[j] += h[(size_t)i * BINS + at];
+        }
       }
-      s = wave_all(s, Sum{});
-      if (lane == 0) sh.part[i] = (double)s * 0x1p-50 * sh.ch.fac[i];
+#pragma unroll
+      for (int j = 0; j < U; ++j) {
+        s[j] = wave_all(s[j], Sum{});
+        if (lane == 0 && i0 + j * NW < nch) sh.part[i0 + j * NW] = (double)s[j] * 0x1p-50 * sh.ch.fac[i0 + j * NW];
+      }
     }
     __syncthreads();
     if (tid < nch) sh.part[tid] += (double)sh.extra[tid] * unit;
@@ -919,6 +991,7 @@ size_t carve(void* base, size_t rows, size_t chunks, SampleWs* w) {
   w->state = reinterpret_cast<RowState*>(take(rows * sizeof(RowState)));
   w->list = reinterpret_cast<uint2*>(take(rows * LIST * sizeof(uint2)));
   w->listed = reinterpret_cast<uint32_t*>(take(rows * sizeof(uint32_t)));
+  w->holds = reinterpret_cast<uint8_t*>(take(rows * chunks));
   return off;
 }
 
