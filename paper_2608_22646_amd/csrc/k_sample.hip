@@ -21,7 +21,7 @@
 //
 // Which token wins must not depend on rounding or on the order of execution.
 // Weights are float64 throughout; where threads add concurrently they add whole
-// numbers (a weight in units of 2^-50 of its chunk's largest, 2^-40 of its
+// numbers (a weight in units of 2^-36 of its chunk's largest, 2^-40 of its
 // class's), so every sum is the same in any order and good to about 1e-12.
 #include <algorithm>
 #include <type_traits>
@@ -82,10 +82,14 @@ __device__ __forceinline__ double power_of(double d, const double* powers) {
 // The same for any d <= 0 (2^-1000 for what lies below, and for NaN: -inf at an
 // infinite temperature).
 __device__ __forceinline__ double weight_of(double d, const double* powers) { return power_of(fmax(d, -8000.0), powers); }
-// A weight w in [0, 1] as a whole number of 2^-50: the mantissa of 4 + w.
-__device__ __forceinline__ uint64_t fixed50(double w) {
-  return __double_as_longlong(4.0 + w) - 0x4010000000000000ull;
+// What a class sums up, in one word: the count of its logits (at most CHUNK =
+// 2^13) from bit 50 on, their weights (each at most 1) as whole numbers of 2^-36
+// below: the mantissa of 2^16 + w.
+constexpr int COUNT_BIT = 50;
+__device__ __forceinline__ uint64_t class_word(double w) {
+  return __double_as_longlong(65536.0 + w) - (0x40f0000000000000ull - (1ull << COUNT_BIT));
 }
+__device__ __forceinline__ double class_mass(uint64_t word) { return (double)(word & ((1ull << COUNT_BIT) - 1)) * 0x1p-36; }
 
 template <typename V, typename F>
 __device__ __forceinline__ V wave_all(V x, F f) {
@@ -125,10 +129,8 @@ struct RowState {
 
 struct SampleWs {
   ChunkStat* stat;   // [rows, chunks]
-  u64* mass;         // [rows, chunks, BINS] in 2^-50
-  uint32_t* count;   // [rows, chunks, BINS]
+  u64* classes;      // [rows, chunks, BINS]: class_word sums
   double* prefix;    // [rows, BINS]: mass of the classes up to each
-  uint32_t* prefix_n;
   RowState* state;   // [rows]
   uint2* list;       // [rows, LIST]: key, index | slot << 24
   uint32_t* listed;  // [rows]
@@ -191,56 +193,62 @@ __device__ __forceinline__ void load_logits(const T* x, int v, int V, int mask_i
   }
 }
 
-// A thread's logits of a chunk: runs of 16 bytes, NT threads apart.
+// A thread's logits of a chunk: RUNS runs of 16 bytes, NT threads apart.
 template <typename T>
-__device__ __forceinline__ void load_chunk(const T* x, int v0, int V, int mask_id, float (&f)[E / (16 / (int)sizeof(T))][16 / (int)sizeof(T)]) {
-  constexpr int N = 16 / (int)sizeof(T), RUNS = E / N;
-  const int tid = threadIdx.x;
-  if (v0 + CHUNK <= V) {
-    struct __attribute__((packed, aligned(sizeof(T)))) Run {
-      T e[N];
-    };
-    const GLOBAL T* g = (const GLOBAL T*)x + v0;
-    Run r[RUNS];
+struct Slice {
+  static constexpr int N = 16 / (int)sizeof(T), RUNS = E / N;
+  struct __attribute__((packed, aligned(sizeof(T)))) Run {
+    T e[N];
+  };
+  Run r[RUNS];
+  static __device__ __forceinline__ int at(int v0, int i) { return v0 + (i * NT + (int)threadIdx.x) * N; }
+  // whole chunks only; the loads are left in flight
+  __device__ __forceinline__ void fetch(const T* x, int v0) {
+    const GLOBAL T* g = (const GLOBAL T*)x;
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i) r[i] = *(const GLOBAL Run*)(g + (i * NT + tid) * N);
-#pragma unroll
-    for (int i = 0; i < RUNS; ++i)
-#pragma unroll
-      for (int e = 0; e < N; ++e) f[i][e] = to_f(r[i].e[e]);
-    if ((uint32_t)(mask_id - v0) < (uint32_t)CHUNK) {
+    for (int i = 0; i < RUNS; ++i) r[i] = *(const GLOBAL Run*)(g + at(v0, i));
+  }
+  // the logits of a chunk that was fetched (whole) or is read here
+  __device__ __forceinline__ void take(const T* x, int v0, bool whole, int V, int mask_id, float (&f)[RUNS][N]) const {
+    if (whole) {
 #pragma unroll
       for (int i = 0; i < RUNS; ++i)
 #pragma unroll
-        for (int e = 0; e < N; ++e)
-          if (v0 + (i * NT + tid) * N + e == mask_id) f[i][e] = -INFINITY;
-    }
-  } else {
+        for (int e = 0; e < N; ++e) f[i][e] = to_f(r[i].e[e]);
+      if ((uint32_t)(mask_id - v0) < (uint32_t)CHUNK) {
 #pragma unroll
-    for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, v0 + (i * NT + tid) * N, V, mask_id, f[i]);
+        for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+          for (int e = 0; e < N; ++e)
+            if (at(v0, i) + e == mask_id) f[i][e] = -INFINITY;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < RUNS; ++i) load_logits<T, N>(x, at(v0, i), V, mask_id, f[i]);
+    }
   }
-}
+};
 
 template <typename T>
 __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs w) {
-  __shared__ u64 mass[BINS + 64];  // 64 places for what has no class
-  __shared__ uint32_t count[BINS + 64];
+  typedef Slice<T> SL;
+  constexpr int N = SL::N, RUNS = SL::RUNS;
+  __shared__ u64 classes[BINS + 64];  // 64 places for what has no class
   __shared__ double powers[STEPS];
   __shared__ float s_top[NW];
   __shared__ uint32_t s_bad[NW], s_arg[NW];
   __shared__ double s_sum[NW], s_sum1[NW];
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, v0 = chunk * CHUNK;
+  const int row = blockIdx.x / w.chunks, v0 = blockIdx.x % w.chunks * CHUNK;
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
-  constexpr int N = 16 / sizeof(T), RUNS = E / N;  // 16-byte runs
-  float f[RUNS][N];
-  load_chunk<T>(x, v0, a.vocab, a.mask_id, f);
+  const bool whole = v0 + CHUNK <= a.vocab;
+  SL slice;
+  if (whole) slice.fetch(x, v0);
   const Controls c = controls_of(a, row);
   fill_powers(powers);
-  if (c.filter) {
-    mass[tid] = 0;
-    count[tid] = 0;
-  }
+  classes[tid] = 0;
+  float f[RUNS][N];
+  slice.take(x, v0, whole, a.vocab, a.mask_id, f);
   float top = -INFINITY;
   bool broken = false;  // a NaN or +inf among mine
 #pragma unroll
@@ -256,7 +264,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
     for (int i = RUNS - 1; i >= 0; --i)
 #pragma unroll
       for (int e = N - 1; e >= 0; --e)
-        if (!(f[i][e] < INFINITY)) bad = v0 + (i * NT + tid) * N + e;
+        if (!(f[i][e] < INFINITY)) bad = SL::at(v0, i) + e;
   top = wave_all(top, Max{});
   bad = wave_all(bad, Min{});
   if (lane == 0) {
@@ -287,7 +295,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
     for (int i = 0; i < RUNS; ++i)
 #pragma unroll
       for (int e = 0; e < N; ++e)
-        if (f[i][e] == top) arg = min(arg, (uint32_t)(v0 + (i * NT + tid) * N + e));
+        if (f[i][e] == top) arg = min(arg, (uint32_t)(SL::at(v0, i) + e));
   } else if (!c.filter) {
 #pragma unroll
     for (int i = 0; i < RUNS; ++i)
@@ -301,32 +309,23 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
       // per logit: what has no class goes to a place of the lane's own.
       const int base_i = (int)base;
       const double least = qtop - 600.0;
-      auto fill = [&](auto counted) {
 #pragma unroll
-        for (int i = 0; i < RUNS; ++i) {
-          double q[N];
-          int b[N];
-          u64 u[N];
+      for (int i = 0; i < RUNS; ++i) {
+        double q[N];
+        int b[N];
+        u64 u[N];
 #pragma unroll
-          for (int e = 0; e < N; ++e) q[e] = fmax(in_classes(f[i][e], c.rate), least);
+        for (int e = 0; e < N; ++e) q[e] = fmax(in_classes(f[i][e], c.rate), least);
 #pragma unroll
-          for (int e = 0; e < N; ++e) {
-            b[e] = base_i - __double2loint(q[e] + 0x1.8p52);
-            b[e] = b[e] < BINS - 1 ? b[e] : BINS + lane;
-          }
-#pragma unroll
-          for (int e = 0; e < N; ++e) u[e] = fixed50(power_of(q[e] - qtop, powers));
-#pragma unroll
-          for (int e = 0; e < N; ++e) {
-            atomicAdd(mass + b[e], u[e]);
-            if constexpr (decltype(counted)::value) atomicAdd(count + b[e], 1u);
-          }
+        for (int e = 0; e < N; ++e) {
+          b[e] = base_i - __double2loint(q[e] + 0x1.8p52);
+          b[e] = b[e] < BINS - 1 ? b[e] : BINS + lane;
         }
-      };
-      if (c.top_k)
-        fill(std::true_type{});
-      else
-        fill(std::false_type{});
+#pragma unroll
+        for (int e = 0; e < N; ++e) u[e] = class_word(power_of(q[e] - qtop, powers));
+#pragma unroll
+        for (int e = 0; e < N; ++e) atomicAdd(classes + b[e], u[e]);
+      }
     } else {
 #pragma unroll 1
       for (int i = 0; i < E; ++i) {
@@ -335,15 +334,12 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
         for (int j = 0; j < E; ++j) y = j == i ? f[j / N][j % N] : y;
         const double q = in_classes(y, c.rate);
         const int b = (int)fmin(base - rint(q), (double)BINS);
-        if (b < BINS - 1) {
-          atomicAdd(mass + b, fixed50(weight_of(q - qtop, powers)));
-          atomicAdd(count + b, 1u);
-        }
+        if (b < BINS - 1) atomicAdd(classes + b, class_word(weight_of(q - qtop, powers)));
       }
     }
   }
-  arg = wave_all(arg, Min{});
-  sum = wave_all(sum, Sum{});
+  if (c.greedy) arg = wave_all(arg, Min{});
+  if (!c.filter) sum = wave_all(sum, Sum{});
   const double d1 = wave_all((double)sum1, Sum{});
   if (lane == 0) {
     s_arg[wave] = arg;
@@ -360,10 +356,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
     }
     *out = s;
   }
-  if (c.filter) {
-    w.mass[(size_t)blockIdx.x * BINS + tid] = mass[tid];
-    if (c.top_k) w.count[(size_t)blockIdx.x * BINS + tid] = count[tid];
-  }
+  if (c.filter) w.classes[(size_t)blockIdx.x * BINS + tid] = classes[tid];
 }
 
 // Inclusive scan over the workgroup's threads.
@@ -439,29 +432,25 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
     return;
   }
   __syncthreads();
-  const GLOBAL u64* hm = (const GLOBAL u64*)w.mass + (size_t)row * nch * BINS;
-  const GLOBAL uint32_t* hc = (const GLOBAL uint32_t*)w.count + (size_t)row * nch * BINS;
+  const GLOBAL u64* hm = (const GLOBAL u64*)w.classes + (size_t)row * nch * BINS;
   double m = 0;
   uint32_t n = 0;
   constexpr int U = 8;
   for (int i0 = 0; i0 < nch; i0 += U) {
     u64 um[U];
-    uint32_t uc[U];
     bool in[U];
 #pragma unroll
     for (int j = 0; j < U; ++j) {
       const int i = min(i0 + j, nch - 1), k = tid - ch.shift[i];
       // what lies behind a chunk's classes has no mass in the row either
       in[j] = i0 + j < nch && k >= 0 && k < BINS - 1 && tid < BINS - 1;
-      const size_t at = (size_t)i * BINS + (in[j] ? k : 0);
-      um[j] = hm[at];
-      uc[j] = c.top_k ? hc[at] : 0u;
+      um[j] = hm[(size_t)i * BINS + (in[j] ? k : 0)];
     }
 #pragma unroll
     for (int j = 0; j < U; ++j)
       if (in[j]) {
-        m += (double)um[j] * 0x1p-50 * ch.fac[i0 + j];
-        n += uc[j];
+        m += class_mass(um[j]) * ch.fac[i0 + j];
+        n += (uint32_t)(um[j] >> COUNT_BIT);
       }
   }
   m = block_scan(m, bufd);
@@ -469,7 +458,6 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   binw[tid] = m;
   binc[tid] = n;
   w.prefix[(size_t)row * BINS + tid] = m;
-  w.prefix_n[(size_t)row * BINS + tid] = n;
   __syncthreads();
   RowState st{BINS, 0, 0, -1, -1, {-1, -1, -1, -1}, 0.f, 0.f, top.base};
   double least = binw[BINS - 2], most = least;  // bounds of the mass that top-p is a share of
@@ -551,7 +539,10 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
   constexpr int N = 16 / sizeof(T), RUNS = E / N;
   float f[RUNS][N];
-  load_chunk<T>(x, v0, a.vocab, a.mask_id, f);
+  Slice<T> slice;
+  const bool whole = v0 + CHUNK <= a.vocab;
+  if (whole) slice.fetch(x, v0);
+  slice.take(x, v0, whole, a.vocab, a.mask_id, f);
   uint32_t hit = 0, slots = 0;
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
@@ -881,7 +872,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
         const float f = value_of(key);
         if (stays(f, key, v)) atomicAdd(sh.extra + v / CHUNK, (u64)(p.weight(f) * units));
       });
-    const GLOBAL u64* h = (const GLOBAL u64*)w.mass + (size_t)row * nch * BINS;
+    const GLOBAL u64* h = (const GLOBAL u64*)w.classes + (size_t)row * nch * BINS;
     constexpr int U = 4;  // chunks of a wave at a time
     for (int i0 = wave; i0 < nch; i0 += NW * U) {
       u64 s[U];
@@ -894,13 +885,13 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
 #pragma unroll
         for (int k = 0; k < BINS / 64; ++k) {
           const int at = k * 64 + lane;
-          if (at < end) s[j] += h[(size_t)i * BINS + at];
+          if (at < end) s[j] += h[(size_t)i * BINS + at] & ((1ull << COUNT_BIT) - 1);
         }
       }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         s[j] = wave_all(s[j], Sum{});
-        if (lane == 0 && i0 + j * NW < nch) sh.part[i0 + j * NW] = (double)s[j] * 0x1p-50 * sh.ch.fac[i0 + j * NW];
+        if (lane == 0 && i0 + j * NW < nch) sh.part[i0 + j * NW] = (double)s[j] * 0x1p-36 * sh.ch.fac[i0 + j * NW];
       }
     }
     __syncthreads();
@@ -910,31 +901,39 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
   }
 
   // ---- the chunk, then the token, where the running sum passes u times the whole
-  const double part = tid < nch ? sh.part[tid] : 0.0;
-  const double upto = block_scan(part, sh.bufd);
   __syncthreads();
-  sh.part[tid] = upto;
-  if (tid == 0) {
-    sh.a = ~0u;
-    sh.b = 0;
-  }
-  __syncthreads();
-  const double total = sh.part[nch - 1];
+  double total = 0;
+  for (int i0 = 0; i0 < nch; i0 += 64) total += wave_all(i0 + lane < nch ? sh.part[i0 + lane] : 0.0, Sum{});
   float u = a.u[row];
   u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
   const double want = (double)u * total;
-  if (part > 0.0) {
-    if (upto > want) atomicMin(&sh.a, (uint32_t)tid);
-    atomicMax(&sh.b, (uint32_t)tid);  // rounding: the last chunk with mass
+  // every wave by itself: the first chunk with mass whose running sum passes
+  // `want`; if rounding leaves none, the last with mass
+  int at = 0;
+  double run = 0, sums = 0;
+  for (int i0 = 0; i0 < nch; i0 += 64) {
+    const double part = i0 + lane < nch ? sh.part[i0 + lane] : 0.0;
+    double upto = part;
+#pragma unroll
+    for (int x = 1; x < 64; x <<= 1) {
+      const double y = __shfl_up(upto, x, 64);
+      if (lane >= x) upto += y;
+    }
+    upto += sums;
+    const u64 mass = __ballot(part > 0.0), past = __ballot(part > 0.0 && upto > want);
+    if (past | mass) {
+      const int l = past ? __ffsll(past) - 1 : 63 - __clzll(mass);
+      at = i0 + l;
+      run = __shfl(upto - part, l, 64);
+    }
+    if (past) break;
+    sums = __shfl(upto, 63, 64);
   }
-  __syncthreads();
-  const int at = (int)min(sh.a, sh.b);
-  double run = at > 0 ? sh.part[at - 1] : 0.0;
-  __syncthreads();
   if (tid == 0) {
     sh.a = ~0u;
     sh.b = 0;
   }
+  const bool ranked_cut = c.filter && edge < BINS - 1 && cut.key != 0 && cut.key != ~0u && !(reach < INFINITY);
   const int v0 = at * CHUNK + tid * E;
   float y[E];
   load_logits<T, E>(p.x, v0, V, a.mask_id, y);
@@ -943,11 +942,15 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
   for (int i = 0; i < E; ++i) {
     const float f = y[i];
     bool keep = f > -INFINITY;
-    if (c.filter && keep) {
+    if (ranked_cut) {  // the boundary is a member: the rest goes by the ranking
+      const uint32_t key = key_of(f);
+      keep = key > cut.key || (key == cut.key && (uint32_t)(v0 + i) <= cut.last);
+    } else if (c.filter && keep) {
       const int b = class_of(f, c.rate, top.base);
       keep = b < edge ? b < BINS - 1 : b == edge && edge < BINS - 1 && stays(f, key_of(f), v0 + i);
     }
-    e[i] = keep ? p.weight(f) : 0.0;
+    e[i] = 0.0;
+    if (keep) e[i] = p.weight(f);
     sum += e[i];
   }
   const double incl = block_scan(sum, sh.bufd);  // has barriers
@@ -984,10 +987,8 @@ size_t carve(void* base, size_t rows, size_t chunks, SampleWs* w) {
   };
   w->chunks = (int)chunks;
   w->stat = reinterpret_cast<ChunkStat*>(take(rows * chunks * sizeof(ChunkStat)));
-  w->mass = reinterpret_cast<u64*>(take(rows * chunks * BINS * sizeof(u64)));
-  w->count = reinterpret_cast<uint32_t*>(take(rows * chunks * BINS * sizeof(uint32_t)));
+  w->classes = reinterpret_cast<u64*>(take(rows * chunks * BINS * sizeof(u64)));
   w->prefix = reinterpret_cast<double*>(take(rows * BINS * sizeof(double)));
-  w->prefix_n = reinterpret_cast<uint32_t*>(take(rows * BINS * sizeof(uint32_t)));
   w->state = reinterpret_cast<RowState*>(take(rows * sizeof(RowState)));
   w->list = reinterpret_cast<uint2*>(take(rows * LIST * sizeof(uint2)));
   w->listed = reinterpret_cast<uint32_t*>(take(rows * sizeof(uint32_t)));
