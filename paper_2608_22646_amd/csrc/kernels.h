@@ -214,7 +214,7 @@ struct RotaryArgs {
   float gain;
   int tokens;  // of a workgroup (set by the launcher)
 };
-void launch_rotary(RotaryArgs a, hipStream_t s);
+void launch_rotary(const RotaryArgs& a, hipStream_t s);
 
 // k_attn_docs.hip: see dllm_attention; ws of attn_docs_bytes(a) bytes.
 struct AttnView {
