@@ -140,11 +140,15 @@ struct Tile {
   }
 };
 
-// State of 32 rows: running maximum (log2 units), sum and output.
+// State of 32 rows: running maximum (log2 units) and what exponents are taken
+// against (it, or 0 while it is -inf), sum and output; and what the lane's row is.
 template <int HD>
-struct State {
+struct Rows {
   f32x16_t o[HD / 32];
-  float m, l;
+  float m, m_ref, l;
+  int t, h, end;  // query, head, keys that it sees
+  bool mine;      // there is such a row
+  float slope;
 };
 
 // One row tile against the keys kb .. ke - 1 of its document.
@@ -153,7 +157,7 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef Tile<T, HD> TL;
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int NW = QG * KG, D = S - 1, ND = HD / 32;
+  constexpr int NW = QG * KG, ND = HD / 32, TR = 32 * QG;  // TR: rows of the tile
   constexpr int K_BYTES = KT * TL::ROW, TILE = 2 * K_BYTES, STAGE = KG * TILE;
   constexpr int TP = TILE / 1024, PER = TP / QG;  // LDS-DMA instructions of 1 KiB: of a tile, of a wave
   static_assert(TP % (2 * QG) == 0, "the waves of a key group share a tile's loads evenly");
@@ -173,24 +177,21 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
   const int g = unit % a.Hkv, rest = unit / a.Hkv, chunk = rest % p.chunks, dn = rest / p.chunks;
   Doc d = doc_of(a, dn);
   d = Doc{uniform(d.q0), uniform(d.nq), uniform(d.k0), uniform(d.nk), uniform(d.pos), uniform(d.prefix)};
-  const int G = a.Hq / a.Hkv, rows = d.nq * G, r0 = tile * 32 * QG;
+  const int G = a.Hq / a.Hkv, rows = d.nq * G, r0 = tile * TR;
   if (r0 >= rows) return;
-  const int t_last = (min(r0 + 32 * QG, rows) - 1) / G;
+  const int t_last = (min(r0 + TR, rows) - 1) / G;
   const int kb = uniform(chunk * p.chunk_keys), ke = uniform(min(sees(a, d, t_last), p.chunks > 1 ? kb + p.chunk_keys : 0x7fffffff));
   if (chunk > 0 && kb >= ke) return;
   const int tile_first = uniform(sees(a, d, r0 / G));  // keys that every row of the tile sees
-  // this wave's rows and this lane's
+  // this wave's rows
   const int w0 = r0 + 32 * qg, w1 = min(w0 + 32, rows);
   const int see_first = uniform(w0 < rows ? sees(a, d, w0 / G) : 0), see_last = uniform(w0 < rows ? sees(a, d, (w1 - 1) / G) : 0);
-  const int row = w0 + lq, t = row / G, h = g * G + row % G;
-  const bool mine = row < rows;
-  const int my_end = mine ? sees(a, d, t) : 0;
-  const float slope = a.slopes && mine ? a.slopes[h] * LOG2E : 0.f;
-  const bool neg = a.scale < 0.f;  // scores are formed with |scale| and, where it is negative, -q
+  const int seen = min(ke, see_last);  // keys that some row of this wave sees
+  const bool neg = a.scale < 0.f;      // scores are formed with |scale| and, where it is negative, -q
   const float sc = fabsf(a.scale) * LOG2E;
   // capped scores: cap in log2 units, 2 log2(e) / cap per unit of score, and the
   // coefficients of tanh for small ones
-  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f, cap_z = a.cap > 0.f ? 1.f / (cap2 * cap2) : 0.f;
+  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f, cap_1 = a.cap > 0.f ? 1.f / cap2 : 0.f, cap_z = cap_1 * cap_1;
   const float th1 = -0.333313563f * cap_z, th2 = 0.132708743f * cap_z * cap_z, th3 = -0.0475493467f * cap_z * cap_z * cap_z;
   const bool direct = a.cap == 0.f && !a.slopes;
 
@@ -213,119 +214,59 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
     off[x] = r * (isk ? ksb : vsb) + c * 16;
   }
   const uint32_t lds0 = lds_address(lds) + kg * TILE + qg * 1024;
-  auto issue = [&](int u) {
-    const uint32_t to = lds0 + (u % S) * STAGE;
+  auto load = [&](int u, int slot) {  // step u into stage `slot`
     const int t0 = kb + (u * KG + kg) * KT;
     const int left = min(ke - t0, KT);  // reads past the last key give zeros
-    const uint32_t n = left > 0 ? left - 1 : 0, any = left > 0 ? TL::ROW : 0u;
-    const long from = left > 0 ? t0 : 0;
-    const rsrc_t rk = rsrc_of(kp + from * ksb, n * ksb + any), rv = rsrc_of(vp + from * vsb, n * vsb + any);
 #pragma unroll
-    for (int x = 0; x < PER; ++x) {
-      const bool isk = x < PER / 2;
-      dma16(isk ? rk : rv, off[x], to + (isk ? x * QG * 1024 : K_BYTES + (x - PER / 2) * QG * 1024));
+    for (const bool keys : {true, false}) {
+      const uint32_t sb = keys ? ksb : vsb, bytes = left > 0 ? (uint32_t)(left - 1) * sb + TL::ROW : 0u;
+      const rsrc_t rs = rsrc_of((keys ? kp : vp) + (left > 0 ? (long)t0 : 0l) * sb, bytes);
+      const uint32_t to = lds0 + slot * STAGE + (keys ? 0 : K_BYTES);
+#pragma unroll
+      for (int x = 0; x < PER / 2; ++x) dma16(rs, off[keys ? x : PER / 2 + x], to + x * QG * 1024);
     }
   };
   const int nsteps = ke > kb ? (ke - kb + KG * KT - 1) / (KG * KT) : 0;
 
-  // Q operand: this lane's row, dims 16 ks + 8 half .. (bf16), 8 c + 4 half .. (float32)
+  // Q operand: the lane's rows, dims 16 ks + 8 half .. (bf16), 8 c + 4 half .. (float32)
   constexpr int NQ = BF ? HD / 16 : HD / 8;
   typedef float f32x4v __attribute__((ext_vector_type(4)));
   bf16x8_t qb[BF ? NQ : 1];
   f32x4v qf[BF ? 1 : NQ];
-  {
-    const T* qrow = static_cast<const T*>(a.q.data) + dn * a.q.stride_b + (long)(d.q0 + (mine ? t : 0)) * a.q.stride_l +
-                    (mine ? h : 0) * a.q.stride_h;
-#pragma unroll
-    for (int c = 0; c < NQ; ++c) {
-      uint4 w = *reinterpret_cast<const uint4*>(qrow + c * (BF ? 16 : 8) + half * (BF ? 8 : 4));
-      const uint32_t flip = neg ? (BF ? 0x80008000u : 0x80000000u) : 0u;
-      w.x ^= flip;
-      w.y ^= flip;
-      w.z ^= flip;
-      w.w ^= flip;
-      if (!mine) w = make_uint4(0, 0, 0, 0);
-      if constexpr (BF)
-        qb[c] = __builtin_bit_cast(bf16x8_t, w);
-      else
-        qf[c] = __builtin_bit_cast(f32x4v, w);
-    }
-  }
-
-  State<HD> st;
+  Rows<HD> R;
+  const int row = w0 + lq;
+  R.mine = row < rows;
+  R.t = row / G;
+  R.h = g * G + row % G;
+  R.end = R.mine ? sees(a, d, R.t) : 0;
+  R.slope = a.slopes && R.mine ? a.slopes[R.h] * LOG2E : 0.f;
+  R.m = -INFINITY;
+  R.m_ref = 0.f;
+  R.l = 0.f;
 #pragma unroll
   for (int ds = 0; ds < ND; ++ds)
 #pragma unroll
-    for (int r = 0; r < 16; ++r) st.o[ds][r] = 0.f;
-  st.m = -INFINITY;
-  st.l = 0.f;
-  float m_ref = 0.f;  // the maximum that exponents are taken against: m, or 0 while m is -inf
-
+    for (int r = 0; r < 16; ++r) R.o[ds][r] = 0.f;
+  const T* qrow = static_cast<const T*>(a.q.data) + dn * a.q.stride_b + (long)(d.q0 + (R.mine ? R.t : 0)) * a.q.stride_l +
+                  (R.mine ? R.h : 0) * a.q.stride_h;
 #pragma unroll
-  for (int s = 0; s < D; ++s)
-    if (s < nsteps) issue(s);
+  for (int c = 0; c < NQ; ++c) {
+    uint4 w = *reinterpret_cast<const uint4*>(qrow + c * (BF ? 16 : 8) + half * (BF ? 8 : 4));
+    const uint32_t flip = neg ? (BF ? 0x80008000u : 0x80000000u) : 0u;
+    w.x ^= flip;
+    w.y ^= flip;
+    w.z ^= flip;
+    w.w ^= flip;
+    if (!R.mine) w = make_uint4(0, 0, 0, 0);
+    if constexpr (BF)
+      qb[c] = __builtin_bit_cast(bf16x8_t, w);
+    else
+      qf[c] = __builtin_bit_cast(f32x4v, w);
+  }
+
   constexpr int NS = KT / 32;  // 32-key score blocks of a tile
-  for (int u = 0; u < nsteps; ++u) {
-    // stages in flight behind this one: D - 1, fewer at the end
-    if (u + D <= nsteps)
-      wait_vmcnt<PER*(D - 1)>();
-    else
-      wait_vmcnt<0>();
-    // stage u is there; every wave is done with the one refilled next (with one
-    // row group a wave reads only what it loaded itself)
-    if constexpr (QG > 1)
-      barrier_nofence();
-    else
-      asm volatile("" ::: "memory");
-    if (u + D < nsteps) issue(u + D);
-    const int t0 = kb + (u * KG + kg) * KT;
-    char* kt = lds + (u % S) * STAGE + kg * TILE;
-    char* vt = kt + K_BYTES;
-    if (kb + (u + 1) * KG * KT > tile_first) {
-      // Some row does not see some key of this step.  A zero probability still
-      // makes NaN of a value that is no number: such values are added to the rows
-      // that see them here, and zeroed before the products.
-      constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7f800000u;  // exponents of a word
-      uint32_t top = 0;
-      for (int i = qg * 64 + lane; i < K_BYTES / 16; i += QG * 64) {
-        const uint4 w = reinterpret_cast<const uint4*>(vt)[i];
-        for (const uint32_t x : {w.x & EXP, w.y & EXP, w.z & EXP, w.w & EXP})
-          if constexpr (BF)
-            top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us_t, top), __builtin_bit_cast(v2us_t, x)));
-          else
-            top = max(top, x);
-      }
-      bool broken = __ballot((top & 0xffffu) == 0x7f80u || (top >> 16) == 0x7f80u) != 0ull;
-      if constexpr (QG > 1) broken = __syncthreads_or(broken);
-      if (broken) {
-        for (int key = 0; key < KT; ++key) {
-          const char* vrow = vt + key * TL::ROW;
-          const bool seen = t0 + key < min(my_end, ke);
-#pragma unroll
-          for (int ds = 0; ds < ND; ++ds)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-              const int e = ds * 32 + 8 * (r >> 2) + 4 * half + (r & 3), b = e * (int)sizeof(T);
-              const T w = *reinterpret_cast<const T*>(vrow + ((((b >> 4) ^ TL::v_swz(key)) << 4) | (b & 15)));
-              float f;
-              if constexpr (BF)
-                f = bf2f(w);
-              else
-                f = w;
-              if (seen && !(fabsf(f) < INFINITY)) st.o[ds][r] += f;
-            }
-        }
-        if constexpr (QG > 1) __syncthreads();
-        for (int i = qg * 64 + lane; i < K_BYTES / 4; i += QG * 64) {
-          uint32_t* w = reinterpret_cast<uint32_t*>(vt) + i;
-          *w = numbers<T>(*w);
-        }
-        if constexpr (QG > 1) __syncthreads();
-      }
-    }
-    if (t0 >= min(ke, see_last)) continue;  // nothing that this wave's rows see
-
-    f32x16_t s2[NS];
+  // scores x of the keys at kt: register r of block b holds key 32 b + 8 (r / 4) + 4 half + r % 4
+  auto scores = [&](const char* kt, f32x16_t (&x)[NS]) {
     const f32x16_t zero = {};
     if constexpr (BF) {
       bf16x8_t kf[NQ][NS];
@@ -339,12 +280,12 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
 #pragma unroll
       for (int c = 0; c < NQ; ++c)
 #pragma unroll
-        for (int b = 0; b < NS; ++b) s2[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c][b], qb[c], c ? s2[b] : zero, 0, 0, 0);
+        for (int b = 0; b < NS; ++b) x[b] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[c][b], qb[c], c ? x[b] : zero, 0, 0, 0);
       // the K reads run six ahead of their MFMAs
       constexpr int KR = NQ * NS, AHEAD = 6;
       __builtin_amdgcn_sched_group_barrier(0x100, AHEAD, 0);
 #pragma unroll
-      for (int i = 0; i < KR - AHEAD; ++i) {
+      for (int n = 0; n < KR - AHEAD; ++n) {
         __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
         __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
       }
@@ -357,102 +298,122 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
           const int r = b * 32 + lq;
           const f32x4v k4 = *reinterpret_cast<const f32x4v*>(kt + r * TL::ROW + (((c * 2 + half) ^ TL::k_swz(r)) << 4));
 #pragma unroll
-          for (int e = 0; e < 4; ++e) s2[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[c][e], c + e ? s2[b] : zero, 0, 0, 0);
+          for (int e = 0; e < 4; ++e) x[b] = __builtin_amdgcn_mfma_f32_32x32x2f32(k4[e], qf[c][e], c + e ? x[b] : zero, 0, 0, 0);
         }
     }
-
-    // register r of block b holds key t0 + 32 b + 8 (r / 4) + 4 half + r % 4
-    const bool whole = t0 + KT <= min(ke, see_first);
-    float mt = -INFINITY;
-    float fold = sc;  // factor still to be applied in the exponent
-    if (direct && whole) {
+  };
+  // Raises the running maximum to mt (this lane's, in log2 units), but only when it
+  // grows by more than 2^8: probabilities then stay below 2^8, at the same relative
+  // precision.
+  auto raise = [&](float mt) {
+    mt = max_pair32(mt);
+    if (__ballot(mt > R.m + 8.f) != 0ull) {
+      const float m_new = fmaxf(R.m, mt);
+      const float alpha = exp2_hw(R.m - (m_new == -INFINITY ? 0.f : m_new));
+      R.m = m_new;
+      R.m_ref = m_new == -INFINITY ? 0.f : m_new;
+      R.l *= alpha;
 #pragma unroll
-      for (int b = 0; b < NS; ++b)
+      for (int ds = 0; ds < ND; ++ds)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) mt = fmaxf(mt, s2[b][r]);
-      mt *= sc;
-    } else {
-      fold = 1.f;
-      if (a.cap > 0.f) {
+        for (int r = 0; r < 16; ++r) R.o[ds][r] *= alpha;
+    }
+  };
+  // Scores as they are in log2 units: scaled, capped, biased, masked (t0: the
+  // tile's first key; whole: every row of the wave sees all of it), and their maximum.
+  auto shape = [&](f32x16_t (&x)[NS], int t0, bool whole) {
+    if (a.cap > 0.f) {
+      if constexpr (!BF) {
+        // float32: tanh(y) = y + y z Q(z), z = y^2, Q of degree 4, for |y| <= 0.6, so
+        // that small scores keep 1e-7 of themselves (the form by exponentials: of the
+        // cap), and by exponentials above
+#pragma unroll
+        for (int b = 0; b < NS; ++b)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            const float y = x[b][r] * sc, u = y * cap_1, z = u * u;
+            const float q = fmaf(fmaf(fmaf(fmaf(-0.00589395f, z, 0.02079462f), z, -0.05378329f), z, 0.13331915f), z, -0.333333f);
+            const float far = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(exp2_hw(fabsf(x[b][r]) * cap_in) + 1.f), cap2);
+            x[b][r] = fabsf(u) <= 0.6f ? fmaf(y * z, q, y) : copysignf(far, y);
+          }
+      } else {
         float far = 0.f;
 #pragma unroll
         for (int b = 0; b < NS; ++b)
 #pragma unroll
-          for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(s2[b][r]));
-        if (BF && __ballot(!(far * cap_in <= 0.8f)) == 0ull) {
+          for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(x[b][r]));
+        if (__ballot(!(far * cap_in <= 0.8f)) == 0ull) {
           // |x / cap| <= 0.4: tanh(y) = y P(y^2), P of degree 3 to 1e-7 (six
           // instructions in place of two transcendental ones and three)
 #pragma unroll
           for (int b = 0; b < NS; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const float x = s2[b][r] * sc, z = x * x;
-              s2[b][r] = x * fmaf(fmaf(fmaf(th3, z, th2), z, th1), z, 0.999999901f);
+              const float y = x[b][r] * sc, z = y * y;
+              x[b][r] = y * fmaf(fmaf(fmaf(th3, z, th2), z, th1), z, 0.999999901f);
             }
         } else {
-          // cap tanh(x / cap) = cap - 2 cap / (e^(2 x / cap) + 1)
+          // cap tanh(x / cap) = cap - 2 cap / (e^(2 x / cap) + 1), to 1e-7 of the cap
 #pragma unroll
           for (int b = 0; b < NS; ++b)
 #pragma unroll
-            for (int r = 0; r < 16; ++r)
-              s2[b][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(exp2_hw(s2[b][r] * cap_in) + 1.f), cap2);
+            for (int r = 0; r < 16; ++r) x[b][r] = fmaf(-2.f * cap2, __builtin_amdgcn_rcpf(exp2_hw(x[b][r] * cap_in) + 1.f), cap2);
         }
-      } else {
-#pragma unroll
-        for (int b = 0; b < NS; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s2[b][r] *= sc;
       }
-      if (a.slopes) {
-        const float at = (float)((long)d.pos + t - t0 - 4 * half);
-#pragma unroll
-        for (int b = 0; b < NS; ++b)
-#pragma unroll
-          for (int r = 0; r < 16; ++r)
-            s2[b][r] = fmaf(-slope, fabsf(at - (float)(32 * b + 8 * (r >> 2) + (r & 3))), s2[b][r]);
-      }
-      const int end = min(my_end, ke) - t0 - 4 * half;
+    } else {
 #pragma unroll
       for (int b = 0; b < NS; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          if (!whole && 32 * b + 8 * (r >> 2) + (r & 3) >= end) s2[b][r] = -INFINITY;
-          mt = fmaxf(mt, s2[b][r]);
-        }
+        for (int r = 0; r < 16; ++r) x[b][r] *= sc;
     }
-    mt = max_pair32(mt);
-    // the maximum is raised only when it grows by more than 2^8 (probabilities
-    // then stay below 2^8, at the same relative precision)
-    if (__ballot(mt > st.m + 8.f) != 0ull) {
-      const float m_new = fmaxf(st.m, mt);
-      const float alpha = exp2_hw(st.m - (m_new == -INFINITY ? 0.f : m_new));
-      st.m = m_new;
-      m_ref = m_new == -INFINITY ? 0.f : m_new;
-      st.l *= alpha;
+    if (a.slopes) {
+      const float at = (float)((long)d.pos + R.t - t0 - 4 * half);
 #pragma unroll
-      for (int ds = 0; ds < ND; ++ds)
+      for (int b = 0; b < NS; ++b)
 #pragma unroll
-        for (int r = 0; r < 16; ++r) st.o[ds][r] *= alpha;
+        for (int r = 0; r < 16; ++r) x[b][r] = fmaf(-R.slope, fabsf(at - (float)(32 * b + 8 * (r >> 2) + (r & 3))), x[b][r]);
     }
-    // bf16: the sum is that of the rounded probabilities, which the products see
+    const int end = min(R.end, ke) - t0 - 4 * half;
+    float mt = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (!whole && 32 * b + 8 * (r >> 2) + (r & 3) >= end) x[b][r] = -INFINITY;
+        mt = fmaxf(mt, x[b][r]);
+      }
+    return mt;
+  };
+  auto highest = [&](const f32x16_t (&x)[NS]) {
+    float mt = -INFINITY;
+#pragma unroll
+    for (int b = 0; b < NS; ++b)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mt = fmaxf(mt, x[b][r]);
+    return mt;
+  };
+  // probabilities in place of scores x (which `fold` takes to log2 units), and in
+  // pairs pw for bf16, where the sum is that of the rounded ones, which the products see
+  auto exponentials = [&](f32x16_t (&x)[NS], uint32_t (&pw)[BF ? NS * 8 : 1], float fold) {
     float psum = 0.f;
-    uint32_t pw[BF ? NS * 8 : 1];
 #pragma unroll
     for (int b = 0; b < NS; ++b)
 #pragma unroll
       for (int r = 0; r < 16; r += 2) {
-        const float e0 = exp2_hw(fmaf(s2[b][r], fold, -m_ref)), e1 = exp2_hw(fmaf(s2[b][r + 1], fold, -m_ref));
+        const float e0 = exp2_hw(fmaf(x[b][r], fold, -R.m_ref)), e1 = exp2_hw(fmaf(x[b][r + 1], fold, -R.m_ref));
         if constexpr (BF) {
           pw[b * 8 + r / 2] = pack2(e0, e1);
           psum = add2(psum, pw[b * 8 + r / 2]);
         } else {
-          s2[b][r] = e0;
-          s2[b][r + 1] = e1;
+          x[b][r] = e0;
+          x[b][r + 1] = e1;
           psum += e0 + e1;
         }
       }
-    st.l += psum;
-
+    R.l += psum;
+  };
+  // output += values at vt times probabilities: x, in bf16 the pairs pw
+  auto products = [&](char* vt, const f32x16_t (&x)[NS], const uint32_t (&pw)[BF ? NS * 8 : 1]) {
     if constexpr (BF) {
       // slice jk: keys 16 jk + 4 half .. and 16 jk + 8 + 4 half ..; lane n of 16
       // gives the address of row n / 4, columns 4 (n % 4) .. of its 4 x 16 block
@@ -467,17 +428,16 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
       }
 #pragma unroll
       for (int jk = 0; jk < KT / 16; ++jk) {
-        v4s_t x[ND], y[ND];
+        v4s_t lo[ND], hi[ND];
 #pragma unroll
         for (int ds = 0; ds < ND; ++ds) {
-          x[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + jk * 16 * TL::ROW));
-          y[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + (jk * 16 + 8) * TL::ROW));
+          lo[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + jk * 16 * TL::ROW));
+          hi[ds] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4s_t)(va[ds] + (jk * 16 + 8) * TL::ROW));
         }
         const bf16x8_t pf = __builtin_bit_cast(bf16x8_t, make_uint4(pw[jk * 4], pw[jk * 4 + 1], pw[jk * 4 + 2], pw[jk * 4 + 3]));
 #pragma unroll
         for (int ds = 0; ds < ND; ++ds)
-          st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(x[ds], y[ds], 0, 1, 2, 3, 4, 5, 6, 7),
-                                                             pf, st.o[ds], 0, 0, 0);
+          R.o[ds] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_shufflevector(lo[ds], hi[ds], 0, 1, 2, 3, 4, 5, 6, 7), pf, R.o[ds], 0, 0, 0);
       }
     } else {
 #pragma unroll
@@ -490,13 +450,85 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
             const int e = ds * 32 + lq;
             const float w =
                 *reinterpret_cast<const float*>(vt + (key + 4 * half) * TL::ROW + ((((e >> 2) ^ (half << 3)) << 4) | ((e & 3) * 4)));
-            st.o[ds] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, s2[b][r], st.o[ds], 0, 0, 0);
+            R.o[ds] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x[b][r], R.o[ds], 0, 0, 0);
           }
         }
     }
+  };
+  // Before the products of a step in which some row does not see some key: a zero
+  // probability still makes NaN of a value that is no number, so such values are
+  // added here to the rows that see them, and zeroed.
+  auto scrub = [&](int t0, char* vt) {
+    constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7f800000u;  // exponents of a word
+    uint32_t top = 0;
+    for (int i = qg * 64 + lane; i < K_BYTES / 16; i += QG * 64) {
+      const uint4 w = reinterpret_cast<const uint4*>(vt)[i];
+      for (const uint32_t x : {w.x & EXP, w.y & EXP, w.z & EXP, w.w & EXP})
+        if constexpr (BF)
+          top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us_t, top), __builtin_bit_cast(v2us_t, x)));
+        else
+          top = max(top, x);
+    }
+    bool broken = __ballot((top & 0xffffu) == 0x7f80u || (top >> 16) == 0x7f80u) != 0ull;
+    if constexpr (QG > 1) broken = __syncthreads_or(broken);
+    if (!broken) return;
+    for (int key = 0; key < KT; ++key) {
+      const char* vrow = vt + key * TL::ROW;
+#pragma unroll
+      for (int ds = 0; ds < ND; ++ds)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const int e = ds * 32 + 8 * (r >> 2) + 4 * half + (r & 3), b = e * (int)sizeof(T);
+          const T w = *reinterpret_cast<const T*>(vrow + ((((b >> 4) ^ TL::v_swz(key)) << 4) | (b & 15)));
+          float f;
+          if constexpr (BF)
+            f = bf2f(w);
+          else
+            f = w;
+          if (t0 + key < min(R.end, ke) && !(fabsf(f) < INFINITY)) R.o[ds][r] += f;
+        }
+    }
+    if constexpr (QG > 1) __syncthreads();
+    for (int i = qg * 64 + lane; i < K_BYTES / 4; i += QG * 64) {
+      uint32_t* w = reinterpret_cast<uint32_t*>(vt) + i;
+      *w = numbers<T>(*w);
+    }
+    if constexpr (QG > 1) __syncthreads();
+  };
+  constexpr int D = S - 1;  // stages in flight behind the one in use
+  for (int u = 0; u < D && u < nsteps; ++u) load(u, u);
+  for (int u = 0; u < nsteps; ++u) {
+    if (u + D <= nsteps)
+      wait_vmcnt<PER*(D - 1)>();
+    else
+      wait_vmcnt<0>();
+    // stage u is there; every wave is done with the one refilled next (with one
+    // row group a wave reads only what it loaded itself)
+    if constexpr (QG > 1)
+      barrier_nofence();
+    else
+      asm volatile("" ::: "memory");
+    if (u + D < nsteps) load(u + D, (u + D) % S);
+    const int t0 = kb + (u * KG + kg) * KT;
+    char *const slot = lds + (u % S) * STAGE + kg * TILE, *const vt = slot + K_BYTES;
+    if (kb + (u + 1) * KG * KT > tile_first) scrub(t0, vt);
+    if (t0 >= seen) continue;  // nothing that this wave's rows see
+    f32x16_t x[NS];
+    uint32_t pw[BF ? NS * 8 : 1];
+    scores(slot, x);
+    const bool whole = t0 + KT <= min(ke, see_first);
+    float mt, fold = 1.f;  // fold: factor still to be applied in the exponent
+    if (direct && whole) {
+      fold = sc;
+      mt = highest(x) * sc;
+    } else {
+      mt = shape(x, t0, whole);
+    }
+    raise(mt);
+    exponentials(x, pw, fold);
+    products(vt, x, pw);
   }
-  st.l = sum_pair32(st.l);
-
+  R.l = sum_pair32(R.l);
   if constexpr (KG > 1) {
     // the key groups' states join in group order: group 0's wave takes the others'
     __syncthreads();
@@ -507,52 +539,52 @@ __global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, 
       for (int ds = 0; ds < ND; ++ds)
 #pragma unroll
         for (int r = 0; r < 4; ++r)
-          to[(ds * 4 + r) * 64] = make_float4(st.o[ds][4 * r], st.o[ds][4 * r + 1], st.o[ds][4 * r + 2], st.o[ds][4 * r + 3]);
-      to[ND * 4 * 64] = make_float4(st.m, st.l, 0.f, 0.f);
+          to[(ds * 4 + r) * 64] = make_float4(R.o[ds][4 * r], R.o[ds][4 * r + 1], R.o[ds][4 * r + 2], R.o[ds][4 * r + 3]);
+      to[ND * 4 * 64] = make_float4(R.m, R.l, 0.f, 0.f);
     }
     __syncthreads();
     if (kg > 0) return;
     for (int k2 = 1; k2 < KG; ++k2) {
       const float4* from = sh + (size_t)(k2 * QG + qg - QG) * (ND * 4 + 1) * 64 + lane;
       const float4 ml = from[ND * 4 * 64];
-      const float m_new = fmaxf(st.m, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
-      const float fa = exp2_hw(st.m - ref), fb = exp2_hw(ml.x - ref);
-      st.m = m_new;
-      st.l = st.l * fa + ml.y * fb;
+      const float m_new = fmaxf(R.m, ml.x), ref = m_new == -INFINITY ? 0.f : m_new;
+      const float fa = exp2_hw(R.m - ref), fb = exp2_hw(ml.x - ref);
+      R.m = m_new;
+      R.l = R.l * fa + ml.y * fb;
 #pragma unroll
       for (int ds = 0; ds < ND; ++ds)
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
           const float4 w = from[(ds * 4 + r) * 64];
-          st.o[ds][4 * r] = st.o[ds][4 * r] * fa + w.x * fb;
-          st.o[ds][4 * r + 1] = st.o[ds][4 * r + 1] * fa + w.y * fb;
-          st.o[ds][4 * r + 2] = st.o[ds][4 * r + 2] * fa + w.z * fb;
-          st.o[ds][4 * r + 3] = st.o[ds][4 * r + 3] * fa + w.w * fb;
+          R.o[ds][4 * r] = R.o[ds][4 * r] * fa + w.x * fb;
+          R.o[ds][4 * r + 1] = R.o[ds][4 * r + 1] * fa + w.y * fb;
+          R.o[ds][4 * r + 2] = R.o[ds][4 * r + 2] * fa + w.z * fb;
+          R.o[ds][4 * r + 3] = R.o[ds][4 * r + 3] * fa + w.w * fb;
         }
     }
   }
-  if (!mine) return;
+  if (!R.mine) return;
   if (p.chunks > 1) {
     // state of (document, query, head) for this chunk: hd outputs, then (m, l)
-    const size_t at = (((size_t)dn * a.max_q + t) * a.Hq + h) * p.chunks + chunk;
+    const size_t at = (((size_t)dn * a.max_q + R.t) * a.Hq + R.h) * p.chunks + chunk;
     float* to = p.part + at * HD;
 #pragma unroll
     for (int ds = 0; ds < ND; ++ds)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
         *reinterpret_cast<float4*>(to + ds * 32 + 8 * r + 4 * half) =
-            make_float4(st.o[ds][4 * r], st.o[ds][4 * r + 1], st.o[ds][4 * r + 2], st.o[ds][4 * r + 3]);
-    if (half == 0) p.part_ml[at] = make_float2(st.m, st.l);
+            make_float4(R.o[ds][4 * r], R.o[ds][4 * r + 1], R.o[ds][4 * r + 2], R.o[ds][4 * r + 3]);
+    if (half == 0) p.part_ml[at] = make_float2(R.m, R.l);
     return;
   }
-  const float inv = st.l == 0.f ? 0.f : 1.f / st.l;
-  T* to = static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h;
+  const float inv = R.l == 0.f ? 0.f : 1.f / R.l;
+  T* to = static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + R.t) * a.out.stride_l + R.h * a.out.stride_h;
 #pragma unroll
   for (int ds = 0; ds < ND; ++ds)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       const int e = ds * 32 + 8 * r + 4 * half;
-      const float4 w = make_float4(st.o[ds][4 * r] * inv, st.o[ds][4 * r + 1] * inv, st.o[ds][4 * r + 2] * inv, st.o[ds][4 * r + 3] * inv);
+      const float4 w = make_float4(R.o[ds][4 * r] * inv, R.o[ds][4 * r + 1] * inv, R.o[ds][4 * r + 2] * inv, R.o[ds][4 * r + 3] * inv);
       if constexpr (BF)
         *reinterpret_cast<uint2*>(to + e) = make_uint2(pack2(w.x, w.y), pack2(w.z, w.w));
       else

@@ -91,6 +91,28 @@ def test_masks_caps_and_biases(gpu_lib, heads, block, prefix, cap, bias, dtype):
     run_and_check(*heads, dtype, [97, 130], [150, 130], block, None, prefix, cap, slopes, seed=block)
 
 
+@pytest.mark.parametrize("cap", [30.0, 200.0])
+def test_small_capped_scores_keep_their_precision(gpu_lib, cap):
+    """float32, one product a score, two keys of which the other scores 0, values 1 and 0: the
+    output is 1 / (1 + e^-s) with s = cap tanh(x / cap).  In units u = 2^-24: s is off by 8 of
+    itself (scale, product, tanh of relative 1.3, its sums), the probability by s (1 - p) of that
+    and by 8 for exponential, sum, division and rounding."""
+    n, hd, u = 256, 64, 2.0 ** -24
+    x = torch.arange(-n // 2, n // 2, dtype=F32) / 32 + 2.0 ** -9
+    q = torch.zeros(n, 1, hd)
+    q[:, 0, 5] = x
+    k = torch.zeros(2, 1, hd)
+    k[0, 0, 5] = 1
+    v = torch.zeros(2, 1, hd)
+    v[0] = 1
+    say(f"attention two keys cap {cap}")
+    got = to_np(B.attention(q.cuda(), k.cuda(), v.cuda(), B.Docs.packed([n], [2]), cap=cap, scale=1.0), np.float64)[:, 0]
+    s = cap * np.tanh(x.numpy().astype(np.float64) / cap)
+    p = 1 / (1 + np.exp(-s))
+    tol = u * p * (8 * np.abs(s) * (1 - p) + 8)
+    assert (np.abs(got - p[:, None]) <= tol[:, None]).all(), (np.abs(got - p[:, None]) / tol[:, None]).max()
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("q_len,kv", [(1, 4097), (1, 8448), (4, 3001), (32, 2050), (33, 1999), (64, 2048)])
 def test_few_queries_over_a_long_cache(gpu_lib, q_len, kv, dtype):
