@@ -627,15 +627,20 @@ struct Picker {
     const double e = weight_of(in_classes(f, rate) - top.qtop, sh.powers);
     return e < LEAST ? 0.0 : e;
   }
-  // f(key, index) for every member of class b: from the row's list, or where the
-  // list does not hold them all, from the logits.
-  template <typename F>
-  __device__ __forceinline__ void members(int b, F f) const {
+  // Where the list holds all members of class b: its slot, else -1.
+  __device__ __forceinline__ int slot_of(int b) const {
     int slot = -1;
 #pragma unroll
     for (int i = 0; i < SLOTS; ++i)
       if (st.slot[i] == b) slot = i;
-    if (slot >= 0 && listed <= LIST) {
+    return listed <= LIST ? slot : -1;
+  }
+  // f(key, index) for every member of class b: from the row's list, or where the
+  // list does not hold them all, from the logits.
+  template <typename F>
+  __device__ __forceinline__ void members(int b, F f) const {
+    const int slot = slot_of(b);
+    if (slot >= 0) {
       for (uint32_t i = threadIdx.x; i < listed; i += NT) {
         uint2 m;
         if (listed <= KEPT) {
@@ -678,7 +683,7 @@ struct Picker {
     const double edge0 = (top.base - b - 1) / rate, edge1 = (top.base - b + 1) / rate;
     const float f0 = (float)(edge0 - fabs(edge0) * 1e-6), f1 = (float)(edge1 + fabs(edge1) * 1e-6);
     uint32_t lo = rate > 0 ? key_of(f0) : key_of(-INFINITY), hi = rate > 0 ? key_of(f1) : key_of(INFINITY);
-    uint32_t inside = listed <= LIST ? listed : ~0u;  // members in the range, at most
+    uint32_t inside = slot_of(b) >= 0 ? listed : ~0u;  // members in the range, at most
     bool by_key = true;
     uint32_t n0 = 0, key0 = 0;  // members ranked before the range, and their mass; its key, once it is one
     double m0 = 0;
@@ -710,7 +715,7 @@ struct Picker {
         // the last that stays: the one of the highest rank
         const uint32_t r = wave_all(stays ? rank + 1 : 0u, Max{});
         const u64 who = __ballot(stays && rank + 1 == r);
-        if (who == 0) return Cut{by_key && n0 == 0 ? ~0u : key0, 0, m0};  // (none of them)
+        if (who == 0) return Cut{~0u, 0, m0};  // no members (rounding at a class's edge can lead here)
         const int l = __ffsll(who) - 1;
         return Cut{(uint32_t)__shfl(mine.x, l, 64), (uint32_t)__shfl(mine.y, l, 64),
                    __shfl(mass + (double)fixed * unit, l, 64)};

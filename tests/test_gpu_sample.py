@@ -96,6 +96,40 @@ def test_ties(gpu_lib, V, dtype):
     check(z, torch.tensor([0.9, 0.9]), top_k=torch.tensor([1, 1], dtype=torch.int32))
 
 
+def test_boundary_in_a_class_that_is_not_listed(gpu_lib):
+    """Few members where top-k cuts, and top-p's share of them reaching over empty ranks into
+    many: one logit of 0, a hundred about -0.26 (the largest amid them), sixty about -3.47 of
+    which thirty stay."""
+    say("sample boundary not listed")
+    n, R = 400, 64
+    lg = torch.full((n,), -30.0)
+    lg[17] = 0.0
+    lg[100:200] = -3 / 8 * math.log(2) - 1e-5 * (torch.arange(100) - 51).abs()
+    lg[250:310] = -5 * math.log(2) + 1e-4 * (torch.arange(60) % 7)
+    u = torch.arange(R) / R
+    for p in (0.0127, 0.0128, 0.0231, 0.05):
+        _, _, prob = check(lg.expand(R, n).contiguous(), u, top_k=torch.full((R,), 131, dtype=torch.int32), top_p=torch.full((R,), p))
+    assert prob.max() < 1
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("seed", range(4))
+def test_clustered_logits(gpu_lib, seed, dtype):
+    """Rows whose logits lie in few narrow clusters of very unlike sizes, with gaps and ties between."""
+    say(f"sample clusters {seed} {dtype}")
+    R, V = 300, [257, 700, 1200, 9000][seed]
+    g = torch.Generator().manual_seed(100 + seed)
+    sizes = torch.tensor([1.0, 1, 2, 5, 30, 60, 100, V / 2])
+    at = torch.rand(R, 8, generator=g) * 6 * (torch.rand(R, 1, generator=g) > 0.2)
+    which = torch.multinomial(sizes.expand(R, 8), V, replacement=True, generator=g)
+    step = 10.0 ** -torch.randint(1, 7, (R, 1), generator=g).float()
+    lg = -at.gather(1, which) - step * torch.randint(0, 50, (R, V), generator=g) + 3
+    which = torch.rand(R, generator=g)
+    check(lg.to(dtype), uniform(R, seed + 1), temperature=uniform(R, seed + 2, 0.3, 3.0),
+          top_k=torch.where(which < 0.7, torch.randint(1, V, (R,), generator=g), 0).to(torch.int32),
+          top_p=torch.where(which > 0.2, uniform(R, seed + 3) ** 2, 1.0), min_p=torch.where(which > 0.8, uniform(R, seed + 4), 0.0))
+
+
 def test_control_values(gpu_lib):
     """Every control at, around and beyond its ends, in one batch; rows are independent."""
     say("sample control values")
