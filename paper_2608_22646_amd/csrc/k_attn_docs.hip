@@ -153,7 +153,7 @@ struct Rows {
 
 // One row tile against the keys kb .. ke - 1 of its document.
 template <typename T, int HD, int QG, int KG, int KT, int S>
-__global__ void __launch_bounds__(64 * QG * KG, 1) attn_docs_kernel(AttnArgs a, AttnPlan p) {
+__global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kernel(AttnArgs a, AttnPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   typedef Tile<T, HD> TL;
   constexpr bool BF = sizeof(T) == 2;
@@ -674,15 +674,20 @@ Choice choose(const AttnArgs& a) {
   // still give every CU a workgroup, else the narrowest: a wide tile reads keys and
   // values for more rows, a narrow one leaves more waves to split the keys
   const long chunks_max = std::max(1, a.max_kv / CHUNK_MIN);
-  c.qg = f32 ? 4 : 8;
+  // bf16 with two workgroups of 128 rows for every CU: four waves that do not split the
+  // keys, two workgroups a CU, so that one's softmax lies beside the other's products
+  // (8 prompts of 358 .. 1023 tokens, 32 heads: 149 us; one of eight waves and 256 rows
+  // a CU, which reads keys and values half as often: 166; 8448 tokens: 530 both)
+  const bool dense = !f32 && rows > 128 && heads * ceil_div(rows, 128) * chunks_max >= 2 * cus;
+  c.qg = 4;
   while (c.qg > 1 && (rows <= 16 * c.qg || heads * ceil_div(rows, 32 * c.qg) * chunks_max < cus)) c.qg /= 2;
-  c.kg = c.qg == 8 ? 1 : c.qg == 4 ? (f32 ? 1 : 2) : wide_row ? 2 : c.qg == 2 ? 4 : FEW_KG;
-  c.kt = c.qg == 8 ? 64 : 32;
+  c.kg = dense ? 1 : c.qg == 4 ? (f32 ? 1 : 2) : wide_row ? 2 : c.qg == 2 ? 4 : FEW_KG;
+  c.kt = dense ? 64 : 32;
   AttnPlan& p = c.plan;
   p.tiles = ceil_div(rows, 32 * c.qg);
   const long wgs = heads * p.tiles;
   const int step = c.kg * c.kt, steps = std::max(1, ceil_div(a.max_kv, step));
-  const long slots = c.qg == 1 ? FEW_SLOTS * cus : cus;
+  const long slots = dense ? 2 * cus : cus;
   int chunks = 1;
   if (wgs < slots) chunks = (int)std::max(1l, std::min(ceil_div(slots, wgs) + 0l, (long)a.max_kv / CHUNK_LEAST));
   const int per = ceil_div(steps, chunks);
@@ -709,10 +714,10 @@ void launch(const AttnArgs& a, const Choice& c, hipStream_t s) {
     go<T, HD, 1, WIDE ? 2 : FEW_KG, 32, 2>(a, c, s);
   else if (c.qg == 2)
     go<T, HD, 2, WIDE ? 2 : 4, 32, 2>(a, c, s);
-  else if (c.qg == 4)
+  else if (F32 || c.kg == 2)
     go<T, HD, 4, F32 ? 1 : 2, 32, 3>(a, c, s);
   else if constexpr (!F32)
-    go<T, HD, 8, 1, 64, 3>(a, c, s);
+    go<T, HD, 4, 1, 64, 2>(a, c, s);
   if (c.plan.chunks > 1) {
     const long rows = (long)a.docs * a.max_q * a.Hq;
     attn_join_kernel<T, HD><<<ceil_div(rows, 4), 256, 0, s>>>(a, c.plan);
