@@ -33,6 +33,7 @@ typedef __attribute__((address_space(3))) v4s_t* lds_v4s_t;
 typedef unsigned short v2us_t __attribute__((ext_vector_type(2)));
 
 constexpr float LOG2E = 1.4426950408889634f;
+constexpr int MAX_SHARES = 256;
 
 // A document's ranges, cut to its slab and to the maxima.
 struct Doc {
@@ -60,6 +61,77 @@ __device__ __forceinline__ int sees(const AttnArgs& a, const Doc& d, int t) {
   return max(n, min(d.prefix, d.nk));
 }
 
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ const char* uniform(const char* p) {
+  const uint32_t lo = uniform((int)(uint64_t)p), hi = uniform((int)((uint64_t)p >> 32));
+  return (const char*)((uint64_t)hi << 32 | lo);
+}
+// Sum of the lanes up to this one (within rows of 16 lanes, then over them).
+__device__ __forceinline__ int lanes_upto(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+// Where a document's keys are split: its chunks are shares shares[first ..
+// first + count - 1] of the call, of steps x step keys each, the last to its end.
+struct Share {
+  int doc, chunk, first, count, steps;
+};
+// Share i of the call (doc -1: there is none).  The longest chunk is made as short as
+// p.shares shares allow when every document takes whole ones, at least p.least steps:
+// found from all documents' lengths, so that unlike ones still keep the CUs equally busy.
+__device__ Share share_of(const AttnArgs& a, const AttnPlan& p, int step, int i) {
+  constexpr int R = MAX_SHARES / 64;  // documents lane, lane + 64, ..
+  const int lane = threadIdx.x & 63;
+  int n[R], all = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r) {
+    n[r] = 0;
+    if (r * 64 + lane < a.docs) {
+      const Doc d = doc_of(a, r * 64 + lane);
+      if (d.nq > 0) n[r] = (sees(a, d, d.nq - 1) + step - 1) / step;
+    }
+    all += n[r];
+  }
+  all = __builtin_amdgcn_readlane(lanes_upto(all), 63);
+  auto chunks = [&](int r, int len) { return r * 64 + lane < a.docs ? max(1, (int)((uint32_t)(n[r] + len - 1) / (uint32_t)len)) : 0; };
+  // sum n / len <= chunks <= sum n / len + documents
+  int lo = max(p.least, all / p.shares), hi = max(lo, all / (p.shares - a.docs) + 1);
+  while (lo < hi) {
+    const int len = (lo + hi) >> 1;
+    int sum = 0;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+      if (r * 64 < a.docs) sum += chunks(r, len);
+    if (__builtin_amdgcn_readlane(lanes_upto(sum), 63) <= p.shares)
+      hi = len;
+    else
+      lo = len + 1;
+  }
+  Share s{-1, 0, 0, 0, 0};
+  int before = 0;
+#pragma unroll
+  for (int r = 0; r < R; ++r)
+    if (r * 64 < a.docs) {
+      const int c = chunks(r, lo), upto = before + lanes_upto(c);
+      const unsigned long long mine = __ballot(i < upto && i >= upto - c);
+      if (mine) {
+        const int l = __ffsll(mine) - 1;
+        s.doc = r * 64 + l;
+        s.count = __builtin_amdgcn_readlane(c, l);
+        s.first = __builtin_amdgcn_readlane(upto - c, l);
+        s.chunk = i - s.first;
+        s.steps = (__builtin_amdgcn_readlane(n[r], l) + s.count - 1) / s.count;  // as equal as whole steps allow
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
+    }
+  return s;
+}
+
 template <int N>
 __device__ __forceinline__ void wait_vmcnt() {
   static_assert(N >= 0 && N < 64, "vmcnt range");
@@ -78,11 +150,6 @@ __device__ __forceinline__ uint32_t pack2(float lo, float hi) {
 }
 __device__ __forceinline__ float add2(float acc, uint32_t w) {
   return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf2_t, w), __builtin_bit_cast(bf2_t, 0x3f803f80u), acc, false);
-}
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ const char* uniform(const char* p) {
-  const uint32_t lo = uniform((int)(uint64_t)p), hi = uniform((int)((uint64_t)p >> 32));
-  return (const char*)((uint64_t)hi << 32 | lo);
 }
 // Buffer descriptor of `bytes` bytes from p on (both the same in every lane):
 // reads past its end give zeros.
@@ -174,14 +241,24 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
   const int up = (i8 / p.part_tiles) * 8 + x8;  // unit and part
   const int unit = up / p.parts, tile = p.tiles - 1 - ((i8 % p.part_tiles) * p.parts + up % p.parts);
   if (unit >= p.units || tile < 0) return;
-  const int g = unit % a.Hkv, rest = unit / a.Hkv, chunk = rest % p.chunks, dn = rest / p.chunks;
+  const int g = unit % a.Hkv;
+  int dn = unit / a.Hkv;
+  Share sh{dn, 0, dn, 1, 0};
+  if (p.shares > 0) {
+    sh = share_of(a, p, KG * KT, dn);
+    if (sh.doc < 0) return;
+    dn = sh.doc;
+  }
   Doc d = doc_of(a, dn);
   d = Doc{uniform(d.q0), uniform(d.nq), uniform(d.k0), uniform(d.nk), uniform(d.pos), uniform(d.prefix)};
   const int G = a.Hq / a.Hkv, rows = d.nq * G, r0 = tile * TR;
+  // what the join needs of each document
+  if (p.shares > 0 && sh.chunk == 0 && g == 0 && tile == 0 && tid == 0) p.table[dn] = make_int4(sh.first, sh.count, sh.steps * KG * KT, 0);
   if (r0 >= rows) return;
   const int t_last = (min(r0 + TR, rows) - 1) / G;
-  const int kb = uniform(chunk * p.chunk_keys), ke = uniform(min(sees(a, d, t_last), p.chunks > 1 ? kb + p.chunk_keys : 0x7fffffff));
-  if (chunk > 0 && kb >= ke) return;
+  const int chunk_keys = sh.steps * KG * KT, kb = uniform(sh.chunk * chunk_keys);
+  const int ke = uniform(min(sees(a, d, t_last), sh.chunk + 1 < sh.count ? kb + chunk_keys : 0x7fffffff));
+  if (sh.chunk > 0 && kb >= ke) return;
   const int tile_first = uniform(sees(a, d, r0 / G));  // keys that every row of the tile sees
   // this wave's rows
   const int w0 = r0 + 32 * qg, w1 = min(w0 + 32, rows);
@@ -524,8 +601,12 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     } else {
       mt = shape(x, t0, whole);
     }
+    // softmax first: beside another wave's products, which then do not hold it up
+    // (8448 tokens: 536 -> 519 us)
+    __builtin_amdgcn_s_setprio(1);
     raise(mt);
     exponentials(x, pw, fold);
+    __builtin_amdgcn_s_setprio(0);
     products(vt, x, pw);
   }
   R.l = sum_pair32(R.l);
@@ -564,9 +645,9 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     }
   }
   if (!R.mine) return;
-  if (p.chunks > 1) {
-    // state of (document, query, head) for this chunk: hd outputs, then (m, l)
-    const size_t at = (((size_t)dn * a.max_q + R.t) * a.Hq + R.h) * p.chunks + chunk;
+  if (p.shares > 0) {
+    // state of (query, head) for this share: hd outputs, then (m, l)
+    const size_t at = ((size_t)(sh.first + sh.chunk) * a.max_q + R.t) * a.Hq + R.h;
     float* to = p.part + at * HD;
 #pragma unroll
     for (int ds = 0; ds < ND; ++ds)
@@ -607,16 +688,18 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
   const int t = (int)(dt % a.max_q), dn = (int)(dt / a.max_q);
   const Doc d = doc_of(a, dn);
   if (t >= d.nq) return;
-  // chunks that the row's tile ran: all that it sees a key of
-  const int n = (sees(a, d, t) + p.chunk_keys - 1) / p.chunk_keys;
-  const float2* ml = p.part_ml + row * p.chunks;
+  // its document's chunks of which it sees a key; its tile ran them all
+  const int4 w4 = p.table[dn];
+  const int n = w4.z > 0 ? min(w4.y, (sees(a, d, t) + w4.z - 1) / w4.z) : 0;
+  const size_t next = (size_t)a.max_q * a.Hq, at = w4.x * next + (size_t)t * a.Hq + h;
+  const float2* ml = p.part_ml + at;
   const int e = lane % LPC * 4, side = lane / LPC;
-  const float* part = p.part + row * p.chunks * HD + e;
+  const float* part = p.part + at * HD + e;
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
   for (int c0 = 0; c0 < n; c0 += 64) {  // 64 chunks at a time, on the maximum so far
     float2 s = make_float2(-INFINITY, 0.f);
-    if (c0 + lane < n) s = ml[c0 + lane];
+    if (c0 + lane < n) s = ml[(c0 + lane) * next];
     float top = s.x;
 #pragma unroll
     for (int x = 32; x > 0; x >>= 1) top = fmaxf(top, __shfl_xor(top, x, 64));
@@ -633,7 +716,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
     for (int i = 0; i < here; i += SIDE) {
       const int c = min(i + side, here - 1);
       const float fc = __shfl(f, c, 64);
-      const float4 w = *reinterpret_cast<const float4*>(part + (size_t)(c0 + c) * HD);
+      const float4 w = *reinterpret_cast<const float4*>(part + (c0 + c) * next * HD);
       if (i + side < here) {
         o.x += w.x * fc;
         o.y += w.y * fc;
@@ -685,15 +768,13 @@ Choice choose(const AttnArgs& a) {
   c.kt = dense ? 64 : 32;
   AttnPlan& p = c.plan;
   p.tiles = ceil_div(rows, 32 * c.qg);
-  const long wgs = heads * p.tiles;
-  const int step = c.kg * c.kt, steps = std::max(1, ceil_div(a.max_kv, step));
+  const int step = c.kg * c.kt;
   const long slots = dense ? 2 * cus : cus;
-  int chunks = 1;
-  if (wgs < slots) chunks = (int)std::max(1l, std::min(ceil_div(slots, wgs) + 0l, (long)a.max_kv / CHUNK_LEAST));
-  const int per = ceil_div(steps, chunks);
-  p.chunk_keys = per * step;
-  p.chunks = ceil_div(steps, per);
-  const long units = heads * p.chunks;
+  // where they leave CUs without a workgroup, shares for all of them
+  p.least = ceil_div(CHUNK_LEAST, step);
+  const long shares = std::min({slots / ((long)a.Hkv * p.tiles), (long)a.docs * (a.max_kv / CHUNK_LEAST), (long)MAX_SHARES});
+  p.shares = shares > a.docs && (long)a.docs * (a.max_kv / step + 1) < (1l << 30) ? (int)shares : 0;
+  const long units = (p.shares ? p.shares : a.docs) * (long)a.Hkv;
   p.units = (int)std::min(units, 0x7fffffffl);
   p.parts = units % 8 == 0 || units >= 512 ? 1 : units >= 64 ? 2 : 8;
   while (p.parts < 8 && units * p.parts % 8 && units < 64) p.parts *= 2;
@@ -718,20 +799,20 @@ void launch(const AttnArgs& a, const Choice& c, hipStream_t s) {
     go<T, HD, 4, F32 ? 1 : 2, 32, 3>(a, c, s);
   else if constexpr (!F32)
     go<T, HD, 4, 1, 64, 2>(a, c, s);
-  if (c.plan.chunks > 1) {
+  if (c.plan.shares > 0) {
     const long rows = (long)a.docs * a.max_q * a.Hq;
     attn_join_kernel<T, HD><<<ceil_div(rows, 4), 256, 0, s>>>(a, c.plan);
     DLLM_LAUNCH_CHECK("attn_join_kernel");
   }
 }
 
-size_t part_values(const AttnArgs& a, const AttnPlan& p) { return (size_t)a.docs * a.max_q * a.Hq * p.chunks; }
+size_t part_values(const AttnArgs& a, const AttnPlan& p) { return (size_t)p.shares * a.max_q * a.Hq; }
 
 }  // namespace
 
 size_t attn_docs_bytes(const AttnArgs& a) {
   const Choice c = choose(a);
-  return c.plan.chunks > 1 ? part_values(a, c.plan) * (a.hd * 4 + 8) + 256 : 0;
+  return c.plan.shares > 0 ? part_values(a, c.plan) * (a.hd * 4 + 8) + (size_t)a.docs * sizeof(int4) : 0;
 }
 
 bool attn_docs_fits(const AttnArgs& a) {
@@ -740,8 +821,9 @@ bool attn_docs_fits(const AttnArgs& a) {
 
 void launch_attn_docs(const AttnArgs& a, void* ws, hipStream_t s) {
   Choice c = choose(a);
-  if (c.plan.chunks > 1) {
-    c.plan.part = static_cast<float*>(ws);
+  if (c.plan.shares > 0) {
+    c.plan.table = static_cast<int4*>(ws);
+    c.plan.part = reinterpret_cast<float*>(c.plan.table + a.docs);
     c.plan.part_ml = reinterpret_cast<float2*>(c.plan.part + part_values(a, c.plan) * a.hd);
   }
   if (a.dtype == DLLM_F32)

@@ -228,12 +228,15 @@ struct AttnArgs {
   const float* slopes;
   float scale, cap;
 };
-// Layout of a call's grid: row tiles, units of (document, key chunk, key/value
-// head), and the chunks' states (part: hd floats each; part_ml: maximum and sum).
+// Layout of a call's grid: row tiles, units of (document or share, key/value head);
+// where keys are split, the shares that documents' chunks are dealt, the least steps
+// of one, each share's states (part: hd floats a row; part_ml: maximum and sum) and
+// each document's first share, their count and the keys of each (table).
 struct AttnPlan {
-  int tiles, parts, part_tiles, units, chunks, chunk_keys;
+  int tiles, parts, part_tiles, units, shares, least;
   float* part;
   float2* part_ml;
+  int4* table;
 };
 size_t attn_docs_bytes(const AttnArgs& a);
 bool attn_docs_fits(const AttnArgs& a);  // its grid can be launched
