@@ -776,8 +776,9 @@ Choice choose(const AttnArgs& a) {
   p.shares = shares > a.docs && (long)a.docs * (a.max_kv / step + 1) < (1l << 30) ? (int)shares : 0;
   const long units = (p.shares ? p.shares : a.docs) * (long)a.Hkv;
   p.units = (int)std::min(units, 0x7fffffffl);
-  p.parts = units % 8 == 0 || units >= 512 ? 1 : units >= 64 ? 2 : 8;
-  while (p.parts < 8 && units * p.parts % 8 && units < 64) p.parts *= 2;
+  // units that leave XCDs unlike work are dealt in parts of their row tiles
+  p.parts = 1;
+  while (p.parts < (units >= 512 ? 1 : units >= 64 ? 2 : 8) && 2 * p.parts <= p.tiles && units * p.parts % 8) p.parts *= 2;
   p.part_tiles = ceil_div(p.tiles, p.parts);
   c.grid = (long)ceil_div(units * p.parts, 8) * 8 * p.part_tiles;
   return c;
