@@ -91,11 +91,28 @@ __device__ __forceinline__ uint64_t class_word(double w) {
 }
 __device__ __forceinline__ double class_mass(uint64_t word) { return (double)(word & ((1ull << COUNT_BIT) - 1)) * 0x1p-36; }
 
-template <typename V, typename F>
-__device__ __forceinline__ V wave_all(V x, F f) {
-#pragma unroll
-  for (int s = 32; s > 0; s >>= 1) x = f(x, (V)__shfl_xor(x, s, 64));
-  return x;
+// A lane's value moved within the wave by CTRL (a data-parallel primitive, a few
+// cycles where a shuffle through LDS takes a hundred); `old` where none arrives.
+template <int CTRL, int ROWS, typename V>
+__device__ __forceinline__ V moved(V old, V x) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, old), __builtin_bit_cast(int, x), CTRL, ROWS, 0xf, false));
+  } else {
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    const v2i o = __builtin_bit_cast(v2i, old), y = __builtin_bit_cast(v2i, x);
+    return __builtin_bit_cast(V, v2i{__builtin_amdgcn_update_dpp(o.x, y.x, CTRL, ROWS, 0xf, false),
+                                     __builtin_amdgcn_update_dpp(o.y, y.y, CTRL, ROWS, 0xf, false)});
+  }
+}
+template <typename V>
+__device__ __forceinline__ V from_lane(V x, int lane) {
+  if constexpr (sizeof(V) == 4) {
+    return __builtin_bit_cast(V, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+  } else {
+    typedef int v2i __attribute__((ext_vector_type(2)));
+    const v2i y = __builtin_bit_cast(v2i, x);
+    return __builtin_bit_cast(V, v2i{__builtin_amdgcn_readlane(y.x, lane), __builtin_amdgcn_readlane(y.y, lane)});
+  }
 }
 struct Max {
   template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a > b ? a : b; }
@@ -106,6 +123,25 @@ struct Min {
 struct Sum {
   template <typename V> __device__ __forceinline__ V operator()(V a, V b) const { return a + b; }
 };
+// f over the lanes up to this one: within rows of 16 (by 1, 2, 4, 8), then the last
+// lane of row 0 into row 1 and of row 2 into row 3, then of row 1 into rows 2 and 3.
+template <typename V, typename F>
+__device__ __forceinline__ V wave_upto(V x, F f) {
+  auto none = [&] {  // what changes nothing
+    if constexpr (std::is_same_v<F, Sum>)
+      return (V)0;
+    else
+      return x;
+  };
+  x = f(x, moved<0x111, 0xf>(none(), x));
+  x = f(x, moved<0x112, 0xf>(none(), x));
+  x = f(x, moved<0x114, 0xf>(none(), x));
+  x = f(x, moved<0x118, 0xf>(none(), x));
+  x = f(x, moved<0x142, 0xa>(none(), x));
+  return f(x, moved<0x143, 0xc>(none(), x));
+}
+template <typename V, typename F>
+__device__ __forceinline__ V wave_all(V x, F f) { return from_lane(wave_upto(x, f), 63); }
 typedef unsigned long long u64;
 
 // What a chunk leaves: its largest logit, the lowest index of a NaN or +inf (or
@@ -363,11 +399,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
 template <typename V>
 __device__ __forceinline__ V block_scan(V x, V* buf) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const V y = __shfl_up(x, s, 64);
-    if (lane >= s) x += y;
-  }
+  x = wave_upto(x, Sum{});
   if (lane == 63) buf[wave] = x;
   __syncthreads();
   V before = 0;
@@ -558,12 +590,7 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
           }
       }
   // places in the row's list: one reservation per workgroup
-  uint32_t n = __popc(hit), incl = n;
-#pragma unroll
-  for (int s = 1; s < 64; s <<= 1) {
-    const uint32_t y = __shfl_up(incl, s, 64);
-    if (lane >= s) incl += y;
-  }
+  const uint32_t n = __popc(hit), incl = wave_upto(n, Sum{});
   if (lane == 63) s_n[wave] = incl;
   __syncthreads();
   if (tid == 0) {
@@ -608,7 +635,7 @@ struct Picker {
     uint2 list[KEPT];  // the row's list, where it fits
     u64 sub_mass[NT];
     uint32_t sub_count[NT];
-    uint2 few[FEW];
+    uint4 few[FEW];
     double powers[STEPS], bufd[NW];
     uint32_t bufu[NW], a, b, n;
     int i;
@@ -694,21 +721,22 @@ struct Picker {
         if (tid == 0) sh.n = 0;
         __syncthreads();
         members(b, [&](uint32_t key, uint32_t v) {
-          if (in_range(key, v)) sh.few[min(atomicAdd(&sh.n, 1u), (uint32_t)FEW - 1)] = make_uint2(key, v);
+          if (!in_range(key, v)) return;
+          const u64 fixed = (u64)(weight(value_of(key)) * units);
+          sh.few[min(atomicAdd(&sh.n, 1u), (uint32_t)FEW - 1)] = make_uint4(key, v, (uint32_t)fixed, (uint32_t)(fixed >> 32));
         });
         __syncthreads();
         const int n = (int)sh.n;
-        const uint2 mine = lane < n ? sh.few[lane] : make_uint2(0, ~0u);
-        const u64 fixed = lane < n ? (u64)(weight(value_of(mine.x)) * units) : 0;
+        const uint4 mine = lane < n ? sh.few[lane] : make_uint4(0, ~0u, 0, 0);
+        auto fixed_of = [](const uint4& m) { return (u64)m.w << 32 | m.z; };
         uint32_t rank = 0;
         u64 before = 0;
+#pragma unroll 8
         for (int j = 0; j < n; ++j) {
-          const uint32_t kj = __shfl(mine.x, j, 64), vj = __shfl(mine.y, j, 64);
-          const u64 wj = __shfl(fixed, j, 64);
-          if (kj > mine.x || (kj == mine.x && vj < mine.y)) {
-            ++rank;
-            before += wj;
-          }
+          const uint4 o = sh.few[j];
+          const bool first = o.x > mine.x || (o.x == mine.x && o.y < mine.y);
+          rank += first;
+          before += first ? fixed_of(o) : 0;
         }
         const double mass = m0 + (double)before * unit;
         const bool stays = lane < n && n0 + rank < limit && mass < target;
@@ -717,8 +745,7 @@ struct Picker {
         const u64 who = __ballot(stays && rank + 1 == r);
         if (who == 0) return Cut{~0u, 0, m0};  // no members (rounding at a class's edge can lead here)
         const int l = __ffsll(who) - 1;
-        return Cut{(uint32_t)__shfl(mine.x, l, 64), (uint32_t)__shfl(mine.y, l, 64),
-                   __shfl(mass + (double)fixed * unit, l, 64)};
+        return Cut{from_lane(mine.x, l), from_lane(mine.y, l), from_lane(mass + (double)fixed_of(mine) * unit, l)};
       }
       if (by_key && hi == lo) {
         // many equal members: those with the lowest indices
@@ -918,21 +945,15 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
   double run = 0, sums = 0;
   for (int i0 = 0; i0 < nch; i0 += 64) {
     const double part = i0 + lane < nch ? sh.part[i0 + lane] : 0.0;
-    double upto = part;
-#pragma unroll
-    for (int x = 1; x < 64; x <<= 1) {
-      const double y = __shfl_up(upto, x, 64);
-      if (lane >= x) upto += y;
-    }
-    upto += sums;
+    const double upto = wave_upto(part, Sum{}) + sums;
     const u64 mass = __ballot(part > 0.0), past = __ballot(part > 0.0 && upto > want);
     if (past | mass) {
       const int l = past ? __ffsll(past) - 1 : 63 - __clzll(mass);
       at = i0 + l;
-      run = __shfl(upto - part, l, 64);
+      run = from_lane(upto - part, l);
     }
     if (past) break;
-    sums = __shfl(upto, 63, 64);
+    sums = from_lane(upto, 63);
   }
   if (tid == 0) {
     sh.a = ~0u;
