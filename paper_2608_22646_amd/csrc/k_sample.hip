@@ -37,8 +37,8 @@ constexpr int BINS = 512;               // 64 octaves; the last class stands for
 constexpr double PER_NAT = 11.541560327111707;  // 8 / ln 2
 constexpr double LEAST = 0x1p-63;       // weights below count as none
 constexpr int LIST = 8192;              // members listed of a row
-constexpr int SLOTS = 4;                // classes listed of a row
-constexpr int MAX_CHUNKS = (1 << 22) / CHUNK;
+constexpr int INDEX_BITS = 22;          // of a listed member's second word; its class above
+constexpr int MAX_CHUNKS = (1 << INDEX_BITS) / CHUNK;
 static_assert(BINS == NT, "a thread per class");
 
 // Global memory, said outright: pointers out of structures are else read as flat ones.
@@ -155,12 +155,14 @@ struct ChunkStat {
 // What sample_edge_kernel leaves: the boundary as far as the classes tell it.
 // Under top-k the classes below `ek` stay, of class ek - 1 the first rk members
 // only where rk > 0; [lo, hi] are the classes in which top-p's boundary can fall;
-// class bm holds min-p's (-1: none).
+// class bm holds min-p's (-1: none).  Listed are the members of classes [p0, p1],
+// k1 and m1 (-1: none).
 struct RowState {
   int ek, rk, lo, hi, bm;
-  int slot[SLOTS];    // classes listed, -1: none
+  int p0, p1, k1, m1;
   float least, most;  // every listed member lies within
   double base;        // class of the row's maximum
+  __device__ __forceinline__ bool lists(int b) const { return (b >= p0 && b <= p1) || b == k1 || b == m1; }
 };
 
 struct SampleWs {
@@ -168,7 +170,7 @@ struct SampleWs {
   u64* classes;      // [rows, chunks, BINS]: class_word sums
   double* prefix;    // [rows, BINS]: mass of the classes up to each
   RowState* state;   // [rows]
-  uint2* list;       // [rows, LIST]: key, index | slot << 24
+  uint2* list;       // [rows, LIST]: key, index | class << INDEX_BITS
   uint32_t* listed;  // [rows]
   uint8_t* holds;    // [rows, chunks]: 1 where a chunk has members of the listed classes
   int chunks;
@@ -491,7 +493,7 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   binc[tid] = n;
   w.prefix[(size_t)row * BINS + tid] = m;
   __syncthreads();
-  RowState st{BINS, 0, 0, -1, -1, {-1, -1, -1, -1}, 0.f, 0.f, top.base};
+  RowState st{BINS, 0, 0, -1, -1, 0, -1, -1, -1, 0.f, 0.f, top.base};
   double least = binw[BINS - 2], most = least;  // bounds of the mass that top-p is a share of
   if (c.top_k) {
     if (tid < BINS - 1 && n >= (uint32_t)c.top_k && (tid == 0 || binc[tid - 1] < (uint32_t)c.top_k)) s_k = tid;
@@ -525,25 +527,31 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
     edge = min(edge, st.bm + 1);
   }
   // members are needed of the classes in which the boundary may fall, and of
-  // top-k's where top-p is a share of what it keeps
-  int used = 0, first = BINS, final = 0;
-  auto list = [&](int b) {
-    bool there = false;
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i) there |= st.slot[i] == b;
-    if (there || used >= SLOTS) return;
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i)
-      if (i == used) st.slot[i] = b;
-    ++used;
+  // top-k's where top-p is a share of what it keeps; listed are those that fit
+  const bool by_p = c.top_p < 1.0 && st.lo < edge;  // top-p may decide
+  uint32_t room = LIST;
+  int first = BINS, final = 0;
+  auto single = [&](int b) {
+    const uint32_t members = binc[b] - (b ? binc[b - 1] : 0u);
+    if (members > room) return -1;
+    room -= members;
     first = min(first, b);
     final = max(final, b);
+    return b;
   };
-  const bool by_p = c.top_p < 1.0 && st.lo < edge;  // top-p may decide
-  if (st.rk > 0 && (by_p || st.ek == edge)) list(st.ek - 1);
-  if (st.bm >= 0 && st.bm < BINS - 1 && st.bm + 1 == edge) list(st.bm);
-  if (by_p)
-    for (int b = st.lo; b <= st.hi && b < edge && used < SLOTS; ++b) list(b);
+  if (st.rk > 0 && (by_p || st.ek == edge)) st.k1 = single(st.ek - 1);
+  if (st.bm >= 0 && st.bm < BINS - 1 && st.bm + 1 == edge) st.m1 = single(st.bm);
+  if (by_p) {
+    const int end = min(min(st.hi, edge - 1), st.lo + 63);
+    const uint32_t before = st.lo ? binc[st.lo - 1] : 0u;
+    st.p0 = st.lo;
+    st.p1 = st.lo - 1;
+    while (st.p1 < end && binc[st.p1 + 1] - before <= room) ++st.p1;
+    if (st.p1 >= st.p0) {
+      first = min(first, st.p0);
+      final = max(final, st.p1);
+    }
+  }
   // logits outside [least, most] lie in none of them (a margin covers float32)
   const double hi = (top.base - first + 1) / c.rate, lo = (top.base - final - 1) / c.rate;
   st.most = c.rate > 0 ? (float)(hi + fabs(hi) * 1e-6) : INFINITY;
@@ -551,11 +559,13 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   if (tid == 0) w.state[row] = st;
   for (int i = tid; i < nch; i += NT) {
     u64 have = 0;
-#pragma unroll
-    for (int j = 0; j < SLOTS; ++j) {
-      const int k = st.slot[j] - ch.shift[i];
-      if (st.slot[j] >= 0 && k >= 0) have |= hm[(size_t)i * BINS + k];
-    }
+    auto look = [&](int b) {
+      const int k = b - ch.shift[i];
+      if (b >= 0 && k >= 0) have |= hm[(size_t)i * BINS + k];
+    };
+    look(st.k1);
+    look(st.m1);
+    for (int b = st.p0; b <= st.p1; ++b) look(b);
     w.holds[(size_t)row * nch + i] = have != 0;
   }
 }
@@ -575,20 +585,13 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
   const bool whole = v0 + CHUNK <= a.vocab;
   if (whole) slice.fetch(x, v0);
   slice.take(x, v0, whole, a.vocab, a.mask_id, f);
-  uint32_t hit = 0, slots = 0;
+  uint32_t hit = 0;
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
     for (int e = 0; e < N; ++e)
-      if (f[i][e] >= st.least && f[i][e] <= st.most && f[i][e] > -INFINITY) {
-        const int b = class_of(f[i][e], c.rate, st.base);
-#pragma unroll
-        for (int k = 0; k < SLOTS; ++k)
-          if (b == st.slot[k]) {
-            hit |= 1u << (i * N + e);
-            slots |= (uint32_t)k << 2 * (i * N + e);
-          }
-      }
+      if (f[i][e] >= st.least && f[i][e] <= st.most && f[i][e] > -INFINITY)
+        hit |= (uint32_t)st.lists(class_of(f[i][e], c.rate, st.base)) << (i * N + e);
   // places in the row's list: one reservation per workgroup
   const uint32_t n = __popc(hit), incl = wave_upto(n, Sum{});
   if (lane == 63) s_n[wave] = incl;
@@ -611,7 +614,7 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
       if (hit >> (i * N + e) & 1) {
         if (at < LIST)
           w.list[(size_t)row * LIST + at] =
-              make_uint2(key_of(f[i][e]), (uint32_t)(v0 + (i * NT + tid) * N + e) | (slots >> 2 * (i * N + e) & 3) << 24);
+              make_uint2(key_of(f[i][e]), (uint32_t)(v0 + (i * NT + tid) * N + e) | (uint32_t)class_of(f[i][e], c.rate, st.base) << INDEX_BITS);
         ++at;
       }
 }
@@ -654,20 +657,11 @@ struct Picker {
     const double e = weight_of(in_classes(f, rate) - top.qtop, sh.powers);
     return e < LEAST ? 0.0 : e;
   }
-  // Where the list holds all members of class b: its slot, else -1.
-  __device__ __forceinline__ int slot_of(int b) const {
-    int slot = -1;
-#pragma unroll
-    for (int i = 0; i < SLOTS; ++i)
-      if (st.slot[i] == b) slot = i;
-    return listed <= LIST ? slot : -1;
-  }
   // f(key, index) for every member of class b: from the row's list, or where the
-  // list does not hold them all, from the logits.
+  // list does not hold them, from the logits.
   template <typename F>
   __device__ __forceinline__ void members(int b, F f) const {
-    const int slot = slot_of(b);
-    if (slot >= 0) {
+    if (st.lists(b)) {
       for (uint32_t i = threadIdx.x; i < listed; i += NT) {
         uint2 m;
         if (listed <= KEPT) {
@@ -676,7 +670,7 @@ struct Picker {
           m.x = list[i].x;
           m.y = list[i].y;
         }
-        if ((int)(m.y >> 24) == slot) f(m.x, m.y & 0xffffffu);
+        if ((int)(m.y >> INDEX_BITS) == b) f(m.x, m.y & ((1u << INDEX_BITS) - 1));
       }
       return;
     }
@@ -710,7 +704,7 @@ struct Picker {
     const double edge0 = (top.base - b - 1) / rate, edge1 = (top.base - b + 1) / rate;
     const float f0 = (float)(edge0 - fabs(edge0) * 1e-6), f1 = (float)(edge1 + fabs(edge1) * 1e-6);
     uint32_t lo = rate > 0 ? key_of(f0) : key_of(-INFINITY), hi = rate > 0 ? key_of(f1) : key_of(INFINITY);
-    uint32_t inside = slot_of(b) >= 0 ? listed : ~0u;  // members in the range, at most
+    uint32_t inside = st.lists(b) ? listed : ~0u;  // members in the range, at most
     bool by_key = true;
     uint32_t n0 = 0, key0 = 0;  // members ranked before the range, and their mass; its key, once it is one
     double m0 = 0;

@@ -96,19 +96,22 @@ def test_ties(gpu_lib, V, dtype):
     check(z, torch.tensor([0.9, 0.9]), top_k=torch.tensor([1, 1], dtype=torch.int32))
 
 
-def test_boundary_in_a_class_that_is_not_listed(gpu_lib):
+@pytest.mark.parametrize("many", [100, 9000])
+def test_boundary_far_from_top_ks(gpu_lib, many):
     """Few members where top-k cuts, and top-p's share of them reaching over empty ranks into
-    many: one logit of 0, a hundred about -0.26 (the largest amid them), sixty about -3.47 of
-    which thirty stay."""
-    say("sample boundary not listed")
-    n, R = 400, 64
+    many (9000: more than are listed of a row): one logit of 0, many about -0.26 (the largest amid
+    them), sixty about -3.47 of which thirty stay."""
+    say(f"sample boundary far from top-k's {many}")
+    n, R = 300 + many, 64
     lg = torch.full((n,), -30.0)
     lg[17] = 0.0
-    lg[100:200] = -3 / 8 * math.log(2) - 1e-5 * (torch.arange(100) - 51).abs()
-    lg[250:310] = -5 * math.log(2) + 1e-4 * (torch.arange(60) % 7)
+    lg[100:100 + many] = -3 / 8 * math.log(2) - 1e-3 / many * (torch.arange(many) - many // 2 - 1).abs()
+    lg[150 + many:210 + many] = -5 * math.log(2) + 1e-4 * (torch.arange(60) % 7)
     u = torch.arange(R) / R
-    for p in (0.0127, 0.0128, 0.0231, 0.05):
-        _, _, prob = check(lg.expand(R, n).contiguous(), u, top_k=torch.full((R,), 131, dtype=torch.int32), top_p=torch.full((R,), p))
+    mass = 1 + many * 2 ** -0.375
+    for share in (1.004, 1.012, 1.83, 3.97, 0.3 * many):
+        _, _, prob = check(lg.expand(R, n).contiguous(), u, top_k=torch.full((R,), many + 31, dtype=torch.int32),
+                           top_p=torch.full((R,), share / (mass + 0.94)))
     assert prob.max() < 1
 
 
