@@ -36,7 +36,7 @@ constexpr int CHUNK = 8192, NT = 512, E = CHUNK / NT, NW = NT / 64;
 constexpr int BINS = 512;               // 64 octaves; the last class stands for everything without mass
 constexpr double PER_NAT = 11.541560327111707;  // 8 / ln 2
 constexpr double LEAST = 0x1p-63;       // weights below count as none
-constexpr int LIST = 8192;              // members listed of a row
+constexpr int LIST = 1 << 15;            // members listed of a row
 constexpr int INDEX_BITS = 22;          // of a listed member's second word; its class above
 constexpr int MAX_CHUNKS = (1 << INDEX_BITS) / CHUNK;
 static_assert(BINS == NT, "a thread per class");
@@ -675,19 +675,38 @@ struct Picker {
       return;
     }
     constexpr int N = 16 / sizeof(T), U = 16 / N;
+    float least, most;
+    bounds(b, least, most);
+    typedef float f16v __attribute__((ext_vector_type(16)));
+    float ahead[U][N];
+    auto fetch = [&](int v0) {
+#pragma unroll
+      for (int i = 0; i < U; ++i) load_logits<T, N>(x, v0 + (i * NT + (int)threadIdx.x) * N, V, mask_id, ahead[i]);
+    };
+    fetch(0);
     for (int v0 = 0; v0 < V; v0 += NT * N * U) {
-      float y[U][N];
+      f16v y;
+      uint32_t hit = 0;
 #pragma unroll
-      for (int i = 0; i < U; ++i) load_logits<T, N>(x, v0 + (i * NT + (int)threadIdx.x) * N, V, mask_id, y[i]);
+      for (int i = 0; i < 16; ++i) {
+        y[i] = ahead[i / N][i % N];
+        hit |= (uint32_t)(y[i] >= least && y[i] <= most && y[i] > -INFINITY) << i;
+      }
+      if (v0 + NT * N * U < V) fetch(v0 + NT * N * U);
 #pragma unroll 1
-      for (int i = 0; i < U * N; ++i) {
-        float f1 = 0.f;  // y[i / N][i % N], from registers
-#pragma unroll
-        for (int j = 0; j < U * N; ++j) f1 = j == i ? y[j / N][j % N] : f1;
-        if (f1 > -INFINITY && class_of(f1, rate, top.base) == b)
+      for (int i = 0; i < 16; ++i) {  // (the same i in every lane: y[i] is one register)
+        if (__ballot(hit >> i & 1) == 0) continue;
+        const float f1 = y[i];
+        if ((hit >> i & 1) && class_of(f1, rate, top.base) == b)
           f(key_of(f1), (uint32_t)(v0 + (i / N * NT + (int)threadIdx.x) * N + i % N));
       }
     }
+  }
+  // Logits that lie outside are not of class b (a margin covers float32).
+  __device__ __forceinline__ void bounds(int b, float& least, float& most) const {
+    const double lo = (top.base - b - 1) / rate, hi = (top.base - b + 1) / rate;
+    least = rate > 0 ? (float)(lo - fabs(lo) * 1e-6) : -INFINITY;
+    most = rate > 0 ? (float)(hi + fabs(hi) * 1e-6) : INFINITY;
   }
   // Class b's weights are at most 2^top_of(b); its sums are whole numbers of 2^(top_of(b) - 40).
   static __device__ __forceinline__ int top_of(int b) { return ((1 - b) >> 3) + 1; }
@@ -701,10 +720,36 @@ struct Picker {
     const double unit = ldexp(1.0, top_of(b) - 40), units = ldexp(1.0, 40 - top_of(b));
     target = fmax(target, 1e-300);  // the first of all stays
     // the range: keys [lo, hi] from above, then indices [lo, hi] from below
-    const double edge0 = (top.base - b - 1) / rate, edge1 = (top.base - b + 1) / rate;
-    const float f0 = (float)(edge0 - fabs(edge0) * 1e-6), f1 = (float)(edge1 + fabs(edge1) * 1e-6);
-    uint32_t lo = rate > 0 ? key_of(f0) : key_of(-INFINITY), hi = rate > 0 ? key_of(f1) : key_of(INFINITY);
+    uint32_t lo = ~0u, hi = 0;
     uint32_t inside = st.lists(b) ? listed : ~0u;  // members in the range, at most
+    if (inside > KEPT) {
+      // the members' own range: one round of parts then mostly does, and equal ones show
+      if (tid == 0) {
+        sh.a = ~0u;
+        sh.b = 0;
+      }
+      __syncthreads();
+      members(b, [&](uint32_t key, uint32_t) {
+        lo = min(lo, key);
+        hi = max(hi, key);
+      });
+      lo = wave_all(lo, Min{});
+      hi = wave_all(hi, Max{});
+      if (lane == 0) {
+        atomicMin(&sh.a, lo);
+        atomicMax(&sh.b, hi);
+      }
+      __syncthreads();
+      lo = sh.a;
+      hi = sh.b;
+      __syncthreads();
+      if (lo > hi) return Cut{~0u, 0, 0.0};  // no members (rounding at a class's edge can lead here)
+    } else {
+      float least, most;
+      bounds(b, least, most);
+      lo = key_of(least);
+      hi = key_of(most);
+    }
     bool by_key = true;
     uint32_t n0 = 0, key0 = 0;  // members ranked before the range, and their mass; its key, once it is one
     double m0 = 0;
@@ -737,7 +782,7 @@ struct Picker {
         // the last that stays: the one of the highest rank
         const uint32_t r = wave_all(stays ? rank + 1 : 0u, Max{});
         const u64 who = __ballot(stays && rank + 1 == r);
-        if (who == 0) return Cut{~0u, 0, m0};  // no members (rounding at a class's edge can lead here)
+        if (who == 0) return Cut{~0u, 0, m0};  // no members
         const int l = __ffsll(who) - 1;
         return Cut{from_lane(mine.x, l), from_lane(mine.y, l), from_lane(mass + (double)fixed_of(mine) * unit, l)};
       }
