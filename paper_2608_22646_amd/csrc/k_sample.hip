@@ -36,7 +36,7 @@ constexpr int CHUNK = 8192, NT = 512, E = CHUNK / NT, NW = NT / 64;
 constexpr int BINS = 512;               // 64 octaves; the last class stands for everything without mass
 constexpr double PER_NAT = 11.541560327111707;  // 8 / ln 2
 constexpr double LEAST = 0x1p-63;       // weights below count as none
-constexpr int LIST = 1 << 15;            // members listed of a row
+constexpr int LIST = 1 << 15;            // members listed of a row, at most
 constexpr int INDEX_BITS = 22;          // of a listed member's second word; its class above
 constexpr int MAX_CHUNKS = (1 << INDEX_BITS) / CHUNK;
 static_assert(BINS == NT, "a thread per class");
@@ -170,10 +170,10 @@ struct SampleWs {
   u64* classes;      // [rows, chunks, BINS]: class_word sums
   double* prefix;    // [rows, BINS]: mass of the classes up to each
   RowState* state;   // [rows]
-  uint2* list;       // [rows, LIST]: key, index | class << INDEX_BITS
+  uint2* list;       // [rows, list_len]: key, index | class << INDEX_BITS
   uint32_t* listed;  // [rows]
   uint8_t* holds;    // [rows, chunks]: 1 where a chunk has members of the listed classes
-  int chunks;
+  int chunks, list_len;
 };
 
 // A row's controls.
@@ -529,7 +529,7 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   // members are needed of the classes in which the boundary may fall, and of
   // top-k's where top-p is a share of what it keeps; listed are those that fit
   const bool by_p = c.top_p < 1.0 && st.lo < edge;  // top-p may decide
-  uint32_t room = LIST;
+  uint32_t room = w.list_len;
   int first = BINS, final = 0;
   auto single = [&](int b) {
     const uint32_t members = binc[b] - (b ? binc[b - 1] : 0u);
@@ -612,8 +612,8 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
 #pragma unroll
     for (int e = 0; e < N; ++e)
       if (hit >> (i * N + e) & 1) {
-        if (at < LIST)
-          w.list[(size_t)row * LIST + at] =
+        if (at < (uint32_t)w.list_len)
+          w.list[(size_t)row * w.list_len + at] =
               make_uint2(key_of(f[i][e]), (uint32_t)(v0 + (i * NT + tid) * N + e) | (uint32_t)class_of(f[i][e], c.rate, st.base) << INDEX_BITS);
         ++at;
       }
@@ -860,7 +860,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
   if (c.filter) sh.prefix[tid] = w.prefix[(size_t)row * BINS + tid];
   sh.extra[tid] = 0;
   __syncthreads();
-  P p{sh, static_cast<const T*>(a.logits) + (long)row * a.row_stride, (const GLOBAL uint2*)w.list + (size_t)row * LIST,
+  P p{sh, static_cast<const T*>(a.logits) + (long)row * a.row_stride, (const GLOBAL uint2*)w.list + (size_t)row * w.list_len,
       join_chunks(stat, nch, c, sh.powers, sh.ch), c.rate, V, a.mask_id, 0, RowState{}};
   const RowTop& top = p.top;
   if (top.bad != ~0u || top.big == -INFINITY) {
@@ -1043,7 +1043,8 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
 int chunks_of(int vocab) { return ceil_div(vocab, CHUNK); }
 
 // Carves the workspace (null: sizes only); returns the bytes.
-size_t carve(void* base, size_t rows, size_t chunks, SampleWs* w) {
+size_t carve(void* base, size_t rows, int vocab, SampleWs* w) {
+  const size_t chunks = chunks_of(vocab);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     char* at = static_cast<char*>(base) + off;
@@ -1051,11 +1052,12 @@ size_t carve(void* base, size_t rows, size_t chunks, SampleWs* w) {
     return at;
   };
   w->chunks = (int)chunks;
+  w->list_len = std::min(LIST, vocab);
   w->stat = reinterpret_cast<ChunkStat*>(take(rows * chunks * sizeof(ChunkStat)));
   w->classes = reinterpret_cast<u64*>(take(rows * chunks * BINS * sizeof(u64)));
   w->prefix = reinterpret_cast<double*>(take(rows * BINS * sizeof(double)));
   w->state = reinterpret_cast<RowState*>(take(rows * sizeof(RowState)));
-  w->list = reinterpret_cast<uint2*>(take(rows * LIST * sizeof(uint2)));
+  w->list = reinterpret_cast<uint2*>(take(rows * w->list_len * sizeof(uint2)));
   w->listed = reinterpret_cast<uint32_t*>(take(rows * sizeof(uint32_t)));
   w->holds = reinterpret_cast<uint8_t*>(take(rows * chunks));
   return off;
@@ -1082,12 +1084,12 @@ bool sample_fits(int rows, int vocab) { return (long)rows * chunks_of(vocab) < (
 
 size_t sample_bytes(int rows, int vocab) {
   SampleWs w;
-  return carve(nullptr, rows, chunks_of(vocab), &w);
+  return carve(nullptr, rows, vocab, &w);
 }
 
 void launch_sample(const SampleArgs& a, void* ws, hipStream_t s) {
   SampleWs w;
-  carve(ws, a.rows, chunks_of(a.vocab), &w);
+  carve(ws, a.rows, a.vocab, &w);
   a.dtype == DLLM_F32 ? launch<float>(a, w, s) : launch<bf16_t>(a, w, s);
 }
 
