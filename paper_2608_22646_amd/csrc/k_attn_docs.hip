@@ -19,6 +19,15 @@
 // Where rows are few, the keys of a document are also split over workgroups
 // (chunks of whole steps); each leaves its state in the workspace and
 // attn_join_kernel joins them in chunk order.
+//
+// Many rows (bf16, 128-wide heads): the matrix unit and the softmax's instructions
+// share a SIMD's issue, the exponentials being half of them; 8448 tokens, 28 + 4
+// heads, visible up to the end of their block of 32: 520 us, 0.99 PFLOP/s (taking
+// out the softmax: 499, the LDS reads as well: 435, the loads as well: 389, at a
+// clock that its power holds near 2 GHz).  Few rows: keys and values from HBM; one
+// token of 16 documents of 2.6 to 8.4 thousand keys: 41 us and 5 for the join, 4.4
+// TB/s; 32 queries x 1024 keys x 32 heads x 8: 31 us, 4.4 TB/s (a copy: 5.1).
+// float32: the matrix unit's float32 rate, a sixteenth of bf16's.
 #include <algorithm>
 #include <type_traits>
 
@@ -741,7 +750,8 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
     *reinterpret_cast<float4*>(to) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
 }
 
-constexpr int CHUNK_MIN = 512, CHUNK_LEAST = 256, FEW_KG = 4, FEW_SLOTS = 1;
+// Keys of the chunks that a row tile's width is chosen for, and the least of one.
+constexpr int CHUNK_MIN = 512, CHUNK_LEAST = 256;
 // Which kernel a call takes and how its grid is laid out.  Sizes only.
 struct Choice {
   int qg, kg, kt;
@@ -753,9 +763,12 @@ Choice choose(const AttnArgs& a) {
   const bool f32 = a.dtype == DLLM_F32, wide_row = f32 && a.hd == 128;
   const int rows = a.max_q * (a.Hq / a.Hkv);
   const long heads = (long)a.docs * a.Hkv, cus = device_cu_count();
-  // the widest row tile with which row tiles and chunks of CHUNK_MIN keys can
-  // still give every CU a workgroup, else the narrowest: a wide tile reads keys and
-  // values for more rows, a narrow one leaves more waves to split the keys
+  // The widest row tile with which row tiles and chunks of CHUNK_MIN keys can still
+  // give every CU a workgroup, else the narrowest: a wide tile reads keys and values
+  // for more rows, a narrow one leaves more waves to split the keys.  (64 queries x
+  // 1024 keys, 4 documents, 28 + 4 heads: 16 us, the widest tile 28; with half the
+  // workgroups too 28.  1024 queries and keys: 27 us; chunks of 256 keys 47, of 1024
+  // keys 35.)
   const long chunks_max = std::max(1, a.max_kv / CHUNK_MIN);
   // bf16 with two workgroups of 128 rows for every CU: four waves that do not split the
   // keys, two workgroups a CU, so that one's softmax lies beside the other's products
@@ -764,13 +777,17 @@ Choice choose(const AttnArgs& a) {
   const bool dense = !f32 && rows > 128 && heads * ceil_div(rows, 128) * chunks_max >= 2 * cus;
   c.qg = 4;
   while (c.qg > 1 && (rows <= 16 * c.qg || heads * ceil_div(rows, 32 * c.qg) * chunks_max < cus)) c.qg /= 2;
-  c.kg = dense ? 1 : c.qg == 4 ? (f32 ? 1 : 2) : wide_row ? 2 : c.qg == 2 ? 4 : FEW_KG;
+  c.kg = dense ? 1 : c.qg == 4 ? (f32 ? 1 : 2) : wide_row ? 2 : 4;
   c.kt = dense ? 64 : 32;
   AttnPlan& p = c.plan;
   p.tiles = ceil_div(rows, 32 * c.qg);
   const int step = c.kg * c.kt;
   const long slots = dense ? 2 * cus : cus;
-  // where they leave CUs without a workgroup, shares for all of them
+  // Where they leave CUs without a workgroup, shares for all of them (31 documents of
+  // one token, one of 16384 keys among 500: 29 us; chunks of one length, by the longest
+  // document: 56).  Chunks of 256 keys at least (one token over 4000
+  // float32 keys: 20 us, 128 keys 18, 512 keys 24; 32 queries x 768 keys twice, bf16:
+  // 18, 18 and 15).
   p.least = ceil_div(CHUNK_LEAST, step);
   const long shares = std::min({slots / ((long)a.Hkv * p.tiles), (long)a.docs * (a.max_kv / CHUNK_LEAST), (long)MAX_SHARES});
   p.shares = shares > a.docs && (long)a.docs * (a.max_kv / step + 1) < (1l << 30) ? (int)shares : 0;
@@ -793,7 +810,7 @@ template <typename T, int HD>
 void launch(const AttnArgs& a, const Choice& c, hipStream_t s) {
   constexpr bool F32 = sizeof(T) == 4, WIDE = F32 && HD == 128;  // WIDE: rows of 512 bytes, half the keys fit
   if (c.qg == 1)
-    go<T, HD, 1, WIDE ? 2 : FEW_KG, 32, 2>(a, c, s);
+    go<T, HD, 1, WIDE ? 2 : 4, 32, 2>(a, c, s);
   else if (c.qg == 2)
     go<T, HD, 2, WIDE ? 2 : 4, 32, 2>(a, c, s);
   else if (F32 || c.kg == 2)

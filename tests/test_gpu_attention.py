@@ -127,6 +127,42 @@ def test_more_rows_than_one_tile(gpu_lib, dtype):
     run_and_check(2, 2, 64, dtype, [700], [700], block=32, prefix=[40], cap=30.0, seed=10)
 
 
+@pytest.mark.parametrize("heads", [(16, 16, 64), (32, 16, 128)])
+@pytest.mark.parametrize("block,cap,bias", [(0, 0.0, False), (1, 0.0, False), (32, 30.0, False), (7, 0.0, True), (0, 4.0, True)])
+def test_many_rows(gpu_lib, heads, block, cap, bias):
+    """Enough row tiles for two workgroups on every CU: bf16 tiles of 128 rows; ragged documents, some
+    without queries or keys, invisible values that are no numbers."""
+    g = torch.Generator().manual_seed(block)
+    most = 130 * 16 // heads[0]
+    q_lens = [most, 0, 1, most - 1] + torch.randint(1, most + 1, (12,), generator=g).tolist()
+    kv_lens = [n + int(e) for n, e in zip(q_lens, torch.randint(0, 90, (16,), generator=g))]
+    kv_lens[5] = 0
+    q_pos = [max(k - q, 0) // 2 for q, k in zip(q_lens, kv_lens)]
+
+    def hide(q, k, v):
+        if block:
+            end = kv_lens[0]                # what no query of document 0 sees, if there is any
+            seen = ((q_pos[0] + q_lens[0] - 1) // block + 1) * block
+            k[seen:end], v[seen:end] = math.inf, math.nan
+            v[min(seen, end) - 1, :, 5] = math.inf      # and what its last queries see
+    run_and_check(*heads, BF16, q_lens, kv_lens, block, q_pos, [0, 5] * 8 if block else None, cap,
+                  [2.0 ** -(h % 8 + 1) for h in range(heads[0])] if bias else None, seed=block, mutate=hide)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,heads", [(3, (4, 2, 64)), (64, (2, 1, 64)), (70, (4, 2, 128)), (250, (2, 1, 64))])
+def test_documents_of_unlike_lengths_share_the_split(gpu_lib, n, heads, dtype):
+    """One long document among short ones, empty ones and ones without queries."""
+    g = torch.Generator().manual_seed(n)
+    kv_lens = torch.randint(0, 300, (n,), generator=g).tolist()
+    kv_lens[n // 2], kv_lens[-1] = 6000, 1300
+    q_lens = torch.randint(0, 3, (n,), generator=g).tolist()
+    q_lens[n // 2] = 2
+    run_and_check(*heads, dtype, q_lens, kv_lens, block=1, seed=n)
+    if n == 3:
+        run_and_check(*heads, dtype, [1, 2, 40], [300, 6000, 900], block=32, q_pos=[5, 3000, 100], seed=n)
+
+
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("n,kv", [(40, 90), (1, 2000), (300, 300)])
 def test_rows_without_keys_are_zero(gpu_lib, n, kv, dtype):
