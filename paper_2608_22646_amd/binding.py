@@ -551,17 +551,16 @@ def _column(t, n, dtype, device, name):
     return t.data_ptr()
 
 
-def _rows(t, shape, like, name):
-    """The view of a [B, L, H, hd] tensor whose last dimension is contiguous."""
-    b, l, h, e = t.stride() if t.dim() == 4 else (0, 0, 0, 0)
-    if t.shape != shape or e != 1:
+def _rows(t, shape, dtype, device, name):
+    """The view of a [B, L, H, hd] or [L, H, hd] tensor whose last dimension is contiguous."""
+    st = t.stride()
+    if t.shape != shape or st[-1] != 1 or t.dtype is not dtype or t.device != device:
         _refuse(t.shape == shape, -2, f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
-        _refuse(e == 1 or t.numel() == 0, -2, f"{name}: elements of a head must be contiguous")
-    if t.dtype != like.dtype or t.device != like.device:
-        _refuse(False, -1, f"{name} must be {like.dtype} on {like.device}")
+        _refuse(st[-1] == 1 or t.numel() == 0, -2, f"{name}: elements of a head must be contiguous")
+        _refuse(t.dtype is dtype and t.device == device, -1, f"{name} must be {dtype} on {device}")
     # a dimension of one element is never stepped over: its stride says nothing
-    n = t.shape
-    return View(t.data_ptr(), b if n[0] > 1 else 0, l if n[1] > 1 else n[3], h if n[2] > 1 else 0)
+    return View(t.data_ptr(), st[0] if len(shape) == 4 and shape[0] > 1 else 0, st[-3] if shape[-3] > 1 else shape[-1],
+                st[-2] if shape[-2] > 1 else 0)
 
 
 def _workspace(nbytes, device):
@@ -600,21 +599,23 @@ def rotary(cfg: Rotary, q, k=None, pos=None, pos0=0, q_out=None, k_out=None, inv
     if scope is not None:
         with scope:
             return rotary(cfg, q, k, pos, pos0, q_out, k_out, inverse)
-    dt = _dtype(q, "q")
-    B, L, n_q, hd = q.shape
-    _refuse(hd == cfg.head_dim, -2, f"q has heads of {hd} elements, cfg of {cfg.head_dim}")
-    p = _column(pos, B * L, torch.int32, q.device, "pos")
-    q_out = torch.empty(q.shape, dtype=q.dtype, device=q.device) if q_out is None else q_out
-    vq, vqo = _rows(q, q.shape, q, "q"), _rows(q_out, q.shape, q, "q_out")
+    dt, dtype, dev = _dtype(q, "q"), q.dtype, q.device
+    shape = B, L, n_q, hd = tuple(q.shape)
+    if hd != cfg.head_dim:
+        _refuse(False, -2, f"q has heads of {hd} elements, cfg of {cfg.head_dim}")
+    p = _column(pos, B * L, torch.int32, dev, "pos")
+    q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
+    vq, vqo = _rows(q, shape, dtype, dev, "q"), _rows(q_out, shape, dtype, dev, "q_out")
     vk = vko = None
     n_k = 0
     if k is not None:
         n_k = k.shape[2]
-        k_out = torch.empty(k.shape, dtype=q.dtype, device=q.device) if k_out is None else k_out
         shape = (B, L, n_k, hd)
-        vk, vko = _rows(k, shape, q, "k"), _rows(k_out, shape, q, "k_out")
+        vk = _rows(k, shape, dtype, dev, "k")
+        k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
+        vko = _rows(k_out, shape, dtype, dev, "k_out")
     check(lib().dllm_rotary(cfg.to_c(), dt, B, L, p, pos0, vq, vqo, n_q, vk, vko, n_k, int(bool(inverse)),
-                            _raw_stream(q.device.index)))
+                            _raw_stream(dev.index)))
     return q_out, (k_out if k is not None else None)
 
 
@@ -677,22 +678,19 @@ def attention_workspace_size(q, k, v, docs: Docs | None = None):
 
 
 def _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes):
-    dev = q.device
-    one = q.dim() == 3
-    if one:
-        q, k, v, out = q[None], k[None], v[None], out[None]
-    B, T, Hq, hd = q.shape
-    S, Hkv = k.shape[1], k.shape[2]
-    kv = (B, S, Hkv, hd)
-    views = [_rows(q, q.shape, q, "q"), _rows(k, kv, q, "k"), _rows(v, kv, q, "v"), _rows(out, q.shape, q, "out")]
+    dev, dtype = q.device, q.dtype
+    shape, kv = tuple(q.shape), tuple(k.shape)
+    one = len(shape) == 3
+    T, Hq, hd = shape[-3:]
+    S, Hkv = kv[-3:-1]
+    kv = (S, Hkv, hd) if one else (shape[0], S, Hkv, hd)
+    views = [_rows(q, shape, dtype, dev, "q"), _rows(k, kv, dtype, dev, "k"), _rows(v, kv, dtype, dev, "v"),
+             _rows(out, shape, dtype, dev, "out")]
     arrays = (docs.q_start, docs.q_len, docs.kv_start, docs.kv_len, docs.q_pos, docs.prefix)
     n = docs.count
     if n is None:
-        n = next((t.numel() for t in arrays if t is not None), 1) if one else B
-    _refuse(one or n == B, -2, "a dense batch has one document per slab")
-    if one:
-        for w in views:
-            w.stride_b = 0
+        n = next((t.numel() for t in arrays if t is not None), 1) if one else shape[0]
+    _refuse(one or n == shape[0], -2, "a dense batch has one document per slab")
     ptrs = [_column(t, n, torch.int32, dev, name) for t, name in zip(arrays, _DOC_ARRAYS)]
     return AttnArgs(dt, Hq, Hkv, hd, *views, n, T, S, T if docs.max_q is None else docs.max_q,
                     S if docs.max_kv is None else docs.max_kv, *ptrs, _column(slopes, Hq, torch.float32, dev, "slopes"),
