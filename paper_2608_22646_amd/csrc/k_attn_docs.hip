@@ -275,10 +275,14 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
   const int seen = min(ke, see_last);  // keys that some row of this wave sees
   const bool neg = a.scale < 0.f;      // scores are formed with |scale| and, where it is negative, -q
   const float sc = fabsf(a.scale) * LOG2E;
-  // capped scores: cap in log2 units, 2 log2(e) / cap per unit of score, and the
-  // coefficients of tanh for small ones
-  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f, cap_1 = a.cap > 0.f ? 1.f / cap2 : 0.f, cap_z = cap_1 * cap_1;
-  const float th1 = -0.333313563f * cap_z, th2 = 0.132708743f * cap_z * cap_z, th3 = -0.0475493467f * cap_z * cap_z * cap_z;
+  // capped scores: cap and 1 / cap in log2 units, 2 log2(e) / cap per unit of score,
+  // and for small bf16 ones the coefficients of cap tanh(x / cap) / x in x^2 (in
+  // numbers of any size that a float32 x^2 may meet)
+  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f, cap_1 = a.cap > 0.f ? 1.f / cap2 : 0.f;
+  const float th = sc * cap_1 * (sc * cap_1);
+  const bool series = th <= 1e8f && sc <= 1e6f;
+  const float th0 = 0.999999901f * sc, th1 = -0.333313563f * th * sc, th2 = 0.132708743f * th * th * sc;
+  const float th3 = -0.0475493467f * th * th * th * sc;
   const bool direct = a.cap == 0.f && !a.slopes;
 
   // K and V of this head, as bytes; a tile's buffer starts at its first key
@@ -428,15 +432,15 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
         for (int b = 0; b < NS; ++b)
 #pragma unroll
           for (int r = 0; r < 16; ++r) far = fmaxf(far, fabsf(x[b][r]));
-        if (__ballot(!(far * cap_in <= 0.8f)) == 0ull) {
-          // |x / cap| <= 0.4: tanh(y) = y P(y^2), P of degree 3 to 1e-7 (six
+        if (series && __ballot(!(far * cap_in <= 0.8f)) == 0ull) {
+          // |x / cap| <= 0.4: tanh(y) = y P(y^2), P of degree 3 to 1e-7 (five
           // instructions in place of two transcendental ones and three)
 #pragma unroll
           for (int b = 0; b < NS; ++b)
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
-              const float y = x[b][r] * sc, z = y * y;
-              x[b][r] = y * fmaf(fmaf(fmaf(th3, z, th2), z, th1), z, 0.999999901f);
+              const float z = x[b][r] * x[b][r];
+              x[b][r] *= fmaf(fmaf(fmaf(th3, z, th2), z, th1), z, th0);
             }
         } else {
           // cap tanh(x / cap) = cap - 2 cap / (e^(2 x / cap) + 1), to 1e-7 of the cap
