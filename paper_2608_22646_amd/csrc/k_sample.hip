@@ -640,7 +640,7 @@ struct Picker {
     uint32_t sub_count[NT];
     uint4 few[FEW];
     double powers[STEPS], bufd[NW];
-    uint32_t bufu[NW], a, b, n;
+    uint32_t bufu[NW], first[NW], last[NW], a, b, n;
     int i;
     double m;
   };
@@ -856,12 +856,18 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     if (a.conf) a.conf[row] = conf;
     if (a.prob) a.prob[row] = prob;
   };
+  RowState st{};
+  uint32_t listed = 0;
+  if (c.filter) {  // (early: these loads pass beside the join of the chunks)
+    st = w.state[row];
+    listed = w.listed[row];
+    sh.prefix[tid] = w.prefix[(size_t)row * BINS + tid];
+  }
   fill_powers(sh.powers);
-  if (c.filter) sh.prefix[tid] = w.prefix[(size_t)row * BINS + tid];
   sh.extra[tid] = 0;
   __syncthreads();
   P p{sh, static_cast<const T*>(a.logits) + (long)row * a.row_stride, (const GLOBAL uint2*)w.list + (size_t)row * w.list_len,
-      join_chunks(stat, nch, c, sh.powers, sh.ch), c.rate, V, a.mask_id, 0, RowState{}};
+      join_chunks(stat, nch, c, sh.powers, sh.ch), c.rate, V, a.mask_id, listed, st};
   const RowTop& top = p.top;
   if (top.bad != ~0u || top.big == -INFINITY) {
     if (tid == 0) {
@@ -894,9 +900,6 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     return ((double)top.big - f) * c.inv_t <= reach && (key > cut.key || (key == cut.key && v <= cut.last));
   };
   if (c.filter) {
-    p.st = w.state[row];
-    p.listed = w.listed[row];
-    const RowState& st = p.st;
     const double* prefix = sh.prefix;
     if (p.listed <= P::KEPT)
       for (uint32_t i = tid; i < p.listed; i += NT) sh.list[i] = make_uint2(p.list[i].x, p.list[i].y);
@@ -994,10 +997,6 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     if (past) break;
     sums = from_lane(upto, 63);
   }
-  if (tid == 0) {
-    sh.a = ~0u;
-    sh.b = 0;
-  }
   const bool ranked_cut = c.filter && edge < BINS - 1 && cut.key != 0 && cut.key != ~0u && !(reach < INFINITY);
   const int v0 = at * CHUNK + tid * E;
   float y[E];
@@ -1029,13 +1028,24 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
       if (run > want && mine == ~0u) mine = v0 + i;
     }
   }
-  if (mine != ~0u) atomicMin(&sh.a, mine);
-  if (last) atomicMax(&sh.b, last);
+  mine = wave_all(mine, Min{});
+  last = wave_all(last, Max{});
+  if (lane == 0) {
+    sh.first[wave] = mine;
+    sh.last[wave] = last;
+  }
   __syncthreads();
-  if (tid == 0) {
-    // (rounding inside the chunk: its last kept token)
-    const uint32_t token = min(sh.a != ~0u ? sh.a : sh.b - 1, (uint32_t)V - 1);
-    const float f = to_f(p.x[token]);
+#pragma unroll
+  for (int i = 0; i < NW; ++i) {
+    mine = min(mine, sh.first[i]);
+    last = max(last, sh.last[i]);
+  }
+  // (rounding inside the chunk: its last kept token)
+  const uint32_t token = mine != ~0u ? mine : last - 1;
+  if ((int)token >= v0 && (int)token < v0 + E) {
+    float f = 0.f;
+#pragma unroll
+    for (int i = 0; i < E; ++i) f = v0 + i == (int)token ? y[i] : f;
     answer((int)token, (float)(weight_of(((double)f - top.big) * PER_NAT, sh.powers) / all1), (float)(p.weight(f) / total));
   }
 }
