@@ -278,12 +278,13 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
   // capped scores: cap and 1 / cap in log2 units, 2 log2(e) / cap per unit of score,
   // and for small bf16 ones the coefficients of cap tanh(x / cap) / x in x^2 (in
   // numbers of any size that a float32 x^2 may meet)
-  const float cap2 = a.cap * LOG2E, cap_in = a.cap > 0.f ? 2.f * sc / a.cap : 0.f, cap_1 = a.cap > 0.f ? 1.f / cap2 : 0.f;
+  const bool capped = a.cap > 0.f;
+  const float cap2 = a.cap * LOG2E, cap_in = capped ? fminf(2.f * sc / a.cap, 3e38f) : 0.f, cap_1 = capped ? fminf(1.f / cap2, 3e38f) : 0.f;
   const float th = sc * cap_1 * (sc * cap_1);
   const bool series = th <= 1e8f && sc <= 1e6f;
   const float th0 = 0.999999901f * sc, th1 = -0.333313563f * th * sc, th2 = 0.132708743f * th * th * sc;
   const float th3 = -0.0475493467f * th * th * th * sc;
-  const bool direct = a.cap == 0.f && !a.slopes;
+  const bool direct = !capped && !a.slopes;
 
   // K and V of this head, as bytes; a tile's buffer starts at its first key
   const char* kp = uniform(static_cast<const char*>(a.k.data) +
@@ -412,7 +413,7 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
   // Scores as they are in log2 units: scaled, capped, biased, masked (t0: the
   // tile's first key; whole: every row of the wave sees all of it), and their maximum.
   auto shape = [&](f32x16_t (&x)[NS], int t0, bool whole) {
-    if (a.cap > 0.f) {
+    if (capped) {
       if constexpr (!BF) {
         // float32: tanh(y) = y + y z Q(z), z = y^2, Q of degree 4, for |y| <= 0.6, so
         // that small scores keep 1e-7 of themselves (the form by exponentials: of the

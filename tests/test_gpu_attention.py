@@ -31,8 +31,9 @@ def tolerance(ref, mass, top, dot, n, hd, dtype, scale, cap):
 
 
 def run_and_check(Hq, Hkv, hd, dtype, q_lens, kv_lens, block=0, q_pos=None, prefix=None, cap=0.0, slopes=None, scale=None,
-                  seed=0, std=1.3, pad=3, mutate=None):
-    """Packed documents (pad rows behind the last one); mutate(q, k, v) changes the inputs first."""
+                  seed=0, std=1.3, pad=3, mutate=None, acts_as=None):
+    """Packed documents (pad rows behind the last one); mutate(q, k, v) changes the inputs first;
+    acts_as: the cap that the oracle takes instead."""
     T, S = sum(q_lens), sum(kv_lens)
     say(f"attention {Hq}/{Hkv}x{hd} {dtype} q{q_lens} kv{kv_lens} block {block} pos {q_pos} prefix {prefix} cap {cap} "
         f"slopes {slopes is not None}")
@@ -46,7 +47,7 @@ def run_and_check(Hq, Hkv, hd, dtype, q_lens, kv_lens, block=0, q_pos=None, pref
     got = B.attention(q, k, v, docs, block=block, cap=cap, slopes=sl, scale=scale, out=out)
     torch.cuda.synchronize()
     assert got is out and torch.equal(out[T:], behind)
-    verify(got, q, k, v, q_lens, kv_lens, block, q_pos, prefix, cap, None if slopes is None else np.float32(slopes), scale,
+    verify(got, q, k, v, q_lens, kv_lens, block, q_pos, prefix, cap if acts_as is None else acts_as, None if slopes is None else np.float32(slopes), scale,
            dtype)
     return got
 
@@ -218,6 +219,16 @@ def test_extreme_scores(gpu_lib, dtype):
         q[2, 1] = math.nan
     got = run_and_check(2, 2, 64, dtype, [40], [40], block=1, seed=9, mutate=nan_query)
     assert torch.isnan(got[2, 1].float()).all() and torch.isfinite(got[2, 0].float()).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("cap", [1e-40, 1e-20, 1e30])
+def test_caps_of_any_size(gpu_lib, cap, dtype):
+    """A cap that leaves nothing of the scores, or all; some scores are 0."""
+    def zero(q, k, v):
+        q[3] = 0
+        k[20] = 0
+    run_and_check(4, 2, 64, dtype, [40], [70], cap=cap, seed=11, mutate=zero, acts_as=0.0 if cap > 1 else None)
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
