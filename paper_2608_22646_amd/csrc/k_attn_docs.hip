@@ -318,6 +318,8 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     }
   };
   const int nsteps = ke > kb ? (ke - kb + KG * KT - 1) / (KG * KT) : 0;
+  constexpr int D = S - 1;  // stages in flight behind the one in use
+  for (int u = 0; u < D && u < nsteps; ++u) load(u, u);
 
   // Q operand: the lane's rows, dims 16 ks + 8 half .. (bf16), 8 c + 4 half .. (float32)
   constexpr int NQ = BF ? HD / 16 : HD / 8;
@@ -586,8 +588,6 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     }
     if constexpr (QG > 1) __syncthreads();
   };
-  constexpr int D = S - 1;  // stages in flight behind the one in use
-  for (int u = 0; u < D && u < nsteps; ++u) load(u, u);
   for (int u = 0; u < nsteps; ++u) {
     if (u + D <= nsteps)
       wait_vmcnt<PER*(D - 1)>();

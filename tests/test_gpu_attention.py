@@ -47,8 +47,8 @@ def run_and_check(Hq, Hkv, hd, dtype, q_lens, kv_lens, block=0, q_pos=None, pref
     got = B.attention(q, k, v, docs, block=block, cap=cap, slopes=sl, scale=scale, out=out)
     torch.cuda.synchronize()
     assert got is out and torch.equal(out[T:], behind)
-    verify(got, q, k, v, q_lens, kv_lens, block, q_pos, prefix, cap if acts_as is None else acts_as, None if slopes is None else np.float32(slopes), scale,
-           dtype)
+    verify(got, q, k, v, q_lens, kv_lens, block, q_pos, prefix, cap if acts_as is None else acts_as,
+           None if slopes is None else np.float32(slopes), scale, dtype)
     return got
 
 
