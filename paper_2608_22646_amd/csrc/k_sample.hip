@@ -19,10 +19,18 @@
 //
 // Calls without top-k, top-p and min-p need the first and the last alone.
 //
+// Many rows: the first kernel is bound by the float64 weights and the classes' LDS
+// additions (256 rows x 152064 float32: 47 us, 3.3 TB/s; without the additions 20 us
+// less, without the weights 13), the collection by HBM (31 us, 5 TB/s, where every
+// chunk has members); few rows by the latency of four dependent launches (1 row x
+// 126464: 28 us; 5.7, 6.2, 4.5 and 12).  A chunk is 8192 logits in 512 threads' registers:
+// 19 chunks of a vocabulary of 152064 let one row use 19 CUs; a workgroup that kept its
+// place over chunks had half the waves a CU (70 us against 52).
+//
 // Which token wins must not depend on rounding or on the order of execution.
 // Weights are float64 throughout; where threads add concurrently they add whole
-// numbers (a weight in units of 2^-36 of its chunk's largest, 2^-40 of its
-// class's), so every sum is the same in any order and good to about 1e-12.
+// numbers (a weight in units of 2^-40 of its class's), so every sum is the same in
+// any order and good to about 1e-12.
 #include <algorithm>
 #include <type_traits>
 
@@ -82,14 +90,24 @@ __device__ __forceinline__ double power_of(double d, const double* powers) {
 // The same for any d <= 0 (2^-1000 for what lies below, and for NaN: -inf at an
 // infinite temperature).
 __device__ __forceinline__ double weight_of(double d, const double* powers) { return power_of(fmax(d, -8000.0), powers); }
-// What a class sums up, in one word: the count of its logits (at most CHUNK =
-// 2^13) from bit 50 on, their weights (each at most 1) as whole numbers of 2^-36
-// below: the mantissa of 2^16 + w.
+// What a class sums up, in one word.  A logit at a distance of f classes, |f| <= 1/2,
+// from its class's centre weighs v = 2^(f / 8) of the centre's weight: by the Taylor
+// polynomial of degree 6, whose remainder is 6e-14.  The count of the logits (at most
+// CHUNK = 2^13) stands from bit 50 on, below it the sum of their v - 15/16 (each below
+// 1/8) in whole numbers of 2^-40: the mantissa of 2^12 + 1/16 + (v - 1).
 constexpr int COUNT_BIT = 50;
-__device__ __forceinline__ uint64_t class_word(double w) {
-  return __double_as_longlong(65536.0 + w) - (0x40f0000000000000ull - (1ull << COUNT_BIT));
+__device__ __forceinline__ uint64_t class_word(double f) {
+  constexpr double L = 0.08664339756999316;  // ln 2 / 8
+  double p = fma(L * L * L * L * L * L / 720, f, L * L * L * L * L / 120);
+  p = fma(p, f, L * L * L * L / 24);
+  p = fma(p, f, L * L * L / 6);
+  p = fma(p, f, L * L / 2);
+  p = fma(p, f, L);
+  return __double_as_longlong(fma(p, f, 4096.0625)) - (0x40b0000000000000ull - (1ull << COUNT_BIT));
 }
-__device__ __forceinline__ double class_mass(uint64_t word) { return (double)(word & ((1ull << COUNT_BIT) - 1)) * 0x1p-36; }
+// The mass, of the centre's weight, of `count` logits whose words' lower parts sum up to `low`.
+__device__ __forceinline__ double class_mass(uint64_t low, uint32_t count) { return (double)low * 0x1p-40 + count * 0.9375; }
+__device__ __forceinline__ uint64_t low_of(uint64_t word) { return word & ((1ull << COUNT_BIT) - 1); }
 
 // A lane's value moved within the wave by CTRL (a data-parallel primitive, a few
 // cycles where a shuffle through LDS takes a hundred); `old` where none arrives.
@@ -283,7 +301,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
   SL slice;
   if (whole) slice.fetch(x, v0);
   const Controls c = controls_of(a, row);
-  fill_powers(powers);
+  if (!c.filter) fill_powers(powers);
   classes[tid] = 0;
   float f[RUNS][N];
   slice.take(x, v0, whole, a.vocab, a.mask_id, f);
@@ -349,18 +367,21 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
       const double least = qtop - 600.0;
 #pragma unroll
       for (int i = 0; i < RUNS; ++i) {
-        double q[N];
+        double q[N], t[N];
         int b[N];
         u64 u[N];
 #pragma unroll
-        for (int e = 0; e < N; ++e) q[e] = fmax(in_classes(f[i][e], c.rate), least);
+        for (int e = 0; e < N; ++e) {
+          q[e] = fmax(in_classes(f[i][e], c.rate), least);
+          t[e] = q[e] + 0x1.8p52;
+        }
 #pragma unroll
         for (int e = 0; e < N; ++e) {
-          b[e] = base_i - __double2loint(q[e] + 0x1.8p52);
+          b[e] = base_i - __double2loint(t[e]);
           b[e] = b[e] < BINS - 1 ? b[e] : BINS + lane;
         }
 #pragma unroll
-        for (int e = 0; e < N; ++e) u[e] = class_word(power_of(q[e] - qtop, powers));
+        for (int e = 0; e < N; ++e) u[e] = class_word(q[e] - (t[e] - 0x1.8p52));
 #pragma unroll
         for (int e = 0; e < N; ++e) atomicAdd(classes + b[e], u[e]);
       }
@@ -372,7 +393,7 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
         for (int j = 0; j < E; ++j) y = j == i ? f[j / N][j % N] : y;
         const double q = in_classes(y, c.rate);
         const int b = (int)fmin(base - rint(q), (double)BINS);
-        if (b < BINS - 1) atomicAdd(classes + b, class_word(weight_of(q - qtop, powers)));
+        if (b < BINS - 1) atomicAdd(classes + b, class_word(q - rint(q)));
       }
     }
   }
@@ -467,7 +488,7 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   }
   __syncthreads();
   const GLOBAL u64* hm = (const GLOBAL u64*)w.classes + (size_t)row * nch * BINS;
-  double m = 0;
+  u64 low = 0;
   uint32_t n = 0;
   constexpr int U = 8;
   for (int i0 = 0; i0 < nch; i0 += U) {
@@ -483,11 +504,11 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
 #pragma unroll
     for (int j = 0; j < U; ++j)
       if (in[j]) {
-        m += class_mass(um[j]) * ch.fac[i0 + j];
+        low += low_of(um[j]);
         n += (uint32_t)(um[j] >> COUNT_BIT);
       }
   }
-  m = block_scan(m, bufd);
+  double m = block_scan(class_mass(low, n) * weight_of(top.base - top.qtop - tid, powers), bufd);
   n = block_scan(n, bufu);
   binw[tid] = m;
   binc[tid] = n;
@@ -634,7 +655,7 @@ struct Picker {
     Chunks ch;
     double part[MAX_CHUNKS];  // kept mass of a chunk
     u64 extra[MAX_CHUNKS];
-    double prefix[BINS];
+    double prefix[BINS], centre[BINS];  // mass up to a class; weight of its centre
     uint2 list[KEPT];  // the row's list, where it fits
     u64 sub_mass[NT];
     uint32_t sub_count[NT];
@@ -901,6 +922,7 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
   };
   if (c.filter) {
     const double* prefix = sh.prefix;
+    sh.centre[tid] = weight_of(top.base - top.qtop - tid, sh.powers);
     if (p.listed <= P::KEPT)
       for (uint32_t i = tid; i < p.listed; i += NT) sh.list[i] = make_uint2(p.list[i].x, p.list[i].y);
     __syncthreads();
@@ -949,23 +971,26 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
     const GLOBAL u64* h = (const GLOBAL u64*)w.classes + (size_t)row * nch * BINS;
     constexpr int U = 4;  // chunks of a wave at a time
     for (int i0 = wave; i0 < nch; i0 += NW * U) {
-      u64 s[U];
+      double s[U];
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         const int i = i0 + j * NW;
         // classes of the chunk before the edge
-        const int end = i < nch ? min(edge, BINS - 1) - sh.ch.shift[min(i, nch - 1)] : 0;
+        const int shift = sh.ch.shift[min(i, nch - 1)], end = i < nch ? min(edge, BINS - 1) - shift : 0;
         s[j] = 0;
 #pragma unroll
         for (int k = 0; k < BINS / 64; ++k) {
           const int at = k * 64 + lane;
-          if (at < end) s[j] += h[(size_t)i * BINS + at] & ((1ull << COUNT_BIT) - 1);
+          if (at < end) {
+            const u64 word = h[(size_t)i * BINS + at];
+            s[j] += class_mass(low_of(word), (uint32_t)(word >> COUNT_BIT)) * sh.centre[at + shift];
+          }
         }
       }
 #pragma unroll
       for (int j = 0; j < U; ++j) {
         s[j] = wave_all(s[j], Sum{});
-        if (lane == 0 && i0 + j * NW < nch) sh.part[i0 + j * NW] = (double)s[j] * 0x1p-36 * sh.ch.fac[i0 + j * NW];
+        if (lane == 0 && i0 + j * NW < nch) sh.part[i0 + j * NW] = s[j];
       }
     }
     __syncthreads();
