@@ -20,10 +20,9 @@
 // Calls without top-k, top-p and min-p need the first and the last alone.
 //
 // Many rows: the first kernel is bound by the float64 weights and the classes' LDS
-// additions (256 rows x 152064 float32: 47 us, 3.3 TB/s; without the additions 20 us
-// less, without the weights 13), the collection by HBM (31 us, 5 TB/s, where every
-// chunk has members); few rows by the latency of four dependent launches (1 row x
-// 126464: 28 us; 5.7, 6.2, 4.5 and 12).  A chunk is 8192 logits in 512 threads' registers:
+// additions (256 rows x 152064 float32: 44 us, 3.6 TB/s; with weights by a table 52),
+// the collection by HBM (31 us, 5 TB/s, where every chunk has members); few rows by the
+// latency of four dependent launches (1 row x 126464: 29 us; 5.0, 6.7, 4.2 and 12.5).  A chunk is 8192 logits in 512 threads' registers:
 // 19 chunks of a vocabulary of 152064 let one row use 19 CUs; a workgroup that kept its
 // place over chunks had half the waves a CU (70 us against 52).
 //
