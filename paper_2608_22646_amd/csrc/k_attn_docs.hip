@@ -700,17 +700,28 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
   const int h = (int)(row % a.Hq);
   const long dt = row / a.Hq;
   const int t = (int)(dt % a.max_q), dn = (int)(dt / a.max_q);
+  const int4 w4 = p.table[dn];
   const Doc d = doc_of(a, dn);
   if (t >= d.nq) return;
   // its document's chunks of which it sees a key; its tile ran them all
-  const int4 w4 = p.table[dn];
   const int n = w4.z > 0 ? min(w4.y, (sees(a, d, t) + w4.z - 1) / w4.z) : 0;
   const size_t next = (size_t)a.max_q * a.Hq, at = w4.x * next + (size_t)t * a.Hq + h;
   const float2* ml = p.part_ml + at;
   const int e = lane % LPC * 4, side = lane / LPC;
   const float* part = p.part + at * HD + e;
+  constexpr int EARLY = 4;  // outputs asked for beside the first maxima and sums
+  float4 early[EARLY];
+#pragma unroll
+  for (int j = 0; j < EARLY; ++j)
+    early[j] = j * SIDE + side < n ? *reinterpret_cast<const float4*>(part + (j * SIDE + side) * next * HD) : make_float4(0.f, 0.f, 0.f, 0.f);
   float m = -INFINITY, l = 0.f;
   float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+  auto add = [&](const float4& w, float f) {
+    o.x += w.x * f;
+    o.y += w.y * f;
+    o.z += w.z * f;
+    o.w += w.w * f;
+  };
   for (int c0 = 0; c0 < n; c0 += 64) {  // 64 chunks at a time, on the maximum so far
     float2 s = make_float2(-INFINITY, 0.f);
     if (c0 + lane < n) s = ml[(c0 + lane) * next];
@@ -726,17 +737,19 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
     o.z *= f0;
     o.w *= f0;
     const int here = min(64, n - c0);
+    if (c0 == 0) {
+#pragma unroll
+      for (int j = 0; j < EARLY; ++j) {
+        const float fc = __shfl(f, j * SIDE + side, 64);
+        if (j * SIDE + side < here) add(early[j], fc);
+      }
+    }
 #pragma unroll 4
-    for (int i = 0; i < here; i += SIDE) {
+    for (int i = c0 == 0 ? EARLY * SIDE : 0; i < here; i += SIDE) {
       const int c = min(i + side, here - 1);
       const float fc = __shfl(f, c, 64);
       const float4 w = *reinterpret_cast<const float4*>(part + (c0 + c) * next * HD);
-      if (i + side < here) {
-        o.x += w.x * fc;
-        o.y += w.y * fc;
-        o.z += w.z * fc;
-        o.w += w.w * fc;
-      }
+      if (i + side < here) add(w, fc);
     }
   }
 #pragma unroll
