@@ -688,14 +688,15 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
 #endif
 }
 
-// Joins a row's chunk states in chunk order: a wave per row, its lanes first a
+// Joins a row's chunk states in a fixed order: W waves per row, their lanes first a
 // chunk's (maximum, sum) each, then 16 bytes of output each, in HD / 4 lanes per
-// chunk, 256 / HD chunks side by side.
-template <typename T, int HD>
+// chunk, W 256 / HD chunks side by side.
+template <typename T, int HD, int W>
 __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) {
-  constexpr int LPC = HD / 4, SIDE = 64 / LPC;  // lanes per chunk, chunks side by side
-  const int lane = threadIdx.x & 63;
-  const long row = (long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  constexpr int LPC = HD / 4, SIDE = 64 / LPC * W;  // lanes per chunk, chunks side by side
+  __shared__ float4 sums[W > 1 ? W - 1 : 1][LPC];
+  const int lane = threadIdx.x & 63, wave = (threadIdx.x >> 6) % W;  // of the row
+  const long row = ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) / W;
   if (row >= (long)a.docs * a.max_q * a.Hq) return;
   const int h = (int)(row % a.Hq);
   const long dt = row / a.Hq;
@@ -707,7 +708,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
   const int n = w4.z > 0 ? min(w4.y, (sees(a, d, t) + w4.z - 1) / w4.z) : 0;
   const size_t next = (size_t)a.max_q * a.Hq, at = w4.x * next + (size_t)t * a.Hq + h;
   const float2* ml = p.part_ml + at;
-  const int e = lane % LPC * 4, side = lane / LPC;
+  const int e = lane % LPC * 4, side = wave * (64 / LPC) + lane / LPC;
   const float* part = p.part + at * HD + e;
   constexpr int EARLY = 4;  // outputs asked for beside the first maxima and sums
   float4 early[EARLY];
@@ -758,6 +759,13 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
     o.y += __shfl_xor(o.y, x, 64);
     o.z += __shfl_xor(o.z, x, 64);
     o.w += __shfl_xor(o.w, x, 64);
+  }
+  if constexpr (W > 1) {
+    if (wave > 0 && lane < LPC) sums[wave - 1][lane] = o;
+    __syncthreads();
+    if (side > 0) return;
+#pragma unroll
+    for (int i = 0; i < W - 1; ++i) add(sums[i][lane], 1.f);
   }
   if (side > 0) return;
   const float inv = l == 0.f ? 0.f : 1.f / l;
@@ -836,8 +844,14 @@ void launch(const AttnArgs& a, const Choice& c, hipStream_t s) {
   else if constexpr (!F32)
     go<T, HD, 4, 1, 64, 2>(a, c, s);
   if (c.plan.shares > 0) {
+    // four waves a row while that is at most sixteen a CU (28 heads' token over 8448 keys:
+    // 17 us, one wave a row 21; 31 documents, one of them long: 24 and 28; 40: 45 and 44;
+    // 32 queries of ten: 43 and 32)
     const long rows = (long)a.docs * a.max_q * a.Hq;
-    attn_join_kernel<T, HD><<<ceil_div(rows, 4), 256, 0, s>>>(a, c.plan);
+    if (rows <= 4l * device_cu_count())
+      attn_join_kernel<T, HD, 4><<<(unsigned)rows, 256, 0, s>>>(a, c.plan);
+    else
+      attn_join_kernel<T, HD, 1><<<ceil_div(rows, 4), 256, 0, s>>>(a, c.plan);
     DLLM_LAUNCH_CHECK("attn_join_kernel");
   }
 }
