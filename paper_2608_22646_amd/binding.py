@@ -563,6 +563,13 @@ def _rows(t, shape, dtype, device, name):
                 st[-2] if shape[-2] > 1 else 0)
 
 
+def _new_rows(like, shape):
+    """A new tensor of a [B, L, H, hd] shape, of like's type, and its view."""
+    t = torch.empty_like(like, memory_format=torch.contiguous_format)
+    n = shape[2] * shape[3]
+    return t, View(t.data_ptr(), shape[1] * n, n, shape[3])
+
+
 def _workspace(nbytes, device):
     """A 256-byte aligned buffer (torch's own allocations are)."""
     buf = torch.empty(nbytes, dtype=torch.uint8, device=device)
@@ -604,16 +611,19 @@ def rotary(cfg: Rotary, q, k=None, pos=None, pos0=0, q_out=None, k_out=None, inv
     if hd != cfg.head_dim:
         _refuse(False, -2, f"q has heads of {hd} elements, cfg of {cfg.head_dim}")
     p = _column(pos, B * L, torch.int32, dev, "pos")
-    q_out = torch.empty_like(q, memory_format=torch.contiguous_format) if q_out is None else q_out
-    vq, vqo = _rows(q, shape, dtype, dev, "q"), _rows(q_out, shape, dtype, dev, "q_out")
-    vk = vko = None
-    n_k = 0
+    vq, vk, vko, n_k = _rows(q, shape, dtype, dev, "q"), None, None, 0
+    if q_out is None:
+        q_out, vqo = _new_rows(q, shape)
+    else:
+        vqo = _rows(q_out, shape, dtype, dev, "q_out")
     if k is not None:
         n_k = k.shape[2]
         shape = (B, L, n_k, hd)
         vk = _rows(k, shape, dtype, dev, "k")
-        k_out = torch.empty_like(k, memory_format=torch.contiguous_format) if k_out is None else k_out
-        vko = _rows(k_out, shape, dtype, dev, "k_out")
+        if k_out is None:
+            k_out, vko = _new_rows(k, shape)
+        else:
+            vko = _rows(k_out, shape, dtype, dev, "k_out")
     check(lib().dllm_rotary(cfg.to_c(), dt, B, L, p, pos0, vq, vqo, n_q, vk, vko, n_k, int(bool(inverse)),
                             _raw_stream(dev.index)))
     return q_out, (k_out if k is not None else None)
