@@ -17,7 +17,8 @@
 //     members, the kept mass of each chunk, and the chunk and then the token where
 //     the running sum of kept weights, in index order, passes u times its total.
 //
-// Calls without top-k, top-p and min-p need the first and the last alone.
+// Calls without top-k, top-p and min-p need the first and the last alone; few rows of
+// one chunk run all of them in one launch (sample_row_kernel).
 //
 // Many rows: the first kernel is bound by the float64 weights and the classes' LDS
 // additions (256 rows x 152064 float32: 44 us, 3.6 TB/s; with weights by a table 52),
@@ -284,23 +285,27 @@ struct Slice {
   }
 };
 
+struct ChunkShared {
+  u64 classes[BINS + 64];  // 64 places for what has no class
+  double powers[STEPS], sum[NW], sum1[NW];
+  float top[NW];
+  uint32_t bad[NW], arg[NW];
+};
+// Chunk `block % chunks` of row `block / chunks`.
 template <typename T>
-__global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs w) {
+__device__ __forceinline__ void chunk_phase(const SampleArgs& a, const SampleWs& w, int block, ChunkShared& sh) {
   typedef Slice<T> SL;
   constexpr int N = SL::N, RUNS = SL::RUNS;
-  __shared__ u64 classes[BINS + 64];  // 64 places for what has no class
-  __shared__ double powers[STEPS];
-  __shared__ float s_top[NW];
-  __shared__ uint32_t s_bad[NW], s_arg[NW];
-  __shared__ double s_sum[NW], s_sum1[NW];
+  u64* const classes = sh.classes;
+  const double* const powers = sh.powers;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int row = blockIdx.x / w.chunks, v0 = blockIdx.x % w.chunks * CHUNK;
+  const int row = block / w.chunks, v0 = block % w.chunks * CHUNK;
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
   const bool whole = v0 + CHUNK <= a.vocab;
   SL slice;
   if (whole) slice.fetch(x, v0);
   const Controls c = controls_of(a, row);
-  if (!c.filter) fill_powers(powers);
+  if (!c.filter) fill_powers(sh.powers);
   classes[tid] = 0;
   float f[RUNS][N];
   slice.take(x, v0, whole, a.vocab, a.mask_id, f);
@@ -323,16 +328,16 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
   top = wave_all(top, Max{});
   bad = wave_all(bad, Min{});
   if (lane == 0) {
-    s_top[wave] = top;
-    s_bad[wave] = bad;
+    sh.top[wave] = top;
+    sh.bad[wave] = bad;
   }
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < NW; ++i) {
-    top = fmaxf(top, s_top[i]);
-    bad = min(bad, s_bad[i]);
+    top = fmaxf(top, sh.top[i]);
+    bad = min(bad, sh.bad[i]);
   }
-  ChunkStat* out = w.stat + blockIdx.x;
+  ChunkStat* out = w.stat + block;
   if (bad != ~0u || top == -INFINITY) {  // the row is decided, or no candidate here
     if (tid == 0) *out = ChunkStat{top, bad, ~0u, 0, 0.0, 0.0};
     return;
@@ -400,21 +405,26 @@ __global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs
   if (!c.filter) sum = wave_all(sum, Sum{});
   const double d1 = wave_all((double)sum1, Sum{});
   if (lane == 0) {
-    s_arg[wave] = arg;
-    s_sum[wave] = sum;
-    s_sum1[wave] = d1;
+    sh.arg[wave] = arg;
+    sh.sum[wave] = sum;
+    sh.sum1[wave] = d1;
   }
   __syncthreads();
   if (tid == 0) {
     ChunkStat s{top, bad, ~0u, 0, 0.0, 0.0};
     for (int i = 0; i < NW; ++i) {
-      s.arg = min(s.arg, s_arg[i]);
-      s.sum += s_sum[i];
-      s.sum1 += s_sum1[i];
+      s.arg = min(s.arg, sh.arg[i]);
+      s.sum += sh.sum[i];
+      s.sum1 += sh.sum1[i];
     }
     *out = s;
   }
-  if (c.filter) w.classes[(size_t)blockIdx.x * BINS + tid] = classes[tid];
+  if (c.filter) w.classes[(size_t)block * BINS + tid] = classes[tid];
+}
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_chunk_kernel(SampleArgs a, SampleWs w) {
+  __shared__ ChunkShared sh;
+  chunk_phase<T>(a, w, blockIdx.x, sh);
 }
 
 // Inclusive scan over the workgroup's threads.
@@ -466,17 +476,22 @@ __device__ __forceinline__ RowTop join_chunks(const ChunkStat* stat, int nch, co
   return r;
 }
 
-__global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs w) {
-  __shared__ Chunks ch;
-  __shared__ double powers[STEPS], binw[BINS], bufd[NW];
-  __shared__ uint32_t binc[BINS], bufu[NW];
-  __shared__ int s_k, s_lo, s_hi;
-  const int tid = threadIdx.x, row = blockIdx.x, nch = w.chunks;
+struct EdgeShared {
+  Chunks ch;
+  double powers[STEPS], binw[BINS], bufd[NW];
+  uint32_t binc[BINS], bufu[NW];
+  int k, lo, hi;
+};
+__device__ __forceinline__ void edge_phase(const SampleArgs& a, const SampleWs& w, int row, EdgeShared& sh) {
+  Chunks& ch = sh.ch;
+  double *const powers = sh.powers, *const binw = sh.binw, *const bufd = sh.bufd;
+  uint32_t *const binc = sh.binc, *const bufu = sh.bufu;
+  const int tid = threadIdx.x, nch = w.chunks;
   const Controls c = controls_of(a, row);
   if (!c.filter) return;
   fill_powers(powers);
   if (tid == 0) {
-    s_k = s_lo = s_hi = -1;
+    sh.k = sh.lo = sh.hi = -1;
     w.listed[row] = 0;
   }
   __syncthreads();
@@ -516,9 +531,9 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   RowState st{BINS, 0, 0, -1, -1, 0, -1, -1, -1, 0.f, 0.f, top.base};
   double least = binw[BINS - 2], most = least;  // bounds of the mass that top-p is a share of
   if (c.top_k) {
-    if (tid < BINS - 1 && n >= (uint32_t)c.top_k && (tid == 0 || binc[tid - 1] < (uint32_t)c.top_k)) s_k = tid;
+    if (tid < BINS - 1 && n >= (uint32_t)c.top_k && (tid == 0 || binc[tid - 1] < (uint32_t)c.top_k)) sh.k = tid;
     __syncthreads();
-    const int b = s_k;
+    const int b = sh.k;
     if (b >= 0) {
       most = least = binw[b];
       st.ek = b + 1;
@@ -533,12 +548,12 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
     const double t0 = fmax(c.top_p * least * (1.0 - 1e-9), 0.0), t1 = fmax(c.top_p * most * (1.0 + 1e-9), 0.0);
     if (tid < BINS - 1) {
       const double before = tid ? binw[tid - 1] : -1.0;
-      if (m >= t0 && before < t0) s_lo = tid;
-      if (m >= t1 && before < t1) s_hi = tid;
+      if (m >= t0 && before < t0) sh.lo = tid;
+      if (m >= t1 && before < t1) sh.hi = tid;
     }
     __syncthreads();
-    st.lo = max(s_lo, 0);
-    st.hi = min(s_hi >= 0 ? s_hi : BINS - 2, edge - 1);
+    st.lo = max(sh.lo, 0);
+    st.hi = min(sh.hi >= 0 ? sh.hi : BINS - 2, edge - 1);
     edge = min(edge, st.hi + 1);
   }
   if (c.min_p > 0.0) {
@@ -590,13 +605,21 @@ __global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs 
   }
 }
 
+__global__ void __launch_bounds__(NT) sample_edge_kernel(SampleArgs a, SampleWs w) {
+  __shared__ EdgeShared sh;
+  edge_phase(a, w, blockIdx.x, sh);
+}
+
+struct CollectShared {
+  uint32_t n[NW], at;
+};
+// Members of chunk `block % chunks` of row `block / chunks`.
 template <typename T>
-__global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, SampleWs w) {
-  __shared__ uint32_t s_n[NW], s_at;
+__device__ __forceinline__ void collect_phase(const SampleArgs& a, const SampleWs& w, int block, CollectShared& sh) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int row = blockIdx.x / w.chunks, chunk = blockIdx.x % w.chunks, v0 = chunk * CHUNK;
+  const int row = block / w.chunks, chunk = block % w.chunks, v0 = chunk * CHUNK;
   const Controls c = controls_of(a, row);
-  if (!c.filter || !w.holds[blockIdx.x]) return;
+  if (!c.filter || !w.holds[block]) return;
   const RowState st = w.state[row];
   const T* x = static_cast<const T*>(a.logits) + (long)row * a.row_stride;
   constexpr int N = 16 / sizeof(T), RUNS = E / N;
@@ -614,19 +637,24 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
         hit |= (uint32_t)st.lists(class_of(f[i][e], c.rate, st.base)) << (i * N + e);
   // places in the row's list: one reservation per workgroup
   const uint32_t n = __popc(hit), incl = wave_upto(n, Sum{});
-  if (lane == 63) s_n[wave] = incl;
+  if (lane == 63) sh.n[wave] = incl;
   __syncthreads();
   if (tid == 0) {
     uint32_t all = 0;
     for (int i = 0; i < NW; ++i) {
-      const uint32_t k = s_n[i];
-      s_n[i] = all;
+      const uint32_t k = sh.n[i];
+      sh.n[i] = all;
       all += k;
     }
-    s_at = all ? atomicAdd(w.listed + row, all) : 0;
+    if (w.chunks == 1) {  // (no other workgroup adds members)
+      w.listed[row] = all;
+      sh.at = 0;
+    } else {
+      sh.at = all ? atomicAdd(w.listed + row, all) : 0;
+    }
   }
   __syncthreads();
-  uint32_t at = s_at + s_n[wave] + incl - n;
+  uint32_t at = sh.at + sh.n[wave] + incl - n;
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
@@ -637,6 +665,12 @@ __global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, Sample
               make_uint2(key_of(f[i][e]), (uint32_t)(v0 + (i * NT + tid) * N + e) | (uint32_t)class_of(f[i][e], c.rate, st.base) << INDEX_BITS);
         ++at;
       }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_collect_kernel(SampleArgs a, SampleWs w) {
+  __shared__ CollectShared sh;
+  collect_phase<T>(a, w, blockIdx.x, sh);
 }
 
 // A class's members up to a boundary: those with a key above `key`, and those
@@ -864,11 +898,10 @@ struct Picker {
 };
 
 template <typename T>
-__global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs w) {
+__device__ __forceinline__ void pick_phase(const SampleArgs& a, const SampleWs& w, int row, typename Picker<T>::Shared& sh) {
   typedef Picker<T> P;
-  __shared__ typename P::Shared sh;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int row = blockIdx.x, nch = w.chunks, V = a.vocab;
+  const int nch = w.chunks, V = a.vocab;
   const ChunkStat* stat = w.stat + (size_t)row * nch;
   const Controls c = controls_of(a, row);
   auto answer = [&](int token, float conf, float prob) {
@@ -1074,6 +1107,32 @@ __global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs 
   }
 }
 
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_pick_kernel(SampleArgs a, SampleWs w) {
+  __shared__ typename Picker<T>::Shared sh;
+  pick_phase<T>(a, w, blockIdx.x, sh);
+}
+
+// All four for rows of one chunk: a workgroup's own stores are there after a barrier.
+template <typename T>
+__global__ void __launch_bounds__(NT) sample_row_kernel(SampleArgs a, SampleWs w) {
+  __shared__ union Shared {
+    ChunkShared chunk;
+    EdgeShared edge;
+    CollectShared collect;
+    typename Picker<T>::Shared pick;
+  } sh;
+  chunk_phase<T>(a, w, blockIdx.x, sh.chunk);
+  __syncthreads();
+  if (a.top_k || a.top_p || a.min_p) {
+    edge_phase(a, w, blockIdx.x, sh.edge);
+    __syncthreads();
+    collect_phase<T>(a, w, blockIdx.x, sh.collect);
+    __syncthreads();
+  }
+  pick_phase<T>(a, w, blockIdx.x, sh.pick);
+}
+
 int chunks_of(int vocab) { return ceil_div(vocab, CHUNK); }
 
 // Carves the workspace (null: sizes only); returns the bytes.
@@ -1099,6 +1158,14 @@ size_t carve(void* base, size_t rows, int vocab, SampleWs* w) {
 
 template <typename T>
 void launch(const SampleArgs& a, const SampleWs& w, hipStream_t s) {
+  // rows of one chunk in one launch while every CU has one at most (256 rows x 8192, all
+  // controls: 29 us, four launches 33; 1024 rows: 106 and 89, since the other kernels
+  // leave room for more workgroups a CU than the last)
+  if (w.chunks == 1 && a.rows <= device_cu_count()) {
+    sample_row_kernel<T><<<a.rows, NT, 0, s>>>(a, w);
+    DLLM_LAUNCH_CHECK("sample_row_kernel");
+    return;
+  }
   const unsigned n = (unsigned)a.rows * w.chunks;
   sample_chunk_kernel<T><<<n, NT, 0, s>>>(a, w);
   DLLM_LAUNCH_CHECK("sample_chunk_kernel");

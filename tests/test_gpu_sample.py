@@ -235,3 +235,16 @@ def test_binding_checks_shapes(gpu_lib):
         with pytest.raises(B.DllmError):
             call()
     assert B.sample(x[:0], u[:0])[0].shape == (0,)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("R", [255, 256, 257, 300, 600])
+def test_rows_of_one_chunk(gpu_lib, R, dtype):
+    """Vocabularies of at most one chunk, on both sides of the row count up to which one launch does it all."""
+    for V in (700, 8192):
+        say(f"sample one chunk {R}x{V} {dtype}")
+        lg = randn((R, V), dtype, R + V, 2.0)
+        lg[3], lg[4, 5], lg[5] = -math.inf, math.nan, 0.0
+        c = controls(R, V, R, "tkpm")
+        c["temperature"][7] = 0.0
+        check(lg, uniform(R, V), mask_id=9, **c)
