@@ -85,8 +85,8 @@ __device__ __forceinline__ int lanes_upto(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
   return x;
 }
-// Where a document's keys are split: its chunks are shares shares[first ..
-// first + count - 1] of the call, of steps x step keys each, the last to its end.
+// Where keys are split: the document's chunks are shares first .. first + count - 1
+// of the call, of `steps` steps each, the last to the document's end.
 struct Share {
   int doc, chunk, first, count, steps;
 };
@@ -810,8 +810,8 @@ Choice choose(const AttnArgs& a) {
   const int step = c.kg * c.kt;
   const long slots = dense ? 2 * cus : cus;
   // Where they leave CUs without a workgroup, shares for all of them (31 documents of
-  // one token, one of 16384 keys among 500: 29 us; chunks of one length, by the longest
-  // document: 56).  Chunks of 256 keys at least (one token over 4000
+  // one token, one of 16384 keys among 500: 29 us; chunks as many for every document, by
+  // the longest: 56).  Chunks of 256 keys at least (one token over 4000
   // float32 keys: 20 us, 128 keys 18, 512 keys 24; 32 queries x 768 keys twice, bf16:
   // 18, 18 and 15).
   p.least = ceil_div(CHUNK_LEAST, step);
