@@ -528,9 +528,11 @@ int dllm_attention(const dllm_attn_args* args, void* workspace, size_t workspace
  * the first, min_p > 1 counts as 1, and u is cut to [0, 1) (NaN: 0).
  * A row with a NaN or +inf candidate gives the first such index with conf and
  * prob NaN; a row without candidates gives token -1 with conf and prob 0.
- * Candidates with w below 2^-63 count as without mass.  Sums are held in 64
+ * Candidates with w below 2^-63 may count as without mass.  Sums are held in 64
  * bits and do not depend on the order of execution: equal inputs give equal
- * outputs.
+ * outputs.  Candidates that tie for the largest logit weigh exactly 1; of the mass of
+ * the others 2^-37 counts as nothing where a share is compared, so that shares
+ * which are equal (top_p's or u's of levels of equal logits) are taken as equal.
  */
 typedef struct dllm_sample_args {
   const void* logits; /* device, dtype */

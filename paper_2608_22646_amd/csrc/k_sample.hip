@@ -27,10 +27,16 @@
 // 19 chunks of a vocabulary of 152064 let one row use 19 CUs; a workgroup that kept its
 // place over chunks had half the waves a CU (70 us against 52).
 //
-// Which token wins must not depend on rounding or on the order of execution.
-// Weights are float64 throughout; where threads add concurrently they add whole
-// numbers (a weight in units of 2^-40 of its class's), so every sum is the same in
-// any order and good to about 1e-12.
+// Which token wins must not depend on the order of execution, and not on rounding
+// where shares are equal.  Weights are float64 throughout; where threads add
+// concurrently they add whole numbers (a weight in units of 2^-40 of its class's), so
+// every sum is the same in any order, but one taken over classes and one over members
+// agree only to some 2e-12.  A share of the mass can fall exactly between two
+// candidates only where it is that share of every level of equal logits, since weights
+// of unlike ones have no rational relation.  So candidates that tie for the maximum are
+// counted, and weigh exactly 1 in every sum, and of what is not theirs SLACK is taken
+// off (top-p) or added (u) before a share of it is compared: equal shares then compare
+// as equal, and top-p's among ties alone are exact.
 #include <algorithm>
 #include <type_traits>
 
@@ -44,6 +50,7 @@ constexpr int CHUNK = 8192, NT = 512, E = CHUNK / NT, NW = NT / 64;
 constexpr int BINS = 512;               // 64 octaves; the last class stands for everything without mass
 constexpr double PER_NAT = 11.541560327111707;  // 8 / ln 2
 constexpr double LEAST = 0x1p-63;       // weights below count as none
+constexpr double SLACK = 0x1p-37;       // of masses that are compared
 constexpr int LIST = 1 << 15;            // members listed of a row, at most
 constexpr int INDEX_BITS = 22;          // of a listed member's second word; its class above
 constexpr int MAX_CHUNKS = (1 << INDEX_BITS) / CHUNK;
@@ -163,11 +170,12 @@ __device__ __forceinline__ V wave_all(V x, F f) { return from_lane(wave_upto(x, 
 typedef unsigned long long u64;
 
 // What a chunk leaves: its largest logit, the lowest index of a NaN or +inf (or
-// ~0), the lowest index of the maximum, and its sums at the row's temperature
-// (where nothing is filtered) and at temperature 1, relative to the largest weight.
+// ~0), the lowest index of the maximum (greedy rows), how many candidates have it, and
+// its sums at the row's temperature (where nothing is filtered) and at temperature 1,
+// relative to the largest weight.
 struct ChunkStat {
   float top;
-  uint32_t bad, arg, pad;
+  uint32_t bad, arg, ties;
   double sum, sum1;
 };
 // What sample_edge_kernel leaves: the boundary as far as the classes tell it.
@@ -289,7 +297,7 @@ struct ChunkShared {
   u64 classes[BINS + 64];  // 64 places for what has no class
   double powers[STEPS], sum[NW], sum1[NW];
   float top[NW];
-  uint32_t bad[NW], arg[NW];
+  uint32_t bad[NW], arg[NW], ties[NW];
 };
 // Chunk `block % chunks` of row `block / chunks`.
 template <typename T>
@@ -347,6 +355,11 @@ __device__ __forceinline__ void chunk_phase(const SampleArgs& a, const SampleWs&
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
     for (int e = 0; e < N; ++e) sum1 += __builtin_amdgcn_exp2f((f[i][e] - top) * 1.4426950408889634f);
+  uint32_t ties = 0;  // of the wave
+#pragma unroll
+  for (int i = 0; i < RUNS; ++i)
+#pragma unroll
+    for (int e = 0; e < N; ++e) ties += __popcll(__ballot(f[i][e] == top));
   uint32_t arg = ~0u;
   double sum = 0;
   const double qtop = in_classes(top, c.rate);
@@ -406,6 +419,7 @@ __device__ __forceinline__ void chunk_phase(const SampleArgs& a, const SampleWs&
   const double d1 = wave_all((double)sum1, Sum{});
   if (lane == 0) {
     sh.arg[wave] = arg;
+    sh.ties[wave] = ties;
     sh.sum[wave] = sum;
     sh.sum1[wave] = d1;
   }
@@ -414,6 +428,7 @@ __device__ __forceinline__ void chunk_phase(const SampleArgs& a, const SampleWs&
     ChunkStat s{top, bad, ~0u, 0, 0.0, 0.0};
     for (int i = 0; i < NW; ++i) {
       s.arg = min(s.arg, sh.arg[i]);
+      s.ties += sh.ties[i];
       s.sum += sh.sum[i];
       s.sum1 += sh.sum1[i];
     }
@@ -442,26 +457,37 @@ __device__ __forceinline__ V block_scan(V x, V* buf) {
 }
 
 // The chunks of a row, in LDS: the weight of each one's maximum (0: without
-// mass), and the classes between the row's maximum and its own (BINS: none).
+// mass), the classes between the row's maximum and its own (BINS: none), and its
+// candidates that have the row's maximum.
 struct Chunks {
   double fac[MAX_CHUNKS];
   int shift[MAX_CHUNKS];
+  uint32_t ties[MAX_CHUNKS];
 };
 struct RowTop {
   float big;
-  uint32_t bad;
+  uint32_t bad, ties;
   double qtop, base;
+  // Mass of class 0 of the row or of one of its chunks, in which `some` of the members
+  // tie for the maximum: those weigh 1 each, the others are summed up without them.
+  __device__ __forceinline__ double first_mass(uint64_t low, uint32_t count, uint32_t some, double centre) const {
+    return class_mass(low - some * low_of(class_word(qtop - base)), count - some) * centre + some;
+  }
 };
 // Fills `ch` (no barrier after it) and returns the row's maximum, to every thread.
 __device__ __forceinline__ RowTop join_chunks(const ChunkStat* stat, int nch, const Controls& c, const double* powers,
                                               Chunks& ch) {
-  RowTop r{-INFINITY, ~0u, 0.0, 0.0};
+  RowTop r{-INFINITY, ~0u, 0, 0.0, 0.0};
   const int lane = threadIdx.x & 63;
   for (int i = lane; i < nch; i += 64) {  // every wave by itself
-    r.big = fmaxf(r.big, stat[i].top);
+    const float top = stat[i].top;
+    r.ties = (top > r.big ? 0 : r.ties) + (top >= r.big ? stat[i].ties : 0);
+    r.big = fmaxf(r.big, top);
     r.bad = min(r.bad, stat[i].bad);
   }
+  const float mine = r.big;
   r.big = wave_all(r.big, Max{});
+  r.ties = wave_all(mine == r.big ? r.ties : 0u, Sum{});
   r.bad = wave_all(r.bad, Min{});
   if (r.big == -INFINITY) return r;
   r.qtop = in_classes(r.big, c.rate);
@@ -472,6 +498,7 @@ __device__ __forceinline__ RowTop join_chunks(const ChunkStat* stat, int nch, co
     const double q = in_classes(top, c.rate), e = top > -INFINITY ? weight_of(q - r.qtop, powers) : 0.0;
     ch.fac[i] = e >= LEAST ? e : 0.0;
     ch.shift[i] = e >= LEAST ? (int)(r.base - rint(q)) : BINS;
+    ch.ties[i] = top == r.big ? stat[i].ties : 0;
   }
   return r;
 }
@@ -522,7 +549,8 @@ __device__ __forceinline__ void edge_phase(const SampleArgs& a, const SampleWs& 
         n += (uint32_t)(um[j] >> COUNT_BIT);
       }
   }
-  double m = block_scan(class_mass(low, n) * weight_of(top.base - top.qtop - tid, powers), bufd);
+  const double centre = weight_of(top.base - top.qtop - tid, powers);
+  double m = block_scan(tid == 0 ? top.first_mass(low, n, top.ties, centre) : class_mass(low, n) * centre, bufd);
   n = block_scan(n, bufu);
   binw[tid] = m;
   binc[tid] = n;
@@ -971,16 +999,17 @@ __device__ __forceinline__ void pick_phase(const SampleArgs& a, const SampleWs& 
     for (int pass = by_p && bk >= 0 ? 0 : 1; pass < 2; ++pass) {
       if (pass == 1) {
         if (by_p) {
-          const double all = c.top_p * (bk >= 0 ? mass_before(bk) + cut.mass : prefix[min(st.ek, BINS - 1) - 1]);
+          const double all = bk >= 0 ? mass_before(bk) + cut.mass : prefix[min(st.ek, BINS - 1) - 1];
+          const double share = c.top_p * (all - fmax(all - top.ties, 0.0) * SLACK);
           int b = st.lo;
-          while (b < st.hi && prefix[b] < all) ++b;
+          while (b < st.hi && prefix[b] < share) ++b;
           if (b < edge) {
             edge = b;
             limit = ~0u;
           }
           if (b == edge) {
             ranked = true;
-            target = all - mass_before(b);
+            target = share - mass_before(b);
           }
         }
         if (st.bm >= 0 && st.bm <= edge) {
@@ -1009,13 +1038,15 @@ __device__ __forceinline__ void pick_phase(const SampleArgs& a, const SampleWs& 
         const int i = i0 + j * NW;
         // classes of the chunk before the edge
         const int shift = sh.ch.shift[min(i, nch - 1)], end = i < nch ? min(edge, BINS - 1) - shift : 0;
+        const uint32_t ties = lane == 0 ? sh.ch.ties[min(i, nch - 1)] : 0;
         s[j] = 0;
 #pragma unroll
         for (int k = 0; k < BINS / 64; ++k) {
           const int at = k * 64 + lane;
           if (at < end) {
             const u64 word = h[(size_t)i * BINS + at];
-            s[j] += class_mass(low_of(word), (uint32_t)(word >> COUNT_BIT)) * sh.centre[at + shift];
+            s[j] += k == 0 ? top.first_mass(low_of(word), (uint32_t)(word >> COUNT_BIT), ties, sh.centre[at + shift])
+                           : class_mass(low_of(word), (uint32_t)(word >> COUNT_BIT)) * sh.centre[at + shift];
           }
         }
       }
@@ -1037,7 +1068,7 @@ __device__ __forceinline__ void pick_phase(const SampleArgs& a, const SampleWs& 
   for (int i0 = 0; i0 < nch; i0 += 64) total += wave_all(i0 + lane < nch ? sh.part[i0 + lane] : 0.0, Sum{});
   float u = a.u[row];
   u = u > 0.f ? fminf(u, 1.f - 0x1p-24f) : 0.f;
-  const double want = (double)u * total;
+  const double want = u * (total + fmax(total - top.ties, 0.0) * SLACK);
   // every wave by itself: the first chunk with mass whose running sum passes
   // `want`; if rounding leaves none, the last with mass
   int at = 0;
