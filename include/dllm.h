@@ -487,6 +487,9 @@ int dllm_rotary(const dllm_rotary_cfg* cfg, int32_t dtype, int32_t B, int32_t L,
  * 16-byte aligned; strides multiples of 16 bytes, stride_l >= head_dim, and 64
  * stride_l of k and v below 2^31 bytes; 0 <= max_q <= q_tokens, 0 <= max_kv <=
  * kv_tokens, both at most 2^30; docs <= 65535; scale finite, cap >= 0 and finite, block >= 0.
+ * One launch does all documents, max_q queries of each; it must stay below 2^32
+ * threads (DLLM_ESHAPE): docs * n_kv_heads * ceil(max_q * (n_heads / n_kv_heads) / 32)
+ * may always be up to 2^23, more where a wider tile is taken.
  * docs or max_q of 0: nothing.
  */
 typedef struct dllm_attn_args {

@@ -778,7 +778,7 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
 
 // Keys of the chunks that a row tile's width is chosen for, and the least of one.
 constexpr int CHUNK_MIN = 512, CHUNK_LEAST = 256;
-// Which kernel a call takes and how its grid is laid out.  Sizes only.
+// Which kernel a call takes and how its grid is laid out.  Sizes only, docs and max_q at least 1.
 struct Choice {
   int qg, kg, kt;
   AttnPlan plan;
@@ -865,8 +865,11 @@ size_t attn_docs_bytes(const AttnArgs& a) {
   return c.plan.shares > 0 ? part_values(a, c.plan) * (a.hd * 4 + 8) + (size_t)a.docs * sizeof(int4) : 0;
 }
 
+// A launch's threads must be below 2^32.
 bool attn_docs_fits(const AttnArgs& a) {
-  return (long)a.docs * a.Hkv * ceil_div((long)a.max_q * (a.Hq / a.Hkv), 32) < (1l << 28);
+  if (a.docs == 0 || a.max_q == 0) return true;
+  const Choice c = choose(a);
+  return c.grid * (64 * c.qg * c.kg) < (1l << 32);
 }
 
 void launch_attn_docs(const AttnArgs& a, void* ws, hipStream_t s) {
