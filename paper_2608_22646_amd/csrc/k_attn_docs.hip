@@ -151,6 +151,8 @@ __device__ __forceinline__ void barrier_nofence() {
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
+// Of a wave's LDS accesses, which run in order: the compiler moves none past this.
+__device__ __forceinline__ void wave_order() { asm volatile("" ::: "memory"); }
 typedef __bf16 bf2_t __attribute__((ext_vector_type(2)));
 typedef float f2_t __attribute__((ext_vector_type(2)));
 // Two floats to bf16 in one instruction, and acc + the sum of two bf16.
@@ -215,6 +217,12 @@ struct Tile {
     return CH >= 16 ? (r & 3) << 2 : ((r >> 1) & 1) << 2;
   }
 };
+
+// LDS tiles hold what LDS-DMA brought and are read as several types; accesses that
+// the compiler must not move past each other for their types' sake go through these.
+typedef uint32_t __attribute__((may_alias)) word_t;
+typedef uint32_t quad_t __attribute__((ext_vector_type(4), may_alias));
+typedef float __attribute__((may_alias)) value_t;
 
 // State of 32 rows: running maximum (log2 units) and what exponents are taken
 // against (it, or 0 while it is -inf), sum and output; and what the lane's row is.
@@ -542,7 +550,7 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
           for (int ds = 0; ds < ND; ++ds) {
             const int e = ds * 32 + lq;
             const float w =
-                *reinterpret_cast<const float*>(vt + (key + 4 * half) * TL::ROW + ((((e >> 2) ^ (half << 3)) << 4) | ((e & 3) * 4)));
+                *reinterpret_cast<const value_t*>(vt + (key + 4 * half) * TL::ROW + ((((e >> 2) ^ (half << 3)) << 4) | ((e & 3) * 4)));
             R.o[ds] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x[b][r], R.o[ds], 0, 0, 0);
           }
         }
@@ -555,7 +563,7 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     constexpr uint32_t EXP = BF ? 0x7f807f80u : 0x7f800000u;  // exponents of a word
     uint32_t top = 0;
     for (int i = qg * 64 + lane; i < K_BYTES / 16; i += QG * 64) {
-      const uint4 w = reinterpret_cast<const uint4*>(vt)[i];
+      const quad_t w = reinterpret_cast<const quad_t*>(vt)[i];
       for (const uint32_t x : {w.x & EXP, w.y & EXP, w.z & EXP, w.w & EXP})
         if constexpr (BF)
           top = __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(v2us_t, top), __builtin_bit_cast(v2us_t, x)));
@@ -572,21 +580,25 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
           const int e = ds * 32 + 8 * (r >> 2) + 4 * half + (r & 3), b = e * (int)sizeof(T);
-          const T w = *reinterpret_cast<const T*>(vrow + ((((b >> 4) ^ TL::v_swz(key)) << 4) | (b & 15)));
-          float f;
-          if constexpr (BF)
-            f = bf2f(w);
-          else
-            f = w;
+          // (bf16: the word that holds the element, whose upper half is that of an odd one)
+          const uint32_t w = *reinterpret_cast<const word_t*>(vrow + ((((b >> 4) ^ TL::v_swz(key)) << 4) | (b & 12)));
+          const float f = __uint_as_float(BF ? (r & 1 ? w & 0xffff0000u : w << 16) : w);
           if (t0 + key < min(R.end, ke) && !(fabsf(f) < INFINITY)) R.o[ds][r] += f;
         }
     }
-    if constexpr (QG > 1) __syncthreads();
+    // other lanes' reads lie before the stores, and the stores before other lanes' reads
+    if constexpr (QG > 1)
+      __syncthreads();
+    else
+      wave_order();
     for (int i = qg * 64 + lane; i < K_BYTES / 4; i += QG * 64) {
-      uint32_t* w = reinterpret_cast<uint32_t*>(vt) + i;
+      word_t* w = reinterpret_cast<word_t*>(vt) + i;
       *w = numbers<T>(*w);
     }
-    if constexpr (QG > 1) __syncthreads();
+    if constexpr (QG > 1)
+      __syncthreads();
+    else
+      wave_order();
   };
   for (int u = 0; u < nsteps; ++u) {
     if (u + D <= nsteps)
@@ -598,7 +610,7 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     if constexpr (QG > 1)
       barrier_nofence();
     else
-      asm volatile("" ::: "memory");
+      wave_order();
     if (u + D < nsteps) load(u + D, (u + D) % S);
     const int t0 = kb + (u * KG + kg) * KT;
     char *const slot = lds + (u % S) * STAGE + kg * TILE, *const vt = slot + K_BYTES;
