@@ -173,11 +173,15 @@ __device__ __forceinline__ uint32_t lds_address(const char* p) {
 }
 // 16 bytes per lane from the buffer to LDS at `to` + 16 lane.  Written out, since
 // the compiler lets no transposing LDS read pass while an LDS-DMA load that it
-// knows of is in flight; the waits for these loads are wait_vmcnt's alone.  (m0 is
-// nobody else's here: nothing in this file makes the compiler use it.  The idle
-// cycles are what a descriptor fresh from readfirstlane needs before its use.)
+// knows of is in flight; the waits for these loads are wait_vmcnt's alone.  m0, which
+// the compiler cannot be told of, is left as it was.  (The idle cycles are what a
+// descriptor fresh from readfirstlane needs before its use.)
 __device__ __forceinline__ void dma16(rsrc_t rs, uint32_t off, uint32_t to) {
-  asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(uniform((int)to)), "v"(off), "s"(rs) : "memory");
+  uint32_t m0;
+  asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %1\n\ts_nop 4\n\tbuffer_load_dwordx4 %2, %3, 0 offen lds\n\ts_mov_b32 m0, %0"
+               : "=&s"(m0)
+               : "s"(uniform((int)to)), "v"(off), "s"(rs)
+               : "memory");
 }
 // 2^x by the hardware instruction alone: results below 2^-126 count as zero.
 __device__ __forceinline__ float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
