@@ -28,7 +28,8 @@
 // place over chunks had half the waves a CU (70 us against 52).
 //
 // Which token wins must not depend on the order of execution, and not on rounding
-// where shares are equal.  Weights are float64 throughout; where threads add
+// where shares are equal.  Weights are float64 (those behind conf, which no choice here
+// depends on, float32, and their sum float64); where threads add
 // concurrently they add whole numbers (a weight in units of 2^-40 of its class's), so
 // every sum is the same in any order, but one taken over classes and one over members
 // agree only to some 2e-12.  A share of the mass can fall exactly between two
@@ -350,11 +351,11 @@ __device__ __forceinline__ void chunk_phase(const SampleArgs& a, const SampleWs&
     if (tid == 0) *out = ChunkStat{top, bad, ~0u, 0, 0.0, 0.0};
     return;
   }
-  float sum1 = 0.f;  // at temperature 1
+  double sum1 = 0;  // at temperature 1, of float32 weights
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
 #pragma unroll
-    for (int e = 0; e < N; ++e) sum1 += __builtin_amdgcn_exp2f((f[i][e] - top) * 1.4426950408889634f);
+    for (int e = 0; e < N; ++e) sum1 += (double)__builtin_amdgcn_exp2f((f[i][e] - top) * 1.4426950408889634f);
   uint32_t ties = 0;  // of the wave
 #pragma unroll
   for (int i = 0; i < RUNS; ++i)
@@ -416,12 +417,12 @@ __device__ __forceinline__ void chunk_phase(const SampleArgs& a, const SampleWs&
   }
   if (c.greedy) arg = wave_all(arg, Min{});
   if (!c.filter) sum = wave_all(sum, Sum{});
-  const double d1 = wave_all((double)sum1, Sum{});
+  sum1 = wave_all(sum1, Sum{});
   if (lane == 0) {
     sh.arg[wave] = arg;
     sh.ties[wave] = ties;
     sh.sum[wave] = sum;
-    sh.sum1[wave] = d1;
+    sh.sum1[wave] = sum1;
   }
   __syncthreads();
   if (tid == 0) {
