@@ -30,3 +30,18 @@ def test_broken_values_reach_their_own_dimension(gpu_lib, n, kv, q_pos, heads, d
         for dims, bad in ((slice(0, hd, 2), math.nan), (slice(1, hd, 2), math.inf), (slice(2, hd, 4), -math.inf), (slice(hd - 1, hd), math.nan)):
             got = run_and_check(*heads, dtype, [n], [kv], block=1, q_pos=[q_pos], seed=key, mutate=at(key, dims, bad))
             assert torch.isfinite(got[:key - q_pos].float()).all()
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("share", [0.2, 0.27, 0.285, 0.39, 0.41, 0.59, 0.61, 2.0])
+def test_caps_on_both_sides_of_their_forms(gpu_lib, share, dtype):
+    """Caps of which the largest score is a given share: small ones go by a series, large ones by exponentials."""
+    say(f"attention cap forms {share} {dtype}")
+    top = []
+
+    def measure(q, k, v):
+        s = torch.einsum("thd,shd->hts", q.cpu().double(), k.cpu().double().repeat_interleave(2, 1)) / 8
+        top.append(float(s.abs().max()))
+    for n, kv in ((3, 90), (300, 300)):
+        run_and_check(4, 2, 64, dtype, [n], [kv], seed=kv, mutate=measure, cap=1e30, acts_as=0.0)
+        run_and_check(4, 2, 64, dtype, [n], [kv], seed=kv, cap=top[-1] / share)
