@@ -235,6 +235,7 @@ struct Rows {
   f32x16_t o[HD / 32];
   float m, m_ref, l;
   int t, h, end;  // query, head, keys that it sees
+  int at;         // position that its distances are taken from
   bool mine;      // there is such a row
   float slope;
 };
@@ -344,7 +345,17 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
   R.t = row / G;
   R.h = g * G + row % G;
   R.end = R.mine ? sees(a, d, R.t) : 0;
-  R.slope = a.slopes && R.mine ? a.slopes[R.h] * LOG2E : 0.f;
+  R.slope = 0.f;
+  R.at = 0;
+  if (a.slopes) {
+    if (R.mine) R.slope = a.slopes[R.h] * LOG2E;
+    // From the first or last visible key, where the position lies before or behind all
+    // of them: the scores differ by one amount, which the softmax does not see, and
+    // float32 need not hold it.  (One key further where the slope is infinite: a distance
+    // of zero would be no number.)
+    const int out = fabsf(R.slope) < INFINITY ? 0 : 1;
+    R.at = (int)max(min((long)d.pos + R.t, (long)R.end - 1 + out), (long)-out);
+  }
   R.m = -INFINITY;
   R.m_ref = 0.f;
   R.l = 0.f;
@@ -472,7 +483,7 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
         for (int r = 0; r < 16; ++r) x[b][r] *= sc;
     }
     if (a.slopes) {
-      const float at = (float)((long)d.pos + R.t - t0 - 4 * half);
+      const float at = (float)(R.at - t0 - 4 * half);
 #pragma unroll
       for (int b = 0; b < NS; ++b)
 #pragma unroll
