@@ -576,6 +576,13 @@ def _workspace(nbytes, device):
     return buf if buf.data_ptr() % 256 == 0 else device_buffer(nbytes, device)
 
 
+def _given(ws, device):
+    """The caller's workspace, which lies on the operands' device."""
+    if ws.device != device or not ws.is_contiguous():
+        _refuse(False, -1, f"ws must be contiguous on {device}")
+    return ws
+
+
 @dataclass(frozen=True)
 class Rotary:
     """Constants of a rotary embedding (dllm_rotary_cfg); scaling: none, linear or parts."""
@@ -675,7 +682,9 @@ def attention(q, k, v, docs: Docs | None = None, block=0, scale=None, cap=0.0, s
         n = _sz()
         check(lib().dllm_attention_workspace_size(a, n))
         ws = _workspace(n.value, dev) if n.value else None
-    check(lib().dllm_attention(a, _ptr(ws), 0 if ws is None else ws.numel(), _raw_stream(dev.index)))
+    else:
+        _given(ws, dev)
+    check(lib().dllm_attention(a, _ptr(ws), 0 if ws is None else ws.nbytes, _raw_stream(dev.index)))
     return out
 
 
@@ -730,7 +739,9 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask
     if ws is None:
         n = sample_workspace_size(R, V)
         ws = _workspace(n, dev) if n else None
-    check(lib().dllm_sample(a, _ptr(ws), 0 if ws is None else ws.numel(), _raw_stream(dev.index)))
+    else:
+        _given(ws, dev)
+    check(lib().dllm_sample(a, _ptr(ws), 0 if ws is None else ws.nbytes, _raw_stream(dev.index)))
     return token, conf, prob
 
 
