@@ -518,6 +518,12 @@ def _refuse(ok, code, msg):
         raise DllmError(code, msg)
 
 
+def _in32(*numbers):
+    """Numbers that the C side takes as int32 (ctypes would cut them to 32 bits)."""
+    if max(numbers) > 0x7fffffff or min(numbers) < -0x80000000:
+        _refuse(False, -2, f"{numbers}: beyond 32 bits")
+
+
 def _dtype(t, name):
     _refuse(t.dtype in _DTYPES, -1, f"{name} must be float32 or bfloat16")
     return _DTYPES[t.dtype]
@@ -617,6 +623,7 @@ def rotary(cfg: Rotary, q, k=None, pos=None, pos0=0, q_out=None, k_out=None, inv
     shape = B, L, n_q, hd = tuple(q.shape)
     if hd != cfg.head_dim:
         _refuse(False, -2, f"q has heads of {hd} elements, cfg of {cfg.head_dim}")
+    _in32(pos0)
     p = _column(pos, B * L, torch.int32, dev, "pos")
     vq, vk, vko, n_k = _rows(q, shape, dtype, dev, "q"), None, None, 0
     if q_out is None:
@@ -710,10 +717,12 @@ def _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes):
     if n is None:
         n = next((t.numel() for t in arrays if t is not None), 1) if one else shape[0]
     _refuse(one or n == shape[0], -2, "a dense batch has one document per slab")
+    max_q, max_kv = T if docs.max_q is None else docs.max_q, S if docs.max_kv is None else docs.max_kv
+    _in32(n, T, S, max_q, max_kv, block)
     ptrs = [_column(t, n, torch.int32, dev, name) for t, name in zip(arrays, _DOC_ARRAYS)]
-    return AttnArgs(dt, Hq, Hkv, hd, *views, n, T, S, T if docs.max_q is None else docs.max_q,
-                    S if docs.max_kv is None else docs.max_kv, *ptrs, _column(slopes, Hq, torch.float32, dev, "slopes"),
-                    1.0 / math.sqrt(hd) if scale is None else scale, cap, block)
+    return AttnArgs(dt, Hq, Hkv, hd, *views, n, T, S, max_q, max_kv, *ptrs,
+                    _column(slopes, Hq, torch.float32, dev, "slopes"), 1.0 / math.sqrt(hd) if scale is None else scale, cap,
+                    block)
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask_id=-1, ws=None, stream=None):
@@ -729,6 +738,7 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask
     R, V = logits.shape
     st = logits.stride()
     _refuse(st[1] == 1 or V == 1, -2, "logits: a row must be contiguous")
+    _in32(R, V, mask_id)
     cols = [_column(u, R, torch.float32, dev, "u"), _column(temperature, R, torch.float32, dev, "temperature"),
             _column(top_k, R, torch.int32, dev, "top_k"), _column(top_p, R, torch.float32, dev, "top_p"),
             _column(min_p, R, torch.float32, dev, "min_p")]
@@ -746,6 +756,7 @@ def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask
 
 
 def sample_workspace_size(rows, vocab):
+    _in32(rows, vocab)
     n = _sz()
     check(lib().dllm_sample_workspace_size(rows, vocab, n))
     return n.value

@@ -14,6 +14,32 @@ def test_a_given_workspace_lies_on_the_operands_device():
             B._given(bad, device)
 
 
+@pytest.mark.parametrize("far", [1 << 31, (1 << 32) + 5, -(1 << 31) - 1])
+def test_numbers_beyond_32_bits_are_refused(far):
+    """They reach the C side cut to 32 bits otherwise: 2^32 + 5 as 5.  (No tensor here is on a GPU: what lies before
+    the library is called.)"""
+    q, k = torch.zeros((4, 4, 64)), torch.zeros((6, 2, 64))
+    args = lambda docs, block=0: B._attn_args(B.DLLM_F32, q, k, k, q, docs, block, None, 0.0, None)  # noqa: E731
+    assert args(B.Docs(max_q=4), 1).max_q == 4
+    for call in (lambda: B._in32(far), lambda: B._in32(0, far, -1), lambda: args(B.Docs(max_q=far)), lambda: args(B.Docs(max_kv=far)),
+                 lambda: args(B.Docs(count=far)), lambda: args(B.Docs(), far), lambda: B.sample_workspace_size(far, 100),
+                 lambda: B.sample_workspace_size(1, far)):
+        with pytest.raises(B.DllmError):
+            call()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("far", [1 << 31, (1 << 32) + 5, -(1 << 31) - 1])
+def test_calls_with_numbers_beyond_32_bits_are_refused(gpu_lib, far):
+    q = torch.zeros((1, 4, 4, 64), device="cuda")
+    x, u = torch.zeros((3, 50), device="cuda"), torch.zeros(3, device="cuda")
+    for call in (lambda: B.rotary(B.Rotary(64), q, pos0=far), lambda: B.attention(q, q, q, block=far), lambda: B.sample(x, u, mask_id=far)):
+        with pytest.raises(B.DllmError):
+            call()
+    B.rotary(B.Rotary(64), q, pos0=(1 << 31) - 1)
+    torch.cuda.synchronize()
+
+
 @pytest.mark.gpu
 def test_a_workspace_on_the_host_is_refused(gpu_lib):
     q, k = torch.zeros((1, 2, 64), device="cuda"), torch.zeros((9000, 2, 64), device="cuda")
