@@ -8,6 +8,7 @@ has not been built (python -m paper_2608_22646_amd.build).
 from __future__ import annotations
 
 import ctypes
+import itertools
 import math
 import os
 from dataclasses import dataclass
@@ -660,9 +661,10 @@ class Docs:
     @classmethod
     def packed(cls, q_lens, kv_lens=None, q_pos=None, prefix=None, device="cuda"):
         """Documents that follow each other without gaps, from host lists."""
-        kv_lens = q_lens if kv_lens is None else kv_lens
+        q_lens = list(q_lens)
+        kv_lens = q_lens if kv_lens is None else list(kv_lens)
         ints = lambda v: None if v is None else torch.tensor(list(v), dtype=torch.int32, device=device)  # noqa: E731
-        starts = lambda v: [sum(v[:i]) for i in range(len(v))]  # noqa: E731
+        starts = lambda v: list(itertools.accumulate([0, *v[:-1]])) if v else []  # noqa: E731
         return cls(ints(starts(q_lens)), ints(q_lens), ints(starts(kv_lens)), ints(kv_lens), max(q_lens, default=0),
                    max(kv_lens, default=0), ints(q_pos), ints(prefix))
 

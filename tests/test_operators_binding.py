@@ -14,6 +14,32 @@ def test_a_given_workspace_lies_on_the_operands_device():
             B._given(bad, device)
 
 
+def test_packed_documents():
+    docs = B.Docs.packed([3, 0, 5], (4, 2, 7), [1, 2, 3], device="cpu")
+    assert docs.q_start.tolist() == [0, 3, 3] and docs.kv_start.tolist() == [0, 4, 6] and (docs.max_q, docs.max_kv) == (5, 7)
+    assert docs.q_len.tolist() == [3, 0, 5] and docs.kv_len.tolist() == [4, 2, 7] and docs.q_pos.tolist() == [1, 2, 3]
+    assert docs.prefix is None and docs.q_start.dtype == torch.int32
+    none = B.Docs.packed([], device="cpu")
+    assert none.q_start.numel() == 0 and (none.max_q, none.max_kv) == (0, 0)
+    assert B.Docs.packed(iter([2, 1]), device="cpu").kv_start.tolist() == [0, 2]
+
+
+def test_packing_the_most_documents_takes_one_pass():
+    """65535 documents, the most of a call: every length is read a few times, not once for each document behind it."""
+    reads = 0
+
+    class Length(int):
+        def __radd__(self, other):
+            nonlocal reads
+            reads += 1
+            return int(other) + int(self)
+
+        def __add__(self, other):
+            return self.__radd__(other)
+    docs = B.Docs.packed([Length(2)] * 65535, device="cpu")
+    assert docs.q_start[-1] == 2 * 65534 and reads <= 4 * 65535
+
+
 @pytest.mark.parametrize("far", [1 << 31, (1 << 32) + 5, -(1 << 31) - 1])
 def test_numbers_beyond_32_bits_are_refused(far):
     """They reach the C side cut to 32 bits otherwise: 2^32 + 5 as 5.  (No tensor here is on a GPU: what lies before
