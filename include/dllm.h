@@ -434,7 +434,7 @@ enum {
  * where the scaling names them.  Angles are formed in float64 and reduced there
  * to within an eighth of a turn, so far positions lose nothing.
  * Requirements: head_dim in [2, 512], rot_dim even, 2 <= rot_dim <= min(head_dim,
- * 256), at most 4096 heads each; base, factor, orig_len > 0; high > low; gain finite.
+ * 256), at most 4096 heads each; base, factor, orig_len > 0; high > low; gain finite in float32.
  */
 typedef struct dllm_rotary_cfg {
   int32_t head_dim, rot_dim, interleaved, scaling;

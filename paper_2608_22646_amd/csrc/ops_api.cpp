@@ -28,7 +28,7 @@ void check_rotary(const dllm_rotary_cfg* c) {
   require(c->rot_dim >= 2 && c->rot_dim % 2 == 0 && c->rot_dim <= c->head_dim && c->rot_dim <= 256, DLLM_ESHAPE,
           "rot_dim must be even and in [2, min(head_dim, 256)]");
   require(std::isfinite(c->base) && c->base > 0, DLLM_EINVAL, "base must be positive");
-  require(std::isfinite(c->gain), DLLM_EINVAL, "gain must be finite");
+  require(std::isfinite((float)c->gain), DLLM_EINVAL, "gain must be a finite float32");
   require(c->scaling >= DLLM_ROPE_PLAIN && c->scaling <= DLLM_ROPE_PARTS, DLLM_EINVAL, "unknown scaling");
   if (c->scaling != DLLM_ROPE_PLAIN)
     require(std::isfinite(c->factor) && c->factor > 0, DLLM_EINVAL, "factor must be positive");

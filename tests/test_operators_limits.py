@@ -1,11 +1,12 @@
 """Limits of the stand-alone operators that the host checks, on both sides of each (CPU only: no address
 handed over here is real, and what is accepted is only asked for its workspace)."""
 import ctypes
+import math
 
 import pytest
 
 from paper_2608_22646_amd import binding as B
-from test_operators_abi import attn_args
+from test_operators_abi import attn_args, rotary_rc
 
 # documents, query heads, key/value heads, head_dim, most queries, type; a few documents and a head more do not fit
 LARGEST = [
@@ -38,3 +39,9 @@ def test_attention_always_takes_what_the_header_says():
                               max_q=max_q, max_kv=4096)
                 assert docs * n_kv * -(-max_q * group // 32) <= 1 << 23
                 assert B.lib().dllm_attention_workspace_size(a, n) == 0, (docs, n_kv, group, max_q, B.lib().dllm_last_error())
+
+
+@pytest.mark.parametrize("gain,code", [(1e39, -1), (-1e300, -1), (math.nan, -1), (3e38, 0), (0.0, 0)])
+def test_rotary_refuses_a_gain_that_float32_cannot_hold(gain, code):
+    """The sines are multiplied by it in float32: infinity times a sine of 0 is no number."""
+    assert rotary_rc(cfg=dict(gain=gain), Bn=1 if code else 0) == code
