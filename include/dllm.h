@@ -472,8 +472,8 @@ int dllm_rotary(const dllm_rotary_cfg* cfg, int32_t dtype, int32_t B, int32_t L,
  * h reads key/value head h / (n_heads / n_kv_heads).
  * A query that sees no key, or none with a score above -inf, gives zeros.  What
  * lies at invisible keys never reaches a result, NaN and infinities included;
- * a NaN score makes its query's output NaN, a visible NaN or infinite value the
- * dimension it stands in.  Rows of out that belong to no document keep their contents.
+ * a NaN score makes its query's output NaN, a visible NaN or infinite value leaves
+ * NaN or an infinity in the dimension it stands in.  Rows of out that belong to no document keep their contents.
  *
  * Arrays are device int32 [docs]; NULL stands for: starts 0, q_len = q_tokens,
  * kv_len = kv_tokens, q_pos = kv_len - q_len (queries at the end of the keys),
@@ -483,7 +483,8 @@ int dllm_rotary(const dllm_rotary_cfg* cfg, int32_t dtype, int32_t B, int32_t L,
  * Storage: float32 (products on the float32 matrix cores) or bf16 (products
  * accumulate in float32, softmax in float32; probabilities enter the second
  * product as bf16).  Out must not overlap q, k or v.
- * Requirements: head_dim 64 or 128; n_heads % n_kv_heads == 0; data pointers
+ * Requirements: head_dim 64 or 128; n_heads % n_kv_heads == 0, n_heads <= 4096 and
+ * max_q * (n_heads / n_kv_heads) <= 2^31 - 256; data pointers
  * 16-byte aligned; strides multiples of 16 bytes, stride_l >= head_dim, and 64
  * stride_l of k and v below 2^31 bytes; 0 <= max_q <= q_tokens, 0 <= max_kv <=
  * kv_tokens, both at most 2^30; docs <= 65535; scale finite, cap >= 0 and finite, block >= 0.
