@@ -30,7 +30,7 @@ def tied(V, n, logits, dtype, others=-math.inf):
 
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
-@pytest.mark.parametrize("V,n", [(700, 2), (700, 4), (3001, 10), (5000, 1000), (20000, 2), (40000, 64), (40000, 1000), (30000, 24000)])
+@pytest.mark.parametrize("V,n", [(700, 2), (700, 4), (3001, 10), (5000, 1000), (20000, 2), (40000, 64), (40000, 1000), (30000, 24000), (152064, 120000)])
 def test_top_p_of_tied_candidates(gpu_lib, V, n, dtype):
     """The first ceil(top_p n) of n tied stay, at every logit (a constant added changes nothing), alone or by top-k."""
     say(f"sample shares {V} {n} {dtype}")
