@@ -22,10 +22,10 @@
 //
 // Many rows (bf16, 128-wide heads): the matrix unit and the softmax's instructions
 // share a SIMD's issue, the exponentials being half of them; 8448 tokens, 28 + 4
-// heads, visible up to the end of their block of 32: 520 us, 0.99 PFLOP/s (taking
-// out the softmax: 499, the LDS reads as well: 435, the loads as well: 389, at a
-// clock that its power holds near 2 GHz).  Few rows: keys and values from HBM; one
-// token of 16 documents of 2.6 to 8.4 thousand keys: 41 us and 5 for the join, 4.4
+// heads, visible up to the end of their block of 32: 517 us, 1.00 PFLOP/s (when it took
+// 548, that was 499 without the softmax, 435 without the LDS reads as well and 389
+// without the loads as well, at a clock that its power holds near 2 GHz).  Few rows: keys and values from HBM; one
+// token of 16 documents of 2.6 to 8.4 thousand keys: 40 us and 5 for the join, 4.4
 // TB/s; 32 queries x 1024 keys x 32 heads x 8: 31 us, 4.4 TB/s (a copy: 5.1).
 // float32: the matrix unit's float32 rate, a sixteenth of bf16's.
 #include <algorithm>
@@ -509,7 +509,10 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     return mt;
   };
   // probabilities in place of scores x (which `fold` takes to log2 units), and in
-  // pairs pw for bf16, where the sum is that of the rounded ones, which the products see
+  // pairs pw for bf16, the type that the matrix unit takes beside values of bf16's range
+  // (IEEE half, eight times finer, ends at 65504, and values with it).  Each is off by
+  // 2^-8 of itself at most; the sum is that of the rounded ones, which the products see.
+  // Against 64 bits outputs are 0.0022 off in all, 0.0017 by their own rounding alone.
   auto exponentials = [&](f32x16_t (&x)[NS], uint32_t (&pw)[BF ? NS * 8 : 1], float fold) {
     float psum = 0.f;
 #pragma unroll

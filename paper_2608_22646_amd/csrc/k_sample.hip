@@ -20,12 +20,14 @@
 // Calls without top-k, top-p and min-p need the first and the last alone; few rows of
 // one chunk run all of them in one launch (sample_row_kernel).
 //
-// Many rows: the first kernel is bound by the float64 weights and the classes' LDS
-// additions (256 rows x 152064 float32: 44 us, 3.6 TB/s; with weights by a table 52),
-// the collection by HBM (31 us, 5 TB/s, where every chunk has members); few rows by the
-// latency of four dependent launches (1 row x 126464: 29 us; 5.0, 6.7, 4.2 and 12.5).  A chunk is 8192 logits in 512 threads' registers:
-// 19 chunks of a vocabulary of 152064 let one row use 19 CUs; a workgroup that kept its
-// place over chunks had half the waves a CU (70 us against 52).
+// Many rows: the first kernel is bound by the float64 weights and sums and the classes'
+// LDS additions (256 rows x 152064 float32: 48 us, 3.2 TB/s), the collection by HBM (31
+// us, 5 TB/s, where every chunk has members); few rows by the chain of dependent steps
+// in and between the kernels (1 row x 126464: 29 us; 5.5, 6.4, 4.2 and 13.4.  It is not
+// the launches: a row of 3001 logits in one of them takes 27).  A chunk is 8192 logits
+// in 512 threads' registers: 19 chunks of a vocabulary of 152064 let one row use 19 CUs;
+// a workgroup that kept its place over chunks had half the waves a CU (70 us against 52
+// when it was tried).
 //
 // Which token wins must not depend on the order of execution, and not on rounding
 // where shares are equal.  Weights are float64 (those behind conf, which no choice here
@@ -1191,8 +1193,8 @@ size_t carve(void* base, size_t rows, int vocab, SampleWs* w) {
 template <typename T>
 void launch(const SampleArgs& a, const SampleWs& w, hipStream_t s) {
   // rows of one chunk in one launch while every CU has one at most (256 rows x 8192, all
-  // controls: 29 us, four launches 33; 1024 rows: 106 and 89, since the other kernels
-  // leave room for more workgroups a CU than the last)
+  // controls: 34 us, four launches 38; 512 rows: 60 and 57; 1024 rows: 119 and 101, since
+  // the other kernels leave room for more workgroups a CU than the last)
   if (w.chunks == 1 && a.rows <= device_cu_count()) {
     sample_row_kernel<T><<<a.rows, NT, 0, s>>>(a, w);
     DLLM_LAUNCH_CHECK("sample_row_kernel");
