@@ -113,3 +113,22 @@ def test_u_between_repeated_levels(gpu_lib, V, dtype):
               dict(min_p=column(1e-9, R).cuda(), temperature=column(1.3, R).cuda())):
         token = B.sample(cuda, u.repeat(6).cuda(), **c)[0].cpu().long()
         assert torch.equal(token, want), f"{list(c)}: {(token != want).sum()} of {R} rows"
+
+
+@pytest.mark.parametrize("V", [512, 8192, 65536])
+@pytest.mark.parametrize("kept", [1, 3, 4, 7])
+def test_u_between_repeated_levels_that_top_k_keeps(gpu_lib, V, kept):
+    """The same, of which top-k keeps the highest levels whole: in classes of their own, or with one that goes in theirs."""
+    say(f"sample u between kept levels {V} {kept}")
+    levels = torch.tensor([[0.5, -1.25, 2.0, 1.99, -3.0, 0.49, 1.0, -1.26], [3.0, -4.0, 5.0, 1.0, 7.0, 2.0, -9.0, 0.0]])
+    u = torch.arange(0, 64) / 64
+    for row in levels:
+        rank = torch.argsort(torch.argsort(row, descending=True))
+        R = len(u)
+        members = (rank.repeat(V // 8) < kept).nonzero()[:, 0]
+        want = members[(u * len(members)).long()]
+        cuda = row.repeat(V // 8).expand(R, V).contiguous().cuda()
+        k = column(V // 8 * kept, R, torch.int32).cuda()
+        for t in (1.0, 0.7):
+            token = B.sample(cuda, u.cuda(), column(t, R).cuda(), k)[0].cpu().long()
+            assert torch.equal(token, want), f"T {t}: {(token != want).sum()} of {R} rows"
