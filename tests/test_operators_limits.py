@@ -34,7 +34,7 @@ def test_attention_always_takes_what_the_header_says():
     for dtype in (B.DLLM_F32, B.DLLM_BF16):
         for hd in (64, 128):
             for docs, n_kv, group, max_q in ((1, 1, 1, 1 << 28), (32768, 256, 1, 1), (32768, 128, 1, 33), (1, 64, 4096 // 64, 1 << 16),
-                                             (3, 3, 2, 14913072), (65, 1, 1, 4129760), (8192, 8, 4, 1024), (511, 1, 1, 525312)):
+                                             (3, 3, 2, 14913056), (65, 1, 1, 4129760), (8192, 8, 4, 1024), (511, 1, 1, 525312)):
                 a = attn_args(dtype=dtype, head_dim=hd, docs=docs, n_heads=n_kv * group, n_kv_heads=n_kv, q_tokens=1 << 30, kv_tokens=4096,
                               max_q=max_q, max_kv=4096)
                 assert docs * n_kv * -(-max_q * group // 32) <= 1 << 23
