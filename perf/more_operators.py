@@ -84,7 +84,7 @@ def draw(rng):
             return _shared_case(None, heads, dtype, docs, rng.choice([16, 32, 33, 64]), _log(rng, 64, 400), _log(rng, 30, 4000 // most),
                                 min(docs, rng.choice([1, 1, 2])), mix, rng.choice([0, 0, 32]), cap, bias, rng.choice([0, 0, 1]), pad)
         docs = _log(rng, 1, 12)
-        q = _log(rng, 20, 4000 // most // docs)
+        q = _log(rng, 20, min(1300, 1800 // docs) // most)
         return _shared_case(None, heads, dtype, docs, q, q, _log(rng, 30, 2048 // most), min(docs, rng.choice([1, 1, 2])), mix,
                             rng.choice([0, 1, 32]), cap, bias, rng.choice([0, 0, 1]), pad)
     widths, dtype = rng.choice(list(WIDTHS)), rng.choice(["bf16", "bf16", "bf16", "f32"])
