@@ -558,6 +558,50 @@ typedef struct dllm_sample_args {
 int dllm_sample_workspace_size(int32_t rows, int32_t vocab, size_t* bytes);
 int dllm_sample(const dllm_sample_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
+/*
+ * Low-rank adapters of many requests beside a shared projection.  Row m of x has the
+ * adapter a = which[m]; the projection's columns fall into slices (queries, keys and
+ * values of one product, gate and up) with an A each:
+ *   out[m, n] = base[m, n] + scales[a] sum_{j < ranks[a]} b[a, n, j] sum_k a[a, s(n), j, k] x[m, k]
+ * A row whose which is no adapter (negative, or >= adapters) gets its base.  base is
+ * what the shared projection gave; NULL: zeros.  Slice s holds the columns
+ * slice_end[s - 1] .. slice_end[s] - 1 (the first from 0 on, the last up to d_out).
+ * Views: x {row: stride_l} [rows, d_in]; a {adapter: stride_b, slice: stride_h,
+ * rank: stride_l}, d_in contiguous; b {adapter: stride_b, column: stride_l}, rank
+ * contiguous; base and out {row: stride_l} [rows, d_out].  Strides not named are not read.
+ * ranks: device int32 [adapters], cut to [0, rank]; NULL: rank.  What lies behind an
+ * adapter's rank is not used.  scales: device float32 [adapters]; NULL: 1.
+ * Storage: x, a and b float32 or bf16 (dtype); base and out of out_dtype, bf16 or, for
+ * either dtype, float32.  Both products accumulate in float32; of the inner one 16 bits
+ * enter the outer one where out is bf16, all 24 else; the result is rounded once.  A
+ * result does not depend on the other rows, nor on their order.  A NaN or an infinity in
+ * x or in a row's own adapter reaches that row alone; an infinite element of b may give
+ * NaN where the formula has an infinity.
+ * out may be base (same data and stride); apart from that it must not overlap anything
+ * the call reads.  Data and strides at multiples of 16 bytes are read in such pieces,
+ * others by the element.
+ * Requirements: 0 <= rows <= 2^22; 1 <= d_in, d_out <= 2^20; 0 <= adapters <= 4095; 1 <=
+ * rank <= 256; 1 <= slices <= DLLM_ADAPTER_SLICES, slice_end rising and ending at d_out;
+ * strides not negative, that of out's rows at least d_out.  rows of 0: nothing.
+ */
+enum { DLLM_ADAPTER_SLICES = 4 };
+typedef struct dllm_adapter_args {
+  int32_t dtype, out_dtype;
+  int32_t rows, d_in, d_out, adapters, rank, slices;
+  int32_t slice_end[DLLM_ADAPTER_SLICES]; /* host */
+  dllm_view x, a, b, base, out;
+  const int32_t* which; /* device [rows] */
+  const int32_t* ranks;
+  const float* scales;
+} dllm_adapter_args;
+
+/* Bytes of workspace dllm_adapters needs for these sizes (arrays and tensors are not
+ * looked at).  The workspace, 256-byte aligned, holds nothing between calls. */
+int dllm_adapters_workspace_size(const dllm_adapter_args* args, size_t* bytes);
+/* Errors: DLLM_EINVAL (null pointer, dtype), DLLM_ESHAPE (sizes, strides),
+ * DLLM_ENOMEM (workspace), DLLM_EHIP. */
+int dllm_adapters(const dllm_adapter_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing with HIP events recorded on the launch stream around each
  * launch of the selected kernel classes.  kind: 0 = q/k/v GEMM (with RoPE),
  * 1 = attention, 2 = LM head + reduction, 3 = commit, 4 = norms and

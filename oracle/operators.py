@@ -1,5 +1,5 @@
 """Stand-alone operators in float64 (oracle): rotary positions, attention of
-documents, sampling.  Written from their definitions in include/dllm.h.
+documents, sampling, low-rank adapters.  Written from their definitions in include/dllm.h.
 
 Test infrastructure only; see the package docstring.
 """
@@ -102,3 +102,19 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask_id=-1
     u = min(max(u, 0.0), 1 - 2.0 ** -24) if u == u else 0.0
     token = min(int((c <= u * c[-1]).sum()), int(np.nonzero(kept)[0].max()))
     return token, float(e[token] / e.sum()), float(w[token] / c[-1])
+
+
+def adapters(x, base, A, B, which, ranks, scales, ends):
+    """x [M, K], base [M, N], A [n, S, R, K], B [n, N, R]; ends: each slice's last column + 1.  Returns out [M, N] and
+    mass [M, N] = |scale| sum_j |B_j| sum_k |A_jk x_k|, what the two products' errors are relative to."""
+    out, mass = np.array(base, dtype=np.float64, copy=True), np.zeros(base.shape)
+    for m, a in enumerate(which):
+        if not 0 <= a < len(A):
+            continue
+        r, first = int(min(max(ranks[a], 0), A.shape[2])), 0
+        for s, end in enumerate(ends):
+            b = B[a, first:end, :r]
+            out[m, first:end] += scales[a] * (b @ (A[a, s, :r] @ x[m]))
+            mass[m, first:end] = abs(scales[a]) * (np.abs(b) @ (np.abs(A[a, s, :r]) @ np.abs(x[m])))
+            first = end
+    return out, mass

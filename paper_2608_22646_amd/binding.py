@@ -76,6 +76,15 @@ class SampleArgs(_c.Structure):
                 ("token", _vp), ("conf", _vp), ("prob", _vp)]
 
 
+ADAPTER_SLICES = 4
+
+
+class AdapterArgs(_c.Structure):
+    _fields_ = [("dtype", _i32), ("out_dtype", _i32), ("rows", _i32), ("d_in", _i32), ("d_out", _i32), ("adapters", _i32),
+                ("rank", _i32), ("slices", _i32), ("slice_end", _i32 * ADAPTER_SLICES), ("x", View), ("a", View), ("b", View),
+                ("base", View), ("out", View), ("which", _vp), ("ranks", _vp), ("scales", _vp)]
+
+
 class DllmError(RuntimeError):
     def __init__(self, code, msg):
         super().__init__(f"dllm error {code}: {msg}")
@@ -119,6 +128,8 @@ _SIGS = {
     "dllm_attention": (_i32, [_c.POINTER(AttnArgs), _vp, _sz, _vp]),
     "dllm_sample_workspace_size": (_i32, [_i32, _i32, _c.POINTER(_sz)]),
     "dllm_sample": (_i32, [_c.POINTER(SampleArgs), _vp, _sz, _vp]),
+    "dllm_adapters_workspace_size": (_i32, [_c.POINTER(AdapterArgs), _c.POINTER(_sz)]),
+    "dllm_adapters": (_i32, [_c.POINTER(AdapterArgs), _vp, _sz, _vp]),
     "dllm_prof_enable": (_i32, [_vp, _i32]),
     "dllm_prof_read": (_i32, [_vp, _i32, _c.POINTER(_f64), _c.POINTER(_c.c_int64)]),
     "dllm_prof_every": (_i32, [_vp, _i32]),
@@ -762,3 +773,65 @@ def sample_workspace_size(rows, vocab):
     n = _sz()
     check(lib().dllm_sample_workspace_size(rows, vocab, n))
     return n.value
+
+
+def adapters(x, base, A, B, which, ranks=None, scales=None, slices=None, out=None, ws=None, stream=None):
+    """dllm_adapters on x [rows, d_in] with A [adapters, slices, rank, d_in] (or [adapters, rank, d_in]: one slice) and
+    B [adapters, d_out, rank], any strides with contiguous last dimensions.  base: the shared projection's result [rows,
+    d_out] (None: zeros); which: int32 [rows]; ranks int32 and scales float32 [adapters]; slices: the columns of each slice.
+    out: written and returned (new if None, of base's type, or of x's; base itself: in place)."""
+    _refuse(x.dim() == 2 and A.dim() in (3, 4) and B.dim() == 3, -2,
+            "x must be [rows, d_in], A [adapters, slices, rank, d_in] or [adapters, rank, d_in], B [adapters, d_out, rank]")
+    dev = x.device
+    scope = _elsewhere(dev, stream)
+    if scope is not None:
+        with scope:
+            return adapters(x, base, A, B, which, ranks, scales, slices, out, ws)
+    a, out = _adapter_args(x, base, A, B, which, ranks, scales, slices, out)
+    if ws is None:
+        n = _sz()
+        check(lib().dllm_adapters_workspace_size(a, n))
+        ws = _workspace(n.value, dev) if n.value else None
+    else:
+        _given(ws, dev)
+    check(lib().dllm_adapters(a, _ptr(ws), 0 if ws is None else ws.nbytes, _raw_stream(dev.index)))
+    return out
+
+
+def adapters_workspace_size(x, base, A, B, slices=None):
+    """Bytes of workspace that adapters() needs for operands of these sizes."""
+    n = _sz()
+    a, _ = _adapter_args(x, base, A, B, None, None, None, slices, base)
+    check(lib().dllm_adapters_workspace_size(a, n))
+    return n.value
+
+
+def _matrix(t, shape, dtype, device, name):
+    """The view of a tensor of this shape ([rows, n], [adapters, rows, n] or [adapters, slices, rows, n])."""
+    st = t.stride()
+    if t.shape != shape or (st[-1] != 1 and shape[-1] > 1) or t.dtype is not dtype or t.device != device:
+        _refuse(t.shape == shape, -2, f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
+        _refuse(st[-1] == 1 or shape[-1] <= 1 or t.numel() == 0, -2, f"{name}: elements of a row must be contiguous")
+        _refuse(t.dtype is dtype and t.device == device, -1, f"{name} must be {dtype} on {device}")
+    n = len(shape)
+    return View(t.data_ptr(), st[0] if n > 2 else 0, st[-2], st[1] if n > 3 else 0)
+
+
+def _adapter_args(x, base, A, B, which, ranks, scales, slices, out):
+    dt, dev = _dtype(x, "x"), x.device
+    (M, K), (n, N, R) = x.shape, B.shape
+    S = A.shape[1] if A.dim() == 4 else 1
+    kind = x.dtype if base is None and out is None else (base if base is not None else out).dtype
+    _refuse(kind in _DTYPES, -1, "base and out must be float32 or bfloat16")
+    if out is None:
+        out = torch.empty((M, N), dtype=kind, device=dev)
+    ends = [N] if slices is None else list(itertools.accumulate(slices))
+    _refuse(len(ends) == S, -2, f"A has {S} slices, slices names {len(ends)}")
+    _in32(M, K, n, N, R, *ends)
+    _refuse(S <= ADAPTER_SLICES, -2, f"at most {ADAPTER_SLICES} slices")
+    a = AdapterArgs(dt, _DTYPES[kind], M, K, N, n, R, S, (_i32 * ADAPTER_SLICES)(*ends), _matrix(x, (M, K), x.dtype, dev, "x"),
+                    _matrix(A, (n, S, R, K) if A.dim() == 4 else (n, R, K), x.dtype, dev, "A"),
+                    _matrix(B, (n, N, R), x.dtype, dev, "B"), View() if base is None else _matrix(base, (M, N), kind, dev, "base"),
+                    _matrix(out, (M, N), kind, dev, "out"), _column(which, M, torch.int32, dev, "which"),
+                    _column(ranks, n, torch.int32, dev, "ranks"), _column(scales, n, torch.float32, dev, "scales"))
+    return a, out

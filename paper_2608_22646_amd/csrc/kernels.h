@@ -254,4 +254,27 @@ size_t sample_bytes(int rows, int vocab);
 bool sample_fits(int rows, int vocab);  // its grid can be launched
 void launch_sample(const SampleArgs& a, void* ws, hipStream_t s);
 
+// k_adapters.hip: see dllm_adapters; ws of adapters_bytes(a) bytes.
+struct AdaptersArgs {
+  int dtype, out_dtype, rows, d_in, d_out, adapters, rank, slices;
+  int slice_end[DLLM_ADAPTER_SLICES];
+  AttnView x, a, b, base, out;
+  const int32_t *which, *ranks;
+  const float* scales;
+};
+// Layout of a call: whether the rows are sorted by adapter first, tiles of the grid,
+// 16-blocks of ranks of a shrinking workgroup, shares of d_in and the steps of one,
+// columns of an expanding workgroup, ranks padded to 16; whether
+// whole 16-byte pieces may be read of x and a, and of b, base and out; and what the
+// workspace holds.
+struct AdaptersPlan {
+  int sorted, tiles, j, splits, steps, cols, r16, vec_in, vec;
+  float* part;  // [splits][rows][slices][r16]
+  int4* tile;   // adapter, first place in order, rows
+  int* order;   // [rows]
+};
+__host__ __device__ inline int ceil_steps(int n, int step) { return (n + step - 1) / step; }
+size_t adapters_bytes(const AdaptersArgs& a);
+void launch_adapters(const AdaptersArgs& a, void* ws, hipStream_t s);
+
 }  // namespace dllm

@@ -1,5 +1,5 @@
 // C ABI of the stand-alone operators (see include/dllm.h): argument checks and
-// launches of rotary positions, attention over documents, and sampling.
+// launches of rotary positions, attention over documents, sampling, and adapters.
 #include <math.h>
 
 #include "api.h"
@@ -91,6 +91,32 @@ void check_workspace(const void* ws, size_t bytes, size_t need) {
 void check_sample_sizes(int rows, int vocab) {
   require(rows >= 0 && vocab >= 1 && vocab <= (1 << 22), DLLM_ESHAPE, "rows must be >= 0 and vocab in [1, 2^22]");
   require(sample_fits(rows, vocab), DLLM_ESHAPE, "too many rows of this vocabulary for one call");
+}
+
+// The sizes of an adapters call; false where there is nothing to do.
+bool adapter_sizes(const dllm_adapter_args* p, AdaptersArgs* a) {
+  require(p != nullptr, DLLM_EINVAL, "args is NULL");
+  check_dtype(p->dtype);
+  require(p->out_dtype == DLLM_F32 || p->out_dtype == p->dtype, DLLM_EINVAL, "out_dtype must be DLLM_F32 or dtype");
+  require(p->rows >= 0 && p->rows <= (1 << 22), DLLM_ESHAPE, "rows must be in [0, 2^22]");
+  require(p->d_in >= 1 && p->d_in <= (1 << 20) && p->d_out >= 1 && p->d_out <= (1 << 20), DLLM_ESHAPE,
+          "d_in and d_out must be in [1, 2^20]");
+  require(p->adapters >= 0 && p->adapters <= 4095, DLLM_ESHAPE, "adapters must be in [0, 4095]");
+  require(p->rank >= 1 && p->rank <= 256, DLLM_ESHAPE, "rank must be in [1, 256]");
+  require(p->slices >= 1 && p->slices <= DLLM_ADAPTER_SLICES, DLLM_ESHAPE, "slices must be in [1, DLLM_ADAPTER_SLICES]");
+  for (int s = 0; s < p->slices; ++s)
+    require(p->slice_end[s] > (s ? p->slice_end[s - 1] : 0) && (s + 1 < p->slices || p->slice_end[s] == p->d_out), DLLM_ESHAPE,
+            "slice_end must rise from above 0 and end at d_out");
+  a->dtype = p->dtype;
+  a->out_dtype = p->out_dtype;
+  a->rows = p->rows;
+  a->d_in = p->d_in;
+  a->d_out = p->d_out;
+  a->adapters = p->adapters;
+  a->rank = p->rank;
+  a->slices = p->slices;
+  for (int s = 0; s < p->slices; ++s) a->slice_end[s] = p->slice_end[s];
+  return p->rows > 0;
 }
 
 }  // namespace
@@ -213,6 +239,43 @@ int dllm_sample(const dllm_sample_args* p, void* ws, size_t ws_bytes, void* stre
   a.prob = p->prob;
   check_workspace(ws, ws_bytes, sample_bytes(p->rows, p->vocab));
   launch_sample(a, ws, (hipStream_t)stream);
+  API_END
+}
+
+int dllm_adapters_workspace_size(const dllm_adapter_args* p, size_t* bytes) {
+  API_BEGIN
+  require(bytes != nullptr, DLLM_EINVAL, "bytes is NULL");
+  AdaptersArgs a{};
+  *bytes = adapter_sizes(p, &a) ? adapters_bytes(a) : 0;
+  API_END
+}
+
+int dllm_adapters(const dllm_adapter_args* p, void* ws, size_t ws_bytes, void* stream) {
+  API_BEGIN
+  AdaptersArgs a{};
+  if (!adapter_sizes(p, &a)) return DLLM_OK;
+  check_view(&p->out, "out");
+  require(p->which != nullptr, DLLM_EINVAL, "which is NULL");
+  require(p->rows == 1 || p->out.stride_l >= p->d_out, DLLM_ESHAPE, "stride_l of out must be at least d_out");
+  if (p->base.data) check_view(&p->base, "base");
+  if (p->adapters > 0) {
+    check_view(&p->x, "x");
+    check_view(&p->a, "a");
+    check_view(&p->b, "b");
+  }
+  // strides that no element steps over, or that are not named, say nothing
+  auto used = [&](const dllm_view& v, bool b, bool l, bool h) { return AttnView{v.data, b ? v.stride_b : 0, l ? v.stride_l : 0, h ? v.stride_h : 0}; };
+  a.x = used(p->x, false, p->rows > 1, false);
+  a.a = used(p->a, p->adapters > 1, p->rank > 1, p->slices > 1);
+  a.b = used(p->b, p->adapters > 1, p->d_out > 1, false);
+  a.base = used(p->base, false, p->rows > 1, false);
+  a.out = used(p->out, false, p->rows > 1, false);
+  require(a.base.data != a.out.data || a.base.stride_l == a.out.stride_l, DLLM_ESHAPE, "out that is base must have its stride");
+  a.which = p->which;
+  a.ranks = p->ranks;
+  a.scales = p->scales;
+  check_workspace(ws, ws_bytes, adapters_bytes(a));
+  launch_adapters(a, ws, (hipStream_t)stream);
   API_END
 }
 
