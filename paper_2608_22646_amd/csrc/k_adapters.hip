@@ -14,44 +14,29 @@
 //     columns, column n = 8 c + i by lane c's i-th product, so that a lane reads and
 //     writes 8 consecutive elements of base and out.
 #include <algorithm>
+#include <type_traits>
 
 #include "kernels.h"
+#include "lds_dma.h"
 
 namespace dllm {
 
 namespace {
 
 constexpr int TM = 32;           // rows of a tile
+constexpr int NW = 8;            // waves of a shrinking workgroup
 constexpr int COLS = 128;        // columns of a wave's block
 constexpr int SORT_THREADS = 1024;
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
+typedef uint32_t quad_t __attribute__((ext_vector_type(4), may_alias));  // of LDS that LDS-DMA wrote
 
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 __device__ __forceinline__ int adapter_of(const AdaptersArgs& a, int row) {
   const int w = a.which[row];
   return w >= 0 && w < a.adapters ? w : -1;
 }
 __device__ __forceinline__ int rank_of(const AdaptersArgs& a, int adapter) {
   return a.ranks ? min(max(a.ranks[adapter], 0), a.rank) : a.rank;
-}
-
-// 16 bytes at p, of which the first n elements count (the rest give zeros and are
-// not touched); whole: n is known to be all of them and p a multiple of 16.
-template <typename T>
-__device__ __forceinline__ u32x4_t piece(const T* p, int n, bool whole) {
-  if (whole) return *reinterpret_cast<const u32x4_t*>(p);
-  constexpr int E = 16 / sizeof(T);
-  u32x4_t w = {0, 0, 0, 0};
-#pragma unroll
-  for (int e = 0; e < E; ++e)
-    if (e < n) {
-      if constexpr (sizeof(T) == 2)
-        w[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
-      else
-        w[e] = __float_as_uint(p[e]);
-    }
-  return w;
 }
 
 // A tile's rows in `rows` (LDS), how many, and their adapter (-1: none); count 0:
@@ -65,13 +50,15 @@ __device__ __forceinline__ Tile tile_of(const AdaptersArgs& a, const AdaptersPla
   if (p.sorted) {
     const int4 d = p.tile[i];
     t = Tile{uniform(d.x), uniform(d.z)};
-    if (threadIdx.x < TM && (int)threadIdx.x < t.count) rows[threadIdx.x] = p.order[d.y + threadIdx.x];
+    if ((int)threadIdx.x < t.count) rows[threadIdx.x] = p.order[d.y + threadIdx.x];
   } else {
-    const int row = (i & ~(TM - 1)) + lane;
+    // tile i: the i / groups-th of the 32 rows of group i % groups (rows that share an
+    // adapter leave the first of them at work: those lie on consecutive XCDs)
+    const int groups = (p.tiles + TM - 1) / TM, me = i / groups, row = i % groups * TM + lane;
     const int w = lane < TM && row < a.rows ? adapter_of(a, row) : -2;
-    t.adapter = __builtin_amdgcn_readlane(w, i & (TM - 1));
+    t.adapter = __builtin_amdgcn_readlane(w, me);
     const unsigned long long mine = __ballot(w == t.adapter);
-    t.count = __ffsll(mine) - 1 == (i & (TM - 1)) ? __popcll(mine) : 0;
+    t.count = t.adapter >= -1 && __ffsll(mine) - 1 == me ? __popcll(mine) : 0;
     if (threadIdx.x < 64 && w == t.adapter) rows[__popcll(mine & ((1ull << lane) - 1))] = row;
   }
   __syncthreads();
@@ -170,7 +157,26 @@ struct Kind {
   static constexpr int STEP = 4 * E;        // along k: 64 bytes of a row, a piece for each 16 lanes
 };
 
-// c += the products of two fragments of a step
+// 16 bytes at p, of which the first n elements count (the rest give zeros; none but
+// the first is touched behind them).
+template <typename T>
+__device__ __forceinline__ u32x4_t piece(const T* p, int n) {
+  constexpr int E = Kind<T>::E;
+  T v[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = p[e < n ? e : 0];
+  u32x4_t w = {0, 0, 0, 0};
+#pragma unroll
+  for (int e = 0; e < E; ++e) {
+    if constexpr (sizeof(T) == 2)
+      w[e / 2] |= e < n ? (uint32_t)v[e] << (16 * (e & 1)) : 0u;
+    else
+      w[e] = e < n ? __float_as_uint(v[e]) : 0u;
+  }
+  return w;
+}
+
+// c + the products of two fragments of a step
 template <typename T>
 __device__ __forceinline__ f32x4_t product(u32x4_t x, u32x4_t y, f32x4_t c) {
   if constexpr (sizeof(T) == 2)
@@ -180,319 +186,450 @@ __device__ __forceinline__ f32x4_t product(u32x4_t x, u32x4_t y, f32x4_t c) {
   return c;
 }
 
-// 16 MT rows by 16 J ranks (those of 16-blocks u0 .. of the adapter) over the steps
-// of this share; acc[mt][j]: lane l holds row l % 16, ranks 4 (l / 16) ..
-template <typename T, int MT, int J>
-__device__ __forceinline__ void shrink_tile(const AdaptersArgs& a, const AdaptersPlan& p, const Tile& t, const int* rows, int u0, int n16,
-                                            int s0, int s1, f32x4_t* red) {
-  constexpr int E = Kind<T>::E, STEP = Kind<T>::STEP, U = J >= 8 ? 2 : J == 1 ? 8 : 4;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
-  const T *x[MT], *w[J];
+// Ranks c .. of a row's inner products, as the outer product's operand takes them: scaled,
+// nothing from the adapter's rank on, in PARTS summands.  Piece c / E of slice s lies at
+// h[s][c / E / 4][part][c / E % 4][row].
+template <typename T, int PARTS>
+__device__ __forceinline__ void summands(int c, int rank, float scale, float (&v)[Kind<T>::E], u32x4_t (&w)[PARTS]) {
+  constexpr int E = Kind<T>::E;
 #pragma unroll
-  for (int m = 0; m < MT; ++m) {
-    const int i = m * 16 + l16;
-    x[m] = static_cast<const T*>(a.x.data) + rows[i < t.count ? i : 0] * a.x.stride_l + g * E;
-  }
-  const int units = a.slices * n16, rank = rank_of(a, t.adapter);
+  for (int e = 0; e < E; ++e) v[e] = c + e < rank ? v[e] * scale : 0.f;
 #pragma unroll
-  for (int j = 0; j < J; ++j) {
-    const int u = min(u0 + j, units - 1), s = u / n16;
-    w[j] = static_cast<const T*>(a.a.data) + t.adapter * a.a.stride_b + s * a.a.stride_h +
-           min((u % n16) * 16 + l16, rank - 1) * a.a.stride_l + g * E;
-  }
-  f32x4_t acc[MT][J];
+  for (int q = 0; q < PARTS; ++q) {
+    if constexpr (sizeof(T) == 4) {
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+      for (int e = 0; e < 4; ++e) w[q][e] = __float_as_uint(v[e]);
+    } else {
+      // the value rounded to bf16, then what is left of it (nothing of an infinity)
 #pragma unroll
-    for (int j = 0; j < J; ++j) acc[m][j] = f32x4_t{0, 0, 0, 0};
-  // steps whose pieces are whole, U at a time; then the rest, one at a time
-  const int whole = p.vec_in ? min(s1, a.d_in / STEP) : s0;
-  int b = s0 + wave * U;
-  for (; b + U <= whole; b += 4 * U) {
-    u32x4_t xf[U][MT], wf[U][J];
+      for (int e = 0; e < 8; e += 2) {
+        w[q][e / 2] = pack_bf16x2(v[e], v[e + 1]);
 #pragma unroll
-    for (int i = 0; i < U; ++i) {
-#pragma unroll
-      for (int m = 0; m < MT; ++m) xf[i][m] = *reinterpret_cast<const u32x4_t*>(x[m] + (long)(b + i) * STEP);
-#pragma unroll
-      for (int j = 0; j < J; ++j) wf[i][j] = *reinterpret_cast<const u32x4_t*>(w[j] + (long)(b + i) * STEP);
-    }
-#pragma unroll
-    for (int i = 0; i < U; ++i)
-#pragma unroll
-      for (int m = 0; m < MT; ++m)
-#pragma unroll
-        for (int j = 0; j < J; ++j) acc[m][j] = product<T>(wf[i][j], xf[i][m], acc[m][j]);
-  }
-  for (; b < s1; b += 4 * U)
-    for (int i = b; i < min(b + U, s1); ++i) {
-      const int n = a.d_in - i * STEP - g * E;
-      const bool all = i < whole;
-      u32x4_t xf[MT];
-#pragma unroll
-      for (int m = 0; m < MT; ++m) xf[m] = piece(x[m] + (long)i * STEP, n, all);
-#pragma unroll
-      for (int j = 0; j < J; ++j) {
-        const u32x4_t wf = piece(w[j] + (long)i * STEP, n, all);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) acc[m][j] = product<T>(wf, xf[m], acc[m][j]);
+        for (int d = 0; d < 2; ++d) {
+          const float top = __uint_as_float(d ? w[q][e / 2] & 0xffff0000u : w[q][e / 2] << 16);
+          v[e + d] = fabsf(top) < INFINITY ? v[e + d] - top : 0.f;
+        }
       }
     }
+  }
+}
+// Sum of the shares of E ranks of a row, in their order.
+template <typename T>
+__device__ __forceinline__ void sum_shares(const AdaptersArgs& a, const AdaptersPlan& p, int row, int s, int c, float (&v)[Kind<T>::E]) {
+  constexpr int E = Kind<T>::E;
+  const float* from = p.part + ((size_t)row * a.slices + s) * p.r16 + c;
+  const size_t next = (size_t)a.rows * a.slices * p.r16;
+  auto shares = [&](auto N, int z) {
+    f32x4_t w[N][E / 4];
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int q = 0; q < E / 4; ++q) w[k][q] = *reinterpret_cast<const f32x4_t*>(from + (z + k) * next + 4 * q);
+#pragma unroll
+    for (int k = 0; k < N; ++k)
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[e] += w[k][e / 4][e % 4];
+  };
+#pragma unroll
+  for (int e = 0; e < E; ++e) v[e] = 0.f;
+  int z = 0;
+  for (; z + 4 <= p.splits; z += 4) shares(std::integral_constant<int, 4>{}, z);
+  if (z + 2 <= p.splits) {
+    shares(std::integral_constant<int, 2>{}, z);
+    z += 2;
+  }
+  if (z < p.splits) shares(std::integral_constant<int, 1>{}, z);
+}
+template <typename T, int PARTS>
+__device__ __forceinline__ void keep_piece(const AdaptersArgs& a, const AdaptersPlan& p, int row, int s, int c, int rank, float scale,
+                                           float (&v)[Kind<T>::E]) {
+  constexpr int E = Kind<T>::E;
+  u32x4_t w[PARTS];
+  summands<T, PARTS>(c, rank, scale, v, w);
+#pragma unroll
+  for (int q = 0; q < PARTS; ++q) p.h[(((size_t)s * p.hsteps + c / (4 * E)) * PARTS + q) * 4 * a.rows + (size_t)(c / E % 4) * a.rows + row] = w[q];
+}
+
+// What a shrinking workgroup computes: 16-blocks u0 .. u0 + J - 1 of its adapter's ranks
+// (of `units`, n16 a slice).
+struct Ranks {
+  int rank, n16, units, u0;
+};
+// Row of A behind rank l of block u (the last one behind those that are not there).
+template <typename T>
+__device__ __forceinline__ const T* a_row(const AdaptersArgs& a, int adapter, const Ranks& k, int u, int l) {
+  u = min(u, k.units - 1);
+  return static_cast<const T*>(a.a.data) + adapter * a.a.stride_b + u / k.n16 * a.a.stride_h + min(u % k.n16 * 16 + l, k.rank - 1) * a.a.stride_l;
+}
+
+// The waves' sums of products, acc[mt][j] (lane l: row l % 16, ranks 4 (l / 16) ..), to
+// the workspace.
+template <typename T, int PARTS, int MT, int J>
+__device__ __forceinline__ void gather(const AdaptersArgs& a, const AdaptersPlan& p, const Tile& t, const int* rows, const Ranks& k,
+                                       const f32x4_t (&acc)[MT][J], f32x4_t* red) {
+  constexpr int E = Kind<T>::E, Q = E / 4;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+  const float scale = a.scales ? a.scales[t.adapter] : 1.f;
+  __syncthreads();
 #pragma unroll
   for (int m = 0; m < MT; ++m)
 #pragma unroll
     for (int j = 0; j < J; ++j) red[((wave * MT + m) * J + j) * 64 + lane] = acc[m][j];
   __syncthreads();
-  const size_t width = (size_t)a.slices * p.r16;
-  float* part = p.part + (size_t)blockIdx.y * a.rows * width;
-  for (int i = threadIdx.x; i < MT * J * 64; i += 256) {
-    const int l = i & 63, j = (i >> 6) % J, row = (i >> 6) / J * 16 + (l & 15), u = u0 + j;
-    if (row >= t.count || u >= units) continue;
-    f32x4_t v = red[i];
+  // a piece of E ranks of a row each
+  for (int i = threadIdx.x; i < MT * J * 64 / Q; i += NW * 64) {
+    const int l = i & 15, g4 = (i >> 4) % (4 / Q) * Q, mj = i / (64 / Q), m = mj / J, u = k.u0 + mj % J;
+    if (m * 16 + l >= t.count || u >= k.units) continue;
+    float v[E];
 #pragma unroll
-    for (int k = 1; k < 4; ++k) v += red[k * MT * J * 64 + i];
-    *reinterpret_cast<f32x4_t*>(part + rows[row] * width + (u / n16) * p.r16 + (u % n16) * 16 + 4 * (l >> 4)) = v;
+    for (int q = 0; q < Q; ++q) {
+      f32x4_t sum = red[mj * 64 + (g4 + q) * 16 + l];
+#pragma unroll
+      for (int w = 1; w < NW; ++w) sum += red[(w * MT * J + mj) * 64 + (g4 + q) * 16 + l];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * q + e] = sum[e];
+    }
+    const int row = rows[m * 16 + l], s = u / k.n16, c = u % k.n16 * 16 + 4 * g4;
+    if (p.keep) {
+      keep_piece<T, PARTS>(a, p, row, s, c, k.rank, scale, v);
+    } else {
+      float* to = p.part + (((size_t)blockIdx.y * a.rows + row) * a.slices + s) * p.r16 + c;
+#pragma unroll
+      for (int q = 0; q < Q; ++q) *reinterpret_cast<f32x4_t*>(to + 4 * q) = f32x4_t{v[4 * q], v[4 * q + 1], v[4 * q + 2], v[4 * q + 3]};
+    }
   }
 }
 
-template <typename T, int J>
-__global__ void __launch_bounds__(256) adapters_shrink_kernel(AdaptersArgs a, AdaptersPlan p) {
+// Operands in whole pieces.  Rows of x, then of A, each CHUNK bytes along k a stage, by
+// LDS-DMA: a load brings 1 KiB of one row (what neighbouring lanes read of 16 rows a few
+// KiB apart would lie in few of the L2's channels); piece c of row r in slot c ^ (r % 16),
+// so that 16 rows' pieces meet all banks.  Each wave multiplies two of a stage's 16 steps.
+// One stage at a time and two workgroups a CU, one loading while the other multiplies (8448
+// rows to 2 x 16 ranks, sort and expand included: 196 us; two stages of one workgroup 199).
+constexpr int CHUNK = 1024;
+template <typename T, int PARTS, int MT, int J>
+__device__ __forceinline__ void shrink_tile(const AdaptersArgs& a, const AdaptersPlan& p, const Tile& t, const int* rows, const Ranks& k, char* lds) {
+  constexpr int ROWS = 16 * (MT + J), PER = ROWS / NW;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
+  const uint32_t bytes = (uint32_t)(a.d_in * sizeof(T));
+  // this wave's rows
+  const char* from[PER];
+#pragma unroll
+  for (int i = 0; i < PER; ++i) {
+    const int r = wave + NW * i;
+    const T* q = r < 16 * MT ? static_cast<const T*>(a.x.data) + rows[min(r, t.count - 1)] * a.x.stride_l
+                             : a_row<T>(a, t.adapter, k, k.u0 + (r - 16 * MT) / 16, (r - 16 * MT) % 16);
+    from[i] = uniform(reinterpret_cast<const char*>(q));
+  }
+  const uint32_t to = lds_address(lds) + wave * CHUNK;
+  f32x4_t acc[MT][J];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int j = 0; j < J; ++j) acc[m][j] = f32x4_t{0, 0, 0, 0};
+  const int c0 = blockIdx.y * p.steps, n = min(p.steps, (int)((bytes + CHUNK - 1) / CHUNK) - c0);
+  for (int u = 0; u < n; ++u) {
+    if (u) barrier_nofence();
+#pragma unroll
+    for (int i = 0; i < PER; ++i)
+      dma16(rsrc_of(from[i], bytes), (c0 + u) * CHUNK + (lane ^ ((wave + NW * i) & 15)) * 16, to + i * NW * CHUNK);
+    wait_vmcnt<0>();
+    barrier_nofence();
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int slot = ((wave * 2 + i) * 4 + g) ^ l16;
+      u32x4_t xf[MT], wf[J];
+#pragma unroll
+      for (int m = 0; m < MT; ++m) xf[m] = *reinterpret_cast<const quad_t*>(lds + (m * 16 + l16) * CHUNK + slot * 16);
+#pragma unroll
+      for (int j = 0; j < J; ++j) wf[j] = *reinterpret_cast<const quad_t*>(lds + ((MT + j) * 16 + l16) * CHUNK + slot * 16);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int j = 0; j < J; ++j) acc[m][j] = product<T>(wf[j], xf[m], acc[m][j]);
+    }
+  }
+  gather<T, PARTS>(a, p, t, rows, k, acc, reinterpret_cast<f32x4_t*>(lds));
+}
+
+// Operands that are read by the element: straight into registers, a step a wave.
+template <typename T, int PARTS, int MT>
+__device__ __forceinline__ void shrink_elements(const AdaptersArgs& a, const AdaptersPlan& p, const Tile& t, const int* rows, const Ranks& k,
+                                                f32x4_t* red) {
+  constexpr int E = Kind<T>::E, STEP = Kind<T>::STEP;
+  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
+  const T* x[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) x[m] = static_cast<const T*>(a.x.data) + rows[min(m * 16 + l16, t.count - 1)] * a.x.stride_l;
+  const T* w = a_row<T>(a, t.adapter, k, k.u0, l16);
+  f32x4_t acc[MT][1];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m][0] = f32x4_t{0, 0, 0, 0};
+  const int per = CHUNK / 64, s0 = blockIdx.y * p.steps * per, s1 = min(s0 + p.steps * per, (a.d_in + STEP - 1) / STEP);
+  for (int b = s0 + wave; b < s1; b += NW) {
+    // (a lane's first element may lie behind the last one: that is touched in its place)
+    const int at = b * STEP + g * E, n = a.d_in - at;
+    const u32x4_t wf = piece(w + min(at, a.d_in - 1), n);
+#pragma unroll
+    for (int m = 0; m < MT; ++m) acc[m][0] = product<T>(wf, piece(x[m] + min(at, a.d_in - 1), n), acc[m][0]);
+  }
+  gather<T, PARTS>(a, p, t, rows, k, acc, red);
+}
+
+template <typename T, int PARTS, int J, bool VEC>
+__global__ void __launch_bounds__(NW * 64) adapters_shrink_kernel(AdaptersArgs a, AdaptersPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  __shared__ f32x4_t red[4 * 2 * J * 64];
+  constexpr int STAGES = VEC ? 16 * (2 + J) * CHUNK : 0, SUMS = NW * 2 * J * 1024;
+  __shared__ __attribute__((aligned(1024))) char lds[STAGES > SUMS ? STAGES : SUMS];
   __shared__ int rows[TM];
   const Tile t = tile_of(a, p, blockIdx.x, rows);
   if (t.count == 0 || t.adapter < 0) return;
-  const int n16 = uniform((rank_of(a, t.adapter) + 15) >> 4), u0 = blockIdx.z * J, left = a.slices * n16 - u0;
-  if (left <= 0) return;
-  const int s0 = blockIdx.y * p.steps, s1 = min(s0 + p.steps, ceil_steps(a.d_in, Kind<T>::STEP));
-  if (t.count > 16) {
-    if (J > 4 && left > 4)
-      shrink_tile<T, 2, J>(a, p, t, rows, u0, n16, s0, s1, red);
-    else if (J > 2 && left > 2)
-      shrink_tile<T, 2, J < 4 ? J : 4>(a, p, t, rows, u0, n16, s0, s1, red);
-    else if (J > 1 && left > 1)
-      shrink_tile<T, 2, J < 2 ? J : 2>(a, p, t, rows, u0, n16, s0, s1, red);
+  Ranks k;
+  k.rank = uniform(rank_of(a, t.adapter));
+  k.n16 = (k.rank + 15) >> 4;
+  k.units = a.slices * k.n16;
+  k.u0 = blockIdx.z * J;
+  if (k.u0 >= k.units) return;
+  if constexpr (!VEC) {
+    if (t.count > 16)
+      shrink_elements<T, PARTS, 2>(a, p, t, rows, k, reinterpret_cast<f32x4_t*>(lds));
     else
-      shrink_tile<T, 2, 1>(a, p, t, rows, u0, n16, s0, s1, red);
+      shrink_elements<T, PARTS, 1>(a, p, t, rows, k, reinterpret_cast<f32x4_t*>(lds));
+  } else if (t.count > 16) {
+    if (J > 1 && k.units - k.u0 > 1)
+      shrink_tile<T, PARTS, 2, J>(a, p, t, rows, k, lds);
+    else
+      shrink_tile<T, PARTS, 2, 1>(a, p, t, rows, k, lds);
   } else {
-    if (J > 4 && left > 4)
-      shrink_tile<T, 1, J>(a, p, t, rows, u0, n16, s0, s1, red);
-    else if (J > 2 && left > 2)
-      shrink_tile<T, 1, J < 4 ? J : 4>(a, p, t, rows, u0, n16, s0, s1, red);
-    else if (J > 1 && left > 1)
-      shrink_tile<T, 1, J < 2 ? J : 2>(a, p, t, rows, u0, n16, s0, s1, red);
+    if (J > 1 && k.units - k.u0 > 1)
+      shrink_tile<T, PARTS, 1, J>(a, p, t, rows, k, lds);
     else
-      shrink_tile<T, 1, 1>(a, p, t, rows, u0, n16, s0, s1, red);
+      shrink_tile<T, PARTS, 1, 1>(a, p, t, rows, k, lds);
   }
 #endif
 }
 
-// Eight consecutive elements of base or out as floats.
-struct Eight {
-  float v[8];
-};
-template <typename O>
-__device__ __forceinline__ Eight load8(const O* p, int n, bool whole) {
-  constexpr int W = sizeof(O) / 2;
-  Eight r;
-#pragma unroll
-  for (int w = 0; w < W; ++w) {
-    const u32x4_t x = piece(p + w * (8 / W), n - w * (8 / W), whole);
-#pragma unroll
-    for (int e = 0; e < 8 / W; ++e) {
-      if constexpr (W == 1)
-        r.v[e] = __uint_as_float(e & 1 ? x[e / 2] & 0xffff0000u : x[e / 2] << 16);
-      else
-        r.v[w * 4 + e] = __uint_as_float(x[e]);
-    }
-  }
-  return r;
-}
-template <typename O>
-__device__ __forceinline__ void store8(O* p, const Eight& r, int n, bool whole) {
-  if (whole) {
-    if constexpr (sizeof(O) == 2) {
-      *reinterpret_cast<u32x4_t*>(p) =
-          u32x4_t{pack_bf16x2(r.v[0], r.v[1]), pack_bf16x2(r.v[2], r.v[3]), pack_bf16x2(r.v[4], r.v[5]), pack_bf16x2(r.v[6], r.v[7])};
-    } else {
-      *reinterpret_cast<f32x4_t*>(p) = f32x4_t{r.v[0], r.v[1], r.v[2], r.v[3]};
-      *reinterpret_cast<f32x4_t*>(p + 4) = f32x4_t{r.v[4], r.v[5], r.v[6], r.v[7]};
-    }
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (e < n) Act<O>::store(p, e, r.v[e]);
-  }
+// Sums the shares of the inner products, in their order: a piece of a row each thread.
+template <typename T, int PARTS>
+__global__ void __launch_bounds__(256) adapters_join_kernel(AdaptersArgs a, AdaptersPlan p) {
+#if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int E = Kind<T>::E;
+  const int row = (int)blockIdx.x * 256 + threadIdx.x, s = blockIdx.y / (p.r16 / E), c = blockIdx.y % (p.r16 / E) * E;
+  if (row >= a.rows) return;
+  const int w = adapter_of(a, row);
+  if (w < 0) return;
+  const int rank = rank_of(a, w);
+  if (c >= rank) return;
+  float v[E];
+  sum_shares<T>(a, p, row, s, c, v);
+  keep_piece<T, PARTS>(a, p, row, s, c, rank, a.scales ? a.scales[w] : 1.f, v);
+#endif
 }
 
-// A wave's block: rows of the tile by the columns n0 .. n0 + 127 below `end`.
-// FAST: all of them are there, in whole pieces, and so are b's ranks.
-template <typename T, typename O, int PARTS, int MT, bool FAST>
-__device__ __forceinline__ void expand_block(const AdaptersArgs& a, const Tile& t, const int* rows, const u32x4_t* h, int rank, int steps,
-                                             int n0, int end) {
+// Eight consecutive elements of base, as they were read.
+template <typename O>
+struct Eight {
+  static constexpr int W = sizeof(O) / 2;  // 16-byte pieces
+  u32x4_t w[W];
+  __device__ __forceinline__ float at(int e) const {
+    if constexpr (W == 1) return __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
+    return __uint_as_float(w[(e / 4) % W][e % 4]);
+  }
+};
+
+// A wave's share of a tile: its rows by the columns n0, n0 + 4 COLS, .. below `last`,
+// of a slice that ends at `end`.  VY, VB: base and out, b lie in whole 16-byte pieces.
+// ONE: the ranks are those of one step.
+template <typename T, typename O, int PARTS, bool VY, bool VB, bool ONE>
+__device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const AdaptersPlan& p, const Tile& t, const int* rows, int rank,
+                                               int steps, int slice, int n0, int last, int end) {
   constexpr int E = Kind<T>::E;
-  const int lane = threadIdx.x & 63, l16 = lane & 15, g = lane >> 4;
-  const int n = n0 + 8 * l16, left = end - n;
-  Eight y[MT][4];
+  const int lane = threadIdx.x & 63, g = lane >> 4, MT = (t.count + 15) >> 4;
+  const T* const b = static_cast<const T*>(a.b.data) + max(t.adapter, 0) * a.b.stride_b;
+  // base NULL: what is read in its place counts as zero
+  const O* const base = static_cast<const O*>(a.base.data ? a.base.data : a.out.data);
+  const int64_t base_stride = a.base.data ? a.base.stride_l : a.out.stride_l;
+  const uint32_t given = a.base.data ? 0xffffffffu : 0u;
+  // the part q of step s of the rows 16 m ..
+  const u32x4_t* const h = p.h + (size_t)slice * p.hsteps * PARTS * 4 * a.rows + (size_t)g * a.rows;
+  auto load_h = [&](int s, int q, int m) {
+    const int i = m * 16 + (lane & 15);
+    u32x4_t w = {0, 0, 0, 0};
+    if ((4 * s + g) * E < rank) w = h[(size_t)(s * PARTS + q) * 4 * a.rows + rows[i < t.count ? i : 0]];
+    return w;
+  };
+  u32x4_t hf[ONE ? 2 : 1][PARTS];
+  if constexpr (ONE) {
+    const float scale = a.scales && rank ? a.scales[t.adapter] : 1.f;
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
+    for (int m = 0; m < 2; ++m) {
+      const int i = m * 16 + (lane & 15);
+      float v[E];
+      if (g * E < rank) {
+        sum_shares<T>(a, p, rows[i < t.count ? i : 0], slice, g * E, v);
+      } else {
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = m * 16 + 4 * g + r;
-      if (a.base.data && i < t.count)
-        y[m][r] = load8(static_cast<const O*>(a.base.data) + rows[i] * a.base.stride_l + n, left, FAST);
-      else
-        y[m][r] = Eight{};
+        for (int e = 0; e < E; ++e) v[e] = 0.f;
+      }
+      summands<T, PARTS>(g * E, rank, scale, v, hf[m]);
     }
-  f32x4_t acc[MT][8];
+  }
+  for (int nb = n0; nb < last; nb += 4 * COLS) {
+    const int n = nb + 8 * (lane & 15), left = end - n;
+    const int col = VY ? (left >= 8 ? n : nb) : n;  // columns that are not there: others' are read in their place
+    // b's pieces of step s
+    auto load_b = [&](int s, u32x4_t (&bf)[8]) {
+      const int c = (4 * s + g) * E, c0 = c < rank ? c : 0;  // (ranks that are not there: h has zeros)
 #pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) acc[m][i] = f32x4_t{0, 0, 0, 0};
-  const T* b = static_cast<const T*>(a.b.data) + t.adapter * a.b.stride_b;
-  for (int s = 0; s < steps; ++s) {
-    const int c = (4 * s + g) / PARTS * E;  // the piece's first rank
-    u32x4_t hf[MT], bf[8];
-#pragma unroll
-    for (int m = 0; m < MT; ++m) hf[m] = h[(s * MT + m) * 64 + lane];
-    if constexpr (FAST) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) bf[i] = c < rank ? *reinterpret_cast<const u32x4_t*>(b + (n + i) * a.b.stride_l + c) : u32x4_t{0, 0, 0, 0};
-      if (rank % E) {  // what lies behind the rank is not used, be it no number
+      for (int i = 0; i < 8; ++i) {
+        const T* from = b + min(col + i, end - 1) * a.b.stride_l + c0;
+        if constexpr (VB)
+          bf[i] = *reinterpret_cast<const u32x4_t*>(from);
+        else
+          bf[i] = piece(from, rank - c0);
+      }
+      if (VB && rank % E) {  // what lies behind the rank is not used, be it no number
         u32x4_t keep;
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
-          const int last = rank - c - w * (E / 4);  // elements of the word and behind it
-          keep[w] = last <= 0 ? 0u : E == 8 && last == 1 ? 0xffffu : 0xffffffffu;
+          const int more = rank - c0 - w * (E / 4);  // elements of the word and behind it
+          keep[w] = more <= 0 ? 0u : E == 8 && more == 1 ? 0xffffu : 0xffffffffu;
         }
 #pragma unroll
         for (int i = 0; i < 8; ++i) bf[i] &= keep;
       }
-    } else {
+    };
+    auto load_y = [&](int m, Eight<O> (&y)[4]) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) bf[i] = piece(b + min(n + i, end - 1) * a.b.stride_l + c, rank - c, false);
-    }
+      for (int r = 0; r < 4; ++r) {
+        const int i = m * 16 + 4 * g + r;
+        const O* from = base + rows[i < t.count ? i : 0] * base_stride + col;
+        if constexpr (VY) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-#pragma unroll
-      for (int m = 0; m < MT; ++m) acc[m][i] = product<T>(hf[m], bf[i], acc[m][i]);
-  }
-#pragma unroll
-  for (int m = 0; m < MT; ++m)
-#pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      const int i = m * 16 + 4 * g + r;
-      if (i >= t.count) continue;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) y[m][r].v[e] += acc[m][e][r];
-      store8(static_cast<O*>(a.out.data) + rows[i] * a.out.stride_l + n, y[m][r], left, FAST);
-    }
-}
-
-template <typename T, typename O, int PARTS, int MT>
-__device__ __forceinline__ void expand_tile(const AdaptersArgs& a, const AdaptersPlan& p, const Tile& t, const int* rows, int slice, int n0,
-                                            int end, bool vec, u32x4_t* h) {
-  constexpr int E = Kind<T>::E;
-  const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
-  const int rank = t.adapter < 0 ? 0 : uniform(rank_of(a, t.adapter));
-  const int pieces = (rank + E - 1) / E, steps = (pieces * PARTS + 3) >> 2;
-  if (rank > 0) {
-    // h[step][mt][lane]: row lane % 16, part v % PARTS of the ranks of piece v / PARTS, v = 4 step + lane / 16
-    const float scale = a.scales ? a.scales[t.adapter] : 1.f;
-    const size_t width = (size_t)a.slices * p.r16, next = (size_t)a.rows * width;
-    for (int i = threadIdx.x; i < pieces * MT * 16; i += 256) {
-      const int m = i % (MT * 16), c = i / (MT * 16);
-      float v[E];
-#pragma unroll
-      for (int e = 0; e < E; ++e) v[e] = 0.f;
-      if (m < t.count) {
-        const float* from = p.part + rows[m] * width + slice * p.r16 + c * E;
-#pragma unroll 4
-        for (int z = 0; z < p.splits; ++z) {
-#pragma unroll
-          for (int q = 0; q < E / 4; ++q) {
-            const f32x4_t w = *reinterpret_cast<const f32x4_t*>(from + z * next + 4 * q);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) v[4 * q + e] += w[e];
-          }
-        }
-#pragma unroll
-        for (int e = 0; e < E; ++e) v[e] = c * E + e < rank ? v[e] * scale : 0.f;
-      }
-#pragma unroll
-      for (int q = 0; q < PARTS; ++q) {
-        u32x4_t w;
-        if constexpr (sizeof(T) == 4) {
-#pragma unroll
-          for (int e = 0; e < 4; ++e) w[e] = __float_as_uint(v[e]);
+          for (int k = 0; k < Eight<O>::W; ++k) y[r].w[k] = reinterpret_cast<const u32x4_t*>(from)[k];
         } else {
-          // the value rounded to bf16, then what is left of it (nothing of an infinity)
 #pragma unroll
-          for (int e = 0; e < 8; e += 2) {
-            w[e / 2] = pack_bf16x2(v[e], v[e + 1]);
-#pragma unroll
-            for (int d = 0; d < 2; ++d) {
-              const float top = __uint_as_float(d ? w[e / 2] & 0xffff0000u : w[e / 2] << 16);
-              v[e + d] = fabsf(top) < INFINITY ? v[e + d] - top : 0.f;
-            }
-          }
+          for (int k = 0; k < Eight<O>::W; ++k) y[r].w[k] = piece(from + min(k * 8 / Eight<O>::W, left - 1), left - k * 8 / Eight<O>::W);
         }
-        const int s = c * PARTS + q;
-        h[((s >> 2) * MT + (m >> 4)) * 64 + (s & 3) * 16 + (m & 15)] = w;
       }
+    };
+    auto finish = [&](int m, const Eight<O> (&y)[4], const f32x4_t (&acc)[8]) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        const int i = m * 16 + 4 * g + r;
+        if (i >= t.count || left <= 0) continue;
+        Eight<O> z = y[r];
+#pragma unroll
+        for (int k = 0; k < Eight<O>::W; ++k) z.w[k] &= given;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = z.at(e) + acc[e][r];
+        O* to = static_cast<O*>(a.out.data) + rows[i] * a.out.stride_l + n;
+        if constexpr (VY && sizeof(O) == 2) {
+          *reinterpret_cast<u32x4_t*>(to) = u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+        } else if constexpr (VY) {
+          *reinterpret_cast<f32x4_t*>(to) = f32x4_t{v[0], v[1], v[2], v[3]};
+          *reinterpret_cast<f32x4_t*>(to + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; ++e)
+            if (e < left) Act<O>::store(to, e, v[e]);
+        }
+      }
+    };
+    const f32x4_t zero = {0, 0, 0, 0};
+    u32x4_t bf[ONE ? 1 : 2][8];
+    Eight<O> y[2][4];
+    if constexpr (ONE) {
+      load_y(0, y[0]);
+      if (MT > 1) load_y(1, y[1]);
     }
-    for (int i = threadIdx.x; i < (steps * 4 - pieces * PARTS) * MT * 16; i += 256) {
-      const int m = i % (MT * 16), s = pieces * PARTS + i / (MT * 16);
-      h[((s >> 2) * MT + (m >> 4)) * 64 + (s & 3) * 16 + (m & 15)] = u32x4_t{0, 0, 0, 0};
+    if (steps) load_b(0, bf[0]);
+    if constexpr (ONE) {
+#pragma unroll
+      for (int m = 0; m < 2; ++m) {
+        if (m >= MT) break;
+        f32x4_t acc[8];
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] = product<T>(hf[m][q], bf[0][i], q ? acc[i] : zero);
+        if (!steps)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[i] = zero;
+        finish(m, y[m], acc);
+      }
+    } else {
+      f32x4_t acc[2][8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) acc[0][i] = acc[1][i] = zero;
+      auto step = [&](int s, const u32x4_t (&now)[8], u32x4_t (&later)[8]) {
+        u32x4_t hs[2][PARTS];
+#pragma unroll
+        for (int m = 0; m < 2; ++m)
+#pragma unroll
+          for (int q = 0; q < PARTS; ++q) hs[m][q] = load_h(s, q, m);
+        if (s + 1 < steps) load_b(s + 1, later);
+#pragma unroll
+        for (int q = 0; q < PARTS; ++q)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            acc[0][i] = product<T>(hs[0][q], now[i], acc[0][i]);
+            acc[1][i] = product<T>(hs[1][q], now[i], acc[1][i]);
+          }
+      };
+      for (int s = 0; s < steps; s += 2) {
+        step(s, bf[0], bf[1]);
+        if (s + 1 < steps) step(s + 1, bf[1], bf[0]);
+      }
+      load_y(0, y[0]);
+      if (MT > 1) load_y(1, y[1]);
+      finish(0, y[0], acc[0]);
+      if (MT > 1) finish(1, y[1], acc[1]);
     }
-    __syncthreads();
-  }
-  for (int n = n0 + wave * COLS; n < min(end, n0 + p.cols); n += 4 * COLS) {
-    if (vec && n + COLS <= end)
-      expand_block<T, O, PARTS, MT, true>(a, t, rows, h, rank, steps, n, end);
-    else
-      expand_block<T, O, PARTS, MT, false>(a, t, rows, h, rank, steps, n, end);
   }
 }
 
-template <typename T, typename O, int PARTS>
-__global__ void __launch_bounds__(256) adapters_expand_kernel(AdaptersArgs a, AdaptersPlan p) {
+template <typename T, typename O, int PARTS, bool VY, bool VB, bool ONE>
+__global__ void __launch_bounds__(256, ONE && sizeof(O) == 2 ? 3 : 2) adapters_expand_kernel(AdaptersArgs a, AdaptersPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  extern __shared__ u32x4_t frags[];
   __shared__ int rows[TM];
-  const Tile t = tile_of(a, p, blockIdx.x, rows);
+  int slice = 0, first = 0, block = blockIdx.x % p.blocks;
+  const Tile t = tile_of(a, p, blockIdx.x / p.blocks, rows);
   if (t.count == 0 || (t.adapter < 0 && a.base.data == a.out.data)) return;
-  int slice = 0, first = 0, block = blockIdx.y;
   for (; slice < a.slices - 1; ++slice) {
     const int n = (a.slice_end[slice] - first + p.cols - 1) / p.cols;
     if (block < n) break;
     block -= n;
     first = a.slice_end[slice];
   }
-  const int n0 = first + block * p.cols, end = a.slice_end[slice];
-  const bool vec = p.vec && n0 % (16 / (int)sizeof(O)) == 0;
-  if (t.count > 16)
-    expand_tile<T, O, PARTS, 2>(a, p, t, rows, slice, n0, end, vec, frags);
-  else
-    expand_tile<T, O, PARTS, 1>(a, p, t, rows, slice, n0, end, vec, frags);
+  const int n0 = first + block * p.cols, end = a.slice_end[slice], last = min(end, n0 + p.cols), mine = n0 + uniform(threadIdx.x >> 6) * COLS;
+  const int rank = t.adapter < 0 ? 0 : uniform(rank_of(a, t.adapter));
+  const int steps = (rank + Kind<T>::STEP - 1) / Kind<T>::STEP;
+  expand_columns<T, O, PARTS, VY, VB, ONE>(a, p, t, rows, rank, steps, slice, mine, last, end);
 #endif
 }
+
+int parts_of(const AdaptersArgs& a) { return a.dtype == DLLM_F32 ? 1 : a.out_dtype == DLLM_F32 ? 3 : 2; }
 
 AdaptersPlan plan_of(const AdaptersArgs& a) {
   AdaptersPlan p{};
   const int cus = device_cu_count(), size = a.dtype == DLLM_F32 ? 4 : 2;
   p.r16 = ceil_div(a.rank, 16) * 16;
   p.sorted = a.rows > 64;
-  p.tiles = p.sorted ? std::min(a.rows, ceil_div(a.rows, TM) + a.adapters + 1) : a.rows;
-  const int units = a.slices * p.r16 / 16;
-  p.j = units >= 5 ? 8 : units >= 3 ? 4 : units;
-  const int steps = ceil_steps(a.d_in, 64 / size), full = p.sorted ? ceil_div(a.rows, TM) : ceil_div(a.rows, 2);
-  const int wanted = std::max(1, 2 * cus / (full * ceil_div(units, p.j)));
-  p.splits = std::min({wanted, std::max(1, steps / 8), 16});
-  p.steps = ceil_div(steps, p.splits);
-  p.splits = ceil_div(steps, p.steps);
-  p.cols = 4 * COLS;
-  while (p.cols < 4096 && (long)full * (a.d_out / (2 * p.cols)) >= 4 * cus) p.cols *= 2;
+  const int groups = ceil_div(a.rows, TM);
+  p.tiles = p.sorted ? std::min(a.rows, groups + a.adapters + 1) : a.rows <= TM ? a.rows : groups * TM;
+  const int units = a.slices * p.r16 / 16, full = p.sorted ? groups : std::min(a.rows, groups + a.adapters);
+  p.j = std::min(units, 2);
+  const int wgs = full * ceil_div(units, p.j), chunks = ceil_div((long)a.d_in * size, CHUNK);
+  p.splits = std::max(1, std::min({cus / wgs, chunks, 16}));
+  p.steps = ceil_div(chunks, p.splits);
+  p.splits = ceil_div(chunks, p.steps);
+  p.keep = a.rank > 64 / size && p.splits == 1;
+  p.hsteps = ceil_div(a.rank, 64 / size);
+  const int per = std::max(1, std::min(2, (int)((long)full * ceil_div(a.d_out, 4 * COLS) / (4 * cus))));
+  p.cols = per * 4 * COLS;
+  for (int i = 0; i < a.slices; ++i) p.blocks += ceil_div(a.slice_end[i] - (i ? a.slice_end[i - 1] : 0), p.cols);
   return p;
 }
 
@@ -500,63 +637,79 @@ bool aligned(const AttnView& v, int size) {
   return ((uintptr_t)v.data & 15) == 0 && v.stride_l * size % 16 == 0 && v.stride_b * size % 16 == 0 && v.stride_h * size % 16 == 0;
 }
 
-template <typename T>
-void shrink(const AdaptersArgs& a, const AdaptersPlan& p, hipStream_t s) {
-  const dim3 grid(p.tiles, p.splits, ceil_div(a.slices * p.r16 / 16, p.j));
-  if (p.j == 1)
-    adapters_shrink_kernel<T, 1><<<grid, 256, 0, s>>>(a, p);
-  else if (p.j == 2)
-    adapters_shrink_kernel<T, 2><<<grid, 256, 0, s>>>(a, p);
-  else if (p.j == 4)
-    adapters_shrink_kernel<T, 4><<<grid, 256, 0, s>>>(a, p);
-  else
-    adapters_shrink_kernel<T, 8><<<grid, 256, 0, s>>>(a, p);
-  DLLM_LAUNCH_CHECK("adapters_shrink_kernel");
-}
 template <typename T, typename O, int PARTS>
-void expand(const AdaptersArgs& a, const AdaptersPlan& p, hipStream_t s) {
-  int blocks = 0;
-  for (int i = 0; i < a.slices; ++i) blocks += ceil_div(a.slice_end[i] - (i ? a.slice_end[i - 1] : 0), p.cols);
-  const int steps = ceil_div((long)ceil_div(a.rank, Kind<T>::E) * PARTS, 4);
-  adapters_expand_kernel<T, O, PARTS><<<dim3(p.tiles, blocks), 256, steps * 2 * 1024, s>>>(a, p);
+void run(const AdaptersArgs& a, const AdaptersPlan& p, hipStream_t s) {
+  if (a.adapters > 0) {
+    const dim3 grid(p.tiles, p.splits, ceil_div(a.slices * p.r16 / 16, p.vec_in ? p.j : 1));
+    if (!p.vec_in)
+      adapters_shrink_kernel<T, PARTS, 1, false><<<grid, NW * 64, 0, s>>>(a, p);
+    else if (p.j == 1)
+      adapters_shrink_kernel<T, PARTS, 1, true><<<grid, NW * 64, 0, s>>>(a, p);
+    else
+      adapters_shrink_kernel<T, PARTS, 2, true><<<grid, NW * 64, 0, s>>>(a, p);
+    DLLM_LAUNCH_CHECK("adapters_shrink_kernel");
+    if (a.rank > Kind<T>::STEP && !p.keep) {
+      adapters_join_kernel<T, PARTS><<<dim3(ceil_div(a.rows, 256), a.slices * p.r16 / Kind<T>::E), 256, 0, s>>>(a, p);
+      DLLM_LAUNCH_CHECK("adapters_join_kernel");
+    }
+  }
+  auto go = [&](auto vy, auto vb) {
+    if (a.rank <= Kind<T>::STEP)
+      adapters_expand_kernel<T, O, PARTS, vy, vb, true><<<p.tiles * p.blocks, 256, 0, s>>>(a, p);
+    else
+      adapters_expand_kernel<T, O, PARTS, vy, vb, false><<<p.tiles * p.blocks, 256, 0, s>>>(a, p);
+  };
+  if (!p.vec_b)
+    go(std::false_type{}, std::false_type{});
+  else if (!p.vec_y)
+    go(std::false_type{}, std::true_type{});
+  else
+    go(std::true_type{}, std::true_type{});
   DLLM_LAUNCH_CHECK("adapters_expand_kernel");
 }
 
+size_t up256(size_t n) { return (n + 255) & ~(size_t)255; }
+// Bytes of the workspace's parts: inner products, their shares, tiles and order.
+size_t h_bytes(const AdaptersArgs& a, const AdaptersPlan& p) { return p.hsteps == 1 ? 0 : up256((size_t)a.slices * p.hsteps * parts_of(a) * 4 * a.rows * 16); }
 size_t part_bytes(const AdaptersArgs& a, const AdaptersPlan& p) {
-  return ((size_t)p.splits * a.rows * a.slices * p.r16 * 4 + 255) & ~(size_t)255;
+  return p.keep ? 0 : up256((size_t)p.splits * a.rows * a.slices * p.r16 * 4);
 }
 
 }  // namespace
 
 size_t adapters_bytes(const AdaptersArgs& a) {
   const AdaptersPlan p = plan_of(a);
-  return part_bytes(a, p) + (p.sorted ? p.tiles * sizeof(int4) + a.rows * sizeof(int) : 0);
+  return h_bytes(a, p) + part_bytes(a, p) + (p.sorted ? p.tiles * sizeof(int4) + a.rows * sizeof(int) : 0);
+}
+
+// A launch's threads must be below 2^32.
+bool adapters_fit(const AdaptersArgs& a) {
+  const AdaptersPlan p = plan_of(a);
+  return (long)p.tiles * p.blocks < (1l << 24);
 }
 
 void launch_adapters(const AdaptersArgs& a, void* ws, hipStream_t s) {
   AdaptersPlan p = plan_of(a);
   const int size = a.dtype == DLLM_F32 ? 4 : 2, out = a.out_dtype == DLLM_F32 ? 4 : 2;
-  p.part = static_cast<float*>(ws);
-  p.tile = reinterpret_cast<int4*>(static_cast<char*>(ws) + part_bytes(a, p));
+  char* at = static_cast<char*>(ws);
+  p.h = reinterpret_cast<uint32_t __attribute__((ext_vector_type(4)))*>(at);
+  p.part = reinterpret_cast<float*>(at += h_bytes(a, p));
+  p.tile = reinterpret_cast<int4*>(at += part_bytes(a, p));
   p.order = reinterpret_cast<int*>(p.tile + p.tiles);
-  p.vec_in = aligned(a.x, size) && aligned(a.a, size);
-  p.vec = aligned(a.b, size) && a.rank * size % 16 == 0 && aligned(a.base, out) && aligned(a.out, out);
+  p.vec_in = aligned(a.x, size) && aligned(a.a, size) && a.d_in * size % 16 == 0;
+  p.vec_b = aligned(a.b, size) && a.rank * size % 16 == 0;
+  p.vec_y = aligned(a.base, out) && aligned(a.out, out);
+  for (int i = 0; i < a.slices; ++i) p.vec_y = p.vec_y && a.slice_end[i] % 8 == 0;
   if (p.sorted) {
     adapters_sort_kernel<<<1, SORT_THREADS, (a.adapters + 1) * 8, s>>>(a, p);
     DLLM_LAUNCH_CHECK("adapters_sort_kernel");
   }
-  if (a.adapters > 0) {
-    if (a.dtype == DLLM_F32)
-      shrink<float>(a, p, s);
-    else
-      shrink<bf16_t>(a, p, s);
-  }
   if (a.dtype == DLLM_F32)
-    expand<float, float, 1>(a, p, s);
+    run<float, float, 1>(a, p, s);
   else if (a.out_dtype == DLLM_F32)
-    expand<bf16_t, float, 3>(a, p, s);
+    run<bf16_t, float, 3>(a, p, s);
   else
-    expand<bf16_t, bf16_t, 2>(a, p, s);
+    run<bf16_t, bf16_t, 2>(a, p, s);
 }
 
 }  // namespace dllm

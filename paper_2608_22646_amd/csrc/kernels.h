@@ -262,19 +262,20 @@ struct AdaptersArgs {
   const int32_t *which, *ranks;
   const float* scales;
 };
-// Layout of a call: whether the rows are sorted by adapter first, tiles of the grid,
-// 16-blocks of ranks of a shrinking workgroup, shares of d_in and the steps of one,
-// columns of an expanding workgroup, ranks padded to 16; whether
-// whole 16-byte pieces may be read of x and a, and of b, base and out; and what the
-// workspace holds.
+// Layout of a call: whether the rows are sorted by adapter first; tiles of rows;
+// 16-blocks of ranks of a shrinking workgroup, shares of d_in and the stages of one,
+// whether it leaves inner products (h) or shares of them (part); columns of an expanding workgroup and such blocks of a tile; ranks padded to 16,
+// steps along them; whether whole 16-byte pieces may be read of x and a, of b, and of
+// base and out; and what the workspace holds.
 struct AdaptersPlan {
-  int sorted, tiles, j, splits, steps, cols, r16, vec_in, vec;
-  float* part;  // [splits][rows][slices][r16]
-  int4* tile;   // adapter, first place in order, rows
-  int* order;   // [rows]
+  int sorted, tiles, j, splits, steps, keep, cols, blocks, r16, hsteps, vec_in, vec_b, vec_y;
+  uint32_t __attribute__((ext_vector_type(4))) * h;  // [slices][hsteps][parts][4][rows]: inner products
+  float* part;                                       // [splits][rows][slices][r16]: shares of them
+  int4* tile;                                        // adapter, first place in order, rows
+  int* order;                                        // [rows]
 };
-__host__ __device__ inline int ceil_steps(int n, int step) { return (n + step - 1) / step; }
 size_t adapters_bytes(const AdaptersArgs& a);
+bool adapters_fit(const AdaptersArgs& a);  // its grid can be launched
 void launch_adapters(const AdaptersArgs& a, void* ws, hipStream_t s);
 
 }  // namespace dllm

@@ -116,6 +116,7 @@ bool adapter_sizes(const dllm_adapter_args* p, AdaptersArgs* a) {
   a->rank = p->rank;
   a->slices = p->slices;
   for (int s = 0; s < p->slices; ++s) a->slice_end[s] = p->slice_end[s];
+  require(p->rows == 0 || adapters_fit(*a), DLLM_ESHAPE, "too many rows and columns for one call");
   return p->rows > 0;
 }
 
