@@ -514,6 +514,39 @@ int dllm_attention_workspace_size(const dllm_attn_args* args, size_t* bytes);
 int dllm_attention(const dllm_attn_args* args, void* workspace, size_t workspace_bytes, void* stream);
 
 /*
+ * Attention of documents behind prompts that they share: requests that continue one
+ * prompt hold its keys and values once, and those are read once for the queries of all of
+ * them.  `own` is a call of dllm_attention, for the documents' own keys; document d stands
+ * behind prompt[d] (device int32 [docs]; NULL: all of them behind prompt 0; a number that
+ * is no prompt's: behind none), whose keys its queries all see before their own:
+ *   out_i = sum_j softmax_j(s_ij) v_j  over the prompt's keys and the visible own ones,
+ * scores as in dllm_attention.  Positions count from a document's first own key (own.q_pos,
+ * blocks, own.prefix); key j of a prompt of P keys stands at position j - P.
+ * Prompt p has p_len[p] keys, tokens p_start[p] .. of its slab of pk and pv, which is slab p
+ * (packed: stride_b = 0).  NULL arrays, cut ranges, empty rows and what broken numbers
+ * reach: as for dllm_attention, a prompt's keys being visible to all queries behind it.
+ * Documents of one prompt are served together where they follow each other; another order
+ * costs time only.  Documents must not share queries; where they do, some rows of out may
+ * not be written.  Out must not overlap anything that is read.
+ * Requirements: those of dllm_attention for `own`; pk and pv those of k and v; prompts in
+ * [0, 65535], 0 <= max_p <= p_tokens <= 2^29, kv_tokens <= 2^29; fewer than 2^26 rows
+ * (queries times n_heads) where a document has few.  docs or max_q of 0: nothing; prompts or max_p of 0:
+ * dllm_attention.
+ */
+typedef struct dllm_shared_attn_args {
+  dllm_attn_args own;
+  dllm_view pk, pv;
+  int32_t prompts, p_tokens; /* tokens of a slab of pk and pv */
+  int32_t max_p;             /* no prompt has more (longer ones are cut) */
+  const int32_t *p_start, *p_len; /* [prompts] */
+  const int32_t* prompt;          /* [docs] */
+} dllm_shared_attn_args;
+
+/* As dllm_attention_workspace_size (whether own.q.stride_b is 0 is looked at) and dllm_attention. */
+int dllm_shared_attention_workspace_size(const dllm_shared_attn_args* args, size_t* bytes);
+int dllm_shared_attention(const dllm_shared_attn_args* args, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Sample one token per row of logits [rows, vocab] (row r at logits + r *
  * row_stride elements) from given random numbers.  Candidates are the tokens v
  * != mask_id (mask_id outside [0, vocab): all) with a logit above -inf, ranked by

@@ -68,6 +68,33 @@ def attention(q, k, v, pos, block=0, prefix=0, scale=None, cap=0.0, slopes=None)
     return out, mass, top, dot
 
 
+def shared_attention(q, k, v, pk, pv, pos, block=0, prefix=0, scale=None, cap=0.0, slopes=None):
+    """One document behind a prompt: as attention, with the prompt's keys pk and values pv [P, Hkv, hd] at positions -P .. -1,
+    visible to every query."""
+    T, Hq, hd = q.shape
+    P, G = len(pk), Hq // k.shape[1]
+    scale = 1.0 / math.sqrt(hd) if scale is None else scale
+    out, mass, top, dot = np.zeros((T, Hq, hd)), np.zeros((T, Hq, hd)), np.zeros((T, Hq)), np.zeros((T, Hq))
+    for t in range(T):
+        n = visible(pos + t, len(k), block, prefix)
+        at = np.concatenate([np.arange(-P, 0), np.arange(n)])
+        for h in range(Hq):
+            kk, vv = np.concatenate([pk[:, h // G], k[:n, h // G]]), np.concatenate([pv[:, h // G], v[:n, h // G]])
+            s = scale * (kk @ q[t, h])
+            if cap > 0:
+                s = cap * np.tanh(s / cap)
+            if slopes is not None:
+                s = s - slopes[h] * np.abs(pos + t - at)
+            if len(at) == 0 or s.max() == -np.inf:
+                continue
+            p = np.exp(s - s.max())
+            p /= p.sum()
+            sure = p > 0
+            out[t, h], mass[t, h] = p @ vv, p[sure] @ np.abs(vv[sure])
+            top[t, h], dot[t, h] = np.abs(s[sure]).max(), (np.abs(kk[sure]) @ np.abs(q[t, h])).max()
+    return out, mass, top, dot
+
+
 def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0, mask_id=-1):
     """One row: (token, conf, prob)."""
     x = np.array(logits, dtype=np.float64, copy=True)

@@ -70,6 +70,11 @@ class AttnArgs(_c.Structure):
                 ("prefix", _vp), ("slopes", _vp), ("scale", _f32), ("cap", _f32), ("block", _i32)]
 
 
+class SharedAttnArgs(_c.Structure):
+    _fields_ = [("own", AttnArgs), ("pk", View), ("pv", View), ("prompts", _i32), ("p_tokens", _i32), ("max_p", _i32),
+                ("p_start", _vp), ("p_len", _vp), ("prompt", _vp)]
+
+
 class SampleArgs(_c.Structure):
     _fields_ = [("logits", _vp), ("row_stride", _i64), ("dtype", _i32), ("rows", _i32), ("vocab", _i32),
                 ("mask_id", _i32), ("u", _vp), ("temperature", _vp), ("top_k", _vp), ("top_p", _vp), ("min_p", _vp),
@@ -126,6 +131,8 @@ _SIGS = {
                            _c.POINTER(View), _c.POINTER(View), _i32, _i32, _vp]),
     "dllm_attention_workspace_size": (_i32, [_c.POINTER(AttnArgs), _c.POINTER(_sz)]),
     "dllm_attention": (_i32, [_c.POINTER(AttnArgs), _vp, _sz, _vp]),
+    "dllm_shared_attention_workspace_size": (_i32, [_c.POINTER(SharedAttnArgs), _c.POINTER(_sz)]),
+    "dllm_shared_attention": (_i32, [_c.POINTER(SharedAttnArgs), _vp, _sz, _vp]),
     "dllm_sample_workspace_size": (_i32, [_i32, _i32, _c.POINTER(_sz)]),
     "dllm_sample": (_i32, [_c.POINTER(SampleArgs), _vp, _sz, _vp]),
     "dllm_adapters_workspace_size": (_i32, [_c.POINTER(AdapterArgs), _c.POINTER(_sz)]),
@@ -736,6 +743,74 @@ def _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes):
     return AttnArgs(dt, Hq, Hkv, hd, *views, n, T, S, max_q, max_kv, *ptrs,
                     _column(slopes, Hq, torch.float32, dev, "slopes"), 1.0 / math.sqrt(hd) if scale is None else scale, cap,
                     block)
+
+
+@dataclass
+class Prompts:
+    """The prompts of a shared-attention call: int32 device arrays [prompts] (or None: see dllm_shared_attn_args), the
+    longest length among them, and the prompt of each document (int32 [docs]; None: prompt 0)."""
+    start: torch.Tensor | None = None
+    len: torch.Tensor | None = None
+    max: int | None = None         # None: the slab's tokens
+    of: torch.Tensor | None = None
+    count: int | None = None       # prompts; None: the arrays' length, or the slabs
+
+    @classmethod
+    def packed(cls, lens, of=None, device="cuda"):
+        """Prompts that follow each other without gaps, from host lists."""
+        lens = list(lens)
+        ints = lambda v: None if v is None else torch.tensor(list(v), dtype=torch.int32, device=device)  # noqa: E731
+        return cls(ints(itertools.accumulate([0, *lens[:-1]])) if lens else ints([]), ints(lens), max(lens, default=0), ints(of))
+
+
+def shared_attention(q, k, v, pk, pv, docs: Docs | None = None, prompts: Prompts | None = None, block=0, scale=None, cap=0.0,
+                     slopes=None, out=None, ws=None, stream=None):
+    """dllm_shared_attention.  q, k, v, docs and the numbers as for attention(); pk, pv [P, Hkv, hd]: packed prompts in one
+    slab, or [prompts, P, Hkv, hd]: a slab per prompt.  out: written and returned (new, zeroed, if None); ws: a
+    device_buffer of shared_attention_workspace_size bytes (allocated here if None)."""
+    _refuse(q.dim() in (3, 4) and k.dim() == q.dim() and v.dim() == q.dim() and pk.dim() in (3, 4) and pv.dim() == pk.dim(), -2,
+            "q, k and v must be [tokens, heads, head_dim] or [docs, tokens, heads, head_dim], pk and pv alike with prompts")
+    dev = q.device
+    scope = _elsewhere(dev, stream)
+    if scope is not None:
+        with scope:
+            return shared_attention(q, k, v, pk, pv, docs, prompts, block, scale, cap, slopes, out, ws)
+    dt = _dtype(q, "q")
+    out = torch.zeros(q.shape, dtype=q.dtype, device=dev) if out is None else out
+    a = _shared_args(dt, q, k, v, pk, pv, out, docs or Docs(), prompts or Prompts(), block, scale, cap, slopes)
+    if ws is None:
+        n = _sz()
+        check(lib().dllm_shared_attention_workspace_size(a, n))
+        ws = _workspace(n.value, dev) if n.value else None
+    else:
+        _given(ws, dev)
+    check(lib().dllm_shared_attention(a, _ptr(ws), 0 if ws is None else ws.nbytes, _raw_stream(dev.index)))
+    return out
+
+
+def shared_attention_workspace_size(q, k, v, pk, pv, docs: Docs | None = None, prompts: Prompts | None = None):
+    """Bytes of workspace that shared_attention() needs for operands, documents and prompts of these sizes."""
+    n = _sz()
+    check(lib().dllm_shared_attention_workspace_size(
+        _shared_args(_dtype(q, "q"), q, k, v, pk, pv, q, docs or Docs(), prompts or Prompts(), 0, None, 0.0, None), n))
+    return n.value
+
+
+def _shared_args(dt, q, k, v, pk, pv, out, docs, prompts, block, scale, cap, slopes):
+    own = _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes)
+    dev, shape, one = q.device, tuple(pk.shape), pk.dim() == 3
+    P = shape[-3]
+    want = (P, own.n_kv_heads, own.head_dim) if one else (shape[0], P, own.n_kv_heads, own.head_dim)
+    n = prompts.count
+    if n is None:
+        n = next((t.numel() for t in (prompts.start, prompts.len) if t is not None), 1) if one else shape[0]
+    _refuse(one or n == shape[0], -2, "prompts in slabs: one per slab")
+    max_p = P if prompts.max is None else prompts.max
+    _in32(n, P, max_p)
+    return SharedAttnArgs(own, _rows(pk, want, q.dtype, dev, "pk"), _rows(pv, want, q.dtype, dev, "pv"), n, P, max_p,
+                          _column(prompts.start, n, torch.int32, dev, "prompts.start"),
+                          _column(prompts.len, n, torch.int32, dev, "prompts.len"),
+                          _column(prompts.of, own.docs, torch.int32, dev, "prompts.of"))
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask_id=-1, ws=None, stream=None):

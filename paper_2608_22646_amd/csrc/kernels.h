@@ -242,6 +242,31 @@ size_t attn_docs_bytes(const AttnArgs& a);
 bool attn_docs_fits(const AttnArgs& a);  // its grid can be launched
 void launch_attn_docs(const AttnArgs& a, void* ws, hipStream_t s);
 
+// k_attn_shared.hip: see dllm_shared_attention; ws of attn_shared_bytes(s) bytes.
+struct SharedArgs {
+  AttnArgs own;
+  AttnView pk, pv;
+  int prompts, p_tokens, max_p;
+  const int32_t *p_start, *p_len, *prompt;
+};
+// Layout of a call: whether a document's tiles take its prompt's keys and its own in one
+// go (then the row tiles of a document), workgroups; else queries at most, units at most,
+// workgroups of a round, rows of a document's tile, states at most, and what the
+// workspace holds (shared_plan_kernel).
+struct SharedPlan {
+  bool chain;
+  int tiles, cap, slots, own_rows;
+  long grid, units, states;
+  int* count;  // units without their heads, queries
+  int4 *tok, *seg, *run, *unit;
+  int2* info;  // of a document: its first query, its run
+  float* part;
+  float2* part_ml;
+};
+size_t attn_shared_bytes(const SharedArgs& s);
+bool attn_shared_fits(const SharedArgs& s);  // its grids can be launched
+void launch_attn_shared(const SharedArgs& s, void* ws, hipStream_t st);
+
 // k_sample.hip: see dllm_sample; ws of sample_bytes(rows, vocab) bytes.
 struct SampleArgs {
   const void* logits;

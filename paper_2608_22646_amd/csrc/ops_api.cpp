@@ -1,5 +1,6 @@
 // C ABI of the stand-alone operators (see include/dllm.h): argument checks and
-// launches of rotary positions, attention over documents, sampling, and adapters.
+// launches of rotary positions, attention over documents and behind shared prompts,
+// sampling, and adapters.
 #include <math.h>
 
 #include "api.h"
@@ -80,6 +81,50 @@ bool attn_args(const dllm_attn_args* p, AttnArgs* a) {
 }
 
 AttnView attn_view(const dllm_view& v) { return AttnView{v.data, v.stride_b, v.stride_l, v.stride_h}; }
+
+// The operands of an attention call.
+void attn_operands(const dllm_attn_args* p, AttnArgs* out) {
+  AttnArgs& a = *out;
+  const int size = p->dtype == DLLM_F32 ? 4 : 2;
+  check_attn_view(p->q, size, p->head_dim, p->docs, "q");
+  check_attn_view(p->out, size, p->head_dim, p->docs, "out");
+  if (p->max_kv > 0) {
+    check_attn_view(p->k, size, p->head_dim, p->docs, "k");
+    check_attn_view(p->v, size, p->head_dim, p->docs, "v");
+    require(p->k.stride_l * size < (1 << 25) && p->v.stride_l * size < (1 << 25), DLLM_ESHAPE,
+            "64 stride_l of k and v must be below 2^31 bytes");
+  }
+  a.q = attn_view(p->q);
+  a.k = attn_view(p->k);
+  a.v = attn_view(p->v);
+  a.out = attn_view(p->out);
+  a.q_start = p->q_start;
+  a.q_len = p->q_len;
+  a.kv_start = p->kv_start;
+  a.kv_len = p->kv_len;
+  a.q_pos = p->q_pos;
+  a.prefix = p->prefix;
+  a.slopes = p->slopes;
+}
+
+// The sizes of a call behind shared prompts; false where there is nothing to do.
+bool shared_args(const dllm_shared_attn_args* p, SharedArgs* s) {
+  require(p != nullptr, DLLM_EINVAL, "args is NULL");
+  const bool some = attn_args(&p->own, &s->own);
+  require(p->prompts >= 0 && p->prompts <= 65535, DLLM_ESHAPE, "prompts must be in [0, 65535]");
+  require(p->max_p >= 0 && p->max_p <= p->p_tokens && p->p_tokens <= (1 << 29), DLLM_ESHAPE,
+          "max_p must be in [0, p_tokens], p_tokens at most 2^29");
+  require(p->own.kv_tokens <= (1 << 29), DLLM_ESHAPE, "kv_tokens must be at most 2^29");
+  s->own.q.stride_b = p->own.q.stride_b;
+  s->prompts = p->prompts;
+  s->p_tokens = p->p_tokens;
+  s->max_p = p->max_p;
+  s->p_start = p->p_start;
+  s->p_len = p->p_len;
+  s->prompt = p->prompt;
+  require(!some || attn_shared_fits(*s), DLLM_ESHAPE, "too many documents, heads and queries for one call");
+  return some;
+}
 
 void check_workspace(const void* ws, size_t bytes, size_t need) {
   if (need == 0) return;
@@ -182,28 +227,36 @@ int dllm_attention(const dllm_attn_args* p, void* ws, size_t ws_bytes, void* str
   API_BEGIN
   AttnArgs a{};
   if (!attn_args(p, &a)) return DLLM_OK;
-  const int size = p->dtype == DLLM_F32 ? 4 : 2;
-  check_attn_view(p->q, size, p->head_dim, p->docs, "q");
-  check_attn_view(p->out, size, p->head_dim, p->docs, "out");
-  if (p->max_kv > 0) {
-    check_attn_view(p->k, size, p->head_dim, p->docs, "k");
-    check_attn_view(p->v, size, p->head_dim, p->docs, "v");
-    require(p->k.stride_l * size < (1 << 25) && p->v.stride_l * size < (1 << 25), DLLM_ESHAPE,
-            "64 stride_l of k and v must be below 2^31 bytes");
-  }
-  a.q = attn_view(p->q);
-  a.k = attn_view(p->k);
-  a.v = attn_view(p->v);
-  a.out = attn_view(p->out);
-  a.q_start = p->q_start;
-  a.q_len = p->q_len;
-  a.kv_start = p->kv_start;
-  a.kv_len = p->kv_len;
-  a.q_pos = p->q_pos;
-  a.prefix = p->prefix;
-  a.slopes = p->slopes;
+  attn_operands(p, &a);
   check_workspace(ws, ws_bytes, attn_docs_bytes(a));
   launch_attn_docs(a, ws, (hipStream_t)stream);
+  API_END
+}
+
+int dllm_shared_attention_workspace_size(const dllm_shared_attn_args* p, size_t* bytes) {
+  API_BEGIN
+  require(bytes != nullptr, DLLM_EINVAL, "bytes is NULL");
+  SharedArgs s{};
+  *bytes = shared_args(p, &s) ? attn_shared_bytes(s) : 0;
+  API_END
+}
+
+int dllm_shared_attention(const dllm_shared_attn_args* p, void* ws, size_t ws_bytes, void* stream) {
+  API_BEGIN
+  SharedArgs s{};
+  if (!shared_args(p, &s)) return DLLM_OK;
+  attn_operands(&p->own, &s.own);
+  if (p->prompts > 0 && p->max_p > 0) {
+    const int size = p->own.dtype == DLLM_F32 ? 4 : 2;
+    check_attn_view(p->pk, size, p->own.head_dim, p->prompts, "pk");
+    check_attn_view(p->pv, size, p->own.head_dim, p->prompts, "pv");
+    require(p->pk.stride_l * size < (1 << 25) && p->pv.stride_l * size < (1 << 25), DLLM_ESHAPE,
+            "64 stride_l of pk and pv must be below 2^31 bytes");
+    s.pk = attn_view(p->pk);
+    s.pv = attn_view(p->pv);
+  }
+  check_workspace(ws, ws_bytes, attn_shared_bytes(s));
+  launch_attn_shared(s, ws, (hipStream_t)stream);
   API_END
 }
 
