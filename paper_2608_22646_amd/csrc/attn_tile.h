@@ -163,14 +163,14 @@ constexpr int attend_lds() {
 // row is and returns its query (any row's where there is none); done(R) is called with
 // the state of each row that there is.
 template <typename T, int HD, int QG, int KG, int KT, int S, bool CHAIN, typename RowsOf, typename Done>
-__device__ __forceinline__ void attend(const AttnArgs& a, char* lds, const Keys& k1, const Keys& k2, RowsOf rows_of, Done done) {
+__device__ __forceinline__ void attend(const AttnArgs& a, char* lds, int tid, const Keys& k1, const Keys& k2, RowsOf rows_of, Done done) {
   typedef Tile<T, HD> TL;
   constexpr bool BF = sizeof(T) == 2;
-  constexpr int NW = QG * KG, ND = HD / 32;
+  constexpr int ND = HD / 32;
   constexpr int K_BYTES = KT * TL::ROW, TILE = 2 * K_BYTES, STAGE = KG * TILE;
   constexpr int TP = TILE / 1024, PER = TP / QG;  // LDS-DMA instructions of 1 KiB: of a tile, of a wave
   static_assert(TP % (2 * QG) == 0, "the waves of a key group share a tile's loads evenly");
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int qg = wave % QG, kg = wave / QG;
   const int lq = lane & 31, half = lane >> 5;
   const bool neg = a.scale < 0.f;      // scores are formed with |scale| and, where it is negative, -q
@@ -214,7 +214,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, const Keys&
       for (int x = 0; x < PER / 2; ++x) dma16(rs, CHAIN && next ? off2[keys ? x : PER / 2 + x] : off[keys ? x : PER / 2 + x], to + x * QG * 1024);
     }
   };
-  constexpr int D = S - 1;  // stages in flight behind the one in use
+  constexpr int D = S > 1 ? S - 1 : 1;  // stages in flight behind the one in use (of a single stage, before it)
   for (int u = 0; u < D && u < nsteps; ++u) load(u, u);
 
   // Q operand: the lane's rows, dims 16 ks + 8 half .. (bf16), 8 c + 4 half .. (float32)
@@ -487,6 +487,12 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, const Keys&
       wave_order();
   };
   for (int u = 0; __builtin_expect(u < nsteps, 1); ++u) {
+    if constexpr (S == 1) {
+      if (u > 0) {
+        if constexpr (QG > 1) barrier_nofence();
+        load(u, 0);
+      }
+    }
     if (u + D <= nsteps)
       wait_vmcnt<PER*(D - 1)>();
     else
@@ -497,7 +503,7 @@ __device__ __forceinline__ void attend(const AttnArgs& a, char* lds, const Keys&
       barrier_nofence();
     else
       wave_order();
-    if (u + D < nsteps) load(u + D, (u + D) % S);
+    if (S > 1 && u + D < nsteps) load(u + D, (u + D) % S);
     const bool next = CHAIN && u >= n1;
     const int kb = next ? k2.kb : k1.kb, ke = next ? k2.ke : k1.ke, tile_first = next ? k2.tile_first : k1.tile_first;
     const int see_first = next ? k2.see_first : k1.see_first, see_last = next ? k2.see_last : k1.see_last;

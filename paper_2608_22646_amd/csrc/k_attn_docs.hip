@@ -142,7 +142,7 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     return static_cast<const T*>(a.q.data) + dn * a.q.stride_b + (long)(d.q0 + (R.mine ? R.t : 0)) * a.q.stride_l +
            (R.mine ? R.h : 0) * a.q.stride_h;
   };
-  attend<T, HD, QG, KG, KT, S, false>(a, lds, k, k, rows_of, [&](const Rows<HD>& R) {
+  attend<T, HD, QG, KG, KT, S, false>(a, lds, tid, k, k, rows_of, [&](const Rows<HD>& R) {
     if (p.shares > 0)  // state of (query, head) for this share
       keep_state(R, p.part, p.part_ml, ((size_t)(sh.first + sh.chunk) * a.max_q + R.t) * a.Hq + R.h);
     else

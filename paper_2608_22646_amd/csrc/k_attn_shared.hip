@@ -21,7 +21,8 @@ namespace {
 
 constexpr int PLAN_THREADS = 1024;
 constexpr int UNIT_KEYS = 128, LEAST_KEYS = 256;  // chunks are multiples of this, and at least that
-constexpr int STACK_ROWS = 128;                   // rows of a prompt's tile
+constexpr int UNIT_COST = 4;                      // in UNIT_KEYS
+constexpr int MANY_ROWS = 128;                    // rows of a tile of many
 
 // A prompt's range, cut to its slab and to the maximum.
 struct Prompt {
@@ -44,6 +45,26 @@ __device__ __forceinline__ int prompt_of(const SharedArgs& s, int d) {
 __device__ __forceinline__ int distances_from(long i, int before, int end, float slope) {
   const int out = fabsf(slope) < INFINITY ? 0 : 1;
   return (int)max(min(i, (long)end - 1 + out), (long)-before - out);
+}
+
+// Rows of a segment's tiles (of up to 64 rows: few), and how many tiles.
+__host__ __device__ __forceinline__ int tile_rows(const SharedPlan& p, int rows) { return rows > 64 ? MANY_ROWS : p.few_rows; }
+__host__ __device__ __forceinline__ int tiles_of(const SharedPlan& p, int rows) {
+  return rows > 64 ? (rows + MANY_ROWS - 1) / MANY_ROWS : (int)((uint32_t)(rows + p.few_rows - 1) / (uint32_t)p.few_rows);
+}
+// How far keys are split, of `all` units with `work` times UNIT_KEYS keys in all (without
+// their heads): chunks no shorter than `least`, in UNIT_KEYS, and no more units than `most`.
+// Where there are fewer units than workgroups run at once, as many more as make them one
+// round; else only what is longer than a workgroup's part of the whole, a unit's start and
+// end counting as UNIT_COST.
+struct Cut {
+  int least, most;
+};
+__device__ __forceinline__ Cut cut_of(const SharedPlan& p, int all, int work, int heads) {
+  const uint32_t slots = (uint32_t)p.slots / (uint32_t)heads;  // (at least 1 unit, whatever the heads)
+  if ((uint32_t)all < slots) return Cut{max(LEAST_KEYS / UNIT_KEYS, (int)((uint32_t)work / slots)), (int)slots};
+  const float part = ((float)work + (float)all * UNIT_COST) * (float)heads / (float)p.slots;
+  return Cut{max(LEAST_KEYS / UNIT_KEYS, (int)part), 0x7fffffff};
 }
 
 // ---- what is stacked and split how -------------------------------------------------
@@ -73,7 +94,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
 #if defined(__HIP_DEVICE_COMPILE__)
   const AttnArgs& a = s.own;
   __shared__ int sums[PLAN_THREADS / 64];
-  __shared__ int first_l[PLAN_THREADS + 1], prompt_l[PLAN_THREADS], q0_l[PLAN_THREADS];
+  __shared__ int first_l[PLAN_THREADS + 1], prompt_l[PLAN_THREADS];
   __shared__ Doc doc_l[PLAN_THREADS];
   const int tid = threadIdx.x, N = blockDim.x, G = a.Hq / a.Hkv;
   // documents, and the runs among them
@@ -143,7 +164,6 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
     }
     if (rows == 0) keys = 0;
   };
-  auto tiles_of = [&](int i, int rows) { return (rows + (i < runs ? STACK_ROWS : p.own_rows) - 1) / (i < runs ? STACK_ROWS : p.own_rows); };
   // two segments a thread held, where there are no more
   const bool few = segs <= 2 * N;
   int rows_h[2] = {0, 0}, keys_h[2] = {0, 0}, tiles_h[2] = {0, 0};
@@ -152,7 +172,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
   for (int i = tid, k = 0; i < segs; i += N, ++k) {
     int rows, keys;
     size_of(i, rows, keys);
-    const int t = keys > 0 ? tiles_of(i, rows) : 0;
+    const int t = keys > 0 ? tiles_of(p, rows) : 0;
     if (few) {
       rows_h[k & 1] = rows;
       keys_h[k & 1] = keys;
@@ -171,11 +191,9 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
   if ((tid & 63) == 0) sums[tid >> 6] = longest;
   __syncthreads();
   for (int w = 0; w < N >> 6; ++w) longest = max(longest, sums[w]);
-  // The shortest chunks with which the units, at a key/value head each, are no more than
-  // fit the rounds over the CUs that they take at least.
-  const int heads = a.Hkv, rounds = (int)(((long)all_units * heads + p.slots - 1) / p.slots);
-  const int most = (int)((long)rounds * p.slots / heads);
-  int lo = LEAST_KEYS / UNIT_KEYS, hi = max(lo, (longest + UNIT_KEYS - 1) / UNIT_KEYS);
+  const int heads = a.Hkv;
+  const Cut cut = cut_of(p, all_units, all_work, heads);
+  int lo = cut.least, hi = max(lo, (longest + UNIT_KEYS - 1) / UNIT_KEYS);
   if (few) {
     while (lo < hi) {
       const int len = (lo + hi) >> 1;
@@ -183,13 +201,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
 #pragma unroll
       for (int k = 0; k < 2; ++k) c += (keys_h[k] + len * UNIT_KEYS - 1) / (len * UNIT_KEYS) * tiles_h[k];
       before_of(c, sums, n);
-      if (n <= most)
+      if (n <= cut.most)
         hi = len;
       else
         lo = len + 1;
     }
-  } else {
-    lo = most > all_units ? min(hi, max(lo, all_work / (most - all_units) + 1)) : hi;
+  } else if (cut.most < 0x7fffffff) {
+    lo = cut.most > all_units ? min(hi, max(lo, all_work / (cut.most - all_units) + 1)) : hi;
   }
   const int len = lo * UNIT_KEYS;
   // segments' units and states
@@ -199,7 +217,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
     int rows = 0, keys = 0, tiles = 0;
     if (i < segs) {
       size_of(i, rows, keys);
-      tiles = keys > 0 ? tiles_of(i, rows) : 0;
+      tiles = keys > 0 ? tiles_of(p, rows) : 0;
     }
     const int chunks = (keys + len - 1) / len;
     const int each = chunks > 1 ? ((keys + chunks - 1) / chunks + UNIT_KEYS - 1) / UNIT_KEYS * UNIT_KEYS : keys;
@@ -210,7 +228,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
       p.seg[seg_at(i)] = make_int4(s0, chunks, rows, each);
       for (int e = 0; e < chunks * tiles && e0 + e < p.units; ++e) {
         const int c = e / tiles, t = e - c * tiles;
-        p.unit[2 * (size_t)(e0 + e)] = make_int4(i < runs ? ~run.z : i - runs, t * (i < runs ? STACK_ROWS : p.own_rows), rows, c * each);
+        p.unit[2 * (size_t)(e0 + e)] = make_int4(i < runs ? ~run.z : i - runs, t * tile_rows(p, rows), rows, c * each);
         p.unit[2 * (size_t)(e0 + e) + 1] = make_int4(min(keys, (c + 1) * each), s0 + c * rows * heads, run.x, 0);
       }
     }
@@ -238,86 +256,256 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
 #endif
 }
 
+// ---- the same, by each workgroup for itself ----------------------------------------
+// At most 64 documents: lane d of the first wave holds document d, and the run of
+// documents behind one prompt that starts with it.
+struct Split {  // of a segment: its first unit, its first state, row tiles, rows of a head, chunks and their keys
+  int unit, state, tiles, rows, chunks, each;
+};
+struct Segments {  // of a document, and of the run that starts with it
+  Split stack, own;
+  Doc doc;
+  int first;                // the document's first query among all
+  int prompt, p_k0, p_nk;   // its prompt (-1: none)
+  int run;                  // the document that its run starts with (-1: behind no prompt)
+};
+struct Table {
+  Segments of[64];
+  int first[64];
+  int units, queries;
+  // The document that has query i of the call.
+  __device__ __forceinline__ int holder(int i) const {
+    int lo = 0;
+#pragma unroll
+    for (int k = 32; k > 0; k >>= 1) lo += first[lo + k] <= i ? k : 0;
+    return lo;
+  }
+};
+__device__ __forceinline__ int lane_of(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
+
+// By one wave.  The arrays are asked for at once: in the place of one that is not there,
+// memory of the workspace, whose values are not looked at.
+__device__ __forceinline__ void plan_docs(const SharedArgs& s, const SharedPlan& p, Table& t) {
+  const AttnArgs& a = s.own;
+  const int lane = threadIdx.x & 63, G = a.Hq / a.Hkv, heads = a.Hkv;
+  const int* const none = reinterpret_cast<const int*>(p.seg);
+  auto some = [&](const int* x) { return x ? x : none; };
+  const int d = min(lane, a.docs - 1);
+  const int q0 = some(a.q_start)[d], nq = some(a.q_len)[d], k0 = some(a.kv_start)[d], nk = some(a.kv_len)[d], pos = some(a.q_pos)[d],
+            prefix = some(a.prefix)[d], pr = some(s.prompt)[d];
+  Doc x;  // as doc_of
+  x.q0 = a.q_start ? min(max(q0, 0), a.q_tokens) : 0;
+  x.nq = min(min(max(a.q_len ? nq : a.q_tokens, 0), a.q_tokens - x.q0), a.max_q);
+  x.k0 = a.kv_start ? min(max(k0, 0), a.kv_tokens) : 0;
+  x.nk = min(min(max(a.kv_len ? nk : a.kv_tokens, 0), a.kv_tokens - x.k0), a.max_kv);
+  x.pos = a.q_pos ? pos : x.nk - x.nq;
+  x.prefix = a.prefix ? prefix : 0;
+  const bool there = lane < a.docs;
+  if (!there) x.nq = 0;
+  const int prompt = there ? (s.prompt ? (pr >= 0 && pr < s.prompts ? pr : -1) : 0) : -1;
+  const int pk = min(max(prompt, 0), s.prompts - 1), pk0 = (s.p_start ? s.p_start : none)[s.p_start ? pk : 0], pn = (s.p_len ? s.p_len : none)[s.p_len ? pk : 0];
+  Prompt y;  // as prompt_at
+  y.k0 = s.p_start ? min(max(pk0, 0), s.p_tokens) : 0;
+  y.nk = prompt < 0 ? 0 : min(min(max(s.p_len ? pn : s.p_tokens, 0), s.p_tokens - y.k0), s.max_p);
+  const int upto = lanes_upto(x.nq), queries = min(lane_of(upto, 63), p.cap), first = min(upto - x.nq, p.cap);
+  x.nq = min(x.nq, p.cap - first);  // (documents that share queries: cut)
+  // runs: from a document whose prompt is not the last one's to the next such
+  const int prev = __shfl_up(prompt, 1, 64);
+  const bool border = there && prompt != (lane ? prev : -1);
+  const unsigned long long borders = __ballot(border), starts = __ballot(border && prompt >= 0), mine = (2ull << lane) - 1;
+  const int next = __ffsll(borders & ~mine) - 1, end = __shfl(first, max(next, 0), 64);
+  Split st, ow;
+  st.rows = border && prompt >= 0 ? ((next >= 0 ? end : queries) - first) * G : 0;
+  ow.rows = x.nq * G;
+  const int keys_s = st.rows > 0 ? y.nk : 0, keys_o = x.nq > 0 ? sees(a, x, x.nq - 1) : 0;
+  st.tiles = keys_s > 0 ? tiles_of(p, st.rows) : 0;
+  ow.tiles = keys_o > 0 ? tiles_of(p, ow.rows) : 0;
+  const int ks = (keys_s + UNIT_KEYS - 1) / UNIT_KEYS, ko = (keys_o + UNIT_KEYS - 1) / UNIT_KEYS;
+  const int all = lane_of(lanes_upto(st.tiles + ow.tiles), 63), work = lane_of(lanes_upto(st.tiles * ks + ow.tiles * ko), 63);
+  const Cut cut = cut_of(p, all, work, heads);
+  int longest = max(ks, ko);
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, 64));
+  // the shortest chunks that give no more units; sum of keys / len <= units <= that and one more for each
+  uint32_t lo = cut.least, hi = max(cut.least, longest);
+  if (cut.most > all) hi = max(lo, min(hi, (uint32_t)work / (uint32_t)(cut.most - all) + 1));
+  while (lo < hi) {
+    const uint32_t len = (lo + hi) >> 1;
+    const int c = (ks + len - 1) / len * st.tiles + (ko + len - 1) / len * ow.tiles;
+    if (lane_of(lanes_upto(c), 63) <= cut.most)
+      hi = len;
+    else
+      lo = len + 1;
+  }
+  int units = 0, states = 0;
+  auto split = [&](Split& z, int keys, int k) {
+    z.chunks = (k + lo - 1) / lo;
+    z.each = z.chunks > 1 ? ((uint32_t)(keys + z.chunks - 1) / (uint32_t)z.chunks + UNIT_KEYS - 1) / UNIT_KEYS * UNIT_KEYS : keys;
+    const int n = z.chunks * z.tiles, m = z.chunks * z.rows * heads, un = lanes_upto(n), um = lanes_upto(m);
+    z.unit = units + un - n;
+    z.state = states + um - m;
+    units += lane_of(un, 63);
+    states += lane_of(um, 63);
+  };
+  split(st, keys_s, ks);
+  split(ow, keys_o, ko);
+  t.of[lane] = Segments{st, ow, x, first, prompt, y.k0, y.nk, prompt >= 0 ? 63 - __clzll(starts & mine) : -1};
+  t.first[lane] = there ? first : 0x7fffffff;
+  if (lane == 0) {
+    t.units = units;
+    t.queries = queries;
+  }
+}
+// What the join takes of query i (see shared_plan_kernel).
+__device__ __forceinline__ void tell_query(const SharedArgs& s, const SharedPlan& p, const Table& t, int i) {
+  const AttnArgs& a = s.own;
+  const Segments& x = t.of[t.holder(i)];
+  const Segments& y = t.of[max(x.run, 0)];
+  const int G = a.Hq / a.Hkv, at = i - x.first, end = sees(a, x.doc, at), each = x.own.each;
+  p.tok[3 * (size_t)i] = make_int4((int)(&x - t.of), x.doc.q0 + at, 0, 0);
+  p.tok[3 * (size_t)i + 1] =
+      make_int4(x.own.state + at * G, x.own.rows, each > 0 ? min(x.own.chunks, (int)((uint32_t)(end + each - 1) / (uint32_t)each)) : 0, 0);
+  p.tok[3 * (size_t)i + 2] = make_int4(y.stack.state + (i - y.first) * G, y.stack.rows, x.run >= 0 ? y.stack.chunks : 0, 0);
+}
+
 // ---- units ------------------------------------------------------------------------
 template <typename T, int HD, int QG, int KG, int KT, int S>
 struct Shape {
   static constexpr int qg = QG, kg = KG, kt = KT, s = S, lds = attend_lds<T, HD, QG, KG, KT, S>();
+  static_assert(QG * KG == 4 && lds <= 64 * 1024, "four waves, two workgroups a CU");
 };
+// Tiles of 128 rows; of few rows, where the waves split the keys, each with a stage of
+// its own: beside the other workgroup's four waves their loads need no second one.  (Rows
+// of 512 bytes: half the keys fit.)
 template <typename T, int HD>
 struct Shapes {
-  static constexpr bool WIDE = sizeof(T) == 4 && HD == 128;  // rows of 512 bytes, half the keys fit
-  typedef Shape<T, HD, 4, 2, 32, WIDE ? 2 : 3> Stack;
-  typedef Shape<T, HD, WIDE ? 4 : 2, WIDE ? 2 : 4, 32, 2> Own;
-  static constexpr int lds = Stack::lds > Own::lds ? Stack::lds : Own::lds;
+  static constexpr bool F32 = sizeof(T) == 4, WIDE = F32 && HD == 128;
+  typedef Shape<T, HD, 4, 1, F32 ? 32 : 64, F32 && !WIDE ? 4 : 2> Many;
+  typedef Shape<T, HD, WIDE ? 2 : 1, WIDE ? 2 : 4, 32, F32 || HD == 128 ? 1 : 2> Few;
+  static constexpr int lds = Many::lds > Few::lds ? Many::lds : Few::lds;
 };
-constexpr int own_rows(bool f32, int hd) { return f32 && hd == 128 ? 128 : 64; }
 
-template <typename T, int HD>
-__global__ void __launch_bounds__(512, 1) shared_units_kernel(SharedArgs s, SharedPlan p) {
+// SELF: every workgroup plans for itself; else shared_plan_kernel has.
+template <typename T, int HD, bool SELF>
+__global__ void __launch_bounds__(256, 2) shared_units_kernel(SharedArgs s, SharedPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
-  typedef typename Shapes<T, HD>::Stack Stack;
-  typedef typename Shapes<T, HD>::Own Own;
   __shared__ __attribute__((aligned(1024))) char lds[Shapes<T, HD>::lds];
+  __shared__ std::conditional_t<SELF, Table, int> table;
   const AttnArgs& a = s.own;
-  const int G = a.Hq / a.Hkv, wave = uniform((int)threadIdx.x >> 6), lq = threadIdx.x & 31;
-  const long n = (long)p.count[0] * a.Hkv;
-  for (long u = blockIdx.x; u < n; u += gridDim.x) {
-    if (u != (long)blockIdx.x) __syncthreads();  // the last unit's LDS is free
-    const int e = (int)(u / a.Hkv), g = (int)(u % a.Hkv);
-    const int4 u0 = p.unit[2 * (size_t)e], u1 = p.unit[2 * (size_t)e + 1];
-    const int who = uniform(u0.x), r0 = uniform(u0.y), rows = uniform(u0.z);
-    const size_t state = (size_t)uniform(u1.y) + (size_t)g * rows;
-    auto keep = [&](const Rows<HD>& R) { keep_state(R, p.part, p.part_ml, state + (size_t)R.t * G + R.h % G); };
-    if (who < 0) {
-      const Prompt pr = prompt_at(s, ~who);
-      Keys k = keys_at<T>(s.pk, s.pv, ~who, pr.k0, g);
-      k.kb = uniform(u0.w);
-      k.ke = k.tile_first = k.see_first = k.see_last = uniform(u1.x);
-      const int before = uniform(pr.nk), row = r0 + 32 * (wave % Stack::qg) + lq, first = uniform(u1.z);
-      if (r0 + 32 * (wave % Stack::qg) >= rows) k.see_first = k.see_last = 0;
-      auto rows_of = [&](Rows<HD>& R) {
-        R.mine = row < rows;
-        R.t = R.mine ? row / G : 0;
-        R.h = g * G + (R.mine ? row % G : 0);
-        R.end = R.mine ? k.ke : 0;
-        R.slope = 0.f;
-        R.at = 0;
-        const int4 q = p.tok[3 * (size_t)(first + R.t)];
-        if (a.slopes) {
-          if (R.mine) R.slope = a.slopes[R.h] * LOG2E;
-          R.at = distances_from(q.z, before, q.w, R.slope) + before;
-        }
-        return static_cast<const T*>(a.q.data) + q.x * a.q.stride_b + q.y * a.q.stride_l + R.h * a.q.stride_h;
-      };
-      attend<T, HD, Stack::qg, Stack::kg, Stack::kt, Stack::s, false>(a, lds, k, k, rows_of, keep);
+  const int G = a.Hq / a.Hkv;
+  const auto& t = table;
+  if constexpr (SELF) {
+    if (threadIdx.x < 64) plan_docs(s, p, table);
+    __syncthreads();
+  }
+  const uint32_t n = (uint32_t)a.Hkv * (uint32_t)uniform([&] {
+    if constexpr (SELF) return t.units;
+    else return p.count[0];
+  }());
+  for (uint32_t u = blockIdx.x; u < n; u += gridDim.x) {
+    if (u != blockIdx.x) __syncthreads();  // the last unit's LDS is free
+    // (hidden from the compiler, which would keep what is the same for all units in registers)
+    int tid = threadIdx.x;
+    asm volatile("" : "+v"(tid));
+    const int wave = uniform(tid >> 6), lane = tid & 63, lq = lane & 31;
+    const uint32_t e = u / (uint32_t)a.Hkv, g = u - e * (uint32_t)a.Hkv;
+    int who, r0, rows, kb, kend, state0, first, before;  // (see shared_plan_kernel)
+    Doc d;
+    Keys k;
+    if constexpr (SELF) {
+      const Split &x = t.of[lane].stack, &y = t.of[lane].own;
+      const int l0 = __ffsll(__ballot(e - x.unit < (uint32_t)(x.chunks * x.tiles))) - 1;
+      const int l = l0 >= 0 ? l0 : __ffsll(__ballot(e - y.unit < (uint32_t)(y.chunks * y.tiles))) - 1;
+      // its numbers, one a lane
+      static_assert(sizeof(Segments) == 23 * 4, "Segments is 23 ints");
+      const int rec = reinterpret_cast<const int*>(&t.of[l])[min(lane, 22)];
+      const int z = l0 >= 0 ? 0 : 6;
+      const int i = (int)e - lane_of(rec, z), tiles = lane_of(rec, z + 2), c = (uint32_t)i / (uint32_t)tiles, each = lane_of(rec, z + 5);
+      rows = lane_of(rec, z + 3);
+      d = Doc{lane_of(rec, 12), lane_of(rec, 13), lane_of(rec, 14), lane_of(rec, 15), lane_of(rec, 16), lane_of(rec, 17)};
+      first = lane_of(rec, 18);
+      before = lane_of(rec, 21);
+      who = l0 >= 0 ? ~lane_of(rec, 19) : l;
+      r0 = (i - c * tiles) * tile_rows(p, rows);
+      kb = c * each;
+      kend = c + 1 < lane_of(rec, z + 4) ? kb + each : l0 >= 0 ? before : 0x7fffffff;
+      state0 = lane_of(rec, z + 1) + c * rows * a.Hkv;
+      k = who < 0 ? keys_at<T>(s.pk, s.pv, ~who, lane_of(rec, 20), g) : keys_at<T>(a.k, a.v, who, d.k0, g);
     } else {
-      Doc d = doc_of(a, who);
-      d = Doc{uniform(d.q0), uniform(d.nq), uniform(d.k0), uniform(d.nk), uniform(d.pos), uniform(d.prefix)};
-      const int kb = uniform(u0.w), t_last = (min(r0 + 32 * Own::qg, rows) - 1) / G, ke = uniform(min(sees(a, d, t_last), u1.x));
-      if (kb >= ke && kb > 0) continue;
-      const int w0 = r0 + 32 * (wave % Own::qg), w1 = min(w0 + 32, rows), row = w0 + lq;
-      Keys k = keys_at<T>(a.k, a.v, who, d.k0, g);
+      const int4 u0 = p.unit[2 * (size_t)e], u1 = p.unit[2 * (size_t)e + 1];
+      who = uniform(u0.x);
+      r0 = uniform(u0.y);
+      rows = uniform(u0.z);
+      kb = uniform(u0.w);
+      kend = uniform(u1.x);
+      state0 = uniform(u1.y);
+      first = uniform(u1.z);
+      const int pn = who < 0 ? ~who : prompt_of(s, who);
+      const Prompt pr = pn >= 0 ? prompt_at(s, pn) : Prompt{0, 0};
+      before = uniform(pr.nk);
+      if (who >= 0) {
+        d = doc_of(a, who);
+        d = Doc{uniform(d.q0), uniform(d.nq), uniform(d.k0), uniform(d.nk), uniform(d.pos), uniform(d.prefix)};
+      }
+      k = who < 0 ? keys_at<T>(s.pk, s.pv, ~who, uniform(pr.k0), g) : keys_at<T>(a.k, a.v, who, d.k0, g);
+    }
+    auto run = [&](auto shape) {
+      typedef decltype(shape) X;
+      const int w0 = r0 + 32 * (wave % X::qg), w1 = min(w0 + 32, rows), row = w0 + lq;
       k.kb = kb;
-      k.ke = ke;
-      k.tile_first = uniform(sees(a, d, r0 / G));
-      k.see_first = uniform(w0 < rows ? sees(a, d, w0 / G) : 0);
-      k.see_last = uniform(w0 < rows ? sees(a, d, (w1 - 1) / G) : 0);
+      if (who < 0) {
+        k.ke = k.tile_first = kend;
+        k.see_first = k.see_last = w0 < rows ? kend : 0;
+      } else {
+        k.ke = uniform(min(sees(a, d, (min(r0 + 32 * X::qg, rows) - 1) / G), kend));
+        if (kb >= k.ke && kb > 0) return;
+        k.tile_first = uniform(sees(a, d, r0 / G));
+        k.see_first = uniform(w0 < rows ? sees(a, d, w0 / G) : 0);
+        k.see_last = uniform(w0 < rows ? sees(a, d, (w1 - 1) / G) : 0);
+      }
       auto rows_of = [&](Rows<HD>& R) {
         R.mine = row < rows;
         R.t = R.mine ? row / G : 0;
-        R.h = g * G + (R.mine ? row % G : 0);
-        R.end = R.mine ? sees(a, d, R.t) : 0;
+        R.h = (int)g * G + (R.mine ? row - R.t * G : 0);
         R.slope = 0.f;
         R.at = 0;
+        int doc = who, token = d.q0 + R.t, end;
+        long i = (long)d.pos + R.t;
+        if (who >= 0) {
+          end = sees(a, d, R.t);
+        } else if constexpr (SELF) {
+          doc = t.holder(first + R.t);
+          const Doc q = t.of[doc].doc;
+          const int x = first + R.t - t.first[doc];
+          token = q.q0 + x;
+          i = (long)q.pos + x;
+          end = sees(a, q, x);
+        } else {
+          const int4 q = p.tok[3 * (size_t)(first + R.t)];
+          doc = q.x;
+          token = q.y;
+          i = q.z;
+          end = q.w;
+        }
+        R.end = R.mine ? (who < 0 ? k.ke : end) : 0;
         if (a.slopes) {
           if (R.mine) R.slope = a.slopes[R.h] * LOG2E;
-          const int pr = prompt_of(s, who);
-          R.at = distances_from((long)d.pos + R.t, pr >= 0 ? prompt_at(s, pr).nk : 0, R.end, R.slope);
+          R.at = distances_from(i, before, end, R.slope) + (who < 0 ? before : 0);
         }
-        return static_cast<const T*>(a.q.data) + who * a.q.stride_b + (long)(d.q0 + R.t) * a.q.stride_l + R.h * a.q.stride_h;
+        return static_cast<const T*>(a.q.data) + doc * a.q.stride_b + token * a.q.stride_l + R.h * a.q.stride_h;
       };
-      attend<T, HD, Own::qg, Own::kg, Own::kt, Own::s, false>(a, lds, k, k, rows_of, keep);
-    }
+      const size_t state = (size_t)state0 + (size_t)g * rows;
+      attend<T, HD, X::qg, X::kg, X::kt, X::s, false>(
+          a, lds, tid, k, k, rows_of, [&](const Rows<HD>& R) { keep_state(R, p.part, p.part_ml, state + (size_t)R.t * G + (R.h - (int)g * G)); });
+    };
+    if (tile_rows(p, rows) == MANY_ROWS)
+      run(typename Shapes<T, HD>::Many{});
+    else
+      run(typename Shapes<T, HD>::Few{});
+  }
+  if constexpr (SELF) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) p.count[1] = t.queries;
+    for (int i = blockIdx.x + threadIdx.x * gridDim.x; i < t.queries; i += 256 * gridDim.x) tell_query(s, p, t, i);
   }
 #endif
 }
@@ -382,7 +570,7 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) shared_chain_k
     }
     return static_cast<const T*>(a.q.data) + dn * a.q.stride_b + (long)(d.q0 + R.t) * a.q.stride_l + R.h * a.q.stride_h;
   };
-  attend<T, HD, QG, KG, KT, S, true>(a, lds, k1, k2, rows_of, [&](const Rows<HD>& R) {
+  attend<T, HD, QG, KG, KT, S, true>(a, lds, threadIdx.x, k1, k2, rows_of, [&](const Rows<HD>& R) {
     store_row(R, static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + R.t) * a.out.stride_l + R.h * a.out.stride_h);
   });
 #endif
@@ -394,10 +582,10 @@ SharedPlan choose(const SharedArgs& s) {
   SharedPlan p{};
   const int G = a.Hq / a.Hkv, rows = a.max_q * G, cus = device_cu_count();
   const bool f32 = a.dtype == DLLM_F32;
-  p.slots = cus;
-  p.own_rows = own_rows(f32, a.hd);
-  p.tiles = ceil_div(rows, 128);
-  p.chain = rows > 128 && (long)a.docs * a.Hkv * p.tiles >= 2 * cus;
+  p.slots = 2 * cus;
+  p.few_rows = f32 && a.hd == 128 ? 64 : 32;
+  p.tiles = ceil_div(rows, MANY_ROWS);
+  p.chain = rows > MANY_ROWS && (long)a.docs * a.Hkv * p.tiles >= 2 * cus;
   if (p.chain) {
     p.grid = ((long)a.docs * a.Hkv + 7) / 8 * 8 * p.tiles;
     return p;
@@ -405,13 +593,14 @@ SharedPlan choose(const SharedArgs& s) {
   const long packed = a.q.stride_b == 0 ? a.q_tokens : (long)a.docs * a.max_q;
   p.cap = (int)std::min(std::min((long)a.docs * a.max_q, packed), 0x7fffffffl);
   // units without a split: of the runs (as many as documents, but where prompts' documents
-  // follow each other no more than those and one more for each without) and the documents
-  const long stack = ((long)p.cap * G + STACK_ROWS - 1) / STACK_ROWS;
-  const long own = std::min((long)a.docs * ceil_div(rows, p.own_rows), ((long)p.cap * G + p.own_rows - 1) / p.own_rows + a.docs);
-  p.units = stack + (s.prompt ? a.docs : 1) + own + p.slots / a.Hkv + 1;
-  const long expected = (stack + (s.prompt ? std::min(a.docs, s.prompts) : 1) + own) * a.Hkv;
-  p.grid = std::min((expected + cus - 1) / cus * cus, 1l << 22);
-  p.states = 2l * p.cap * a.Hq + (long)p.slots * STACK_ROWS;
+  // follow each other no more than those) and of the documents
+  const long whole = ((long)p.cap * G + MANY_ROWS - 1) / MANY_ROWS;
+  const long own = std::min((long)a.docs * std::max(tiles_of(p, std::min(rows, 64)), tiles_of(p, rows)), whole + 2l * a.docs);
+  p.units = whole + 2l * (s.prompt ? a.docs : 1) + own + 2 * p.slots / a.Hkv + 1;
+  const long expected = (whole + (s.prompt ? std::min(a.docs, s.prompts) : 1) + own) * a.Hkv;
+  p.grid = std::min((expected + p.slots - 1) / p.slots * p.slots, 1l << 22);
+  // (cut_of: chunks beyond the first are fewer than 4/3 of the workgroups that run at once)
+  p.states = 2l * p.cap * a.Hq + 2l * p.slots * MANY_ROWS;
   return p;
 }
 
@@ -447,9 +636,13 @@ void launch(const SharedArgs& s, const SharedPlan& p, hipStream_t st) {
     return;
   }
   const int docs = s.own.docs;
-  shared_plan_kernel<<<1, docs <= 64 ? 64 : docs <= 256 ? 256 : PLAN_THREADS, 0, st>>>(s, p);
-  DLLM_LAUNCH_CHECK("shared_plan_kernel");
-  shared_units_kernel<T, HD><<<(unsigned)p.grid, 512, 0, st>>>(s, p);
+  if (docs <= 64) {
+    shared_units_kernel<T, HD, true><<<(unsigned)p.grid, 256, 0, st>>>(s, p);
+  } else {
+    shared_plan_kernel<<<1, docs <= 256 ? 256 : PLAN_THREADS, 0, st>>>(s, p);
+    DLLM_LAUNCH_CHECK("shared_plan_kernel");
+    shared_units_kernel<T, HD, false><<<(unsigned)p.grid, 256, 0, st>>>(s, p);
+  }
   DLLM_LAUNCH_CHECK("shared_units_kernel");
   const long rows = (long)p.cap * s.own.Hq;
   if (rows <= 4l * device_cu_count())
@@ -475,7 +668,7 @@ bool attn_shared_fits(const SharedArgs& s) {
   if (alone(s)) return attn_docs_fits(s.own);
   const SharedPlan p = choose(s);
   if (p.chain) return p.grid * 256 < (1l << 32);
-  return p.states < (1l << 31) && p.units < (1l << 31) && (long)p.cap * s.own.Hq < (1l << 26);
+  return p.states < (1l << 31) && p.units * s.own.Hkv < (1l << 31) && (long)p.cap * s.own.Hq < (1l << 26);
 }
 
 void launch_attn_shared(const SharedArgs& s, void* ws, hipStream_t st) {

@@ -251,11 +251,11 @@ struct SharedArgs {
 };
 // Layout of a call: whether a document's tiles take its prompt's keys and its own in one
 // go (then the row tiles of a document), workgroups; else queries at most, units at most,
-// workgroups of a round, rows of a document's tile, states at most, and what the
+// workgroups of a round, rows of a tile of few, states at most, and what the
 // workspace holds (shared_plan_kernel).
 struct SharedPlan {
   bool chain;
-  int tiles, cap, slots, own_rows;
+  int tiles, cap, slots, few_rows;
   long grid, units, states;
   int* count;  // units without their heads, queries
   int4 *tok, *seg, *run, *unit;
