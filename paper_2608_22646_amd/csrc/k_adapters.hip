@@ -233,7 +233,11 @@ __device__ __forceinline__ void sum_shares(const AdaptersArgs& a, const Adapters
 #pragma unroll
   for (int e = 0; e < E; ++e) v[e] = 0.f;
   int z = 0;
-  for (; z + 4 <= p.splits; z += 4) shares(std::integral_constant<int, 4>{}, z);
+  for (; z + 8 <= p.splits; z += 8) shares(std::integral_constant<int, 8>{}, z);
+  if (z + 4 <= p.splits) {
+    shares(std::integral_constant<int, 4>{}, z);
+    z += 4;
+  }
   if (z + 2 <= p.splits) {
     shares(std::integral_constant<int, 2>{}, z);
     z += 2;
@@ -411,18 +415,17 @@ __global__ void __launch_bounds__(NW * 64) adapters_shrink_kernel(AdaptersArgs a
 
 // Sums the shares of the inner products, in their order: a piece of a row each thread.
 template <typename T, int PARTS>
-__global__ void __launch_bounds__(256) adapters_join_kernel(AdaptersArgs a, AdaptersPlan p) {
+__global__ void __launch_bounds__(64) adapters_join_kernel(AdaptersArgs a, AdaptersPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   constexpr int E = Kind<T>::E;
-  const int row = (int)blockIdx.x * 256 + threadIdx.x, s = blockIdx.y / (p.r16 / E), c = blockIdx.y % (p.r16 / E) * E;
+  const int row = (int)blockIdx.x * 64 + threadIdx.x, s = blockIdx.y / (p.r16 / E), c = blockIdx.y % (p.r16 / E) * E;
   if (row >= a.rows) return;
   const int w = adapter_of(a, row);
+  float v[E];
+  sum_shares<T>(a, p, row, s, c, v);  // (beside the adapter; what an adapter does not have is not used)
   if (w < 0) return;
   const int rank = rank_of(a, w);
-  if (c >= rank) return;
-  float v[E];
-  sum_shares<T>(a, p, row, s, c, v);
-  keep_piece<T, PARTS>(a, p, row, s, c, rank, a.scales ? a.scales[w] : 1.f, v);
+  if (c < rank) keep_piece<T, PARTS>(a, p, row, s, c, rank, a.scales ? a.scales[w] : 1.f, v);
 #endif
 }
 
@@ -538,13 +541,13 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
       }
     };
     const f32x4_t zero = {0, 0, 0, 0};
-    u32x4_t bf[ONE ? 1 : 2][8];
+    u32x4_t bf[1][8];
     Eight<O> y[2][4];
     if constexpr (ONE) {
       load_y(0, y[0]);
       if (MT > 1) load_y(1, y[1]);
     }
-    if (steps) load_b(0, bf[0]);
+    if (ONE && steps) load_b(0, bf[0]);
     if constexpr (ONE) {
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
@@ -563,24 +566,20 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
       f32x4_t acc[2][8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) acc[0][i] = acc[1][i] = zero;
-      auto step = [&](int s, const u32x4_t (&now)[8], u32x4_t (&later)[8]) {
+      for (int s = 0; s < steps; ++s) {
         u32x4_t hs[2][PARTS];
 #pragma unroll
         for (int m = 0; m < 2; ++m)
 #pragma unroll
           for (int q = 0; q < PARTS; ++q) hs[m][q] = load_h(s, q, m);
-        if (s + 1 < steps) load_b(s + 1, later);
+        load_b(s, bf[0]);
 #pragma unroll
         for (int q = 0; q < PARTS; ++q)
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
-            acc[0][i] = product<T>(hs[0][q], now[i], acc[0][i]);
-            acc[1][i] = product<T>(hs[1][q], now[i], acc[1][i]);
+            acc[0][i] = product<T>(hs[0][q], bf[0][i], acc[0][i]);
+            acc[1][i] = product<T>(hs[1][q], bf[0][i], acc[1][i]);
           }
-      };
-      for (int s = 0; s < steps; s += 2) {
-        step(s, bf[0], bf[1]);
-        if (s + 1 < steps) step(s + 1, bf[1], bf[0]);
       }
       load_y(0, y[0]);
       if (MT > 1) load_y(1, y[1]);
@@ -591,7 +590,7 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
 }
 
 template <typename T, typename O, int PARTS, bool VY, bool VB, bool ONE>
-__global__ void __launch_bounds__(256, ONE && sizeof(O) == 2 ? 3 : 2) adapters_expand_kernel(AdaptersArgs a, AdaptersPlan p) {
+__global__ void __launch_bounds__(256, sizeof(O) == 2 ? 3 : 2) adapters_expand_kernel(AdaptersArgs a, AdaptersPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ int rows[TM];
   int slice = 0, first = 0, block = blockIdx.x % p.blocks;
@@ -649,7 +648,7 @@ void run(const AdaptersArgs& a, const AdaptersPlan& p, hipStream_t s) {
       adapters_shrink_kernel<T, PARTS, 2, true><<<grid, NW * 64, 0, s>>>(a, p);
     DLLM_LAUNCH_CHECK("adapters_shrink_kernel");
     if (a.rank > Kind<T>::STEP && !p.keep) {
-      adapters_join_kernel<T, PARTS><<<dim3(ceil_div(a.rows, 256), a.slices * p.r16 / Kind<T>::E), 256, 0, s>>>(a, p);
+      adapters_join_kernel<T, PARTS><<<dim3(ceil_div(a.rows, 64), a.slices * p.r16 / Kind<T>::E), 64, 0, s>>>(a, p);
       DLLM_LAUNCH_CHECK("adapters_join_kernel");
     }
   }

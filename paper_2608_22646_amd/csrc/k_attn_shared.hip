@@ -20,7 +20,7 @@ namespace dllm {
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
-constexpr int UNIT_KEYS = 128, LEAST_KEYS = 256;  // chunks are multiples of this, and at least that
+constexpr int UNIT_KEYS = 128;                    // chunks are multiples of this
 constexpr int UNIT_COST = 4;                      // in UNIT_KEYS
 constexpr int MANY_ROWS = 128;                    // rows of a tile of many
 
@@ -62,9 +62,9 @@ struct Cut {
 };
 __device__ __forceinline__ Cut cut_of(const SharedPlan& p, int all, int work, int heads) {
   const uint32_t slots = (uint32_t)p.slots / (uint32_t)heads;  // (at least 1 unit, whatever the heads)
-  if ((uint32_t)all < slots) return Cut{max(LEAST_KEYS / UNIT_KEYS, (int)((uint32_t)work / slots)), (int)slots};
+  if ((uint32_t)all < slots) return Cut{max(1, (int)((uint32_t)work / slots)), (int)slots};
   const float part = ((float)work + (float)all * UNIT_COST) * (float)heads / (float)p.slots;
-  return Cut{max(LEAST_KEYS / UNIT_KEYS, (int)part), 0x7fffffff};
+  return Cut{max(1, (int)part), 0x7fffffff};
 }
 
 // ---- what is stacked and split how -------------------------------------------------
