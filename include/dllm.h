@@ -529,9 +529,9 @@ int dllm_attention(const dllm_attn_args* args, void* workspace, size_t workspace
  * costs time only.  Documents must not share queries; where they do, some rows of out may
  * not be written.  Out must not overlap anything that is read.
  * Requirements: those of dllm_attention for `own`; pk and pv those of k and v; prompts in
- * [0, 65535], 0 <= max_p <= p_tokens <= 2^29, kv_tokens <= 2^29; fewer than 2^26 rows
- * (queries times n_heads) where a document has few.  docs or max_q of 0: nothing; prompts or max_p of 0:
- * dllm_attention.
+ * [0, 65535], 0 <= max_p <= p_tokens <= 2^29, kv_tokens <= 2^29; where documents have
+ * few rows, fewer than 2^26 rows (queries times n_heads) and 2^30 pairs of a row tile and 128 keys.
+ * docs or max_q of 0: nothing; prompts or max_p of 0: dllm_attention.
  */
 typedef struct dllm_shared_attn_args {
   dllm_attn_args own;
@@ -542,7 +542,7 @@ typedef struct dllm_shared_attn_args {
   const int32_t* prompt;          /* [docs] */
 } dllm_shared_attn_args;
 
-/* As dllm_attention_workspace_size (whether own.q.stride_b is 0 is looked at) and dllm_attention. */
+/* As dllm_attention_workspace_size (whether own.out.stride_b is 0 is looked at) and dllm_attention. */
 int dllm_shared_attention_workspace_size(const dllm_shared_attn_args* args, size_t* bytes);
 int dllm_shared_attention(const dllm_shared_attn_args* args, void* workspace, size_t workspace_bytes, void* stream);
 

@@ -89,9 +89,10 @@ def shared_attention(q, k, v, pk, pv, pos, block=0, prefix=0, scale=None, cap=0.
                 continue
             p = np.exp(s - s.max())
             p /= p.sum()
-            sure = p > 0
-            out[t, h], mass[t, h] = p @ vv, p[sure] @ np.abs(vv[sure])
-            top[t, h], dot[t, h] = np.abs(s[sure]).max(), (np.abs(kk[sure]) @ np.abs(q[t, h])).max()
+            some = p > 0
+            out[t, h], mass[t, h] = p @ vv, p @ np.abs(vv)
+            if some.any():
+                top[t, h], dot[t, h] = np.abs(s[some]).max(), (np.abs(kk[some]) @ np.abs(q[t, h])).max()
     return out, mass, top, dot
 
 

@@ -791,8 +791,10 @@ def shared_attention(q, k, v, pk, pv, docs: Docs | None = None, prompts: Prompts
 def shared_attention_workspace_size(q, k, v, pk, pv, docs: Docs | None = None, prompts: Prompts | None = None):
     """Bytes of workspace that shared_attention() needs for operands, documents and prompts of these sizes."""
     n = _sz()
-    check(lib().dllm_shared_attention_workspace_size(
-        _shared_args(_dtype(q, "q"), q, k, v, pk, pv, q, docs or Docs(), prompts or Prompts(), 0, None, 0.0, None), n))
+    a = _shared_args(_dtype(q, "q"), q, k, v, pk, pv, q, docs or Docs(), prompts or Prompts(), 0, None, 0.0, None)
+    if q.dim() == 4 and q.shape[0] > 1:
+        a.own.out.stride_b = 1  # slabs of out, though q's may be one that is expanded
+    check(lib().dllm_shared_attention_workspace_size(a, n))
     return n.value
 
 
@@ -874,9 +876,10 @@ def adapters(x, base, A, B, which, ranks=None, scales=None, slices=None, out=Non
 
 
 def adapters_workspace_size(x, base, A, B, slices=None):
-    """Bytes of workspace that adapters() needs for operands of these sizes."""
+    """Bytes of workspace that adapters() needs for operands of these sizes (base None: of x's type)."""
     n = _sz()
-    a, _ = _adapter_args(x, base, A, B, None, None, None, slices, base)
+    out = x.new_empty((1, B.shape[1])).expand(x.shape[0], -1) if base is None else base
+    a, _ = _adapter_args(x, base, A, B, None, None, None, slices, out)
     check(lib().dllm_adapters_workspace_size(a, n))
     return n.value
 

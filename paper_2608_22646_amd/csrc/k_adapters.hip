@@ -546,9 +546,11 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
     if constexpr (ONE) {
       load_y(0, y[0]);
       if (MT > 1) load_y(1, y[1]);
-    }
-    if (ONE && steps) load_b(0, bf[0]);
-    if constexpr (ONE) {
+      if (steps)
+        load_b(0, bf[0]);
+      else
+#pragma unroll
+        for (int i = 0; i < 8; ++i) bf[0][i] = u32x4_t{0, 0, 0, 0};
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         if (m >= MT) break;
@@ -557,9 +559,6 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
         for (int q = 0; q < PARTS; ++q)
 #pragma unroll
           for (int i = 0; i < 8; ++i) acc[i] = product<T>(hf[m][q], bf[0][i], q ? acc[i] : zero);
-        if (!steps)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc[i] = zero;
         finish(m, y[m], acc);
       }
     } else {

@@ -167,8 +167,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
   // two segments a thread held, where there are no more
   const bool few = segs <= 2 * N;
   int rows_h[2] = {0, 0}, keys_h[2] = {0, 0}, tiles_h[2] = {0, 0};
-  int units = 0, longest = 0;
-  long work = 0;  // tiles times keys
+  int units = 0, longest = 0, work = 0;  // work: tiles times keys, in UNIT_KEYS (the host sees to it that all fit)
   for (int i = tid, k = 0; i < segs; i += N, ++k) {
     int rows, keys;
     size_of(i, rows, keys);
@@ -179,12 +178,12 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
       tiles_h[k & 1] = t;
     }
     units += t;
-    work += (long)t * keys;
+    work += t * ((keys + UNIT_KEYS - 1) / UNIT_KEYS);
     longest = max(longest, keys);
   }
   int all_units, all_work, n;
   before_of(units, sums, all_units);
-  before_of((int)min((work + UNIT_KEYS - 1) / UNIT_KEYS, 0x1fffffl), sums, all_work);
+  before_of(work, sums, all_work);
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) longest = max(longest, __shfl_xor(longest, o, 64));
   __syncthreads();
@@ -590,17 +589,20 @@ SharedPlan choose(const SharedArgs& s) {
     p.grid = ((long)a.docs * a.Hkv + 7) / 8 * 8 * p.tiles;
     return p;
   }
-  const long packed = a.q.stride_b == 0 ? a.q_tokens : (long)a.docs * a.max_q;
+  const long packed = a.out.stride_b == 0 ? a.q_tokens : (long)a.docs * a.max_q;
   p.cap = (int)std::min(std::min((long)a.docs * a.max_q, packed), 0x7fffffffl);
   // units without a split: of the runs (as many as documents, but where prompts' documents
   // follow each other no more than those) and of the documents
   const long whole = ((long)p.cap * G + MANY_ROWS - 1) / MANY_ROWS;
   const long own = std::min((long)a.docs * std::max(tiles_of(p, std::min(rows, 64)), tiles_of(p, rows)), whole + 2l * a.docs);
-  p.units = whole + 2l * (s.prompt ? a.docs : 1) + own + 2 * p.slots / a.Hkv + 1;
+  const long base = whole + 2l * a.docs + own, keys = ceil_div(std::max(s.max_p, a.max_kv), UNIT_KEYS);
+  // (cut_of: chunks beyond the first are fewer than 4/3 of the workgroups that run at once)
+  const long more = std::min(2l * p.slots / a.Hkv + 1, base * (keys - 1));
+  p.units = base + more;
+  p.work = base * keys;
   const long expected = (whole + (s.prompt ? std::min(a.docs, s.prompts) : 1) + own) * a.Hkv;
   p.grid = std::min((expected + p.slots - 1) / p.slots * p.slots, 1l << 22);
-  // (cut_of: chunks beyond the first are fewer than 4/3 of the workgroups that run at once)
-  p.states = 2l * p.cap * a.Hq + 2l * p.slots * MANY_ROWS;
+  p.states = 2l * p.cap * a.Hq + more * a.Hkv * MANY_ROWS;
   return p;
 }
 
@@ -668,7 +670,7 @@ bool attn_shared_fits(const SharedArgs& s) {
   if (alone(s)) return attn_docs_fits(s.own);
   const SharedPlan p = choose(s);
   if (p.chain) return p.grid * 256 < (1l << 32);
-  return p.states < (1l << 31) && p.units * s.own.Hkv < (1l << 31) && (long)p.cap * s.own.Hq < (1l << 26);
+  return p.states < (1l << 31) && p.units * s.own.Hkv < (1l << 31) && p.work < (1l << 30) && (long)p.cap * s.own.Hq < (1l << 26);
 }
 
 void launch_attn_shared(const SharedArgs& s, void* ws, hipStream_t st) {

@@ -250,13 +250,13 @@ struct SharedArgs {
   const int32_t *p_start, *p_len, *prompt;
 };
 // Layout of a call: whether a document's tiles take its prompt's keys and its own in one
-// go (then the row tiles of a document), workgroups; else queries at most, units at most,
-// workgroups of a round, rows of a tile of few, states at most, and what the
+// go (then the row tiles of a document), workgroups; else queries at most, units at most, tiles
+// times 128 keys at most, workgroups of a round, rows of a tile of few, states at most, and what the
 // workspace holds (shared_plan_kernel).
 struct SharedPlan {
   bool chain;
   int tiles, cap, slots, few_rows;
-  long grid, units, states;
+  long grid, units, work, states;
   int* count;  // units without their heads, queries
   int4 *tok, *seg, *run, *unit;
   int2* info;  // of a document: its first query, its run

@@ -115,7 +115,7 @@ bool shared_args(const dllm_shared_attn_args* p, SharedArgs* s) {
   require(p->max_p >= 0 && p->max_p <= p->p_tokens && p->p_tokens <= (1 << 29), DLLM_ESHAPE,
           "max_p must be in [0, p_tokens], p_tokens at most 2^29");
   require(p->own.kv_tokens <= (1 << 29), DLLM_ESHAPE, "kv_tokens must be at most 2^29");
-  s->own.q.stride_b = p->own.q.stride_b;
+  s->own.out.stride_b = p->own.out.stride_b;
   s->prompts = p->prompts;
   s->p_tokens = p->p_tokens;
   s->max_p = p->max_p;

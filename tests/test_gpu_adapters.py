@@ -164,3 +164,55 @@ def test_rows_and_outputs_beyond_32_bit_offsets(gpu_lib):
     Y.copy_(base)
     which = [m % 2 for m in range(M)]
     verify(B.adapters(X, Y, A, Bm, ints(which), out=Y).clone(), x, base, A, Bm, which, None, None, (N,))
+
+
+@pytest.mark.parametrize("M", [30, 200])
+def test_captured_and_on_other_streams(gpu_lib, M):
+    """Two calls in one graph with a workspace each, replayed with other inputs and eager work between; a call on
+    another stream."""
+    x, base, A, Bm = inputs(M, 512, (256, 128), 5, 40, BF16, BF16)
+    which = ints(m % 6 - 1 for m in range(M))
+    call = lambda ws, out, s=None: B.adapters(x, base, A, Bm, which, slices=(256, 128), out=out, ws=ws, stream=s)  # noqa: E731
+    need = B.adapters_workspace_size(x, base, A, Bm, slices=(256, 128))
+    assert need == B.adapters_workspace_size(x, None, A, Bm, slices=(256, 128))
+    ws, outs = [B.device_buffer(need) for _ in range(3)], [torch.empty_like(base) for _ in range(3)]
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        call(ws[0], outs[0])
+        side.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            call(ws[0], outs[0])
+            call(ws[1], outs[1])
+    for i in range(4):
+        x.copy_(randn(x.shape, BF16, 20 + i))
+        which.copy_(ints((m * (i + 2)) % 6 - 1 for m in range(M)))
+        torch.cuda.synchronize()
+        g.replay()
+        eager = B.adapters(x, base, A, Bm, which, slices=(256, 128))
+        torch.cuda.synchronize()
+        assert torch.equal(outs[0], eager) and torch.equal(outs[1], eager)
+    call(ws[2], outs[2], torch.cuda.Stream())
+    torch.cuda.synchronize()
+    assert torch.equal(outs[2], eager)
+
+
+def test_infinities_follow_the_formula(gpu_lib):
+    """An infinite scale, and inner products beyond bf16's pieces: infinities keep their sign, where b is not zero."""
+    x, base, A, Bm = inputs(40, 64, (72,), 2, 8, BF16, F32)
+    Bm.fill_(0.5)
+    x.fill_(1.0)
+    A[0], A[1] = 3e37, -3e37
+    which = [m % 2 for m in range(40)]
+    got = B.adapters(x, base, A, Bm, ints(which))
+    assert all(torch.isinf(got[m]).all() and (got[m] > 0).all() == (m % 2 == 0) for m in range(40))
+    A.fill_(1.0)
+    got = B.adapters(x, base, A, Bm, ints(which), scales=torch.tensor([float("inf"), float("nan")], device="cuda"))
+    assert (got[::2] == float("inf")).all() and torch.isnan(got[1::2]).all()
+
+
+def test_no_adapter_at_all(gpu_lib):
+    x, base, A, Bm = inputs(10, 64, (72,), 2, 8, BF16, BF16)
+    out = base.clone()
+    assert torch.equal(B.adapters(x, out, A, Bm, ints([-1] * 10), out=out), base)
+    assert not B.adapters(x, None, A[:0], Bm[:0], ints([0] * 10)).any()
