@@ -11,6 +11,7 @@ import ctypes
 import itertools
 import math
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -576,16 +577,30 @@ def _column(t, n, dtype, device, name):
     return t.data_ptr()
 
 
+# The larger argument structures are packed from plain numbers in one go: constructing them field by field, views
+# within them, takes a third of a small call's time.
+_VIEW = "Pqqq"
+_ATTN = struct.Struct("@4i" + 4 * _VIEW + "5i7P2fi0P")
+_SHARED = struct.Struct(_ATTN.format + 2 * _VIEW + "3i3P")
+_ADAPTER = struct.Struct(f"@8i{ADAPTER_SLICES}i" + 5 * _VIEW + "3P")
+assert [x.size for x in (_ATTN, _SHARED, _ADAPTER)] == [_c.sizeof(x) for x in (AttnArgs, SharedAttnArgs, AdapterArgs)]
+
+
 def _rows(t, shape, dtype, device, name):
     """The view of a [B, L, H, hd] or [L, H, hd] tensor whose last dimension is contiguous."""
+    return View(*_row_numbers(t, shape, dtype, device, name))
+
+
+def _row_numbers(t, shape, dtype, device, name):
+    """The fields of such a view."""
     st = t.stride()
     if t.shape != shape or st[-1] != 1 or t.dtype is not dtype or t.device != device:
         _refuse(t.shape == shape, -2, f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
         _refuse(st[-1] == 1 or t.numel() == 0, -2, f"{name}: elements of a head must be contiguous")
         _refuse(t.dtype is dtype and t.device == device, -1, f"{name} must be {dtype} on {device}")
     # a dimension of one element is never stepped over: its stride says nothing
-    return View(t.data_ptr(), st[0] if len(shape) == 4 and shape[0] > 1 else 0, st[-3] if shape[-3] > 1 else shape[-1],
-                st[-2] if shape[-2] > 1 else 0)
+    return (t.data_ptr(), st[0] if len(shape) == 4 and shape[0] > 1 else 0, st[-3] if shape[-3] > 1 else shape[-1],
+            st[-2] if shape[-2] > 1 else 0)
 
 
 def _new_rows(like, shape):
@@ -723,26 +738,32 @@ def attention_workspace_size(q, k, v, docs: Docs | None = None):
     return n.value
 
 
-def _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes):
+def _attn_args(*operands):
+    return AttnArgs.from_buffer_copy(_ATTN.pack(*_attn_numbers(*operands)))
+
+
+def _attn_numbers(dt, q, k, v, out, docs, block, scale, cap, slopes):
+    """The fields of dllm_attn_args."""
     dev, dtype = q.device, q.dtype
     shape, kv = tuple(q.shape), tuple(k.shape)
     one = len(shape) == 3
     T, Hq, hd = shape[-3:]
     S, Hkv = kv[-3:-1]
     kv = (S, Hkv, hd) if one else (shape[0], S, Hkv, hd)
-    views = [_rows(q, shape, dtype, dev, "q"), _rows(k, kv, dtype, dev, "k"), _rows(v, kv, dtype, dev, "v"),
-             _rows(out, shape, dtype, dev, "out")]
+    vq, vk = _row_numbers(q, shape, dtype, dev, "q"), _row_numbers(k, kv, dtype, dev, "k")
+    vv, vo = _row_numbers(v, kv, dtype, dev, "v"), _row_numbers(out, shape, dtype, dev, "out")
     arrays = (docs.q_start, docs.q_len, docs.kv_start, docs.kv_len, docs.q_pos, docs.prefix)
     n = docs.count
     if n is None:
         n = next((t.numel() for t in arrays if t is not None), 1) if one else shape[0]
-    _refuse(one or n == shape[0], -2, "a dense batch has one document per slab")
+    if not one and n != shape[0]:
+        _refuse(False, -2, "a dense batch has one document per slab")
     max_q, max_kv = T if docs.max_q is None else docs.max_q, S if docs.max_kv is None else docs.max_kv
     _in32(n, T, S, max_q, max_kv, block)
-    ptrs = [_column(t, n, torch.int32, dev, name) for t, name in zip(arrays, _DOC_ARRAYS)]
-    return AttnArgs(dt, Hq, Hkv, hd, *views, n, T, S, max_q, max_kv, *ptrs,
-                    _column(slopes, Hq, torch.float32, dev, "slopes"), 1.0 / math.sqrt(hd) if scale is None else scale, cap,
-                    block)
+    ptrs = [0 if t is None else _column(t, n, torch.int32, dev, name) for t, name in zip(arrays, _DOC_ARRAYS)]
+    return (dt, Hq, Hkv, hd, *vq, *vk, *vv, *vo, n, T, S, max_q, max_kv, *ptrs,
+            0 if slopes is None else _column(slopes, Hq, torch.float32, dev, "slopes"),
+            _f32(1.0 / math.sqrt(hd) if scale is None else scale).value, _f32(cap).value, block)
 
 
 @dataclass
@@ -799,20 +820,21 @@ def shared_attention_workspace_size(q, k, v, pk, pv, docs: Docs | None = None, p
 
 
 def _shared_args(dt, q, k, v, pk, pv, out, docs, prompts, block, scale, cap, slopes):
-    own = _attn_args(dt, q, k, v, out, docs, block, scale, cap, slopes)
+    own = _attn_numbers(dt, q, k, v, out, docs, block, scale, cap, slopes)
     dev, shape, one = q.device, tuple(pk.shape), pk.dim() == 3
-    P = shape[-3]
-    want = (P, own.n_kv_heads, own.head_dim) if one else (shape[0], P, own.n_kv_heads, own.head_dim)
+    P, heads = shape[-3], own[2:4]
+    want = (P, *heads) if one else (shape[0], P, *heads)
     n = prompts.count
     if n is None:
         n = next((t.numel() for t in (prompts.start, prompts.len) if t is not None), 1) if one else shape[0]
-    _refuse(one or n == shape[0], -2, "prompts in slabs: one per slab")
+    if not one and n != shape[0]:
+        _refuse(False, -2, "prompts in slabs: one per slab")
     max_p = P if prompts.max is None else prompts.max
     _in32(n, P, max_p)
-    return SharedAttnArgs(own, _rows(pk, want, q.dtype, dev, "pk"), _rows(pv, want, q.dtype, dev, "pv"), n, P, max_p,
-                          _column(prompts.start, n, torch.int32, dev, "prompts.start"),
-                          _column(prompts.len, n, torch.int32, dev, "prompts.len"),
-                          _column(prompts.of, own.docs, torch.int32, dev, "prompts.of"))
+    ints = lambda t, n, name: 0 if t is None else _column(t, n, torch.int32, dev, name)  # noqa: E731
+    return SharedAttnArgs.from_buffer_copy(_SHARED.pack(
+        *own, *_row_numbers(pk, want, q.dtype, dev, "pk"), *_row_numbers(pv, want, q.dtype, dev, "pv"), n, P, max_p,
+        ints(prompts.start, n, "prompts.start"), ints(prompts.len, n, "prompts.len"), ints(prompts.of, own[20], "prompts.of")))
 
 
 def sample(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, mask_id=-1, ws=None, stream=None):
@@ -884,15 +906,18 @@ def adapters_workspace_size(x, base, A, B, slices=None):
     return n.value
 
 
+_NO_VIEW = (0, 0, 0, 0)
+
+
 def _matrix(t, shape, dtype, device, name):
-    """The view of a tensor of this shape ([rows, n], [adapters, rows, n] or [adapters, slices, rows, n])."""
+    """The fields of the view of a tensor of this shape ([rows, n], [adapters, rows, n] or [adapters, slices, rows, n])."""
     st = t.stride()
     if t.shape != shape or (st[-1] != 1 and shape[-1] > 1) or t.dtype is not dtype or t.device != device:
         _refuse(t.shape == shape, -2, f"{name} must have the shape {tuple(shape)}, not {tuple(t.shape)}")
         _refuse(st[-1] == 1 or shape[-1] <= 1 or t.numel() == 0, -2, f"{name}: elements of a row must be contiguous")
         _refuse(t.dtype is dtype and t.device == device, -1, f"{name} must be {dtype} on {device}")
     n = len(shape)
-    return View(t.data_ptr(), st[0] if n > 2 else 0, st[-2], st[1] if n > 3 else 0)
+    return t.data_ptr(), st[0] if n > 2 else 0, st[-2], st[1] if n > 3 else 0
 
 
 def _adapter_args(x, base, A, B, which, ranks, scales, slices, out):
@@ -907,9 +932,10 @@ def _adapter_args(x, base, A, B, which, ranks, scales, slices, out):
     _refuse(len(ends) == S, -2, f"A has {S} slices, slices names {len(ends)}")
     _in32(M, K, n, N, R, *ends)
     _refuse(S <= ADAPTER_SLICES, -2, f"at most {ADAPTER_SLICES} slices")
-    a = AdapterArgs(dt, _DTYPES[kind], M, K, N, n, R, S, (_i32 * ADAPTER_SLICES)(*ends), _matrix(x, (M, K), x.dtype, dev, "x"),
-                    _matrix(A, (n, S, R, K) if A.dim() == 4 else (n, R, K), x.dtype, dev, "A"),
-                    _matrix(B, (n, N, R), x.dtype, dev, "B"), View() if base is None else _matrix(base, (M, N), kind, dev, "base"),
-                    _matrix(out, (M, N), kind, dev, "out"), _column(which, M, torch.int32, dev, "which"),
-                    _column(ranks, n, torch.int32, dev, "ranks"), _column(scales, n, torch.float32, dev, "scales"))
+    cols = [0 if t is None else _column(t, m, kind_, dev, name) for t, m, kind_, name in
+            ((which, M, torch.int32, "which"), (ranks, n, torch.int32, "ranks"), (scales, n, torch.float32, "scales"))]
+    a = AdapterArgs.from_buffer_copy(_ADAPTER.pack(
+        dt, _DTYPES[kind], M, K, N, n, R, S, *ends, *(0,) * (ADAPTER_SLICES - S), *_matrix(x, (M, K), x.dtype, dev, "x"),
+        *_matrix(A, (n, S, R, K) if A.dim() == 4 else (n, R, K), x.dtype, dev, "A"), *_matrix(B, (n, N, R), x.dtype, dev, "B"),
+        *(_NO_VIEW if base is None else _matrix(base, (M, N), kind, dev, "base")), *_matrix(out, (M, N), kind, dev, "out"), *cols))
     return a, out
