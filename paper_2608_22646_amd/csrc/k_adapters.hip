@@ -386,13 +386,17 @@ __global__ void __launch_bounds__(NW * 64) adapters_shrink_kernel(AdaptersArgs a
   constexpr int STAGES = VEC ? 16 * (2 + J) * CHUNK : 0, SUMS = NW * 2 * J * 1024;
   __shared__ __attribute__((aligned(1024))) char lds[STAGES > SUMS ? STAGES : SUMS];
   __shared__ int rows[TM];
-  const Tile t = tile_of(a, p, blockIdx.x, rows);
+  // workgroup i runs on XCD i % 8: those of a tile, which read the same rows of x, follow
+  // each other on one
+  const int blocks = gridDim.x / ((p.tiles + 7) & ~7), slot = blockIdx.x >> 3, tile = slot / blocks * 8 + (blockIdx.x & 7);
+  if (tile >= p.tiles) return;
+  const Tile t = tile_of(a, p, tile, rows);
   if (t.count == 0 || t.adapter < 0) return;
   Ranks k;
   k.rank = uniform(rank_of(a, t.adapter));
   k.n16 = (k.rank + 15) >> 4;
   k.units = a.slices * k.n16;
-  k.u0 = blockIdx.z * J;
+  k.u0 = slot % blocks * J;
   if (k.u0 >= k.units) return;
   if constexpr (!VEC) {
     if (t.count > 16)
@@ -638,7 +642,7 @@ bool aligned(const AttnView& v, int size) {
 template <typename T, typename O, int PARTS>
 void run(const AdaptersArgs& a, const AdaptersPlan& p, hipStream_t s) {
   if (a.adapters > 0) {
-    const dim3 grid(p.tiles, p.splits, ceil_div(a.slices * p.r16 / 16, p.vec_in ? p.j : 1));
+    const dim3 grid(((p.tiles + 7) & ~7) * ceil_div(a.slices * p.r16 / 16, p.vec_in ? p.j : 1), p.splits);
     if (!p.vec_in)
       adapters_shrink_kernel<T, PARTS, 1, false><<<grid, NW * 64, 0, s>>>(a, p);
     else if (p.j == 1)
