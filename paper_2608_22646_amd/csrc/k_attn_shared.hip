@@ -509,21 +509,75 @@ __global__ void __launch_bounds__(256, 2) shared_units_kernel(SharedArgs s, Shar
 #endif
 }
 
+// W > 0: W waves a row (join_row).  W = 0, many rows of few states: HD / 4 lanes a row,
+// each 16 bytes of its output, so that twice as many rows are under way.
 template <typename T, int HD, int W>
 __global__ void __launch_bounds__(256) shared_join_kernel(SharedArgs s, SharedPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
+  constexpr int LPR = HD / 4, SIDE = W ? 1 : 64 / LPR;  // lanes of a row, rows of a wave
   const AttnArgs& a = s.own;
-  const long row = ((long)blockIdx.x * 4 + (threadIdx.x >> 6)) / W;
-  const int h = (int)(row % a.Hq), G = a.Hq / a.Hkv;
-  const long i = row / a.Hq;
-  if (i >= p.count[1]) return;
-  const int4 q = p.tok[3 * i], own = p.tok[3 * i + 1], run = p.tok[3 * i + 2];
+  const int lane = threadIdx.x & 63, e = lane % LPR;
+  const uint32_t row = W ? (blockIdx.x * 4u + (threadIdx.x >> 6)) / (W ? W : 1) : (blockIdx.x * 4u + (threadIdx.x >> 6)) * SIDE + lane / LPR;
+  const int h = (int)(row % (uint32_t)a.Hq), G = a.Hq / a.Hkv;
+  const uint32_t i = row / (uint32_t)a.Hq;
+  const size_t i3 = 3 * (size_t)min(i, (uint32_t)p.cap - 1);
+  const int4 q = p.tok[i3], own = p.tok[i3 + 1], run = p.tok[i3 + 2];  // (beside the count: of no query, not used)
+  const bool there = i < (uint32_t)p.count[1];
+  if (W && !there) return;
   const int g = h / G, in = h % G;
   const size_t at_own = (size_t)own.x + (size_t)g * own.y + in, at_run = (size_t)run.x + (size_t)g * run.y + in;
   const size_t next_own = (size_t)own.y * a.Hkv, next_run = (size_t)run.y * a.Hkv;
-  const int chunks = run.z;
-  join_row<T, HD, W>(static_cast<T*>(a.out.data) + q.x * a.out.stride_b + q.y * a.out.stride_l + h * a.out.stride_h, chunks + own.z, p.part,
-                     p.part_ml, [&](int c) { return c < chunks ? at_run + c * next_run : at_own + (c - chunks) * next_own; });
+  const int chunks = run.z, n = there ? chunks + own.z : 0;
+  auto at = [&](int c) { return c < chunks ? at_run + c * next_run : at_own + (c - chunks) * next_own; };
+  T* const to = static_cast<T*>(a.out.data) + q.x * a.out.stride_b + q.y * a.out.stride_l + h * a.out.stride_h;
+  if constexpr (W > 0) {
+    join_row<T, HD, W>(to, n, p.part, p.part_ml, at);
+  } else {
+    constexpr int EARLY = 4;
+    const float* part = p.part + e * 4;
+    float4 early[EARLY];
+#pragma unroll
+    for (int c = 0; c < EARLY; ++c) early[c] = c < n ? *reinterpret_cast<const float4*>(part + at(c) * HD) : make_float4(0.f, 0.f, 0.f, 0.f);
+    float m = -INFINITY, l = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int c0 = 0; __any(c0 < n); c0 += LPR) {  // LPR states at a time, on the maximum so far
+      float2 x = make_float2(-INFINITY, 0.f);
+      if (c0 + e < n) x = p.part_ml[at(c0 + e)];
+      float top = x.x;
+#pragma unroll
+      for (int k = LPR / 2; k > 0; k >>= 1) top = fmaxf(top, __shfl_xor(top, k, 64));
+      const float m_new = fmaxf(m, top), ref = m_new == -INFINITY ? 0.f : m_new, f0 = exp2_hw(m - ref), f = exp2_hw(x.x - ref);
+      m = m_new;
+      float sum = x.y * f;
+#pragma unroll
+      for (int k = LPR / 2; k > 0; k >>= 1) sum += __shfl_xor(sum, k, 64);
+      l = l * f0 + sum;
+      o.x *= f0;
+      o.y *= f0;
+      o.z *= f0;
+      o.w *= f0;
+      auto add = [&](const float4& w, int c) {
+        const float fc = __shfl(f, lane - e + c, 64);
+        if (c0 + c >= n) return;  // (of a state that is not there, nothing: 0 times infinity)
+        o.x += w.x * fc;
+        o.y += w.y * fc;
+        o.z += w.z * fc;
+        o.w += w.w * fc;
+      };
+      if (c0 == 0) {
+#pragma unroll
+        for (int c = 0; c < EARLY; ++c) add(early[c], c);
+      }
+      for (int c = c0 ? 0 : EARLY; c < LPR && __any(c0 + c < n); ++c)
+        add(c0 + c < n ? *reinterpret_cast<const float4*>(part + at(c0 + c) * HD) : make_float4(0.f, 0.f, 0.f, 0.f), c);
+    }
+    if (!there) return;
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    if constexpr (sizeof(T) == 2)
+      *reinterpret_cast<uint2*>(to + e * 4) = make_uint2(pack2(o.x * inv, o.y * inv), pack2(o.z * inv, o.w * inv));
+    else
+      *reinterpret_cast<float4*>(to + e * 4) = make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv);
+  }
 #endif
 }
 
@@ -646,11 +700,16 @@ void launch(const SharedArgs& s, const SharedPlan& p, hipStream_t st) {
     shared_units_kernel<T, HD, false><<<(unsigned)p.grid, 256, 0, st>>>(s, p);
   }
   DLLM_LAUNCH_CHECK("shared_units_kernel");
-  const long rows = (long)p.cap * s.own.Hq;
-  if (rows <= 4l * device_cu_count())
+  // Waves a row by how many rows there are (and the more rows, the fewer chunks each):
+  // four up to four rows a CU, one up to 32 (1232 rows of up to 20 states: 3.9 us, HD / 4
+  // lanes a row 10.2), above that HD / 4 lanes (16384 rows of 2 states: 6.3 us, a wave 8.8).
+  const long rows = (long)p.cap * s.own.Hq, cus = device_cu_count();
+  if (rows <= 4 * cus)
     shared_join_kernel<T, HD, 4><<<(unsigned)rows, 256, 0, st>>>(s, p);
-  else
+  else if (rows <= 32 * cus)
     shared_join_kernel<T, HD, 1><<<ceil_div(rows, 4), 256, 0, st>>>(s, p);
+  else
+    shared_join_kernel<T, HD, 0><<<ceil_div(rows, 4 * (256 / HD)), 256, 0, st>>>(s, p);
   DLLM_LAUNCH_CHECK("shared_join_kernel");
 }
 
