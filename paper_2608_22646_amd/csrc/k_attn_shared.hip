@@ -292,6 +292,8 @@ __device__ __forceinline__ void plan_docs(const SharedArgs& s, const SharedPlan&
   const int d = min(lane, a.docs - 1);
   const int q0 = some(a.q_start)[d], nq = some(a.q_len)[d], k0 = some(a.kv_start)[d], nk = some(a.kv_len)[d], pos = some(a.q_pos)[d],
             prefix = some(a.prefix)[d], pr = some(s.prompt)[d];
+  const int pl = s.prompts > 64 ? 0 : min(lane, s.prompts - 1);  // up to 64 prompts: of prompt `lane`
+  int pk0 = some(s.p_start)[s.p_start ? pl : 0], pn = some(s.p_len)[s.p_len ? pl : 0];
   Doc x;  // as doc_of
   x.q0 = a.q_start ? min(max(q0, 0), a.q_tokens) : 0;
   x.nq = min(min(max(a.q_len ? nq : a.q_tokens, 0), a.q_tokens - x.q0), a.max_q);
@@ -302,7 +304,14 @@ __device__ __forceinline__ void plan_docs(const SharedArgs& s, const SharedPlan&
   const bool there = lane < a.docs;
   if (!there) x.nq = 0;
   const int prompt = there ? (s.prompt ? (pr >= 0 && pr < s.prompts ? pr : -1) : 0) : -1;
-  const int pk = min(max(prompt, 0), s.prompts - 1), pk0 = (s.p_start ? s.p_start : none)[s.p_start ? pk : 0], pn = (s.p_len ? s.p_len : none)[s.p_len ? pk : 0];
+  const int pk = min(max(prompt, 0), s.prompts - 1);
+  if (s.prompts > 64) {
+    pk0 = some(s.p_start)[s.p_start ? pk : 0];
+    pn = some(s.p_len)[s.p_len ? pk : 0];
+  } else {
+    pk0 = __shfl(pk0, pk, 64);
+    pn = __shfl(pn, pk, 64);
+  }
   Prompt y;  // as prompt_at
   y.k0 = s.p_start ? min(max(pk0, 0), s.p_tokens) : 0;
   y.nk = prompt < 0 ? 0 : min(min(max(s.p_len ? pn : s.p_tokens, 0), s.p_tokens - y.k0), s.max_p);
