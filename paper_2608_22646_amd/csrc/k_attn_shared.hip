@@ -639,6 +639,23 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) shared_chain_k
 }
 
 // ---- choice, from sizes only ------------------------------------------------------
+// Whether `tiles` row tiles that take prompt and own keys one after the other are done
+// sooner than units of them (`full` tiles, were they full) and a join.  In microseconds, by
+// steps of 64 keys, each of `step` for a workgroup alone on its CU, which two that share
+// it (float32: one) keep busy: the chain takes its steps, however few workgroups there
+// are; the units divide them, and pay 8 for the join and 0.05 a tile for states.  (bf16, 28
+// + 4 heads: 9 documents of up to 159 queries behind 1231 keys, 325 tiles: 48 us, units 56;
+// 2 of 283 behind 960, 128 tiles: 38 and 36; 3 of 153 behind 23: 16 and 24.  32 + 8 heads: 2
+// of 33 behind 1717, 32 tiles: 70 and 20.  float32, 28 + 4: 12 of 64 behind 149: 93 and 98; 4
+// of 33 behind 23: 64 and 37.)
+bool chain_is_shorter(const SharedArgs& s, long tiles, double full) {
+  const AttnArgs& a = s.own;
+  const bool f32 = a.dtype == DLLM_F32;
+  const int cus = device_cu_count();
+  const double step = f32 ? 10.0 * a.hd / 128 : a.hd == 128 ? 1.9 : 1.4, busy = f32 ? 0.86 * cus : 1.6 * cus;
+  const double steps = ceil_div((long)s.max_p + a.max_kv, 64), rounds = ceil_div(tiles, f32 ? cus : 2 * cus);
+  return steps * step * rounds <= 8 + full * (steps * step / busy + 0.05);
+}
 SharedPlan choose(const SharedArgs& s) {
   const AttnArgs& a = s.own;
   SharedPlan p{};
@@ -647,7 +664,7 @@ SharedPlan choose(const SharedArgs& s) {
   p.slots = 2 * cus;
   p.few_rows = f32 && a.hd == 128 ? 64 : 32;
   p.tiles = ceil_div(rows, MANY_ROWS);
-  p.chain = rows > MANY_ROWS && (long)a.docs * a.Hkv * p.tiles >= 2 * cus;
+  p.chain = rows > 64 && chain_is_shorter(s, (long)a.docs * a.Hkv * p.tiles, (double)a.docs * a.Hkv * rows / MANY_ROWS);
   if (p.chain) {
     p.grid = ((long)a.docs * a.Hkv + 7) / 8 * 8 * p.tiles;
     return p;

@@ -275,3 +275,31 @@ def test_without_prompts_it_is_attention_of_documents(gpu_lib):
         pkp, pvp = (pk[0], pv[0]) if p.count == 0 or p.len is not None else (pk, pv)
         got = B.shared_attention(q, k, v, pkp, pvp, prompts=p, block=1)
         assert (got.float() - ref.float()).abs().max() <= 2.0 ** -7
+
+
+@pytest.mark.parametrize("heads,dtype,q_lens,kv_lens,p_lens,of,block,units", [
+    ((28, 4, 128), BF16, [24, 10, 23], [40, 10, 39], [23], None, 1, False),
+    ((28, 4, 128), BF16, [24, 10, 23], [40, 10, 39], [2000, 65], [0, 0, 1], 1, True),
+    ((28, 4, 128), BF16, [24, 10, 23], [40, 500, 39], [2000, 65], [0, 1, -1], 32, True),
+    ((28, 4, 128), F32, [24, 10, 23], [40, 10, 39], [23], None, 1, True),
+    ((16, 2, 64), BF16, [9, 0, 17], [9, 0, 17], [31, 64], [1, 0, 0], 0, False),
+    ((16, 2, 64), BF16, [9, 0, 17], [1009, 0, 17], [31, 1064], [1, 0, 0], 0, True),
+    ((8, 8, 128), F32, [128 - d % 7 for d in range(32)], [130 + d for d in range(32)], [60, 0], [d % 3 for d in range(32)], 1, False),
+    ((8, 8, 64), F32, [128 - d % 7 for d in range(32)], [130 + d for d in range(32)], [60, 0], [d % 3 for d in range(32)], 32, False),
+    ((8, 8, 64), F32, [128 - d % 7 for d in range(8)], [130 + d for d in range(8)], [60, 0], [d % 3 for d in range(8)], 32, True),
+])
+def test_tiles_that_take_all_keys_and_units_of_them(gpu_lib, heads, dtype, q_lens, kv_lens, p_lens, of, block, units):
+    """Both sides of the choice, which the workspace shows: tiles that take all their keys need none."""
+    slopes = [2.0 ** -(1 + h / 4) for h in range(heads[0])]
+    _, (q, k, v, pk, pv, docs, prompts, _) = run_and_check(*heads, dtype, q_lens, kv_lens, p_lens, of, block, None, None, 30.0, slopes)
+    assert (B.shared_attention_workspace_size(q, k, v, pk, pv, docs, prompts) > 0) == units
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("docs,prompts", [(64, 64), (64, 65), (5, 200), (70, 200)])
+def test_many_prompts(gpu_lib, docs, prompts, dtype):
+    """More prompts than lanes that ask for their ranges at once, most of them of no document."""
+    rng = np.random.default_rng(docs * prompts)
+    lens = rng.integers(0, 90, prompts).tolist()
+    of = np.sort(rng.integers(-1, prompts + 1, docs)).tolist()
+    run_and_check(4, 2, 64, dtype, rng.integers(0, 4, docs).tolist(), rng.integers(4, 40, docs).tolist(), lens, of, block=1)
