@@ -530,7 +530,8 @@ int dllm_attention(const dllm_attn_args* args, void* workspace, size_t workspace
  * not be written.  Out must not overlap anything that is read.
  * Requirements: those of dllm_attention for `own`; pk and pv those of k and v; prompts in
  * [0, 65535], 0 <= max_p <= p_tokens <= 2^29, kv_tokens <= 2^29; where documents have
- * few rows, fewer than 2^26 rows (queries times n_heads) and 2^30 pairs of a row tile and 128 keys.
+ * few rows, fewer than 2^26 rows (queries times n_heads) and 2^30 pairs of a row tile and 128 keys
+ * (float32: 32).
  * docs or max_q of 0: nothing; prompts or max_p of 0: dllm_attention.
  */
 typedef struct dllm_shared_attn_args {

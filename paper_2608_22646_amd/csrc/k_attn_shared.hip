@@ -20,8 +20,6 @@ namespace dllm {
 namespace {
 
 constexpr int PLAN_THREADS = 1024;
-constexpr int UNIT_KEYS = 128;                    // chunks are multiples of this
-constexpr int UNIT_COST = 4;                      // in UNIT_KEYS
 constexpr int MANY_ROWS = 128;                    // rows of a tile of many
 
 // A prompt's range, cut to its slab and to the maximum.
@@ -52,19 +50,21 @@ __host__ __device__ __forceinline__ int tile_rows(const SharedPlan& p, int rows)
 __host__ __device__ __forceinline__ int tiles_of(const SharedPlan& p, int rows) {
   return rows > 64 ? (rows + MANY_ROWS - 1) / MANY_ROWS : (int)((uint32_t)(rows + p.few_rows - 1) / (uint32_t)p.few_rows);
 }
-// How far keys are split, of `all` units with `work` times UNIT_KEYS keys in all (without
-// their heads): chunks no shorter than `least`, in UNIT_KEYS, and no more units than `most`.
-// Where there are fewer units than workgroups run at once, as many more as make them one
-// round; else only what is longer than a workgroup's part of the whole, a unit's start and
-// end counting as UNIT_COST.
+__device__ __forceinline__ int units_of(const SharedPlan& p, int keys) { return (keys + p.unit_keys - 1) >> (31 - __clz(p.unit_keys)); }
+// How far keys are split, of `all` units with `work` times p.unit_keys keys in all
+// (without their heads): chunks no shorter than `least`, in p.unit_keys, and no more units
+// than `most`.  Where there are fewer units than workgroups run at once, as many more as make
+// them one round (half a round of float32, if they are few: two workgroups of a CU would only
+// share its matrix units, and leave twice the states); else only what is longer than a
+// workgroup's part of the whole, a unit's start and end counting as p.unit_cost.
 struct Cut {
   int least, most;
 };
 __device__ __forceinline__ Cut cut_of(const SharedPlan& p, int all, int work, int heads) {
-  const uint32_t slots = (uint32_t)p.slots / (uint32_t)heads;  // (at least 1 unit, whatever the heads)
+  const uint32_t busy = (uint32_t)p.busy / (uint32_t)heads, slots = 2 * (uint32_t)all <= busy ? busy : (uint32_t)p.slots / (uint32_t)heads;
   if ((uint32_t)all < slots) return Cut{max(1, (int)((uint32_t)work / slots)), (int)slots};
-  const float part = ((float)work + (float)all * UNIT_COST) * (float)heads / (float)p.slots;
-  return Cut{max(1, (int)part), 0x7fffffff};
+  const float part = ((float)work + (float)all * p.unit_cost) * (float)heads / (float)p.slots;
+  return Cut{max(1, (int)fminf(part, (float)((1 << 30) / p.unit_keys))), 0x7fffffff};  // (no keys are as many)
 }
 
 // ---- what is stacked and split how -------------------------------------------------
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
   // two segments a thread held, where there are no more
   const bool few = segs <= 2 * N;
   int rows_h[2] = {0, 0}, keys_h[2] = {0, 0}, tiles_h[2] = {0, 0};
-  int units = 0, longest = 0, work = 0;  // work: tiles times keys, in UNIT_KEYS (the host sees to it that all fit)
+  int units = 0, longest = 0, work = 0;  // work: tiles times keys, in unit_keys (the host sees to it that all fit)
   for (int i = tid, k = 0; i < segs; i += N, ++k) {
     int rows, keys;
     size_of(i, rows, keys);
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
       tiles_h[k & 1] = t;
     }
     units += t;
-    work += t * ((keys + UNIT_KEYS - 1) / UNIT_KEYS);
+    work += t * units_of(p, keys);
     longest = max(longest, keys);
   }
   int all_units, all_work, n;
@@ -192,13 +192,13 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
   for (int w = 0; w < N >> 6; ++w) longest = max(longest, sums[w]);
   const int heads = a.Hkv;
   const Cut cut = cut_of(p, all_units, all_work, heads);
-  int lo = cut.least, hi = max(lo, (longest + UNIT_KEYS - 1) / UNIT_KEYS);
+  int lo = cut.least, hi = max(lo, units_of(p, longest));
   if (few) {
     while (lo < hi) {
       const int len = (lo + hi) >> 1;
       int c = 0;
 #pragma unroll
-      for (int k = 0; k < 2; ++k) c += (keys_h[k] + len * UNIT_KEYS - 1) / (len * UNIT_KEYS) * tiles_h[k];
+      for (int k = 0; k < 2; ++k) c += (keys_h[k] + len * p.unit_keys - 1) / (len * p.unit_keys) * tiles_h[k];
       before_of(c, sums, n);
       if (n <= cut.most)
         hi = len;
@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
   } else if (cut.most < 0x7fffffff) {
     lo = cut.most > all_units ? min(hi, max(lo, all_work / (cut.most - all_units) + 1)) : hi;
   }
-  const int len = lo * UNIT_KEYS;
+  const int len = lo * p.unit_keys;
   // segments' units and states
   int entry = 0, state = 0;
   for (int i0 = 0; i0 < segs; i0 += N) {
@@ -219,7 +219,7 @@ __global__ void __launch_bounds__(PLAN_THREADS) shared_plan_kernel(SharedArgs s,
       tiles = keys > 0 ? tiles_of(p, rows) : 0;
     }
     const int chunks = (keys + len - 1) / len;
-    const int each = chunks > 1 ? ((keys + chunks - 1) / chunks + UNIT_KEYS - 1) / UNIT_KEYS * UNIT_KEYS : keys;
+    const int each = chunks > 1 ? units_of(p, (keys + chunks - 1) / chunks) * p.unit_keys : keys;
     int all_e, all_s;
     const int e0 = entry + before_of(chunks * tiles, sums, all_e), s0 = state + before_of(chunks * rows * heads, sums, all_s);
     if (i < segs) {
@@ -328,7 +328,7 @@ __device__ __forceinline__ void plan_docs(const SharedArgs& s, const SharedPlan&
   const int keys_s = st.rows > 0 ? y.nk : 0, keys_o = x.nq > 0 ? sees(a, x, x.nq - 1) : 0;
   st.tiles = keys_s > 0 ? tiles_of(p, st.rows) : 0;
   ow.tiles = keys_o > 0 ? tiles_of(p, ow.rows) : 0;
-  const int ks = (keys_s + UNIT_KEYS - 1) / UNIT_KEYS, ko = (keys_o + UNIT_KEYS - 1) / UNIT_KEYS;
+  const int ks = units_of(p, keys_s), ko = units_of(p, keys_o);
   const int all = lane_of(lanes_upto(st.tiles + ow.tiles), 63), work = lane_of(lanes_upto(st.tiles * ks + ow.tiles * ko), 63);
   const Cut cut = cut_of(p, all, work, heads);
   int longest = max(ks, ko);
@@ -348,7 +348,7 @@ __device__ __forceinline__ void plan_docs(const SharedArgs& s, const SharedPlan&
   int units = 0, states = 0;
   auto split = [&](Split& z, int keys, int k) {
     z.chunks = (k + lo - 1) / lo;
-    z.each = z.chunks > 1 ? ((uint32_t)(keys + z.chunks - 1) / (uint32_t)z.chunks + UNIT_KEYS - 1) / UNIT_KEYS * UNIT_KEYS : keys;
+    z.each = z.chunks > 1 ? units_of(p, (uint32_t)(keys + z.chunks - 1) / (uint32_t)z.chunks) * p.unit_keys : keys;
     const int n = z.chunks * z.tiles, m = z.chunks * z.rows * heads, un = lanes_upto(n), um = lanes_upto(m);
     z.unit = units + un - n;
     z.state = states + um - m;
@@ -662,6 +662,14 @@ SharedPlan choose(const SharedArgs& s) {
   const int G = a.Hq / a.Hkv, rows = a.max_q * G, cus = device_cu_count();
   const bool f32 = a.dtype == DLLM_F32;
   p.slots = 2 * cus;
+  p.busy = f32 ? cus : p.slots;
+  // (bf16, 16 documents of 32 queries behind 1024 and 8448 keys, 32 heads: 43 and 105 us; a cost
+  // of 1 to 3: 45 and 108; 64 keys and 8 are as fast there, but slower where keys are few: 4 documents
+  // of 32 queries behind 656, 28 + 4 heads, 21.5 and 24.1.  float32, whose step takes five
+  // times as long, 2 documents of 50 behind 143: 20.9 us, by 64 keys 25.7, by 128 35.1; 2 of 195
+  // behind 85, 32 heads, which is more than half a round: 44.8, by a CU each 49.7)
+  p.unit_keys = f32 ? 32 : 128;
+  p.unit_cost = f32 ? 1 : 4;
   p.few_rows = f32 && a.hd == 128 ? 64 : 32;
   p.tiles = ceil_div(rows, MANY_ROWS);
   p.chain = rows > 64 && chain_is_shorter(s, (long)a.docs * a.Hkv * p.tiles, (double)a.docs * a.Hkv * rows / MANY_ROWS);
@@ -675,7 +683,7 @@ SharedPlan choose(const SharedArgs& s) {
   // follow each other no more than those) and of the documents
   const long whole = ((long)p.cap * G + MANY_ROWS - 1) / MANY_ROWS;
   const long own = std::min((long)a.docs * std::max(tiles_of(p, std::min(rows, 64)), tiles_of(p, rows)), whole + 2l * a.docs);
-  const long base = whole + 2l * a.docs + own, keys = ceil_div(std::max(s.max_p, a.max_kv), UNIT_KEYS);
+  const long base = whole + 2l * a.docs + own, keys = ceil_div(std::max(s.max_p, a.max_kv), p.unit_keys);
   // (cut_of: chunks beyond the first are fewer than 4/3 of the workgroups that run at once)
   const long more = std::min(2l * p.slots / a.Hkv + 1, base * (keys - 1));
   p.units = base + more;

@@ -251,11 +251,13 @@ struct SharedArgs {
 };
 // Layout of a call: whether a document's tiles take its prompt's keys and its own in one
 // go (then the row tiles of a document), workgroups; else queries at most, units at most, tiles
-// times 128 keys at most, workgroups of a round, rows of a tile of few, states at most, and what the
+// times unit_keys at most, workgroups of a round and how many of
+// them keep the card busy, what chunks are multiples of and a unit's
+// start and end in that, rows of a tile of few, states at most, and what the
 // workspace holds (shared_plan_kernel).
 struct SharedPlan {
   bool chain;
-  int tiles, cap, slots, few_rows;
+  int tiles, cap, slots, busy, unit_keys, unit_cost, few_rows;
   long grid, units, work, states;
   int* count;  // units without their heads, queries
   int4 *tok, *seg, *run, *unit;
