@@ -616,7 +616,9 @@ int dllm_sample(const dllm_sample_args* args, void* workspace, size_t workspace_
  * others by the element.
  * Requirements: 0 <= rows <= 2^22; 1 <= d_in, d_out <= 2^20; 0 <= adapters <= 4095; 1 <=
  * rank <= 256; 1 <= slices <= DLLM_ADAPTER_SLICES, slice_end rising and ending at d_out;
- * strides not negative, that of out's rows at least d_out.  rows of 0: nothing.
+ * strides not negative, that of out's rows at least d_out; of rows / 32 + adapters + 8 tiles,
+ * fewer than 2^24 pairs with 512 columns of a slice and 2^23 with 16 ranks of a slice.
+ * rows of 0: nothing.
  */
 enum { DLLM_ADAPTER_SLICES = 4 };
 typedef struct dllm_adapter_args {

@@ -693,7 +693,7 @@ size_t adapters_bytes(const AdaptersArgs& a) {
 // A launch's threads must be below 2^32.
 bool adapters_fit(const AdaptersArgs& a) {
   const AdaptersPlan p = plan_of(a);
-  return (long)p.tiles * p.blocks < (1l << 24);
+  return (long)p.tiles * p.blocks < (1l << 32) / 256 && ((long)p.tiles + 7) / 8 * 8 * a.slices * p.r16 / 16 < (1l << 32) / (NW * 64);
 }
 
 void launch_adapters(const AdaptersArgs& a, void* ws, hipStream_t s) {

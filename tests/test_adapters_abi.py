@@ -86,3 +86,21 @@ def test_marshalling_refuses(kw, code):
     with pytest.raises(B.DllmError) as e:
         B._adapter_args(**{**a, **kw})
     assert e.value.code == code
+
+
+@pytest.mark.parametrize("rows,code", [(1 << 22, -2), ((1 << 22) - 32 * 7, -2), ((1 << 22) - 32 * 11, 0), (1 << 10, 0)])
+def test_refuses_more_workgroups_than_a_launch_has(rows, code):
+    """4 x 16 blocks of ranks of rows / 32 + 3 tiles, those in eights: below 2^23 workgroups of 512 threads, or refused
+    (2^17 - 7 + 3 tiles are 2^17 in eights, 2^17 - 11 + 3 are 2^17 - 8)."""
+    n = ctypes.c_size_t()
+    a = args(rows=rows, d_in=1, slices=4, slice_end=(16, 32, 48, 64), rank=256, x=view(l=1), a=view(b=1024, l=1, h=256), b=view(b=1 << 14, l=256))
+    assert B.lib().dllm_adapters_workspace_size(a, n) == code
+    if code:
+        assert call(a) == code
+
+
+def test_refuses_more_columns_than_a_launch_has():
+    n = ctypes.c_size_t()
+    wide = dict(d_out=1 << 20, slice_end=(1 << 20, 0, 0, 0), out=view(l=1 << 20), base=view(l=1 << 20), b=view(b=1 << 23, l=8))
+    assert B.lib().dllm_adapters_workspace_size(args(rows=1 << 19, **wide), n) == -2 and call(args(rows=1 << 19, **wide)) == -2
+    assert B.lib().dllm_adapters_workspace_size(args(rows=1 << 18, **wide), n) == 0
