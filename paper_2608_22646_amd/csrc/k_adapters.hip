@@ -66,7 +66,10 @@ __device__ __forceinline__ Tile tile_of(const AdaptersArgs& a, const AdaptersPla
 }
 
 // Sorts the rows by adapter (those without one last) and cuts them into tiles.  The
-// order of an adapter's rows depends on the order of execution; no result does.
+// order of an adapter's rows depends on the order of execution; no result does.  ROWS rows of
+// a thread are asked for at once, and once in all where there are no more (4223 rows: 6.2 us,
+// one after the other 7.6; of up to 1024, one a thread: 3.8, eight 4.1).
+template <int ROWS>
 __global__ void __launch_bounds__(SORT_THREADS) adapters_sort_kernel(AdaptersArgs a, AdaptersPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   extern __shared__ int sh[];
@@ -76,8 +79,8 @@ __global__ void __launch_bounds__(SORT_THREADS) adapters_sort_kernel(AdaptersArg
   for (int i = tid; i < bins; i += SORT_THREADS) at[i] = 0;
   __syncthreads();
   // the place of each row among its bin's, by a wave at once where its rows share one
-  auto add = [&](int row, bool there) {
-    const int w = there ? adapter_of(a, row) : -1, bin = w < 0 ? a.adapters : w;
+  auto add = [&](int w, bool there) {
+    const int bin = w >= 0 && w < a.adapters ? w : a.adapters;
     const unsigned long long all = __ballot(there), same = __ballot(there && bin == uniform(bin));
     int pos = 0;
     if (same == all) {
@@ -89,7 +92,24 @@ __global__ void __launch_bounds__(SORT_THREADS) adapters_sort_kernel(AdaptersArg
     }
     return pos;
   };
-  for (int r0 = tid - lane; r0 < a.rows; r0 += SORT_THREADS) add(r0 + lane, r0 + lane < a.rows);
+  int w[ROWS];
+  auto ask = [&](int r0) {
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k)
+      if (r0 + k * SORT_THREADS < a.rows) w[k] = a.which[min(r0 + k * SORT_THREADS + tid, a.rows - 1)];
+  };
+  auto each_row = [&](int r0, auto f) {
+#pragma unroll
+    for (int k = 0; k < ROWS; ++k) {
+      const int row = r0 + k * SORT_THREADS + tid;
+      if (row - lane < a.rows) f(row, add(w[k], row < a.rows));
+    }
+  };
+  constexpr int GO = ROWS * SORT_THREADS;
+  for (int r0 = 0; r0 < a.rows; r0 += GO) {
+    ask(r0);
+    each_row(r0, [](int, int) {});
+  }
   __syncthreads();
   // sums of the bins before, `each` consecutive bins a thread
   const int each = (bins + SORT_THREADS - 1) / SORT_THREADS, b0 = min(tid * each, bins), b1 = min(b0 + each, bins);
@@ -144,9 +164,11 @@ __global__ void __launch_bounds__(SORT_THREADS) adapters_sort_kernel(AdaptersArg
     p.tile[i] = d;
   }
   __syncthreads();
-  for (int r0 = tid - lane; r0 < a.rows; r0 += SORT_THREADS) {
-    const int row = r0 + lane, pos = add(row, row < a.rows);
-    if (row < a.rows) p.order[pos] = row;
+  for (int r0 = 0; r0 < a.rows; r0 += GO) {
+    if (a.rows > GO) ask(r0);
+    each_row(r0, [&](int row, int pos) {
+      if (row < a.rows) p.order[pos] = row;
+    });
   }
 #endif
 }
@@ -709,7 +731,7 @@ void launch_adapters(const AdaptersArgs& a, void* ws, hipStream_t s) {
   p.vec_y = aligned(a.base, out) && aligned(a.out, out);
   for (int i = 0; i < a.slices; ++i) p.vec_y = p.vec_y && a.slice_end[i] % 8 == 0;
   if (p.sorted) {
-    adapters_sort_kernel<<<1, SORT_THREADS, (a.adapters + 1) * 8, s>>>(a, p);
+    (a.rows > SORT_THREADS ? adapters_sort_kernel<8> : adapters_sort_kernel<1>)<<<1, SORT_THREADS, (a.adapters + 1) * 8, s>>>(a, p);
     DLLM_LAUNCH_CHECK("adapters_sort_kernel");
   }
   if (a.dtype == DLLM_F32)
