@@ -216,3 +216,30 @@ def test_no_adapter_at_all(gpu_lib):
     out = base.clone()
     assert torch.equal(B.adapters(x, out, A, Bm, ints([-1] * 10), out=out), base)
     assert not B.adapters(x, None, A[:0], Bm[:0], ints([0] * 10)).any()
+
+
+@pytest.mark.parametrize("M", [1024, 1025, 8192, 8193, 9001])
+@pytest.mark.parametrize("n", [3, 1500])
+def test_sorts_of_many_rows(gpu_lib, M, n):
+    """One row of a sorting thread, up to eight, and more of them; fewer and more adapters than sorting threads."""
+    which = [(m * 7919) % (n + 2) - 1 for m in range(M)]
+    run(M, 64, (40,), n, 8, BF16, BF16, which, ranks=[a % 9 for a in range(n)], seed=M)
+
+
+def test_most_rows(gpu_lib):
+    """2^22 rows: the largest call.  The reference in float64, gathered on the GPU; the tolerance is verify's."""
+    M, K, N, n, R = 1 << 22, 8, 8, 4095, 2
+    x, base, A, Bm = inputs(M, K, (N,), n, R, BF16, F32)
+    which = (torch.arange(M, device="cuda") * 7919 % (n + 1) - 1).to(torch.int32)
+    got = B.adapters(x, base, A, Bm, which)
+    w = which.clamp(min=0).long()
+    has = (which >= 0).double()[:, None]
+    prod = A[w, 0].double() * x.double()[:, None, :]                      # [M, R, K]
+    terms = Bm[w].double()                                                # [M, N, R]
+    ref = base.double() + has * (terms * prod.sum(-1)[:, None, :]).sum(-1)
+    mass = has * (terms.abs() * prod.abs().sum(-1)[:, None, :]).sum(-1)
+    u = 2.0 ** -24
+    tol = (K + 3 * R + 8) * u * mass * 1.01
+    tol += 2 * u * (ref.abs() + tol) * 1.01 + 1e-37
+    assert bool(((got.double() - ref).abs() <= tol).all())
+    assert torch.equal(got[which < 0], base[which < 0])
