@@ -1,18 +1,27 @@
 // Low-rank adapters of many requests beside a shared projection (dllm_adapters):
 //   out = base + scale B (A x),  A and B those of the row's adapter.
 //
-// Both products run on tiles of up to 32 rows of one adapter.  Few rows: the rows of
-// an adapter among 32 neighbours, found by the workgroup of the first of them.  Many
-// rows: a first launch sorts the rows by adapter, so that a tile is full whatever
-// their order.  Then
-//   shrink: part[z][row][s, j] = the z-th share of sum_k A[s, j, k] x[row, k]; the
-//     four waves of a workgroup take turns along k, operands straight from memory
-//     (16 x 16 tiles, ranks by rows), and meet in LDS;
-//   expand: the shares summed in their order and scaled, the sum in bf16 pieces that
-//     hold 16 of its bits (24 for a float32 output) as the matrix unit's one operand,
-//     B's rows as they lie in memory as the other; a wave computes 32 rows x 128
-//     columns, column n = 8 c + i by lane c's i-th product, so that a lane reads and
-//     writes 8 consecutive elements of base and out.
+// Both products run on tiles of up to 32 rows of one adapter.  Up to 64 rows: the rows of
+// an adapter among 32 neighbours, found by the workgroup of the first of them.  More: a
+// first launch of one workgroup sorts the rows by adapter, so that a tile is full whatever
+// their order (512 rows found by neighbours: 46 to 49 us, sorted 27 to 35).  Then
+//   shrink: part[z][row][s, j] = the z-th share of sum_k A[s, j, k] x[row, k]; rows of x
+//     and of A to LDS, whose steps the eight waves of a workgroup share (16 x 16 tiles,
+//     ranks by rows), and meet in LDS; 32 ranks a workgroup, which reads 64 rows of
+//     operands; k is split where that leaves CUs without a workgroup;
+//   join, where ranks are more than one step of the matrix unit and shares several: their
+//     sum, once for all columns;
+//   expand: the sum, scaled, in bf16 pieces that hold 16 of its bits (24 for a float32
+//     output) as the matrix unit's one operand, B's rows as they lie in memory as the
+//     other; a wave computes 32 rows x 128 columns, column n = 8 c + i by lane c's i-th
+//     product, so that a lane reads and writes 8 consecutive elements of base and out.
+//
+// What bounds them (kernel times, inputs not in a cache): 8448 rows of 4096 to 2 x 12288
+// columns, rank 16: expand 148 to 153 us, HBM at 5.5 TB/s; shrink 32, with 84 MB to read; sort 10.
+// 4223 rows, rank up to 128, 4096 to 4096: expand 39 and shrink 33 us, the L2s' answers to
+// 32-row tiles that each read all of A and B (some 8 TB/s), sort 6.  Few rows: launches and
+// the chain of dependent reads in them (256 rows, 12288 to 4096 float32, ranks up to 64:
+// 3.8, 8.5, 4 and 9 us).
 #include <algorithm>
 #include <type_traits>
 
@@ -650,6 +659,7 @@ AdaptersPlan plan_of(const AdaptersArgs& a) {
   const int groups = ceil_div(a.rows, TM);
   p.tiles = p.sorted ? std::min(a.rows, groups + a.adapters + 1) : a.rows <= TM ? a.rows : groups * TM;
   const int units = a.slices * p.r16 / 16, full = p.sorted ? groups : std::min(a.rows, groups + a.adapters);
+  // (blocks of 16 ranks a workgroup: two, with 64 KiB a stage and two workgroups a CU)
   p.j = std::min(units, 2);
   const int wgs = full * ceil_div(units, p.j), chunks = ceil_div((long)a.d_in * size, CHUNK);
   p.splits = std::max(1, std::min({cus / wgs, chunks, 16}));
@@ -657,6 +667,7 @@ AdaptersPlan plan_of(const AdaptersArgs& a) {
   p.splits = ceil_div(chunks, p.steps);
   p.keep = a.rank > 64 / size && p.splits == 1;
   p.hsteps = ceil_div(a.rank, 64 / size);
+  // columns of a workgroup: 512, or twice that where four rounds of workgroups are left
   const int per = std::max(1, std::min(2, (int)((long)full * ceil_div(a.d_out, 4 * COLS) / (4 * cus))));
   p.cols = per * 4 * COLS;
   for (int i = 0; i < a.slices; ++i) p.blocks += ceil_div(a.slice_end[i] - (i ? a.slice_end[i - 1] : 0), p.cols);

@@ -1,16 +1,23 @@
 // Attention of documents behind prompts that they share (dllm_shared_attention), on the
-// row tiles of attn_tile.h.
+// row tiles of attn_tile.h, in one of two ways (chain_of):
 //
-// Few rows of a document: the queries of consecutive documents of one prompt are stacked
-// into row tiles, which read the prompt's keys once for all of them; each document's own
-// keys are read by a tile of its own rows.  Both are split over workgroups by keys, leave
-// their states in the workspace, and a join takes a row's states over its prompt's chunks
-// and its document's.  What is stacked and split how is found on the device, from the
-// lengths there (shared_plan_kernel): a list of units of like work, those of the prompts,
-// the longer ones, first.
-// Many rows: where every document's own rows fill the CUs with whole tiles, stacking would
-// read no key less often and only add states; a tile then takes the prompt's keys and goes
-// on with its document's, in one launch.
+// Chain, where keys are few or rows fill the CUs: a row tile of a document takes its prompt's
+// keys and goes on with the document's own, in one launch without a workspace.
+// Units, where few rows stand behind many keys: the queries of consecutive documents of one
+// prompt are stacked into row tiles, which read the prompt's keys once for all of them; each
+// document's own keys are read by a tile of its own rows.  Both are split over workgroups by
+// keys, leave their states in the workspace, and a join takes a row's states over its
+// prompt's chunks and its document's.  What is stacked and split how is found on the
+// device, from the lengths there: a list of units of like work, those of the prompts, the
+// longer ones, first (up to 64 documents by each workgroup for itself, 2.4 us; more by a
+// launch before).
+//
+// What bounds them (kernel times, inputs not in a cache): 16 documents of 32 queries behind 8448
+// keys, 32 heads: units 93 to 104 us, 0.7 to 0.8 PFLOP/s, of which two workgroups a CU reach 1.0
+// while both have prompt keys; join 8.  Behind 1024: 37 to 40 and 7, where 67 MB of the
+// documents' own keys come from HBM.  32 single tokens behind 8448 keys: 19 and 5.  8
+// documents of up to 700 queries, chain: 126 to 130, as attention of documents alone (issue
+// of the softmax beside the products).  Small calls: launches, the plan and first tiles.
 #include <algorithm>
 
 #include "attn_tile.h"
@@ -599,10 +606,11 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) shared_chain_k
   const AttnArgs& a = s.own;
   const int G = a.Hq / a.Hkv, wave = uniform((int)threadIdx.x >> 6), qg = wave % QG, lq = threadIdx.x & 31;
   // Workgroup i runs on XCD i % 8: the row tiles of a (document, key/value head), which
-  // read the same keys, go to one XCD, the tiles with most keys first
-  const int i8 = (int)blockIdx.x >> 3, x8 = (int)blockIdx.x & 7;
-  const int unit = (i8 / p.tiles) * 8 + x8, tile = p.tiles - 1 - i8 % p.tiles;
-  if (unit >= a.docs * a.Hkv) return;
+  // read the same keys, go to one XCD (to p.parts of them where there are too few for
+  // eight), the tiles with most keys first
+  const int i8 = (int)blockIdx.x >> 3, up = i8 / p.part_tiles * 8 + ((int)blockIdx.x & 7);  // unit and part
+  const int unit = up / p.parts, tile = p.tiles - 1 - (i8 % p.part_tiles * p.parts + up % p.parts);
+  if (unit >= a.docs * a.Hkv || tile < 0) return;
   const int g = unit % a.Hkv, dn = unit / a.Hkv;
   Doc d = doc_of(a, dn);
   d = Doc{uniform(d.q0), uniform(d.nq), uniform(d.k0), uniform(d.nk), uniform(d.pos), uniform(d.prefix)};
@@ -639,22 +647,73 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) shared_chain_k
 }
 
 // ---- choice, from sizes only ------------------------------------------------------
-// Whether `tiles` row tiles that take prompt and own keys one after the other are done
-// sooner than units of them (`full` tiles, were they full) and a join.  In microseconds, by
-// steps of 64 keys, each of `step` for a workgroup alone on its CU, which two that share
-// it (float32: one) keep busy: the chain takes its steps, however few workgroups there
-// are; the units divide them, and pay 8 for the join and 0.05 a tile for states.  (bf16, 28
-// + 4 heads: 9 documents of up to 159 queries behind 1231 keys, 325 tiles: 48 us, units 56;
-// 2 of 283 behind 960, 128 tiles: 38 and 36; 3 of 153 behind 23: 16 and 24.  32 + 8 heads: 2
-// of 33 behind 1717, 32 tiles: 70 and 20.  float32, 28 + 4: 12 of 64 behind 149: 93 and 98; 4
-// of 33 behind 23: 64 and 37.)
-bool chain_is_shorter(const SharedArgs& s, long tiles, double full) {
+// What a call takes in microseconds, fitted to 288 calls of 1 to 64 rows a document, 1 to
+// 48 documents and 64 to 1000 keys, timed in each form: alone on a CU a row tile takes `base`
+// and `step` for each of its steps of `keys`, its steps over a prompt and its own keys one
+// after the other; a unit takes a start beside its steps.  The form taken is 1 % off the
+// best of four on average, units alone 25 %.  (bf16, 32 heads: 16 documents of 64 queries behind
+// 60 keys: 13 us, units 47; 4 single tokens behind 800 and 200: units 16, chain 20.  28 + 4: 3 of
+// 294 behind 64: 18, units 37.  float32, 28 + 4, 16 of 28 rows behind 400 and 100: units 29, chain 53.)
+struct Shaped {
+  int qg, keys;
+  float base, step;
+};
+// Row tiles that take prompt and own keys in one go, of 32, 64 and 128 rows: however few
+// there are, each takes its steps.
+constexpr Shaped CHAINS[2][2][3] = {{{{1, 128, 5.8f, 0.93f}, {2, 128, 7.f, 0.95f}, {4, 64, 5.5f, 0.96f}},
+                                     {{1, 128, 7.9f, 1.33f}, {2, 128, 9.7f, 1.33f}, {4, 64, 6.8f, 1.32f}}},
+                                    {{{1, 128, 8.f, 2.6f}, {2, 128, 8.5f, 4.5f}, {4, 32, 10.f, 2.27f}},
+                                     {{1, 64, 11.7f, 4.85f}, {2, 64, 11.7f, 4.75f}, {4, 32, 15.f, 4.1f}}}};  // [f32][hd 128]
+// How a call's units, (document, key/value head), of `tiles` row tiles are dealt to XCDs.
+struct Dealt {
+  int tiles, parts, part_tiles;  // a unit's tiles, the parts that it is dealt in, tiles of one
+  long per_xcd;
+};
+Dealt deal(const SharedArgs& s, int qg) {
+  const long units = (long)s.own.docs * s.own.Hkv;
+  Dealt d{ceil_div((long)s.own.max_q * (s.own.Hq / s.own.Hkv), 32 * qg), 1, 0, 0};
+  while (d.parts < (units >= 512 ? 1 : units >= 64 ? 2 : 8) && 2 * d.parts <= d.tiles && units * d.parts % 8) d.parts *= 2;
+  d.part_tiles = ceil_div(d.tiles, d.parts);
+  d.per_xcd = (long)ceil_div(units * d.parts, 8) * d.part_tiles;
+  return d;
+}
+float time_of_chain(const SharedArgs& s, const Shaped& x, bool f32) {
   const AttnArgs& a = s.own;
-  const bool f32 = a.dtype == DLLM_F32;
-  const int cus = device_cu_count();
-  const double step = f32 ? 10.0 * a.hd / 128 : a.hd == 128 ? 1.9 : 1.4, busy = f32 ? 0.86 * cus : 1.6 * cus;
-  const double steps = ceil_div((long)s.max_p + a.max_kv, 64), rounds = ceil_div(tiles, f32 ? cus : 2 * cus);
-  return steps * step * rounds <= 8 + full * (steps * step / busy + 0.05);
+  const long tiles = deal(s, x.qg).per_xcd, cus = std::max(1, device_cu_count() / 8);
+  const bool pairs = !f32 && x.qg == 4;  // two workgroups a CU, which then slow each other
+  const int rounds = ceil_div(tiles, pairs ? 2 * cus : cus);
+  float own = (float)ceil_div(a.max_kv, x.keys);
+  if (a.block > 0 && a.max_q <= a.max_kv && rounds > 1) own *= 1.f - 0.5f * (float)a.max_q / (float)a.max_kv;  // what a mean row sees
+  return 1.5f + (float)rounds * (x.base + (pairs && tiles > cus ? 1.27f : 1.f) * x.step * ((float)ceil_div(s.max_p, x.keys) + own));
+}
+// Units and their join.
+float time_of_units(const SharedArgs& s, const SharedPlan& p, bool f32) {
+  const AttnArgs& a = s.own;
+  const bool wide = a.hd == 128;
+  const int rows = a.max_q * (a.Hq / a.Hkv);
+  const double all = (double)a.docs * rows, own = (double)a.docs * tiles_of(p, rows);
+  const double stacks = std::max(all > 64 ? all / MANY_ROWS : all / p.few_rows, (double)std::min(a.docs, s.prompts));
+  // a tile's p.unit_keys keys, of few and of many rows
+  const float few = f32 ? wide ? 2.4f : 0.65f : wide ? 1.33f : 0.93f, many = f32 ? wide ? 4.1f : 2.27f : wide ? 4.3f : 2.4f;
+  const float own_each = rows > 64 ? many : few, stack_each = all > 64 ? many : few;
+  const double work = own * ceil_div(a.max_kv, p.unit_keys) * own_each + stacks * ceil_div(s.max_p, p.unit_keys) * stack_each;
+  const float fixed = f32 ? wide ? 15.5f : 9.f : wide ? 9.5f : 7.5f, start = f32 ? 6.f : 4.5f, unit = f32 ? wide ? 16.f : 10.f : 9.f;
+  const double share = a.Hkv * (work + unit * (own + stacks)) / ((f32 ? 1.0 : 1.67) * device_cu_count());
+  return fixed + std::max(start + std::max(own_each, stack_each), (float)share) + 2e-4f * (float)(all * a.Hkv);
+}
+// The row groups of a tile that takes all keys of its rows, 0: units.
+int chain_of(const SharedArgs& s, const SharedPlan& p) {
+  const bool f32 = s.own.dtype == DLLM_F32;
+  float best = time_of_units(s, p, f32);
+  int qg = 0;
+  for (const Shaped& x : CHAINS[f32][s.own.hd == 128]) {
+    const float t = time_of_chain(s, x, f32);
+    if (t <= best) {
+      best = t;
+      qg = x.qg;
+    }
+  }
+  return qg;
 }
 SharedPlan choose(const SharedArgs& s) {
   const AttnArgs& a = s.own;
@@ -671,10 +730,13 @@ SharedPlan choose(const SharedArgs& s) {
   p.unit_keys = f32 ? 32 : 128;
   p.unit_cost = f32 ? 1 : 4;
   p.few_rows = f32 && a.hd == 128 ? 64 : 32;
-  p.tiles = ceil_div(rows, MANY_ROWS);
-  p.chain = rows > 64 && chain_is_shorter(s, (long)a.docs * a.Hkv * p.tiles, (double)a.docs * a.Hkv * rows / MANY_ROWS);
+  p.chain = chain_of(s, p);
   if (p.chain) {
-    p.grid = ((long)a.docs * a.Hkv + 7) / 8 * 8 * p.tiles;
+    const Dealt d = deal(s, p.chain);
+    p.tiles = d.tiles;
+    p.parts = d.parts;
+    p.part_tiles = d.part_tiles;
+    p.grid = 8 * d.per_xcd;
     return p;
   }
   const long packed = a.out.stride_b == 0 ? a.q_tokens : (long)a.docs * a.max_q;
@@ -718,7 +780,12 @@ template <typename T, int HD>
 void launch(const SharedArgs& s, const SharedPlan& p, hipStream_t st) {
   constexpr bool F32 = sizeof(T) == 4;
   if (p.chain) {
-    if constexpr (F32)
+    constexpr int KG = F32 && HD == 128 ? 2 : 4;
+    if (p.chain == 1)
+      shared_chain_kernel<T, HD, 1, KG, 32, 2><<<(unsigned)p.grid, 64 * KG, 0, st>>>(s, p);
+    else if (p.chain == 2)
+      shared_chain_kernel<T, HD, 2, KG, 32, 2><<<(unsigned)p.grid, 128 * KG, 0, st>>>(s, p);
+    else if constexpr (F32)
       shared_chain_kernel<T, HD, 4, 1, 32, 3><<<(unsigned)p.grid, 256, 0, st>>>(s, p);
     else
       shared_chain_kernel<T, HD, 4, 1, 64, 2><<<(unsigned)p.grid, 256, 0, st>>>(s, p);
@@ -762,7 +829,7 @@ size_t attn_shared_bytes(const SharedArgs& s) {
 bool attn_shared_fits(const SharedArgs& s) {
   if (alone(s)) return attn_docs_fits(s.own);
   const SharedPlan p = choose(s);
-  if (p.chain) return p.grid * 256 < (1l << 32);
+  if (p.chain) return p.grid * 512 < (1l << 32);  // (at most eight waves)
   return p.states < (1l << 31) && p.units * s.own.Hkv < (1l << 31) && p.work < (1l << 30) && (long)p.cap * s.own.Hq < (1l << 26);
 }
 

@@ -256,8 +256,7 @@ struct SharedArgs {
 // start and end in that, rows of a tile of few, states at most, and what the
 // workspace holds (shared_plan_kernel).
 struct SharedPlan {
-  bool chain;
-  int tiles, cap, slots, busy, unit_keys, unit_cost, few_rows;
+  int chain, tiles, parts, part_tiles, cap, slots, busy, unit_keys, unit_cost, few_rows;
   long grid, units, work, states;
   int* count;  // units without their heads, queries
   int4 *tok, *seg, *run, *unit;

@@ -13,6 +13,16 @@ from test_gpu_attention import randn, tolerance
 
 pytestmark = pytest.mark.gpu
 F32, BF16 = torch.float32, torch.bfloat16
+REACH = 0
+
+
+@pytest.fixture(autouse=True, params=[0, 20000], ids=["short", "long"])
+def reach(request, monkeypatch):
+    """Calls that are told of prompts no longer than they are, which row tiles may read with their own keys in one go, and
+    of far longer ones, whose keys are dealt as units: rows of no number behind the prompts make the slabs as long."""
+    monkeypatch.setitem(globals(), "REACH", request.param)
+
+
 HEADS = [(4, 4, 64), (4, 2, 128), (7, 1, 128), (28, 4, 128), (16, 2, 64)]
 
 
@@ -20,19 +30,27 @@ def starts(lens):
     return np.concatenate([[0], np.cumsum(lens)[:-1]]).astype(int) if len(lens) else np.zeros(0, int)
 
 
+def longer(t, rows):
+    """Rows of NaN behind the prompts of a slab ([.., P, Hkv, hd])."""
+    return torch.cat([t, t.new_full((*t.shape[:-3], rows, *t.shape[-2:]), float("nan"))], dim=-3) if rows else t
+
+
 def run_and_check(Hq, Hkv, hd, dtype, q_lens, kv_lens, p_lens, of=None, block=0, q_pos=None, prefix=None, cap=0.0, slopes=None,
-                  scale=None, seed=0, std=1.3, pad=3, mutate=None, check=True):
+                  scale=None, seed=0, std=1.3, pad=3, mutate=None, check=True, reach=None):
     """Packed documents and prompts (pad rows behind the last one); mutate(q, k, v, pk, pv) changes the inputs first."""
+    reach = REACH if reach is None else reach
     T, S, P = sum(q_lens), sum(kv_lens), sum(p_lens)
     say(f"shared {Hq}/{Hkv}x{hd} {dtype} q{q_lens[:40]} kv{kv_lens[:40]} prompts {p_lens} of {of if of is None else of[:40]} block {block} pos "
         f"{q_pos} prefix {prefix} cap {cap} slopes {slopes is not None}")
     q, k, v, pk, pv = (randn((n + pad, H, hd), dtype, seed + i, std)
                        for i, (n, H) in enumerate([(T, Hq), (S, Hkv), (S, Hkv), (P, Hkv), (P, Hkv)]))
+    pk, pv = longer(pk, reach), longer(pv, reach)
     if mutate:
         mutate(q, k, v, pk, pv)
     out = randn((T + pad, Hq, hd), dtype, seed + 5)
     behind = out[T:].clone()
     docs, prompts = B.Docs.packed(q_lens, kv_lens, q_pos, prefix), B.Prompts.packed(p_lens, of)
+    prompts.max = max(prompts.max, reach)
     sl = None if slopes is None else torch.tensor(slopes, dtype=F32, device="cuda")
     got = B.shared_attention(q, k, v, pk, pv, docs, prompts, block=block, cap=cap, slopes=sl, scale=scale, out=out)
     torch.cuda.synchronize()
@@ -141,6 +159,7 @@ def check_slabs(got, q, k, v, pk, pv, ql, kl, pl, of, dtype, **kw):
 def test_padded_batches_in_slabs(gpu_lib, docs, dtype):
     """Dense slabs of documents and of prompts with lengths; rows behind a document keep what they held."""
     q, k, v, pk, pv = slabs(6, 2, 64, dtype, docs, 9, 50, 140, 3)
+    pk, pv = longer(pk, REACH), longer(pv, REACH)
     ql, kl, pl, of = [d * 2 % 10 for d in range(docs)], [50 - d % 30 for d in range(docs)], [140, 1, 77], [d * 3 // docs for d in range(docs)]
     out = randn(q.shape, dtype, 9)
     before = out.clone()
@@ -154,10 +173,10 @@ def test_queries_that_are_one_slab_expanded(gpu_lib):
     """The same queries for every document, out a slab each; and heads of k and v that lie apart."""
     q, k, v, pk, pv = slabs(4, 2, 64, BF16, 7, 3, 20, 100, 1)
     q = q[:1].expand(7, -1, -1, -1)
-    pk, pv = (t.transpose(1, 2).contiguous().transpose(1, 2) for t in (pk, pv))
+    pk, pv = (longer(t, REACH).transpose(1, 2).contiguous().transpose(1, 2) for t in (pk, pv))
     out = torch.empty((7, 3, 4, 64), dtype=BF16, device="cuda")
     ws = B.device_buffer(B.shared_attention_workspace_size(q, k, v, pk, pv))
-    got = B.shared_attention(q, k, v, pk, pv, out=out, ws=ws, prompts=B.Prompts(of=ints([0] * 7)))
+    got = B.shared_attention(q, k, v, pk, pv, out=out, ws=ws, prompts=B.Prompts(len=ints([100]), of=ints([0] * 7)))
     check_slabs(got, q, k, v, pk, pv, [3] * 7, [20] * 7, [100], [0] * 7, BF16)
 
 
@@ -208,17 +227,18 @@ def test_rows_that_see_nothing(gpu_lib):
 def test_arrays_that_make_no_sense(gpu_lib, docs):
     """Ranges are cut to their slabs and to the maxima, prompts that are none are none."""
     big, low = 2 ** 31 - 1, -2 ** 31
-    q, k, v, pk, pv = slabs(4, 2, 64, BF16, docs, 4, 30, 60, 3)
+    q, k, v, pk, pv = slabs(4, 2, 64, BF16, docs, 4, 30, 60 + REACH, 3)
+    most = 40 + REACH
     pad = lambda v, rest: ints(list(v) + [rest] * (docs - 3))  # noqa: E731
     d = B.Docs(q_start=pad([low, 1, big], 0), q_len=pad([2, big, 5], 1), kv_start=pad([0, 20, low], 0), kv_len=pad([big, big, -4], 3), max_q=3, max_kv=25,
                q_pos=pad([big, low, 0], 0), prefix=pad([low, big, 7], 0))
-    p = B.Prompts(start=ints([low, 50, big]), len=ints([big, big, 9]), max=40, of=pad([0, 1, big], low))
+    p = B.Prompts(start=ints([low, 50, big]), len=ints([big, big, 9]), max=most, of=pad([0, 1, big], low))
     out = randn(q.shape, BF16, 5)
     before = out.clone()
     got = B.shared_attention(q, k, v, pk, pv, d, p, block=4, out=out)
     sl = lambda t, d, a, n: t[d:d + 1, a:a + n]  # noqa: E731
-    verify(got[0, :2], q[0, :2], k[0, :25], v[0, :25], pk[0, :40], pv[0, :40], [2], [25], [40], [0], 4, [big], [low], 0.0, None, None, BF16)
-    verify(got[1, 1:4], q[1, 1:4], k[1, 20:30], v[1, 20:30], pk[1, 50:], pv[1, 50:], [3], [10], [10], [0], 4, [low], [big], 0.0, None, None, BF16)
+    verify(got[0, :2], q[0, :2], k[0, :25], v[0, :25], pk[0, :most], pv[0, :most], [2], [25], [most], [0], 4, [big], [low], 0.0, None, None, BF16)
+    verify(got[1, 1:4], q[1, 1:4], k[1, 20:30], v[1, 20:30], pk[1, 50:], pv[1, 50:], [3], [10], [10 + REACH], [0], 4, [low], [big], 0.0, None, None, BF16)
     assert torch.equal(got[0, 2:], before[0, 2:]) and torch.equal(got[1, :1], before[1, :1]) and torch.equal(got[2], before[2])
 
 
@@ -242,8 +262,9 @@ def test_captured_and_on_other_streams(gpu_lib, docs):
     """Two calls in one graph with a workspace each, replayed with other inputs and eager work between; a call on
     another stream."""
     q, k, v, pk, pv = slabs(8, 2, 64, BF16, docs, 2, 40, 300, 1)
+    pk, pv, length = longer(pk, REACH), longer(pv, REACH), ints([300])
     n = ints([d % 41 for d in range(docs)])
-    call = lambda ws, out, s=None: B.shared_attention(q, k, v, pk, pv, B.Docs(kv_len=n), B.Prompts(of=ints0), block=1, out=out, ws=ws, stream=s)  # noqa: E731
+    call = lambda ws, out, s=None: B.shared_attention(q, k, v, pk, pv, B.Docs(kv_len=n), B.Prompts(len=length, of=ints0), block=1, out=out, ws=ws, stream=s)  # noqa: E731
     ints0 = ints([0] * docs)
     need = B.shared_attention_workspace_size(q, k, v, pk, pv)
     ws, outs = [B.device_buffer(need) for _ in range(3)], [torch.empty_like(q) for _ in range(3)]
@@ -260,7 +281,7 @@ def test_captured_and_on_other_streams(gpu_lib, docs):
         n.copy_(ints([(d * (i + 3)) % 41 for d in range(docs)]))
         torch.cuda.synchronize()
         g.replay()
-        eager = B.shared_attention(q, k, v, pk, pv, B.Docs(kv_len=n), B.Prompts(of=ints0), block=1)
+        eager = B.shared_attention(q, k, v, pk, pv, B.Docs(kv_len=n), B.Prompts(len=length, of=ints0), block=1)
         torch.cuda.synchronize()
         assert torch.equal(outs[0], eager) and torch.equal(outs[1], eager)
     call(ws[2], outs[2], torch.cuda.Stream())
@@ -281,17 +302,19 @@ def test_without_prompts_it_is_attention_of_documents(gpu_lib):
     ((28, 4, 128), BF16, [24, 10, 23], [40, 10, 39], [23], None, 1, False),
     ((28, 4, 128), BF16, [24, 10, 23], [40, 10, 39], [2000, 65], [0, 0, 1], 1, True),
     ((28, 4, 128), BF16, [24, 10, 23], [40, 500, 39], [2000, 65], [0, 1, -1], 32, True),
-    ((28, 4, 128), F32, [24, 10, 23], [40, 10, 39], [23], None, 1, True),
+    ((28, 4, 128), F32, [24, 10, 23], [40, 10, 39], [23], None, 1, False),
+    ((28, 4, 128), F32, [24, 10, 23], [40, 10, 39], [500], None, 1, True),
     ((16, 2, 64), BF16, [9, 0, 17], [9, 0, 17], [31, 64], [1, 0, 0], 0, False),
     ((16, 2, 64), BF16, [9, 0, 17], [1009, 0, 17], [31, 1064], [1, 0, 0], 0, True),
     ((8, 8, 128), F32, [128 - d % 7 for d in range(32)], [130 + d for d in range(32)], [60, 0], [d % 3 for d in range(32)], 1, False),
     ((8, 8, 64), F32, [128 - d % 7 for d in range(32)], [130 + d for d in range(32)], [60, 0], [d % 3 for d in range(32)], 32, False),
-    ((8, 8, 64), F32, [128 - d % 7 for d in range(8)], [130 + d for d in range(8)], [60, 0], [d % 3 for d in range(8)], 32, True),
+    ((8, 8, 64), F32, [128 - d % 7 for d in range(8)], [130 + d for d in range(8)], [60, 0], [d % 3 for d in range(8)], 32, False),
+    ((8, 8, 64), F32, [128 - d % 7 for d in range(8)], [130 + d for d in range(8)], [7000, 0], [d % 3 for d in range(8)], 32, True),
 ])
 def test_tiles_that_take_all_keys_and_units_of_them(gpu_lib, heads, dtype, q_lens, kv_lens, p_lens, of, block, units):
     """Both sides of the choice, which the workspace shows: tiles that take all their keys need none."""
     slopes = [2.0 ** -(1 + h / 4) for h in range(heads[0])]
-    _, (q, k, v, pk, pv, docs, prompts, _) = run_and_check(*heads, dtype, q_lens, kv_lens, p_lens, of, block, None, None, 30.0, slopes)
+    _, (q, k, v, pk, pv, docs, prompts, _) = run_and_check(*heads, dtype, q_lens, kv_lens, p_lens, of, block, None, None, 30.0, slopes, reach=0)
     assert (B.shared_attention_workspace_size(q, k, v, pk, pv, docs, prompts) > 0) == units
 
 

@@ -59,16 +59,18 @@ def test_workspace():
     assert size(None, n) == -1 and size(args(), None) == -1 and call(None) == -1
     for own in (dict(docs=0), dict(max_q=0)):
         assert size(args(own), n) == 0 and n.value == 0 and call(args(own), None, 0) == 0
-    assert size(args(), n) == 0 and n.value > 0
-    assert call(args(), A, n.value - 1) == -4
-    assert call(args(), None, n.value) == -1
-    assert call(args(), A + 128, n.value) == -1
+    split = args(p_tokens=20000, max_p=20000)  # few rows behind many keys
+    assert size(split, n) == 0 and n.value > 0
+    assert call(split, A, n.value - 1) == -4
+    assert call(split, None, n.value) == -1
+    assert call(split, A + 128, n.value) == -1
     # without a prompt's key: the workspace of attention of documents
     long = dict(kv_tokens=8192, max_kv=8192)
     for kw in (dict(prompts=0), dict(max_p=0)):
         a = args(long, **kw)
         assert size(a, n) == 0 and B.lib().dllm_attention_workspace_size(a.own, m) == 0 and n.value == m.value > 0
-    # documents whose own rows fill the CUs: none
+    # row tiles that take prompt and own keys in one go, of few keys or of rows that fill the CUs: none
+    assert size(args(), n) == 0 and n.value == 0
     many = dict(docs=256, q_tokens=256, max_q=256, q=view(b=1 << 17), n_heads=4, n_kv_heads=2)
     assert size(args(many), n) == 0 and n.value == 0
 
