@@ -246,13 +246,13 @@ def test_far_apart_and_far_away(gpu_lib):
     """Prompts further apart than 2^32 bytes; positions far behind every key keep their biases' precision."""
     far = torch.zeros((2, 40_000_000, 64), dtype=BF16, device="cuda")
     pk, pv = randn((2, 90, 1, 64), BF16, 1), randn((2, 90, 1, 64), BF16, 2)
-    K = far.as_strided((2, 90, 1, 64), (40_000_000 * 64, 64 * 100, 64, 1))
-    V = far.as_strided((2, 90, 1, 64), (40_000_000 * 64, 64 * 100, 64, 1), 64)
-    K.copy_(pk)
-    V.copy_(pv)
+    K = far.as_strided((2, 90 + REACH, 1, 64), (40_000_000 * 64, 64 * 100, 64, 1))
+    V = far.as_strided((2, 90 + REACH, 1, 64), (40_000_000 * 64, 64 * 100, 64, 1), 64)
+    K[:, :90].copy_(pk)
+    V[:, :90].copy_(pv)
     q, k, v = randn((5, 2, 64), BF16, 3), randn((9, 1, 64), BF16, 4), randn((9, 1, 64), BF16, 5)
     docs = B.Docs.packed([2, 3], [4, 5], q_pos=[0, 2 ** 31 - 1])
-    got = B.shared_attention(q, k, v, K, V, docs, B.Prompts(of=ints([1, 0])), slopes=torch.tensor([0.3, 0.01], device="cuda"))
+    got = B.shared_attention(q, k, v, K, V, docs, B.Prompts(len=ints([90, 90]), of=ints([1, 0])), slopes=torch.tensor([0.3, 0.01], device="cuda"))
     verify(got, q, k, v, torch.cat([pk[0], pk[1]]), torch.cat([pv[0], pv[1]]), [2, 3], [4, 5], [90, 90], [1, 0], 0, [0, 2 ** 31 - 1], None, 0.0,
            np.float32([0.3, 0.01]), None, BF16)
 
