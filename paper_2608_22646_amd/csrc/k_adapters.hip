@@ -14,7 +14,8 @@
 //   expand: the sum, scaled, in bf16 pieces that hold 16 of its bits (24 for a float32
 //     output) as the matrix unit's one operand, B's rows as they lie in memory as the
 //     other; a wave computes 32 rows x 128 columns, column n = 8 c + i by lane c's i-th
-//     product, so that a lane reads and writes 8 consecutive elements of base and out.
+//     product, so that a lane reads and writes 8 consecutive elements of base and out (64
+//     and 4 where there are few workgroups).
 //
 // What bounds them (kernel times, inputs not in a cache): 8448 rows of 4096 to 2 x 12288
 // columns, rank 16: expand 148 to 153 us, HBM at 5.5 TB/s; shrink 32, with 84 MB to read; sort 10.
@@ -34,7 +35,6 @@ namespace {
 
 constexpr int TM = 32;           // rows of a tile
 constexpr int NW = 8;            // waves of a shrinking workgroup
-constexpr int COLS = 128;        // columns of a wave's block
 constexpr int SORT_THREADS = 1024;
 
 typedef uint32_t u32x4_t __attribute__((ext_vector_type(4)));
@@ -188,23 +188,30 @@ struct Kind {
   static constexpr int STEP = 4 * E;        // along k: 64 bytes of a row, a piece for each 16 lanes
 };
 
-// 16 bytes at p, of which the first n elements count (the rest give zeros; none but
-// the first is touched behind them).
+// N elements at p, of which the first n count (the rest give zeros; none but the first is
+// touched behind them).
+template <typename T, int N>
+struct Words {
+  uint32_t w[N * sizeof(T) / 4];
+};
+template <typename T, int N>
+__device__ __forceinline__ Words<T, N> some(const T* p, int n) {
+  T v[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] = p[e < n ? e : 0];
+  Words<T, N> x{};
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    if constexpr (sizeof(T) == 2)
+      x.w[e / 2] |= e < n ? (uint32_t)v[e] << (16 * (e & 1)) : 0u;
+    else
+      x.w[e] = e < n ? __float_as_uint(v[e]) : 0u;
+  }
+  return x;
+}
 template <typename T>
 __device__ __forceinline__ u32x4_t piece(const T* p, int n) {
-  constexpr int E = Kind<T>::E;
-  T v[E];
-#pragma unroll
-  for (int e = 0; e < E; ++e) v[e] = p[e < n ? e : 0];
-  u32x4_t w = {0, 0, 0, 0};
-#pragma unroll
-  for (int e = 0; e < E; ++e) {
-    if constexpr (sizeof(T) == 2)
-      w[e / 2] |= e < n ? (uint32_t)v[e] << (16 * (e & 1)) : 0u;
-    else
-      w[e] = e < n ? __float_as_uint(v[e]) : 0u;
-  }
-  return w;
+  return __builtin_bit_cast(u32x4_t, some<T, Kind<T>::E>(p, n));
 }
 
 // c + the products of two fragments of a step
@@ -464,24 +471,26 @@ __global__ void __launch_bounds__(64) adapters_join_kernel(AdaptersArgs a, Adapt
 #endif
 }
 
-// Eight consecutive elements of base, as they were read.
-template <typename O>
-struct Eight {
-  static constexpr int W = sizeof(O) / 2;  // 16-byte pieces
-  u32x4_t w[W];
+// C consecutive elements of base, as they were read.
+template <typename O, int C>
+struct Some {
+  static constexpr int W = C * sizeof(O) > 16 ? C * sizeof(O) / 16 : 1, WORDS = C * sizeof(O) / 4 / W;  // pieces of words
+  typedef uint32_t piece_t __attribute__((ext_vector_type(WORDS)));
+  piece_t w[W];
   __device__ __forceinline__ float at(int e) const {
-    if constexpr (W == 1) return __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
+    if constexpr (sizeof(O) == 2) return __uint_as_float(e & 1 ? w[0][e / 2] & 0xffff0000u : w[0][e / 2] << 16);
     return __uint_as_float(w[(e / 4) % W][e % 4]);
   }
 };
 
 // A wave's share of a tile: its rows by the columns n0, n0 + 4 COLS, .. below `last`,
-// of a slice that ends at `end`.  VY, VB: base and out, b lie in whole 16-byte pieces.
+// of a slice that ends at `end`; C columns a lane, COLS a wave.  VY, VB: base and out, b lie in whole 16-byte pieces.
 // ONE: the ranks are those of one step.
-template <typename T, typename O, int PARTS, bool VY, bool VB, bool ONE>
+template <typename T, typename O, int PARTS, bool VY, bool VB, bool ONE, int C>
 __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const AdaptersPlan& p, const Tile& t, const int* rows, int rank,
                                                int steps, int slice, int n0, int last, int end) {
-  constexpr int E = Kind<T>::E;
+  constexpr int E = Kind<T>::E, COLS = 16 * C;
+  typedef Some<O, C> Y;
   const int lane = threadIdx.x & 63, g = lane >> 4, MT = (t.count + 15) >> 4;
   const T* const b = static_cast<const T*>(a.b.data) + max(t.adapter, 0) * a.b.stride_b;
   // base NULL: what is read in its place counts as zero
@@ -513,13 +522,13 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
     }
   }
   for (int nb = n0; nb < last; nb += 4 * COLS) {
-    const int n = nb + 8 * (lane & 15), left = end - n;
-    const int col = VY ? (left >= 8 ? n : nb) : n;  // columns that are not there: others' are read in their place
+    const int n = nb + C * (lane & 15), left = end - n;
+    const int col = VY ? (left >= C ? n : nb) : n;  // columns that are not there: others' are read in their place
     // b's pieces of step s
-    auto load_b = [&](int s, u32x4_t (&bf)[8]) {
+    auto load_b = [&](int s, u32x4_t (&bf)[C]) {
       const int c = (4 * s + g) * E, c0 = c < rank ? c : 0;  // (ranks that are not there: h has zeros)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < C; ++i) {
         const T* from = b + min(col + i, end - 1) * a.b.stride_l + c0;
         if constexpr (VB)
           bf[i] = *reinterpret_cast<const u32x4_t*>(from);
@@ -534,50 +543,54 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
           keep[w] = more <= 0 ? 0u : E == 8 && more == 1 ? 0xffffu : 0xffffffffu;
         }
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bf[i] &= keep;
+        for (int i = 0; i < C; ++i) bf[i] &= keep;
       }
     };
-    auto load_y = [&](int m, Eight<O> (&y)[4]) {
+    auto load_y = [&](int m, Y (&y)[4]) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = m * 16 + 4 * g + r;
         const O* from = base + rows[i < t.count ? i : 0] * base_stride + col;
         if constexpr (VY) {
 #pragma unroll
-          for (int k = 0; k < Eight<O>::W; ++k) y[r].w[k] = reinterpret_cast<const u32x4_t*>(from)[k];
+          for (int k = 0; k < Y::W; ++k) y[r].w[k] = reinterpret_cast<const typename Y::piece_t*>(from)[k];
         } else {
 #pragma unroll
-          for (int k = 0; k < Eight<O>::W; ++k) y[r].w[k] = piece(from + min(k * 8 / Eight<O>::W, left - 1), left - k * 8 / Eight<O>::W);
+          for (int k = 0; k < Y::W; ++k)
+            y[r].w[k] = __builtin_bit_cast(typename Y::piece_t, some<O, C / Y::W>(from + min(k * C / Y::W, left - 1), left - k * C / Y::W));
         }
       }
     };
-    auto finish = [&](int m, const Eight<O> (&y)[4], const f32x4_t (&acc)[8]) {
+    auto finish = [&](int m, const Y (&y)[4], const f32x4_t (&acc)[C]) {
 #pragma unroll
       for (int r = 0; r < 4; ++r) {
         const int i = m * 16 + 4 * g + r;
         if (i >= t.count || left <= 0) continue;
-        Eight<O> z = y[r];
+        Y z = y[r];
 #pragma unroll
-        for (int k = 0; k < Eight<O>::W; ++k) z.w[k] &= given;
-        float v[8];
+        for (int k = 0; k < Y::W; ++k) z.w[k] &= given;
+        float v[C];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = z.at(e) + acc[e][r];
+        for (int e = 0; e < C; ++e) v[e] = z.at(e) + acc[e][r];
         O* to = static_cast<O*>(a.out.data) + rows[i] * a.out.stride_l + n;
         if constexpr (VY && sizeof(O) == 2) {
-          *reinterpret_cast<u32x4_t*>(to) = u32x4_t{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+          typename Y::piece_t w;
+#pragma unroll
+          for (int e = 0; e < C; e += 2) w[e / 2] = pack_bf16x2(v[e], v[e + 1]);
+          *reinterpret_cast<typename Y::piece_t*>(to) = w;
         } else if constexpr (VY) {
-          *reinterpret_cast<f32x4_t*>(to) = f32x4_t{v[0], v[1], v[2], v[3]};
-          *reinterpret_cast<f32x4_t*>(to + 4) = f32x4_t{v[4], v[5], v[6], v[7]};
+#pragma unroll
+          for (int e = 0; e < C; e += 4) *reinterpret_cast<f32x4_t*>(to + e) = f32x4_t{v[e], v[e + 1], v[e + 2], v[e + 3]};
         } else {
 #pragma unroll
-          for (int e = 0; e < 8; ++e)
+          for (int e = 0; e < C; ++e)
             if (e < left) Act<O>::store(to, e, v[e]);
         }
       }
     };
     const f32x4_t zero = {0, 0, 0, 0};
-    u32x4_t bf[1][8];
-    Eight<O> y[2][4];
+    u32x4_t bf[1][C];
+    Y y[2][4];
     if constexpr (ONE) {
       load_y(0, y[0]);
       if (MT > 1) load_y(1, y[1]);
@@ -585,21 +598,21 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
         load_b(0, bf[0]);
       else
 #pragma unroll
-        for (int i = 0; i < 8; ++i) bf[0][i] = u32x4_t{0, 0, 0, 0};
+        for (int i = 0; i < C; ++i) bf[0][i] = u32x4_t{0, 0, 0, 0};
 #pragma unroll
       for (int m = 0; m < 2; ++m) {
         if (m >= MT) break;
-        f32x4_t acc[8];
+        f32x4_t acc[C];
 #pragma unroll
         for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) acc[i] = product<T>(hf[m][q], bf[0][i], q ? acc[i] : zero);
+          for (int i = 0; i < C; ++i) acc[i] = product<T>(hf[m][q], bf[0][i], q ? acc[i] : zero);
         finish(m, y[m], acc);
       }
     } else {
-      f32x4_t acc[2][8];
+      f32x4_t acc[2][C];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) acc[0][i] = acc[1][i] = zero;
+      for (int i = 0; i < C; ++i) acc[0][i] = acc[1][i] = zero;
       for (int s = 0; s < steps; ++s) {
         u32x4_t hs[2][PARTS];
 #pragma unroll
@@ -610,7 +623,7 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
 #pragma unroll
         for (int q = 0; q < PARTS; ++q)
 #pragma unroll
-          for (int i = 0; i < 8; ++i) {
+          for (int i = 0; i < C; ++i) {
             acc[0][i] = product<T>(hs[0][q], bf[0][i], acc[0][i]);
             acc[1][i] = product<T>(hs[1][q], bf[0][i], acc[1][i]);
           }
@@ -629,7 +642,7 @@ __device__ __forceinline__ void expand_columns(const AdaptersArgs& a, const Adap
   }
 }
 
-template <typename T, typename O, int PARTS, bool VY, bool VB, bool ONE>
+template <typename T, typename O, int PARTS, bool VY, bool VB, bool ONE, int C>
 __global__ void __launch_bounds__(256, sizeof(O) == 2 ? 3 : 2) adapters_expand_kernel(AdaptersArgs a, AdaptersPlan p) {
 #if defined(__HIP_DEVICE_COMPILE__)
   __shared__ int rows[TM];
@@ -642,10 +655,10 @@ __global__ void __launch_bounds__(256, sizeof(O) == 2 ? 3 : 2) adapters_expand_k
     block -= n;
     first = a.slice_end[slice];
   }
-  const int n0 = first + block * p.cols, end = a.slice_end[slice], last = min(end, n0 + p.cols), mine = n0 + uniform(threadIdx.x >> 6) * COLS;
+  const int n0 = first + block * p.cols, end = a.slice_end[slice], last = min(end, n0 + p.cols), mine = n0 + uniform(threadIdx.x >> 6) * 16 * C;
   const int rank = t.adapter < 0 ? 0 : uniform(rank_of(a, t.adapter));
   const int steps = (rank + Kind<T>::STEP - 1) / Kind<T>::STEP;
-  expand_columns<T, O, PARTS, VY, VB, ONE>(a, p, t, rows, rank, steps, slice, mine, last, end);
+  expand_columns<T, O, PARTS, VY, VB, ONE, C>(a, p, t, rows, rank, steps, slice, mine, last, end);
 #endif
 }
 
@@ -667,9 +680,13 @@ AdaptersPlan plan_of(const AdaptersArgs& a) {
   p.splits = ceil_div(chunks, p.steps);
   p.keep = a.rank > 64 / size && p.splits == 1;
   p.hsteps = ceil_div(a.rank, 64 / size);
-  // columns of a workgroup: 512, or twice that where four rounds of workgroups are left
-  const int per = std::max(1, std::min(2, (int)((long)full * ceil_div(a.d_out, 4 * COLS) / (4 * cus))));
-  p.cols = per * 4 * COLS;
+  // columns of a workgroup: 512, or twice that where that leaves four for each CU, or half of it
+  // where there would be fewer than CUs (8448 rows to 2 x 12288: 194 us, by 512 205; 4223 rows to
+  // 4096: 80, by 1024 86; 777 rows to 201 + 77 float32: 18.9, by 512 21.7; 256 to 4096 float32:
+  // 25.7 and 27; 2000 to 4096 of rank 64: 32, by 256 33.6)
+  const long wide = (long)full * ceil_div(a.d_out, 512);
+  p.narrow = wide < cus;
+  p.cols = p.narrow ? 256 : wide < 8 * cus ? 512 : 1024;
   for (int i = 0; i < a.slices; ++i) p.blocks += ceil_div(a.slice_end[i] - (i ? a.slice_end[i - 1] : 0), p.cols);
   return p;
 }
@@ -694,11 +711,17 @@ void run(const AdaptersArgs& a, const AdaptersPlan& p, hipStream_t s) {
       DLLM_LAUNCH_CHECK("adapters_join_kernel");
     }
   }
+  auto launch = [&](auto vy, auto vb, auto one) {
+    if (p.narrow)
+      adapters_expand_kernel<T, O, PARTS, vy, vb, one, 4><<<p.tiles * p.blocks, 256, 0, s>>>(a, p);
+    else
+      adapters_expand_kernel<T, O, PARTS, vy, vb, one, 8><<<p.tiles * p.blocks, 256, 0, s>>>(a, p);
+  };
   auto go = [&](auto vy, auto vb) {
     if (a.rank <= Kind<T>::STEP)
-      adapters_expand_kernel<T, O, PARTS, vy, vb, true><<<p.tiles * p.blocks, 256, 0, s>>>(a, p);
+      launch(vy, vb, std::true_type{});
     else
-      adapters_expand_kernel<T, O, PARTS, vy, vb, false><<<p.tiles * p.blocks, 256, 0, s>>>(a, p);
+      launch(vy, vb, std::false_type{});
   };
   if (!p.vec_b)
     go(std::false_type{}, std::false_type{});

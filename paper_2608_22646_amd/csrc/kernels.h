@@ -294,7 +294,7 @@ struct AdaptersArgs {
 // steps along them; whether whole 16-byte pieces may be read of x and a, of b, and of
 // base and out; and what the workspace holds.
 struct AdaptersPlan {
-  int sorted, tiles, j, splits, steps, keep, cols, blocks, r16, hsteps, vec_in, vec_b, vec_y;
+  int sorted, tiles, j, splits, steps, keep, narrow, cols, blocks, r16, hsteps, vec_in, vec_b, vec_y;
   uint32_t __attribute__((ext_vector_type(4))) * h;  // [slices][hsteps][parts][4][rows]: inner products
   float* part;                                       // [splits][rows][slices][r16]: shares of them
   int4* tile;                                        // adapter, first place in order, rows
