@@ -243,3 +243,11 @@ def test_most_rows(gpu_lib):
     tol += 2 * u * (ref.abs() + tol) * 1.01 + 1e-37
     assert bool(((got.double() - ref).abs() <= tol).all())
     assert torch.equal(got[which < 0], base[which < 0])
+
+
+@pytest.mark.parametrize("dtype,kind", KINDS)
+@pytest.mark.parametrize("M,K,widths,n,R", [(8200, 33, (77, 9), 4, 5), (8200, 24, (64, 40), 4, 70), (400, 64, (12280, 8), 3, 40), (2100, 39, (2000, 3), 5, 35),
+                                            (33000, 8, (520,), 3, 8)])
+def test_workgroups_of_more_columns(gpu_lib, M, K, widths, n, R, dtype, kind):
+    """As many workgroups of 512 columns as CUs, and enough for 1024."""
+    run(M, K, widths, n, R, dtype, kind, [(m * 7) % (n + 1) - 1 for m in range(M)], [max(1, R - 3 * a) for a in range(n)], [1.0 - a for a in range(n)])
