@@ -22,7 +22,7 @@
 // 4223 rows, rank up to 128, 4096 to 4096: expand 39 and shrink 33 us, the L2s' answers to
 // 32-row tiles that each read all of A and B (some 8 TB/s), sort 6.  Few rows: launches and
 // the chain of dependent reads in them (256 rows, 12288 to 4096 float32, ranks up to 64:
-// 3.8, 8.5, 4 and 9 us).
+// 3.8, 8.7, 4 and 7.5 us).
 #include <algorithm>
 #include <type_traits>
 
