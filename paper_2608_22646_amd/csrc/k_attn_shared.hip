@@ -819,8 +819,12 @@ bool alone(const SharedArgs& s) { return s.prompts == 0 || s.max_p == 0; }
 
 }  // namespace
 
-size_t attn_shared_bytes(const SharedArgs& s) {
-  if (alone(s)) return attn_docs_bytes(s.own);
+// (As without a block mask, which a query of the size may not know: with one a chain is never
+// slower, so that a call that takes units takes them without it too, laid out alike.)
+size_t attn_shared_bytes(const SharedArgs& of) {
+  if (alone(of)) return attn_docs_bytes(of.own);
+  SharedArgs s = of;
+  s.own.block = 0;
   SharedPlan p = choose(s);
   return p.chain ? 0 : lay_out(s, p, nullptr);
 }

@@ -102,3 +102,18 @@ def test_packed_prompts():
     assert p.start.tolist() == [0, 3, 3] and p.len.tolist() == [3, 0, 5] and p.max == 5 and p.of.tolist() == [2, -1]
     e = B.Prompts.packed([], device="cpu")
     assert e.start.numel() == 0 and e.max == 0 and e.of is None
+
+
+@pytest.mark.parametrize("docs,q,p", [(1, 700, 100), (2, 2000, 300), (3, 294, 64), (1, 405, 357), (8, 40, 200), (16, 64, 60), (4, 700, 2000)])
+@pytest.mark.parametrize("dtype", [B.DLLM_F32, B.DLLM_BF16])
+def test_workspace_of_any_block_mask(docs, q, p, dtype):
+    """The size does not depend on the block mask, which the binding's query is not told of."""
+    size = 0x100 * 4
+    own = dict(dtype=dtype, n_heads=28, n_kv_heads=4, docs=docs, q_tokens=docs * q, kv_tokens=docs * q, max_q=q, max_kv=q,
+               q=view(l=28 * 128), k=view(l=size), v=view(l=size), out=view(l=28 * 128))
+    got = []
+    for block in (0, 1, 32):
+        n = ctypes.c_size_t()
+        assert B.lib().dllm_shared_attention_workspace_size(args(dict(own, block=block), p_tokens=p, max_p=p), n) == 0
+        got.append(n.value)
+    assert got[0] == got[1] == got[2]
