@@ -62,13 +62,14 @@ __device__ __forceinline__ Tile tile_of(const AdaptersArgs& a, const AdaptersPla
     if ((int)threadIdx.x < t.count) rows[threadIdx.x] = p.order[d.y + threadIdx.x];
   } else {
     // tile i: the i / groups-th of the 32 rows of group i % groups (rows that share an
-    // adapter leave the first of them at work: those lie on consecutive XCDs)
+    // adapter leave the first of them at work: those lie on consecutive XCDs).  w of a lane
+    // without a row is -2, also where tile i's own row is not there: no tile, no rows.
     const int groups = (p.tiles + TM - 1) / TM, me = i / groups, row = i % groups * TM + lane;
     const int w = lane < TM && row < a.rows ? adapter_of(a, row) : -2;
     t.adapter = __builtin_amdgcn_readlane(w, me);
     const unsigned long long mine = __ballot(w == t.adapter);
     t.count = t.adapter >= -1 && __ffsll(mine) - 1 == me ? __popcll(mine) : 0;
-    if (threadIdx.x < 64 && w == t.adapter) rows[__popcll(mine & ((1ull << lane) - 1))] = row;
+    if (threadIdx.x < 64 && t.count && w == t.adapter) rows[__popcll(mine & ((1ull << lane) - 1))] = row;
   }
   __syncthreads();
   return t;
