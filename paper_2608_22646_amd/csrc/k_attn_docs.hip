@@ -87,8 +87,8 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
   constexpr int TR = 32 * QG;  // TR: rows of the tile
   __shared__ __attribute__((aligned(1024))) char lds[attend_lds<T, HD, QG, KG, KT, S>()];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int qg = wave % QG;
-  const int lq = lane & 31;
+  const int qg = wave % QG, kg = wave / QG;
+  const int lq = lane & 31, half = lane >> 5;
 
   // Workgroup i runs on XCD i % 8.  A unit is (document, chunk, key/value head);
   // its row tiles, which read the same keys, go to one XCD (to `parts` of them
@@ -117,12 +117,12 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
   if (sh.chunk > 0 && kb >= ke) return;
   // this wave's rows
   const int w0 = r0 + 32 * qg, w1 = min(w0 + 32, rows), row = w0 + lq;
-  Keys k = keys_at<T>(a.k, a.v, dn, d.k0, g);
-  k.kb = kb;
-  k.ke = ke;
-  k.tile_first = uniform(sees(a, d, r0 / G));
-  k.see_first = uniform(w0 < rows ? sees(a, d, w0 / G) : 0);
-  k.see_last = uniform(w0 < rows ? sees(a, d, (w1 - 1) / G) : 0);
+  Keys k1 = keys_at<T>(a.k, a.v, dn, d.k0, g);
+  k1.kb = kb;
+  k1.ke = ke;
+  k1.tile_first = uniform(sees(a, d, r0 / G));
+  k1.see_first = uniform(w0 < rows ? sees(a, d, w0 / G) : 0);
+  k1.see_last = uniform(w0 < rows ? sees(a, d, (w1 - 1) / G) : 0);
   auto rows_of = [&](Rows<HD>& R) {
     R.mine = row < rows;
     R.t = row / G;
@@ -142,12 +142,14 @@ __global__ void __launch_bounds__(64 * QG * KG, KT == 64 ? 2 : 1) attn_docs_kern
     return static_cast<const T*>(a.q.data) + dn * a.q.stride_b + (long)(d.q0 + (R.mine ? R.t : 0)) * a.q.stride_l +
            (R.mine ? R.h : 0) * a.q.stride_h;
   };
-  attend<T, HD, QG, KG, KT, S, false>(a, lds, tid, k, k, rows_of, [&](const Rows<HD>& R) {
-    if (p.shares > 0)  // state of (query, head) for this share
-      keep_state(R, p.part, p.part_ml, ((size_t)(sh.first + sh.chunk) * a.max_q + R.t) * a.Hq + R.h);
-    else
-      store_row(R, static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + R.t) * a.out.stride_l + R.h * a.out.stride_h);
-  });
+  constexpr bool CHAIN = false;
+  const Keys& k2 = k1;
+#include "attn_tile_body.h"
+  if (!R.mine) return;
+  if (p.shares > 0)  // state of (query, head) for this share
+    keep_state(R, p.part, p.part_ml, ((size_t)(sh.first + sh.chunk) * a.max_q + R.t) * a.Hq + R.h);
+  else
+    store_row(R, static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + R.t) * a.out.stride_l + R.h * a.out.stride_h);
 #endif
 }
 
@@ -164,8 +166,8 @@ __global__ void __launch_bounds__(256) attn_join_kernel(AttnArgs a, AttnPlan p) 
   // its document's chunks of which it sees a key; its tile ran them all
   const int n = w4.z > 0 ? min(w4.y, (sees(a, d, t) + w4.z - 1) / w4.z) : 0;
   const size_t next = (size_t)a.max_q * a.Hq, at = w4.x * next + (size_t)t * a.Hq + h;
-  join_row<T, HD, W>(static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h, n, p.part,
-                     p.part_ml, [&](int i) { return at + i * next; });
+  join_row<T, HD, W>(static_cast<T*>(a.out.data) + dn * a.out.stride_b + (long)(d.q0 + t) * a.out.stride_l + h * a.out.stride_h, n,
+                     p.part + at * HD, p.part_ml + at, [&](int i) { return i * next; });
 }
 
 // Keys of the chunks that a row tile's width is chosen for, and the least of one.
