@@ -897,10 +897,12 @@ def adapters(x, base, A, B, which, ranks=None, scales=None, slices=None, out=Non
     return out
 
 
-def adapters_workspace_size(x, base, A, B, slices=None):
-    """Bytes of workspace that adapters() needs for operands of these sizes (base None: of x's type)."""
+def adapters_workspace_size(x, base, A, B, slices=None, out=None):
+    """Bytes of workspace that adapters() needs for operands of these sizes; base and out as there (out None: of base's type,
+    or of x's)."""
     n = _sz()
-    out = x.new_empty((1, B.shape[1])).expand(x.shape[0], -1) if base is None else base
+    if out is None:
+        out = x.new_empty((1, B.shape[1])).expand(x.shape[0], -1) if base is None else base
     a, _ = _adapter_args(x, base, A, B, None, None, None, slices, out)
     check(lib().dllm_adapters_workspace_size(a, n))
     return n.value
