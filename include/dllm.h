@@ -607,10 +607,13 @@ int dllm_sample(const dllm_sample_args* args, void* workspace, size_t workspace_
  * adapter's rank is not used.  scales: device float32 [adapters]; NULL: 1.
  * Storage: x, a and b float32 or bf16 (dtype); base and out of out_dtype, bf16 or, for
  * either dtype, float32.  Both products accumulate in float32; of the inner one 16 bits
- * enter the outer one where out is bf16, all 24 else; the result is rounded once.  A
- * result does not depend on the other rows, nor on their order.  A NaN or an infinity in
- * x or in a row's own adapter reaches that row alone; an infinite element of b may give
- * NaN where the formula has an infinity.
+ * enter the outer one where out is bf16, all 24 else; the result is rounded once.  What the
+ * other rows hold, their adapters and the rows' order do not reach a result: calls of the same
+ * sizes, strides and alignment give a row the same bits.  How many rows, adapters and
+ * ranks there are does: they settle into how many shares d_in is cut, whose sums are added
+ * in order, so that a row of a batch and the same row alone may differ by the rounding of a
+ * float32 sum of d_in products.  A NaN or an infinity in x or in a row's own adapter reaches
+ * that row alone; an infinite element of b may give NaN where the formula has an infinity.
  * out may be base (same data and stride); apart from that it must not overlap anything
  * the call reads.  Data and strides at multiples of 16 bytes are read in such pieces,
  * others by the element.
