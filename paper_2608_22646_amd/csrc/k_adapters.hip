@@ -20,7 +20,10 @@
 // What bounds them (kernel times, inputs not in a cache): 8448 rows of 4096 to 2 x 12288
 // columns, rank 16: expand 148 to 153 us, HBM at 5.5 TB/s; shrink 32, with 84 MB to read; sort 10.
 // 4223 rows, rank up to 128, 4096 to 4096: expand 39 and shrink 33 us, the L2s' answers to
-// 32-row tiles that each read all of A and B (some 8 TB/s), sort 6.  Few rows: launches and
+// 32-row tiles that each read all of A and B (some 8 TB/s), sort 6.  By the element (4223 rows,
+// 4096 to 4095, so that rows begin anywhere): expand of rank 16 51 us, in pieces to 4096
+// columns 19; b too, rank 12, 102; rank 64 54 and 27, 60 115.  There the bf16 kernels of 8
+// columns a lane spill: 12 and 196 bytes at ranks of one step, at more 36 with b.  Few rows: launches and
 // the chain of dependent reads in them (256 rows, 12288 to 4096 float32, ranks up to 64:
 // 3.8, 8.7, 4 and 7.5 us).
 #include <algorithm>

@@ -9,15 +9,20 @@
 // keys, leave their states in the workspace, and a join takes a row's states over its
 // prompt's chunks and its document's.  What is stacked and split how is found on the
 // device, from the lengths there: a list of units of like work, those of the prompts, the
-// longer ones, first (up to 64 documents by each workgroup for itself, 2.4 us; more by a
-// launch before).
+// longer ones, first: up to 64 documents by each workgroup for itself, 2.4 us; more by a
+// launch before, of one workgroup, in which one thread writes all units of a segment: 65
+// single tokens behind 8448 keys 19 us, 65 documents of 32 queries behind 1024 (32 heads)
+// 23, 256 of them 74.
 //
 // What bounds them (kernel times, inputs not in a cache): 16 documents of 32 queries behind 8448
 // keys, 32 heads: units 93 to 104 us, 0.7 to 0.8 PFLOP/s, of which two workgroups a CU reach 1.0
 // while both have prompt keys; join 8.  Behind 1024: 37 to 40 and 7, where 67 MB of the
-// documents' own keys come from HBM.  32 single tokens behind 8448 keys: 19 and 5.  8
-// documents of up to 700 queries, chain: 126 to 130, as attention of documents alone (issue
-// of the softmax beside the products).  Small calls: launches, the plan and first tiles.
+// documents' own keys come from HBM.  32 single tokens behind 8448 keys: 19 and 5; units are
+// numbered heads fastest, so that of 4 heads the two row tiles of a chunk lie on different
+// XCDs, and each prompt key passes through two L2s.  8 documents of up to 700 queries, chain:
+// 125 in a row of calls, 138 to 143 traced, 0.7 PFLOP/s where long prompts in attention of
+// documents reach 1.0: 2.3 rounds of workgroups, the last one not full, beside the issue of
+// the softmax.  Small calls: launches, the plan and first tiles.
 #include <algorithm>
 
 #include "attn_tile.h"
@@ -391,7 +396,10 @@ struct Shape {
 };
 // Tiles of 128 rows; of few rows, where the waves split the keys, each with a stage of
 // its own: beside the other workgroup's four waves their loads need no second one.  (Rows
-// of 512 bytes: half the keys fit.)
+// of 512 bytes: half the keys fit.)  Two workgroups a CU leave a lane 256 registers: float32
+// of 128-wide heads spills 108 bytes of them, 112 where the plan is given (16 documents of 32
+// queries behind 1024 keys, 32 heads: 135 us, the products 80; 32 tokens behind 2048, 28 + 4
+// heads: 53), bf16 that plans for itself 8.
 template <typename T, int HD>
 struct Shapes {
   static constexpr bool F32 = sizeof(T) == 4, WIDE = F32 && HD == 128;
@@ -686,7 +694,9 @@ float time_of_chain(const SharedArgs& s, const Shaped& x, bool f32) {
   if (a.block > 0 && a.max_q <= a.max_kv && rounds > 1) own *= 1.f - 0.5f * (float)a.max_q / (float)a.max_kv;  // what a mean row sees
   return 1.5f + (float)rounds * (x.base + (pairs && tiles > cus ? 1.27f : 1.f) * x.step * ((float)ceil_div(s.max_p, x.keys) + own));
 }
-// Units and their join.
+// Units and their join.  (Stacks as if documents were told apart by prompt also where the array
+// of them is not given and all stand behind prompt 0: the choice decides the workspace's size,
+// which must not depend on the arrays.  Several prompts and no array: on the chain's side.)
 float time_of_units(const SharedArgs& s, const SharedPlan& p, bool f32) {
   const AttnArgs& a = s.own;
   const bool wide = a.hd == 128;
